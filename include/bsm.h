@@ -98,7 +98,7 @@ typedef enum {
     BSM_ERR_TOO_LARGE = 9      /* more patches than bsm_softmax_noalloc's fixed scratch holds */
 } bsm_status;
 
-typedef enum { BSM_F32 = 0, BSM_BF16 = 1 } bsm_dtype;   /* input type == output type */
+typedef enum { BSM_F32 = 0, BSM_BF16 = 1, BSM_F16 = 2 } bsm_dtype;   /* input type == output type; F16: paged calls only */
 
 typedef enum {
     BSM_POLICY_WHOLE_GPU = 0,
@@ -271,6 +271,132 @@ int bsm_bmm(const void *a, const void *bt, void *c, int64_t B, int64_t M, int64_
 int bsm_bmm_ex(const void *a, const void *bt, void *c, int64_t B, int64_t M, int64_t N, int64_t K,
                int out_dtype, int policy, int n_stages, int epi_bufs, int k_blocks_per_stage,
                bsm_stream_t stream);
+
+/* ---- attention over a paged cache ----
+ * The fused form of the scores, softmax and product above for ragged batches
+ * whose keys and values lie in pages: a cache of n_pages pages of page_size
+ * tokens, and per request a table of the pages it owns, in order.  Token p of
+ * request r lies in slot tables[r, p / page_size] * page_size + p % page_size.
+ * One step of a program that serves requests is bsm_paged_tables (where the
+ * step's new tokens go), bsm_paged_write and bsm_paged_attention, the last two
+ * once per layer.  Lengths, tables and slots stay on the device; no call
+ * synchronises or allocates.  Calls share nothing but their arguments, so they
+ * may run on several streams at once, each with its own workspace.
+ * All strides are in elements; every row of head_dim elements is contiguous. */
+
+/*
+ * Block tables and slot maps from the requests' lengths, in one launch.
+ * Request r has cached[r] tokens in the cache and brings fresh[r] new ones
+ * (both >= 0).  With have_r = ceil(cached[r] / page_size) and need_r =
+ * ceil((cached[r] + fresh[r]) / page_size):
+ *   tables[r, have_r .. need_r)  the next need_r - have_r pages of free_pages,
+ *                       handed out in request order; -1 once they have run out.
+ *                       Other entries stay; those before have_r are read.
+ *   starts[r]           fresh[0] + .. + fresh[r-1], n_requests + 1 entries
+ *   lengths[r]          cached[r] + fresh[r]
+ *   owners[t], positions[t], slots[t]   request, position and slot of new token
+ *                       t; the slot is -1 where there is no page, all three are
+ *                       -1 for t >= starts[n_requests]
+ *   info[0..3]          new tokens; pages taken; pages missing; BSM_PAGED_* bits
+ * free_pages is not changed: drop its first info[1] entries.  A repeated call
+ * gives the same answer.  Page ids are not checked here.
+ * Errors: BSM_ERR_INVALID_ARG (sizes, null pointers, outputs that overlap each
+ * other or an input), BSM_ERR_MISALIGNED (8 bytes for slots and info, 4 for the
+ * rest), BSM_ERR_CUDA.
+ */
+#define BSM_PAGED_PAGES 1u      /* free_pages ran out */
+#define BSM_PAGED_WIDTH 2u      /* a request needs more than table_width pages: the rest has no slot */
+#define BSM_PAGED_TOKENS 4u     /* more new tokens than n_slots: the rest is not written */
+#define BSM_PAGED_NEGATIVE 8u   /* a negative length, taken as 0 */
+typedef struct {
+    const int32_t *cached, *fresh;      /* n_requests */
+    const int32_t *free_pages;          /* n_free */
+    int32_t *tables;                    /* n_requests rows of table_width, table_stride apart */
+    int32_t *starts, *lengths;          /* n_requests + 1, n_requests */
+    int64_t *slots;                     /* n_slots */
+    int32_t *positions, *owners;        /* n_slots */
+    int64_t *info;                      /* 4 */
+    int64_t table_stride;
+    int32_t n_requests, n_free, page_size, table_width, n_slots;
+} bsm_paged_tables_desc;
+int bsm_paged_tables(const bsm_paged_tables_desc *d, bsm_stream_t stream);
+
+/*
+ * k_cache[slots[t]] = k[t] and v_cache[slots[t]] = v[t] for every token t and
+ * head, bit for bit.  A negative slot is skipped, one past the cache is skipped
+ * and sets BSM_DEV_BOUNDS; two tokens with the same slot leave either.  dtype
+ * F32, BF16 or F16.  Rows of a multiple of 16 bytes, pointers and strides too
+ * (else BSM_ERR_MISALIGNED); caches must not overlap the other arguments.
+ */
+typedef struct {
+    const void *k, *v;                  /* n_tokens x n_heads x head_dim */
+    void *k_cache, *v_cache;            /* n_pages x page_size x n_heads x head_dim, any order of strides */
+    const int64_t *slots;               /* n_tokens */
+    int64_t k_stride_token, k_stride_head, v_stride_token, v_stride_head;
+    int64_t kv_stride_page, kv_stride_token, kv_stride_head;    /* of both caches */
+    int32_t n_tokens, n_heads, head_dim, page_size, n_pages;
+    int32_t dtype;
+} bsm_paged_write_desc;
+int bsm_paged_write(const bsm_paged_write_desc *d, bsm_stream_t stream);
+
+/*
+ * Attention of new tokens over the cache.  Request r's tokens are starts[r] ..
+ * starts[r+1] - 1 of q, its keys the first lengths[r] tokens of its pages, the
+ * new ones among them as the last.  For its token i of m, at position
+ * p = lengths[r] - m + i, and query head h over key/value head h / (heads_q /
+ * heads_kv):
+ *     s_j = scale * <q, k_j>,  j < lengths[r], with BSM_FLAG_CAUSAL only j <= p
+ *           and, where window > 0, j > p - window
+ *     out = sum_j exp(s_j) v_j / sum_j exp(s_j),  lse = log sum_j exp(s_j)
+ * A token that sees no key (an empty request, a position below 0) gets zeros
+ * and lse = -inf.  Rows of q past starts[n_requests] are not read and theirs of
+ * out not written.  A masked key of the request takes part with weight 0, so an
+ * infinity or a NaN among its values may show; keys that no token of the call
+ * may see (past lengths[r], left of every window) are never used, whatever their
+ * pages hold.
+ *   dtype     BF16 or F16 for q, caches and out (BSM_ERR_UNSUPPORTED: F32);
+ *             products accumulate in fp32, the softmax is fp32, probabilities
+ *             are rounded to dtype for the second product.
+ *   heads_q   a multiple of heads_kv; head_dim a multiple of 8 up to 128 (else
+ *             BSM_ERR_UNSUPPORTED).
+ *   scale     > 0 and finite; window >= 0, > 0 only with BSM_FLAG_CAUSAL.
+ *   lse       n_tokens x heads_q fp32, or null.
+ *   max_new   the most new tokens of any request, as the host knows it.  A hint:
+ *             it selects kernels; a wrong one costs time, not the answer.
+ *   workspace bsm_paged_workspace_bytes bytes, 256-byte aligned, for this call
+ *             alone until its work is done; its contents need no preparation.
+ * The result depends on the batch (the keys are split by what the whole batch
+ * needs) and is the same every time for the same batch.
+ * Lengths, offsets and page ids that lie outside the buffers are cut or skipped
+ * and set BSM_DEV_BOUNDS; nothing outside the buffers is touched.
+ * Pointers 16-byte aligned, strides multiples of 8 (else BSM_ERR_MISALIGNED).
+ * out, lse and workspace must not overlap each other or an input.
+ * Errors: BSM_ERR_INVALID_ARG, BSM_ERR_MISALIGNED, BSM_ERR_UNSUPPORTED,
+ * BSM_ERR_CUDA.  No requests or tokens: BSM_OK, nothing launched.
+ */
+typedef struct {
+    const void *q;                      /* n_tokens x heads_q x head_dim */
+    const void *k_cache, *v_cache;      /* as bsm_paged_write */
+    void *out;                          /* n_tokens x heads_q x head_dim */
+    float *lse;
+    const int32_t *starts, *lengths;    /* n_requests + 1, n_requests */
+    const int32_t *tables;              /* n_requests rows of table_width, table_stride apart */
+    void *workspace;
+    int64_t workspace_bytes;
+    int64_t q_stride_token, q_stride_head, out_stride_token, out_stride_head;
+    int64_t kv_stride_page, kv_stride_token, kv_stride_head;
+    int64_t table_stride;
+    int32_t n_requests, n_tokens, heads_q, heads_kv, head_dim, page_size, n_pages, table_width, max_new;
+    int32_t dtype, window;
+    uint32_t flags;
+    float scale;
+} bsm_paged_desc;
+int bsm_paged_attention(const bsm_paged_desc *d, bsm_stream_t stream);
+
+/* Bytes of workspace that bsm_paged_attention wants on `device` (-1: current)
+ * for calls of these heads and at most max_new new tokens a request; -1 for
+ * arguments it would refuse or without a device. */
+int64_t bsm_paged_workspace_bytes(int device, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t max_new);
 
 /* ---- plans: build the schedule once ("upfront", Sec. 5), run it many times ---- */
 

@@ -19,7 +19,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "_lib", "libbsm.so")
 HEADER = os.path.join(os.path.dirname(PKG), "include", "bsm.h")
 
-F32, BF16 = 0, 1
+F32, BF16, F16 = 0, 1, 2       # (F16: the paged-cache calls only)
 POLICY_WHOLE_GPU, POLICY_RR, POLICY_CBMF, POLICY_CBMF_LB, POLICY_DYNAMIC, POLICY_MINIMAX = range(6)
 POLICIES = {"whole_gpu": POLICY_WHOLE_GPU, "rr": POLICY_RR, "cbmf": POLICY_CBMF,
             "cbmf_lb": POLICY_CBMF_LB, "dynamic": POLICY_DYNAMIC, "minimax": POLICY_MINIMAX}
@@ -29,6 +29,7 @@ OP_FORWARD, OP_BACKWARD = 0, 1
 MAX_DIES = 4
 MAX_SM = 256
 DEV_BOUNDS, DEV_TIMEOUT, DEV_CHECK = 1, 2, 4
+PAGED_PAGES, PAGED_WIDTH, PAGED_TOKENS, PAGED_NEGATIVE = 1, 2, 4, 8
 
 (OK, ERR_INVALID_ARG, ERR_MISALIGNED, ERR_UNSUPPORTED, ERR_CUDA, ERR_DEVICE_BOUNDS,
  ERR_TIMEOUT, ERR_NO_DEVICE, ERR_NOMEM, ERR_TOO_LARGE) = range(10)
@@ -120,6 +121,31 @@ class ScheduleOut(ctypes.Structure):
                 ("work_before", c_i64p), ("work_after", c_i64p)]
 
 
+class PagedTablesDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("cached", "fresh", "free_pages", "tables", "starts", "lengths", "slots",
+                                               "positions", "owners", "info")] + \
+               [("table_stride", ctypes.c_int64)] + \
+               [(n, ctypes.c_int32) for n in ("n_requests", "n_free", "page_size", "table_width", "n_slots")]
+
+
+class PagedWriteDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_cache", "v_cache", "slots")] + \
+               [(n, ctypes.c_int64) for n in ("k_stride_token", "k_stride_head", "v_stride_token", "v_stride_head",
+                                              "kv_stride_page", "kv_stride_token", "kv_stride_head")] + \
+               [(n, ctypes.c_int32) for n in ("n_tokens", "n_heads", "head_dim", "page_size", "n_pages", "dtype")]
+
+
+class PagedDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k_cache", "v_cache", "out", "lse", "starts", "lengths", "tables",
+                                               "workspace")] + \
+               [(n, ctypes.c_int64) for n in ("workspace_bytes", "q_stride_token", "q_stride_head", "out_stride_token",
+                                              "out_stride_head", "kv_stride_page", "kv_stride_token", "kv_stride_head",
+                                              "table_stride")] + \
+               [(n, ctypes.c_int32) for n in ("n_requests", "n_tokens", "heads_q", "heads_kv", "head_dim", "page_size",
+                                              "n_pages", "table_width", "max_new", "dtype", "window")] + \
+               [("flags", ctypes.c_uint32), ("scale", ctypes.c_float)]
+
+
 _lib = None
 
 
@@ -146,6 +172,10 @@ def lib():
         "bsm_softmax_backward": ([vp, vp, vp, i64, i64, i64, ctypes.c_int, ctypes.c_int, vp], ctypes.c_int),
         "bsm_softmax_backward_ragged": ([vp, vp, vp, i64, vp, vp, vp, ctypes.c_int, ctypes.c_int, vp],
                                         ctypes.c_int),
+        "bsm_paged_tables": ([vp, vp], ctypes.c_int),
+        "bsm_paged_write": ([vp, vp], ctypes.c_int),
+        "bsm_paged_attention": ([vp, vp], ctypes.c_int),
+        "bsm_paged_workspace_bytes": ([ctypes.c_int, i32, i32, i32, i32], i64),
         "bsm_plan_desc_init": ([ctypes.POINTER(PlanDesc)], ctypes.c_int),
         "bsm_plan_create": ([ctypes.POINTER(vp), ctypes.POINTER(PlanDesc)], ctypes.c_int),
         "bsm_plan_execute": ([vp, vp], ctypes.c_int),
@@ -348,6 +378,125 @@ def bsm_softmax_ragged(x, y, offsets, rows, cols, dtype: int, policy: int, flags
     _check(lib().bsm_softmax_ragged(_dptr(x, n, "x"), _dptr(y, n, "y"), *where, dtype, policy, flags,
                                     _stream(stream)), "bsm_softmax_ragged")
     del keep
+
+
+_PAGED_DTYPES = {"torch.float32": F32, "torch.bfloat16": BF16, "torch.float16": F16}
+
+
+def _strided(t, what: str, ndim: int):
+    """Address of a CUDA tensor whose last dimension is contiguous; its other
+    strides go to the library, which checks them."""
+    if not t.is_cuda:
+        raise ValueError("%s must be a CUDA tensor (got one on %s)" % (what, t.device))
+    if t.dim() != ndim:
+        raise ValueError("%s must have %d dimensions, not %d" % (what, ndim, t.dim()))
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError("the last dimension of %s must be contiguous" % what)
+    return t.data_ptr()
+
+
+def _ints(t, what: str, size: int, n: int):
+    """Address of a contiguous CUDA tensor of at least n integers of `size` bytes."""
+    if t.element_size() != size or t.is_floating_point():
+        raise ValueError("%s must hold integers of %d bytes" % (what, size))
+    return _dptr(t, n * size, what)
+
+
+def _paged_dtype(*tensors):
+    kinds = {str(t.dtype) for t in tensors}
+    if len(kinds) != 1 or next(iter(kinds)) not in _PAGED_DTYPES:
+        raise ValueError("tensors must share one of the types %s (got %s)"
+                         % (", ".join(sorted(_PAGED_DTYPES)), ", ".join(sorted(kinds))))
+    return _PAGED_DTYPES[next(iter(kinds))]
+
+
+def _caches(k_cache, v_cache):
+    if k_cache.shape != v_cache.shape or k_cache.stride() != v_cache.stride():
+        raise ValueError("k_cache and v_cache must have the same shape and strides")
+    return _strided(k_cache, "k_cache", 4), _strided(v_cache, "v_cache", 4)
+
+
+def bsm_paged_tables(cached, fresh, free_pages, page_size: int, tables, starts, lengths, slots, positions, owners,
+                     info, stream=None):
+    """Block tables and slot maps from the requests' lengths (all CUDA integer
+    tensors: int64 slots and info, int32 the rest; tables [requests, width])."""
+    n, m = cached.numel(), slots.numel()
+    d = PagedTablesDesc()
+    d.cached, d.fresh = _ints(cached, "cached", 4, n), _ints(fresh, "fresh", 4, n)
+    d.free_pages = _ints(free_pages, "free_pages", 4, 0)
+    if tables.element_size() != 4 or tables.is_floating_point() or tables.shape[0] < n:
+        raise ValueError("tables must hold a row of 4-byte integers for every request")
+    d.tables = _strided(tables, "tables", 2)
+    d.starts, d.lengths = _ints(starts, "starts", 4, n + 1), _ints(lengths, "lengths", 4, n)
+    d.slots = _ints(slots, "slots", 8, m)
+    d.positions, d.owners = _ints(positions, "positions", 4, m), _ints(owners, "owners", 4, m)
+    d.info = _ints(info, "info", 8, 4)
+    d.table_stride = tables.stride(0) if n > 1 else tables.shape[1]
+    d.n_requests, d.n_free, d.page_size = n, free_pages.numel(), page_size
+    d.table_width, d.n_slots = tables.shape[1], m
+    rc = lib().bsm_paged_tables(ctypes.addressof(d), _stream(stream))
+    if rc:
+        _check(rc, "bsm_paged_tables")
+
+
+def bsm_paged_write(k, v, k_cache, v_cache, slots, stream=None):
+    """New keys and values [tokens, heads, dim] to their slots of the caches
+    [pages, page_size, heads, dim] (any strides; the last dimension contiguous)."""
+    d = PagedWriteDesc()
+    d.dtype = _paged_dtype(k, v, k_cache, v_cache)
+    d.k, d.v = _strided(k, "k", 3), _strided(v, "v", 3)
+    d.k_cache, d.v_cache = _caches(k_cache, v_cache)
+    if k.shape != v.shape or k.shape[1:] != k_cache.shape[2:]:
+        raise ValueError("k and v must be [tokens, %d, %d]" % tuple(k_cache.shape[2:]))
+    d.n_tokens, d.n_heads, d.head_dim = k.shape
+    d.slots = _ints(slots, "slots", 8, d.n_tokens)
+    d.n_pages, d.page_size = k_cache.shape[:2]
+    d.k_stride_token, d.k_stride_head, _ = k.stride()
+    d.v_stride_token, d.v_stride_head, _ = v.stride()
+    d.kv_stride_page, d.kv_stride_token, d.kv_stride_head, _ = k_cache.stride()
+    rc = lib().bsm_paged_write(ctypes.addressof(d), _stream(stream))
+    if rc:
+        _check(rc, "bsm_paged_write")
+
+
+def bsm_paged_workspace_bytes(heads_q: int, heads_kv: int, head_dim: int, max_new: int, device: int = -1) -> int:
+    n = int(lib().bsm_paged_workspace_bytes(device, heads_q, heads_kv, head_dim, max_new))
+    if n < 0:
+        raise ValueError("no workspace for %d/%d heads of %d, %d new tokens" % (heads_q, heads_kv, head_dim, max_new))
+    return n
+
+
+def bsm_paged_attention(q, k_cache, v_cache, out, starts, lengths, tables, max_new: int, scale: float, workspace,
+                        flags: int = 0, window: int = 0, lse=None, stream=None):
+    """Attention of new tokens q [tokens, heads_q, dim] over caches [pages,
+    page_size, heads_kv, dim] (any strides; the last dimension contiguous)."""
+    d = PagedDesc()
+    d.dtype = _paged_dtype(q, k_cache, v_cache, out)
+    d.q, d.out = _strided(q, "q", 3), _strided(out, "out", 3)
+    d.k_cache, d.v_cache = _caches(k_cache, v_cache)
+    if out.shape != q.shape or q.shape[2] != k_cache.shape[3]:
+        raise ValueError("out must have q's shape, and the caches its last dimension")
+    d.n_tokens, d.heads_q, d.head_dim = q.shape
+    d.n_pages, d.page_size, d.heads_kv, _ = k_cache.shape
+    n = lengths.numel()
+    if tables.element_size() != 4 or tables.is_floating_point() or tables.shape[0] < n:
+        raise ValueError("tables must hold a row of 4-byte integers for every request")
+    d.starts, d.lengths = _ints(starts, "starts", 4, n + 1), _ints(lengths, "lengths", 4, n)
+    d.tables = _strided(tables, "tables", 2)
+    d.table_stride = tables.stride(0) if n > 1 else tables.shape[1]
+    d.n_requests, d.table_width, d.max_new = n, tables.shape[1], max_new
+    d.q_stride_token, d.q_stride_head, _ = q.stride()
+    d.out_stride_token, d.out_stride_head, _ = out.stride()
+    d.kv_stride_page, d.kv_stride_token, d.kv_stride_head, _ = k_cache.stride()
+    if lse is not None:
+        if str(lse.dtype) != "torch.float32":
+            raise ValueError("lse must be float32")
+        d.lse = _dptr(lse, 4 * d.n_tokens * d.heads_q, "lse")
+    d.workspace, d.workspace_bytes = _dptr(workspace, None, "workspace"), workspace.nbytes
+    d.flags, d.window, d.scale = flags, window, scale
+    rc = lib().bsm_paged_attention(ctypes.addressof(d), _stream(stream))
+    if rc:
+        _check(rc, "bsm_paged_attention")
 
 
 class Plan:

@@ -1,0 +1,329 @@
+// bsm_paged_api.cpp -- C ABI of the paged-cache operators: argument checks,
+// how a call's work is tiled and split, the workspace's layout.
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <climits>
+#include <cmath>
+#include <cstring>
+#include <mutex>
+
+#include "bsm_internal.h"
+#include "bsm_paged.h"
+#include "bsm_trace.h"
+
+namespace bsm {
+
+int device_status_word(int device, uint32_t **out);
+
+namespace {
+
+struct PagedDev {
+    bool ready = false;
+    int n_sm = 0;
+    uint32_t *status = nullptr;
+};
+
+std::mutex g_paged_mu;
+PagedDev g_pdev[64];
+
+int paged_device(int device, PagedDev **out)
+{
+    if (device < 0 && cudaGetDevice(&device) != cudaSuccess)
+        return BSM_ERR_NO_DEVICE;
+    if (device < 0 || device >= 64)
+        return BSM_ERR_NO_DEVICE;
+    std::lock_guard<std::mutex> lk(g_paged_mu);
+    PagedDev &d = g_pdev[device];
+    if (!d.ready) {
+        if (cudaDeviceGetAttribute(&d.n_sm, cudaDevAttrMultiProcessorCount, device) != cudaSuccess)
+            return BSM_ERR_NO_DEVICE;
+        if (int rc = device_status_word(device, &d.status))
+            return rc;
+        if (int e = paged_set_smem_limit())
+            return record_cuda_error(e, "cudaFuncSetAttribute(paged)");
+        d.ready = true;
+    }
+    *out = &d;
+    return BSM_OK;
+}
+
+bool misaligned(const void *p, int64_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }
+
+// [address, end) of a strided array (non-negative strides).
+struct Span {
+    uintptr_t lo = 0, hi = 0;
+    bool meets(const Span &o) const { return lo < o.hi && o.lo < hi; }
+};
+
+Span span(const void *p, int64_t bytes) { return Span{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes}; }
+
+// Bytes from the first element to the end of the last of n0 x n1 rows of `row`
+// elements; -1 when the strides make rows overlap or overflow.
+int64_t extent2(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t row, int es)
+{
+    constexpr int64_t kMost = int64_t(1) << 60;
+    if (s0 < 0 || s1 < 0 || (n0 > 1 && s0 > kMost / n0) || (n1 > 1 && s1 > kMost / n1))
+        return -1;
+    // (rows of one token must not overlap, nor those of neighbouring tokens)
+    if ((n1 > 1 && s1 < row) || (n0 > 1 && s0 < row))
+        return -1;
+    if (n0 > 1 && n1 > 1) {
+        const bool inner1 = s0 >= (n1 - 1) * s1 + row, inner0 = s1 >= (n0 - 1) * s0 + row;
+        if (!inner1 && !inner0)
+            return -1;
+    }
+    return ((n0 - 1) * s0 + (n1 - 1) * s1 + row) * es;
+}
+
+int elem_size(int dtype) { return dtype == BSM_F32 ? 4 : 2; }
+
+// Workspace: partial outputs, maxima and sums of cut tiles, and who joins them.
+struct PagedLayout {
+    int64_t rows_o, rows_ml, rows_join, bytes;
+};
+
+PagedLayout paged_layout(int n_sm)
+{
+    PagedLayout l{};
+    auto up = [](int64_t x) { return (x + 255) & ~int64_t(255); };
+    const int64_t units = static_cast<int64_t>(n_sm) * kPagedWarps;
+    l.rows_o = 0;
+    l.rows_ml = l.rows_o + up(units * 2 * kPagedRowTile * kPagedMaxDim * 4);
+    l.rows_join = l.rows_ml + up(units * 2 * kPagedRowTile * 8);
+    l.bytes = l.rows_join + up(units * static_cast<int64_t>(sizeof(PagedJoin)));
+    return l;
+}
+
+bool paged_heads_ok(int32_t hq, int32_t hkv, int32_t d)
+{
+    return hkv >= 1 && hq >= hkv && hq % hkv == 0 && d >= 8 && d <= kPagedMaxDim && d % 8 == 0;
+}
+
+int paged_tables(const bsm_paged_tables_desc *d, bsm_stream_t stream)
+{
+    if (!d || d->n_requests < 0 || d->n_free < 0 || d->page_size < 1 || d->table_width < 1 || d->n_slots < 0 ||
+        d->table_stride < d->table_width)
+        return BSM_ERR_INVALID_ARG;
+    if (!d->starts || !d->info || (d->n_requests > 0 && (!d->cached || !d->fresh || !d->tables || !d->lengths)) ||
+        (d->n_free > 0 && !d->free_pages) || (d->n_slots > 0 && (!d->slots || !d->positions || !d->owners)))
+        return BSM_ERR_INVALID_ARG;
+    if (misaligned(d->slots, 8) || misaligned(d->info, 8) || misaligned(d->cached, 4) || misaligned(d->fresh, 4) ||
+        misaligned(d->free_pages, 4) || misaligned(d->tables, 4) || misaligned(d->starts, 4) ||
+        misaligned(d->lengths, 4) || misaligned(d->positions, 4) || misaligned(d->owners, 4))
+        return BSM_ERR_MISALIGNED;
+    const int64_t n = d->n_requests;
+    const Span in[3] = {span(d->cached, 4 * n), span(d->fresh, 4 * n), span(d->free_pages, 4ll * d->n_free)};
+    const Span out[7] = {span(d->tables, n ? 4 * ((n - 1) * d->table_stride + d->table_width) : 0),
+                         span(d->starts, 4 * (n + 1)), span(d->lengths, 4 * n), span(d->slots, 8ll * d->n_slots),
+                         span(d->positions, 4ll * d->n_slots), span(d->owners, 4ll * d->n_slots), span(d->info, 32)};
+    for (int i = 0; i < 7; ++i) {
+        for (int j = i + 1; j < 7; ++j)
+            if (out[i].meets(out[j]))
+                return BSM_ERR_INVALID_ARG;
+        for (const Span &s : in)
+            if (out[i].meets(s))
+                return BSM_ERR_INVALID_ARG;
+    }
+    PagedDev *dev = nullptr;
+    if (int rc = paged_device(-1, &dev))
+        return rc;
+    TraceRange tr("bsm_paged_tables");
+    PagedTablesArgs a{};
+    a.cached = d->cached;
+    a.fresh = d->fresh;
+    a.free_pages = d->free_pages;
+    a.tables = d->tables;
+    a.starts = d->starts;
+    a.lengths = d->lengths;
+    a.slots = d->slots;
+    a.positions = d->positions;
+    a.owners = d->owners;
+    a.info = d->info;
+    a.table_stride = d->table_stride;
+    a.n = d->n_requests;
+    a.n_free = d->n_free;
+    a.page = d->page_size;
+    a.width = d->table_width;
+    a.n_slots = d->n_slots;
+    if (int e = launch_paged_tables(a, dev->n_sm, stream))
+        return record_cuda_error(e, "paged tables launch");
+    return BSM_OK;
+}
+
+int paged_write(const bsm_paged_write_desc *d, bsm_stream_t stream)
+{
+    if (!d || d->n_tokens < 0 || d->n_heads < 1 || d->head_dim < 1 || d->page_size < 1 || d->n_pages < 0 ||
+        (d->dtype != BSM_F32 && d->dtype != BSM_BF16 && d->dtype != BSM_F16))
+        return BSM_ERR_INVALID_ARG;
+    if (d->n_tokens == 0)
+        return BSM_OK;
+    if (!d->k || !d->v || !d->k_cache || !d->v_cache || !d->slots || d->n_pages == 0)
+        return BSM_ERR_INVALID_ARG;
+    const int es = elem_size(d->dtype);
+    const int64_t row = static_cast<int64_t>(d->head_dim) * es;
+    const int64_t ks = extent2(d->n_tokens, d->k_stride_token, d->n_heads, d->k_stride_head, d->head_dim, es);
+    const int64_t vs = extent2(d->n_tokens, d->v_stride_token, d->n_heads, d->v_stride_head, d->head_dim, es);
+    const int64_t one = extent2(d->page_size, d->kv_stride_token, d->n_heads, d->kv_stride_head, d->head_dim, es);
+    if (ks < 0 || vs < 0 || one < 0 || d->kv_stride_page < 0 ||
+        (d->n_pages > 1 && (d->kv_stride_page * es < one || d->kv_stride_page > (int64_t(1) << 60) / d->n_pages)))
+        return BSM_ERR_INVALID_ARG;
+    if (row % 16 || misaligned(d->k, 16) || misaligned(d->v, 16) || misaligned(d->k_cache, 16) ||
+        misaligned(d->v_cache, 16) || misaligned(d->slots, 8) || (d->k_stride_token * es) % 16 ||
+        (d->k_stride_head * es) % 16 || (d->v_stride_token * es) % 16 || (d->v_stride_head * es) % 16 ||
+        (d->kv_stride_page * es) % 16 || (d->kv_stride_token * es) % 16 || (d->kv_stride_head * es) % 16)
+        return BSM_ERR_MISALIGNED;
+    const int64_t all = (d->n_pages - 1) * d->kv_stride_page * es + one;
+    const Span kc = span(d->k_cache, all), vc = span(d->v_cache, all), k = span(d->k, ks), v = span(d->v, vs),
+               sl = span(d->slots, 8ll * d->n_tokens);
+    // (keys and values may be interleaved in one allocation: only equal places clash)
+    if (d->k_cache == d->v_cache || kc.meets(k) || kc.meets(v) || kc.meets(sl) || vc.meets(k) || vc.meets(v) ||
+        vc.meets(sl))
+        return BSM_ERR_INVALID_ARG;
+    PagedDev *dev = nullptr;
+    if (int rc = paged_device(-1, &dev))
+        return rc;
+    TraceRange tr("bsm_paged_write");
+    PagedWriteArgs a{};
+    a.src[0] = static_cast<const unsigned char *>(d->k);
+    a.src[1] = static_cast<const unsigned char *>(d->v);
+    a.dst[0] = static_cast<unsigned char *>(d->k_cache);
+    a.dst[1] = static_cast<unsigned char *>(d->v_cache);
+    a.slots = d->slots;
+    a.src_token[0] = d->k_stride_token * es;
+    a.src_token[1] = d->v_stride_token * es;
+    a.src_head[0] = d->k_stride_head * es;
+    a.src_head[1] = d->v_stride_head * es;
+    a.dst_page = d->kv_stride_page * es;
+    a.dst_token = d->kv_stride_token * es;
+    a.dst_head = d->kv_stride_head * es;
+    a.n_slots_cache = static_cast<int64_t>(d->n_pages) * d->page_size;
+    a.n_tokens = d->n_tokens;
+    a.page = d->page_size;
+    a.heads = d->n_heads;
+    a.chunks = static_cast<int32_t>(row / 16);
+    a.status = dev->status;
+    if (int e = launch_paged_write(a, dev->n_sm, stream))
+        return record_cuda_error(e, "paged write launch");
+    return BSM_OK;
+}
+
+int paged_attention(const bsm_paged_desc *d, bsm_stream_t stream)
+{
+    if (!d || d->n_requests < 0 || d->n_tokens < 0 || d->page_size < 1 || d->n_pages < 0 || d->table_width < 1 ||
+        d->table_stride < d->table_width || d->max_new < 0 || d->window < 0 || (d->flags & ~BSM_FLAG_CAUSAL) ||
+        (d->dtype != BSM_F32 && d->dtype != BSM_BF16 && d->dtype != BSM_F16))
+        return BSM_ERR_INVALID_ARG;
+    if (!(d->scale > 0.0f) || std::isinf(d->scale) || (d->window > 0 && !(d->flags & BSM_FLAG_CAUSAL)))
+        return BSM_ERR_INVALID_ARG;
+    if (d->heads_kv < 1 || d->heads_q < d->heads_kv || d->heads_q % d->heads_kv || d->head_dim < 1)
+        return BSM_ERR_INVALID_ARG;
+    if (d->dtype == BSM_F32 || !paged_heads_ok(d->heads_q, d->heads_kv, d->head_dim))
+        return BSM_ERR_UNSUPPORTED;
+    if (d->n_requests == 0 || d->n_tokens == 0)
+        return BSM_OK;
+    if (!d->q || !d->k_cache || !d->v_cache || !d->out || !d->starts || !d->lengths || !d->tables || !d->workspace ||
+        d->n_pages == 0)
+        return BSM_ERR_INVALID_ARG;
+    const int64_t qs = extent2(d->n_tokens, d->q_stride_token, d->heads_q, d->q_stride_head, d->head_dim, 2);
+    const int64_t os = extent2(d->n_tokens, d->out_stride_token, d->heads_q, d->out_stride_head, d->head_dim, 2);
+    const int64_t one = extent2(d->page_size, d->kv_stride_token, d->heads_kv, d->kv_stride_head, d->head_dim, 2);
+    if (qs < 0 || os < 0 || one < 0 || d->kv_stride_page < 0 ||
+        (d->n_pages > 1 && (d->kv_stride_page * 2 < one || d->kv_stride_page > (int64_t(1) << 60) / d->n_pages)))
+        return BSM_ERR_INVALID_ARG;
+    if (misaligned(d->q, 16) || misaligned(d->k_cache, 16) || misaligned(d->v_cache, 16) || misaligned(d->out, 16) ||
+        misaligned(d->lse, 4) || misaligned(d->starts, 4) || misaligned(d->lengths, 4) || misaligned(d->tables, 4) ||
+        misaligned(d->workspace, 256) || d->q_stride_token % 8 || d->q_stride_head % 8 || d->out_stride_token % 8 ||
+        d->out_stride_head % 8 || d->kv_stride_page % 8 || d->kv_stride_token % 8 || d->kv_stride_head % 8)
+        return BSM_ERR_MISALIGNED;
+    const int64_t all = (d->n_pages - 1) * d->kv_stride_page * 2 + one, n = d->n_requests;
+    const Span o = span(d->out, os), w = span(d->workspace, d->workspace_bytes),
+               ls = span(d->lse, d->lse ? 4ll * d->n_tokens * d->heads_q : 0);
+    const Span in[6] = {span(d->q, qs), span(d->k_cache, all), span(d->v_cache, all), span(d->starts, 4 * (n + 1)),
+                        span(d->lengths, 4 * n), span(d->tables, 4 * ((n - 1) * d->table_stride + d->table_width))};
+    for (const Span &s : in)
+        if (o.meets(s) || w.meets(s) || ls.meets(s))
+            return BSM_ERR_INVALID_ARG;
+    if (o.meets(w) || o.meets(ls) || w.meets(ls))
+        return BSM_ERR_INVALID_ARG;
+    PagedDev *dev = nullptr;
+    if (int rc = paged_device(-1, &dev))
+        return rc;
+    const PagedLayout lay = paged_layout(dev->n_sm);
+    if (d->workspace_bytes < lay.bytes)
+        return BSM_ERR_INVALID_ARG;
+    TraceRange tr("bsm_paged_attention");
+    const bool f16 = d->dtype == BSM_F16;
+    PagedArgs a{};
+    a.q = d->q;
+    a.k = d->k_cache;
+    a.v = d->v_cache;
+    a.out = d->out;
+    a.lse = d->lse;
+    a.q_token = d->q_stride_token;
+    a.q_head = d->q_stride_head;
+    a.out_token = d->out_stride_token;
+    a.out_head = d->out_stride_head;
+    a.kv_page = d->kv_stride_page;
+    a.kv_token = d->kv_stride_token;
+    a.kv_head = d->kv_stride_head;
+    a.starts = d->starts;
+    a.lengths = d->lengths;
+    a.tables = d->tables;
+    a.table_stride = d->table_stride;
+    a.n = d->n_requests;
+    a.n_tokens = d->n_tokens;
+    a.heads_q = d->heads_q;
+    a.heads_kv = d->heads_kv;
+    a.d = d->head_dim;
+    a.page = d->page_size;
+    a.n_pages = d->n_pages;
+    a.width = d->table_width;
+    a.causal = (d->flags & BSM_FLAG_CAUSAL) ? 1 : 0;
+    a.window = d->window;
+    a.scale_log2 = d->scale * 1.4426950408889634f;
+    a.group = d->heads_q / d->heads_kv;
+    a.status = dev->status;
+    unsigned char *ws = static_cast<unsigned char *>(d->workspace);
+    a.subs = (a.group + kPagedRowTile - 1) / kPagedRowTile;
+    a.sub = (a.group + a.subs - 1) / a.subs;
+    const int64_t rows = static_cast<int64_t>(d->max_new) * a.sub;
+    a.tok = std::max(1, (rows <= 16 ? 16 : kPagedRowTile) / a.sub);
+    a.rows_min = 0;
+    a.rows_max = INT32_MAX;
+    a.units = dev->n_sm * kPagedWarps;
+    a.min_steps = a.d <= 64 ? 1 : 2;
+    a.part_o = reinterpret_cast<float *>(ws + lay.rows_o);
+    a.part_ml = reinterpret_cast<float *>(ws + lay.rows_ml);
+    a.join = reinterpret_cast<PagedJoin *>(ws + lay.rows_join);
+    if (int e = launch_paged_rows(a, f16, dev->n_sm, stream))
+        return record_cuda_error(e, "paged attention launch");
+    if (int e = launch_paged_join(a, f16, kPagedRowTile, stream))
+        return record_cuda_error(e, "paged attention join launch");
+    return BSM_OK;
+}
+
+}  // namespace
+}  // namespace bsm
+
+extern "C" {
+
+int bsm_paged_tables(const bsm_paged_tables_desc *d, bsm_stream_t stream) { return bsm::paged_tables(d, stream); }
+
+int bsm_paged_write(const bsm_paged_write_desc *d, bsm_stream_t stream) { return bsm::paged_write(d, stream); }
+
+int bsm_paged_attention(const bsm_paged_desc *d, bsm_stream_t stream) { return bsm::paged_attention(d, stream); }
+
+int64_t bsm_paged_workspace_bytes(int device, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t max_new)
+{
+    if (max_new < 0 || !bsm::paged_heads_ok(heads_q, heads_kv, head_dim))
+        return -1;
+    bsm::PagedDev *dev = nullptr;
+    if (bsm::paged_device(device, &dev))
+        return -1;
+    return bsm::paged_layout(dev->n_sm).bytes;
+}
+
+}  // extern "C"

@@ -1,0 +1,466 @@
+// bsm_paged_rows.cu -- attention of a few new tokens over a paged cache:
+// tiles of at most 32 rows (tokens times the query heads that share a
+// key/value head), the keys split over every warp of the device.
+//
+//   s = scale q k^T,  p = exp(s - m),  o = sum p v / sum p   (m a running maximum)
+//
+// Bound: the cache's bytes.  A row of 16 query heads costs one key 4 D
+// operations a byte pair, far below what mma.sync gives, so the kernel is
+// built for loads: every warp is on its own, with its own range of the work,
+// its own three stages of 16 keys (8 KiB of K and V at D = 128) filled by
+// 16-byte asynchronous copies, its own running maximum and sum; no barrier of
+// the block after the work is laid out.  24 stages an SM keep 128 to 192 KiB
+// in flight.
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "bsm_paged_dev.h"
+
+namespace bsm {
+namespace {
+
+constexpr int kRowThreads = kPagedWarps * 32;
+constexpr int kRowStages = 3;
+constexpr int kStageBytes = 8192;                       // of one warp: K and V of a step
+
+// keys of a step: 16 rows of 256 bytes, or 32 of 128
+template <int DP> struct RowShape {
+    static constexpr int kKeys = DP == 128 ? 16 : 32;
+    static constexpr int kRowBytes = DP * 2;
+    static constexpr int kChunks = DP / 8;              // 16-byte pieces of a row
+};
+
+struct RowSmem {
+    PagedPrefix<kRowThreads> prefix;
+};
+constexpr int kRowHeader = 4096;
+static_assert(sizeof(RowSmem) <= kRowHeader, "row header");
+constexpr int kRowSmem = kRowHeader + kPagedWarps * kRowStages * kStageBytes;
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, uint32_t bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t *r)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t addr, uint32_t *r)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+}
+
+// d += a b: 16 x 16 times 16 x 8, fp32 sums
+template <bool kF16> __device__ __forceinline__ void mma16(float *d, const uint32_t *a, uint32_t b0, uint32_t b1)
+{
+    if (kF16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+                     "{%0, %1, %2, %3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, "
+                     "%9}, {%0, %1, %2, %3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Where the rows of a tile come from and go to.
+struct RowTile {
+    int32_t token, head, tokens, heads; // first token, first query head, tokens, heads
+    int32_t pos;                        // position of the first token
+};
+
+__device__ __forceinline__ RowTile row_tile(const PagedArgs &a, const PagedSeq &s, const PagedPiece &p)
+{
+    RowTile t;
+    const int32_t kvh = p.head / a.subs, sub = p.head - kvh * a.subs;
+    t.token = s.t0 + p.tile * a.tok;
+    t.tokens = s.m - p.tile * a.tok < a.tok ? s.m - p.tile * a.tok : a.tok;
+    t.head = kvh * a.group + sub * a.sub;
+    t.heads = a.group - sub * a.sub < a.sub ? a.group - sub * a.sub : a.sub;
+    t.pos = s.L - s.m + p.tile * a.tok;
+    return t;
+}
+
+// DP: the head size padded to 64 or 128; MT: 16-row blocks of a tile.
+template <int DP, int MT, bool kF16>
+__global__ void __launch_bounds__(kRowThreads, 1) paged_rows(const PagedArgs a)
+{
+    using Shape = RowShape<DP>;
+    constexpr int kKeys = Shape::kKeys, kChunks = Shape::kChunks, kRB = Shape::kRowBytes;
+    constexpr int kSubs = kKeys / 16;
+    constexpr int kHalf = kKeys * kRB;                  // V behind K in a stage
+    static_assert(2 * kHalf == kStageBytes, "stage");
+    extern __shared__ __align__(128) unsigned char raw[];
+    RowSmem &sm = *reinterpret_cast<RowSmem *>(raw);
+    const int lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
+    const PagedLine<kKeys> line(a);
+    paged_prefix<kKeys, kRowThreads>(line, sm.prefix, blockIdx.x == 0);
+    const int64_t W = sm.prefix.pre[kRowThreads];
+    const PagedCut cut(a, W);
+    // neighbouring units on different SMs: a small batch spreads over the device
+    const int32_t unit = warp * gridDim.x + blockIdx.x;
+    if (lane == 0)
+        a.join[unit].count = 0;
+    if (W == 0 || unit >= cut.units)
+        return;
+    const int64_t begin = cut.begin(unit), end = cut.begin(unit + 1);
+    const int32_t total = static_cast<int32_t>(end - begin);
+    PagedWalk<kKeys> fetch(line, sm.prefix, begin, end), walk(line, sm.prefix, begin, end);
+
+    const uint32_t stages = pg_saddr(raw) + kRowHeader + warp * (kRowStages * kStageBytes);
+    const unsigned char *kbase = static_cast<const unsigned char *>(a.k), *vbase = static_cast<const unsigned char *>(a.v);
+
+    // ---- loads: one step of kKeys keys at a time, in the order of the walk
+    PagedPiece fp{};
+    int32_t fleft = 0, fstep = 0;       // steps left of the piece being fetched, its next step
+    int64_t fhead = 0;
+    // byte offset of this lane's key of the next step (-1: none), read one step ahead
+    auto key_offset = [&]() -> int64_t {
+        const int32_t key = fstep * kKeys + (lane & (kKeys - 1));
+        if (key < fp.keys.lo || key >= fp.keys.hi)
+            return -1;
+        const int32_t e = key / a.page;
+        const int32_t page = a.tables[fp.r * a.table_stride + e];
+        if (page < 0 || page >= a.n_pages) {
+            atomicOr(a.status, BSM_DEV_BOUNDS);
+            return -1;
+        }
+        return 2 * (page * a.kv_page + (key - e * a.page) * a.kv_token + fhead);
+    };
+    auto advance = [&]() {
+        if (fleft == 0) {
+            if (!fetch.next(fp))
+                return;
+            fleft = fp.steps;
+            fstep = fp.first;
+            fhead = (fp.head / a.subs) * a.kv_head;
+        }
+    };
+    int64_t off = -1;
+    int32_t issued = 0;
+    advance();
+    off = key_offset();
+    auto issue = [&]() {
+        if (issued < total) {
+            const uint32_t st = stages + (issued % kRowStages) * kStageBytes;
+            constexpr int kRowsAtOnce = 32 / kChunks;
+            const int c = lane % kChunks;
+#pragma unroll
+            for (int i = 0; i < kKeys / kRowsAtOnce; ++i) {
+                const int row = i * kRowsAtOnce + lane / kChunks;
+                const int64_t o = __shfl_sync(0xffffffffu, off, row);
+                const bool in = o >= 0 && c * 8 < a.d;
+                const int64_t at = in ? o + c * 16 : 0;
+                const uint32_t dst = st + row * kRB + ((c ^ (row & 7)) << 4);
+                cp_async16(dst, kbase + at, in ? 16u : 0u);
+                cp_async16(dst + kHalf, vbase + at, in ? 16u : 0u);
+            }
+            ++issued;
+            --fleft;
+            ++fstep;
+            if (issued < total) {
+                advance();
+                off = key_offset();
+            }
+        }
+        cp_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < kRowStages; ++i)
+        issue();
+
+    // ---- one piece after another
+    PagedPiece p{};
+    int32_t done = 0;
+    while (walk.next(p)) {
+        const RowTile t = row_tile(a, walk.s, p);
+        const int32_t rows = t.tokens * a.sub;
+        // this lane's rows: lane / 4 and lane / 4 + 8 of each 16-row block
+        int32_t lo[MT][2], hi[MT][2];
+        uint32_t q[MT][DP / 16][4];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int row = mt * 16 + i * 8 + lane / 4;
+                const int32_t tt = row / a.sub, h = row - tt * a.sub;
+                const bool live = row < rows && h < t.heads;
+                const int32_t pos = t.pos + tt;
+                hi[mt][i] = !live ? 0 : a.causal ? (pos + 1 < p.keys.hi ? pos + 1 : p.keys.hi) : p.keys.hi;
+                lo[mt][i] = a.window && pos - a.window + 1 > 0 ? pos - a.window + 1 : 0;
+                const uint32_t *src = reinterpret_cast<const uint32_t *>(
+                    static_cast<const unsigned char *>(a.q) + 2 * ((t.token + tt) * a.q_token + (t.head + h) * a.q_head));
+#pragma unroll
+                for (int k = 0; k < DP / 16; ++k) {
+                    const int d0 = k * 16 + (lane & 3) * 2;
+                    q[mt][k][i] = live && d0 < a.d ? src[d0 / 2] : 0u;
+                    q[mt][k][i + 2] = live && d0 + 8 < a.d ? src[d0 / 2 + 4] : 0u;
+                }
+            }
+        }
+        float o[MT][DP / 8][4];
+        float m[MT][2], l[MT][2];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+            for (int n = 0; n < DP / 8; ++n)
+                o[mt][n][0] = o[mt][n][1] = o[mt][n][2] = o[mt][n][3] = 0.0f;
+            m[mt][0] = m[mt][1] = -INFINITY;
+            l[mt][0] = l[mt][1] = 0.0f;
+        }
+        for (int32_t st = 0; st < p.steps; ++st) {
+            cp_wait<kRowStages - 1>();
+            __syncwarp();
+            const uint32_t kst = stages + (done % kRowStages) * kStageBytes;
+#pragma unroll
+            for (int sb = 0; sb < kSubs; ++sb) {
+                const int32_t key0 = (p.first + st) * kKeys + sb * 16;
+                float s[MT][2][4];
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        s[mt][0][j] = s[mt][1][j] = 0.0f;
+                // keys 0-7 / 8-15 and halves of 8 columns: matrices of lanes 0-7, 8-15, 16-23, 24-31
+                const int krow = sb * 16 + (lane & 7) + ((lane >> 4) << 3);
+#pragma unroll
+                for (int k = 0; k < DP / 16; ++k) {
+                    uint32_t b[4];
+                    ldsm4(kst + krow * kRB + (((2 * k + ((lane >> 3) & 1)) ^ (krow & 7)) << 4), b);
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) {
+                        if (mt * 16 < rows) {
+                            mma16<kF16>(s[mt][0], q[mt][k], b[0], b[1]);
+                            mma16<kF16>(s[mt][1], q[mt][k], b[2], b[3]);
+                        }
+                    }
+                }
+                uint32_t pa[MT][4];
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    if (mt * 16 >= rows)
+                        continue;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        float x[4];
+                        float top = m[mt][i];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int32_t key = key0 + (j >> 1) * 8 + (lane & 3) * 2 + (j & 1);
+                            const float v = s[mt][j >> 1][i * 2 + (j & 1)] * a.scale_log2;
+                            x[j] = key >= lo[mt][i] && key < hi[mt][i] ? v : -INFINITY;
+                            top = fmaxf(top, x[j]);
+                        }
+                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                        // a row that has seen no key yet: exponents against 0, all of them -inf
+                        const float ref = top == -INFINITY ? 0.0f : top;
+                        if (__any_sync(0xffffffffu, top != m[mt][i])) {
+                            const float f = pg_exp2(m[mt][i] - ref);
+                            l[mt][i] *= f;
+#pragma unroll
+                            for (int n = 0; n < DP / 8; ++n) {
+                                o[mt][n][2 * i] *= f;
+                                o[mt][n][2 * i + 1] *= f;
+                            }
+                        }
+                        m[mt][i] = top;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            x[j] = pg_exp2(x[j] - ref);
+                            l[mt][i] += x[j];
+                        }
+                        pa[mt][i] = pg_pack<kF16>(x[0], x[1]);
+                        pa[mt][i + 2] = pg_pack<kF16>(x[2], x[3]);
+                    }
+                }
+                const int vrow = sb * 16 + (lane & 15);
+#pragma unroll
+                for (int n = 0; n < DP / 16; ++n) {
+                    uint32_t b[4];
+                    ldsm4t(kst + kHalf + vrow * kRB + (((2 * n + (lane >> 4)) ^ (vrow & 7)) << 4), b);
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) {
+                        if (mt * 16 < rows) {
+                            mma16<kF16>(o[mt][2 * n], pa[mt], b[0], b[1]);
+                            mma16<kF16>(o[mt][2 * n + 1], pa[mt], b[2], b[3]);
+                        }
+                    }
+                }
+            }
+            __syncwarp();
+            ++done;
+            issue();
+        }
+        // ---- the tile's output, or this unit's part of it
+        const bool whole = p.starts && p.ends;
+        const int32_t slot = 2 * unit + (p.starts ? 1 : 0);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                float sum = l[mt][i];
+                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+                const int row = mt * 16 + i * 8 + lane / 4;
+                const int32_t tt = row / a.sub, h = row - tt * a.sub;
+                if (row >= rows || h >= t.heads)
+                    continue;
+                if (whole) {
+                    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+                    uint32_t *dst = reinterpret_cast<uint32_t *>(
+                        static_cast<unsigned char *>(a.out) +
+                        2 * ((t.token + tt) * a.out_token + (t.head + h) * a.out_head));
+#pragma unroll
+                    for (int n = 0; n < DP / 8; ++n)
+                        if (n * 8 < a.d)
+                            dst[n * 4 + (lane & 3)] =
+                                pg_pack<kF16>(o[mt][n][2 * i] * inv, o[mt][n][2 * i + 1] * inv);
+                    if (a.lse && (lane & 3) == 0)
+                        a.lse[static_cast<int64_t>(t.token + tt) * a.heads_q + t.head + h] =
+                            sum == 0.0f ? -INFINITY : (m[mt][i] + log2f(sum)) * 0.6931471805599453f;
+                } else {
+                    float *dst = a.part_o + (static_cast<int64_t>(slot) * kPagedRowTile + row) * kPagedMaxDim;
+#pragma unroll
+                    for (int n = 0; n < DP / 8; ++n)
+                        *reinterpret_cast<float2 *>(dst + n * 8 + (lane & 3) * 2) =
+                            make_float2(o[mt][n][2 * i], o[mt][n][2 * i + 1]);
+                    if ((lane & 3) == 0)
+                        *reinterpret_cast<float2 *>(a.part_ml + (static_cast<int64_t>(slot) * kPagedRowTile + row) * 2) =
+                            make_float2(m[mt][i], sum);
+                }
+            }
+        }
+        if (p.starts && !p.ends && lane == 0) {
+            PagedJoin j{};
+            j.token = t.token;
+            j.head = t.head;
+            j.tokens = t.tokens;
+            j.heads = t.heads;
+            j.count = cut.owner(p.tile_end - 1) - unit + 1;
+            a.join[unit] = j;
+        }
+    }
+    cp_wait<0>();
+}
+
+// Joins the parts of every cut tile: with M the largest of the parts' maxima,
+// o = sum 2^(m_i - M) o_i / sum 2^(m_i - M) l_i, in unit order.  One CTA a unit
+// (most find nothing to do and leave), one warp a row, 16 bytes a lane.
+constexpr int kJoinThreads = 256;
+
+template <bool kF16>
+__global__ void __launch_bounds__(kJoinThreads) paged_join(const PagedArgs a, const int tile_rows)
+{
+    const int unit = blockIdx.x;
+    const PagedJoin j = a.join[unit];
+    if (j.count <= 0)
+        return;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int rows = j.tokens * a.sub;
+    for (int row = warp + static_cast<int>(blockIdx.y) * (kJoinThreads / 32); row < rows;
+         row += static_cast<int>(gridDim.y) * (kJoinThreads / 32)) {
+        const int tt = row / a.sub, h = row - tt * a.sub;
+        if (h >= j.heads)
+            continue;
+        float top = -INFINITY;
+        for (int i = lane; i < j.count; i += 32) {
+            const int64_t slot = i == 0 ? 2 * unit + 1 : 2 * (unit + i);
+            top = fmaxf(top, a.part_ml[(slot * tile_rows + row) * 2]);
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1)
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const float ref = top == -INFINITY ? 0.0f : top;
+        float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        float sum = 0.0f;
+#pragma unroll 8
+        for (int i = 0; i < j.count; ++i) {
+            const int64_t slot = i == 0 ? 2 * unit + 1 : 2 * (unit + i);
+            const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + (slot * tile_rows + row) * 2);
+            const float4 v = *reinterpret_cast<const float4 *>(a.part_o + (slot * tile_rows + row) * kPagedMaxDim + lane * 4);
+            const float f = pg_exp2(ml.x - ref);
+            sum += f * ml.y;
+            acc.x += f * v.x;
+            acc.y += f * v.y;
+            acc.z += f * v.z;
+            acc.w += f * v.w;
+        }
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        if (lane * 4 < a.d) {
+            uint2 w;
+            w.x = pg_pack<kF16>(acc.x * inv, acc.y * inv);
+            w.y = pg_pack<kF16>(acc.z * inv, acc.w * inv);
+            *reinterpret_cast<uint2 *>(static_cast<unsigned char *>(a.out) +
+                                       2 * ((j.token + tt) * a.out_token + (j.head + h) * a.out_head + lane * 4)) = w;
+        }
+        if (a.lse && lane == 0)
+            a.lse[static_cast<int64_t>(j.token + tt) * a.heads_q + j.head + h] =
+                sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+    }
+}
+
+template <int DP, bool kF16> int launch_rows(const PagedArgs &a, int grid, cudaStream_t st)
+{
+    if (a.tok * a.sub <= 16)
+        paged_rows<DP, 1, kF16><<<grid, kRowThreads, kRowSmem, st>>>(a);
+    else
+        paged_rows<DP, 2, kF16><<<grid, kRowThreads, kRowSmem, st>>>(a);
+    return static_cast<int>(cudaGetLastError());
+}
+
+}  // namespace
+
+int launch_paged_rows(const PagedArgs &a, bool f16, int grid, void *stream)
+{
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (a.d <= 64)
+        return f16 ? launch_rows<64, true>(a, grid, st) : launch_rows<64, false>(a, grid, st);
+    return f16 ? launch_rows<128, true>(a, grid, st) : launch_rows<128, false>(a, grid, st);
+}
+
+int launch_paged_join(const PagedArgs &a, bool f16, int tile_rows, void *stream)
+{
+    const int rows = a.tok * a.sub;
+    const dim3 grid(a.units, rows <= 64 ? 1 : 4);
+    if (f16)
+        paged_join<true><<<grid, kJoinThreads, 0, static_cast<cudaStream_t>(stream)>>>(a, tile_rows);
+    else
+        paged_join<false><<<grid, kJoinThreads, 0, static_cast<cudaStream_t>(stream)>>>(a, tile_rows);
+    return static_cast<int>(cudaGetLastError());
+}
+
+int paged_tables_set_smem();
+
+int paged_set_smem_limit()
+{
+    int e = paged_tables_set_smem();
+    auto set = [&](const void *f) {
+        if (!e)
+            e = static_cast<int>(cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowSmem));
+    };
+    set(reinterpret_cast<const void *>(&paged_rows<64, 1, false>));
+    set(reinterpret_cast<const void *>(&paged_rows<64, 2, false>));
+    set(reinterpret_cast<const void *>(&paged_rows<64, 1, true>));
+    set(reinterpret_cast<const void *>(&paged_rows<64, 2, true>));
+    set(reinterpret_cast<const void *>(&paged_rows<128, 1, false>));
+    set(reinterpret_cast<const void *>(&paged_rows<128, 2, false>));
+    set(reinterpret_cast<const void *>(&paged_rows<128, 1, true>));
+    set(reinterpret_cast<const void *>(&paged_rows<128, 2, true>));
+    return e;
+}
+
+}  // namespace bsm
