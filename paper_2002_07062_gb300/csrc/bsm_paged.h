@@ -47,7 +47,7 @@ struct PagedArgs {
     int32_t group;                                  // query heads of a key/value head
     int32_t subs, sub;                              // head groups of one key/value head, heads of each
     int32_t tok;                                    // tokens of a tile
-    int32_t rows_min, rows_max;                     // takes requests of rows_min < tokens * sub <= rows_max
+    int32_t rows_min, rows_max;                     // takes requests of rows_min < tokens * group <= rows_max
     int32_t units, min_steps;                       // units at most; key steps of a unit at least
     float *part_o;                                  // units x 2 x tile rows x padded head size
     float *part_ml;                                 // units x 2 x tile rows x 2
@@ -66,11 +66,15 @@ struct PagedJoin {
 constexpr int kPagedWarps = 8;                      // of the row kernel
 constexpr int kPagedRowTile = 32;                   // most rows of its tiles
 constexpr int kPagedMaxDim = 128;
+constexpr int kPagedTileRows = 256;                 // of the tile kernel: two blocks of 128
+constexpr int kPagedTileKeys = 128;                 // keys of its steps
 
 int launch_paged_tables(const PagedTablesArgs &a, int n_sm, void *stream);
 int launch_paged_write(const PagedWriteArgs &a, int n_sm, void *stream);
 int launch_paged_rows(const PagedArgs &a, bool f16, int grid, void *stream);
 int launch_paged_join(const PagedArgs &a, bool f16, int tile_rows, void *stream);
+// maps: CUtensorMaps of q, k, v (host); box: rows of one copy of k and v
+int launch_paged_tiles(const void *maps, const PagedArgs &a, bool f16, int box, void *stream);
 int paged_set_smem_limit();
 
 }  // namespace bsm

@@ -26,8 +26,13 @@ struct PagedDev {
     uint32_t *status = nullptr;
 };
 
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                 const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
 std::mutex g_paged_mu;
 PagedDev g_pdev[64];
+EncodeTiled g_paged_encode = nullptr;
 
 int paged_device(int device, PagedDev **out)
 {
@@ -42,6 +47,15 @@ int paged_device(int device, PagedDev **out)
             return BSM_ERR_NO_DEVICE;
         if (int rc = device_status_word(device, &d.status))
             return rc;
+        if (!g_paged_encode) {
+            void *fn = nullptr;
+            cudaDriverEntryPointQueryResult q{};
+            if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q) !=
+                    cudaSuccess ||
+                !fn)
+                return BSM_ERR_NO_DEVICE;
+            g_paged_encode = reinterpret_cast<EncodeTiled>(fn);
+        }
         if (int e = paged_set_smem_limit())
             return record_cuda_error(e, "cudaFuncSetAttribute(paged)");
         d.ready = true;
@@ -82,7 +96,7 @@ int elem_size(int dtype) { return dtype == BSM_F32 ? 4 : 2; }
 
 // Workspace: partial outputs, maxima and sums of cut tiles, and who joins them.
 struct PagedLayout {
-    int64_t rows_o, rows_ml, rows_join, bytes;
+    int64_t rows_o, rows_ml, rows_join, tiles_o, tiles_ml, tiles_join, bytes;
 };
 
 PagedLayout paged_layout(int n_sm)
@@ -93,8 +107,39 @@ PagedLayout paged_layout(int n_sm)
     l.rows_o = 0;
     l.rows_ml = l.rows_o + up(units * 2 * kPagedRowTile * kPagedMaxDim * 4);
     l.rows_join = l.rows_ml + up(units * 2 * kPagedRowTile * 8);
-    l.bytes = l.rows_join + up(units * static_cast<int64_t>(sizeof(PagedJoin)));
+    l.tiles_o = l.rows_join + up(units * static_cast<int64_t>(sizeof(PagedJoin)));
+    l.tiles_ml = l.tiles_o + up(static_cast<int64_t>(n_sm) * 2 * kPagedTileRows * kPagedMaxDim * 4);
+    l.tiles_join = l.tiles_ml + up(static_cast<int64_t>(n_sm) * 2 * kPagedTileRows * 8);
+    l.bytes = l.tiles_join + up(static_cast<int64_t>(n_sm) * static_cast<int64_t>(sizeof(PagedJoin)));
     return l;
+}
+
+// A tensor map of 16-bit elements with rows of 64 columns and the 128-byte
+// swizzle: dims[0] elements contiguous, strides of the others in elements.
+// False where the encoder refuses (a stride past its range).
+bool paged_map(CUtensorMap *m, bool f16, const void *base, int rank, const int64_t *dims, const int64_t *strides,
+               const int *box)
+{
+    cuuint64_t d[4], s[3];
+    cuuint32_t b[4], e[4] = {1u, 1u, 1u, 1u};
+    for (int i = 0; i < rank; ++i) {
+        d[i] = static_cast<cuuint64_t>(dims[i]);
+        b[i] = static_cast<cuuint32_t>(box[i]);
+        // (the stride of a dimension of one entry is never used: any valid one will do)
+        if (i > 0)
+            s[i - 1] = static_cast<cuuint64_t>(dims[i] > 1 ? strides[i] * 2 : 16);
+    }
+    return g_paged_encode(m, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+                          static_cast<cuuint32_t>(rank), const_cast<void *>(base), d, s, b, e,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Heads of one key/value head's group that share a tile of at most `rows` rows.
+void split_group(PagedArgs &a, int rows)
+{
+    a.subs = (a.group + rows - 1) / rows;
+    a.sub = (a.group + a.subs - 1) / a.subs;
 }
 
 bool paged_heads_ok(int32_t hq, int32_t hkv, int32_t d)
@@ -287,12 +332,31 @@ int paged_attention(const bsm_paged_desc *d, bsm_stream_t stream)
     a.group = d->heads_q / d->heads_kv;
     a.status = dev->status;
     unsigned char *ws = static_cast<unsigned char *>(d->workspace);
-    a.subs = (a.group + kPagedRowTile - 1) / kPagedRowTile;
-    a.sub = (a.group + a.subs - 1) / a.subs;
+    // Requests of more than 32 rows (new tokens times the heads that share a
+    // key/value head) go to the tile kernel, where pages are whole groups of
+    // eight rows (the copies' swizzle).
+    int box = 1;
+    while (box < kPagedTileKeys && d->page_size % (2 * box) == 0)
+        box *= 2;
+    PagedArgs b = a;
+    split_group(b, kPagedTileRows / 2);
+    b.tok = 2 * (kPagedTileRows / 2 / b.sub);
+    CUtensorMap maps[3];
+    bool tiles = box >= 8 && static_cast<int64_t>(d->max_new) * a.group > kPagedRowTile;
+    if (tiles) {
+        const int64_t qd[3] = {d->head_dim, d->heads_q, d->n_tokens}, qst[3] = {1, d->q_stride_head, d->q_stride_token};
+        const int qb[3] = {64, b.sub, b.tok / 2};
+        const int64_t kd[4] = {d->head_dim, d->page_size, d->heads_kv, d->n_pages};
+        const int64_t kst[4] = {1, d->kv_stride_token, d->kv_stride_head, d->kv_stride_page};
+        const int kb[4] = {64, box, 1, 1};
+        tiles = paged_map(&maps[0], f16, d->q, 3, qd, qst, qb) && paged_map(&maps[1], f16, d->k_cache, 4, kd, kst, kb) &&
+                paged_map(&maps[2], f16, d->v_cache, 4, kd, kst, kb);
+    }
+    split_group(a, kPagedRowTile);
     const int64_t rows = static_cast<int64_t>(d->max_new) * a.sub;
     a.tok = std::max(1, (rows <= 16 ? 16 : kPagedRowTile) / a.sub);
     a.rows_min = 0;
-    a.rows_max = INT32_MAX;
+    a.rows_max = tiles ? kPagedRowTile : INT32_MAX;
     a.units = dev->n_sm * kPagedWarps;
     a.min_steps = a.d <= 64 ? 1 : 2;
     a.part_o = reinterpret_cast<float *>(ws + lay.rows_o);
@@ -302,6 +366,17 @@ int paged_attention(const bsm_paged_desc *d, bsm_stream_t stream)
         return record_cuda_error(e, "paged attention launch");
     if (int e = launch_paged_join(a, f16, kPagedRowTile, stream))
         return record_cuda_error(e, "paged attention join launch");
+    if (tiles) {
+        b.rows_min = kPagedRowTile;
+        b.rows_max = INT32_MAX;
+        b.units = dev->n_sm;
+        b.min_steps = 1;
+        b.part_o = reinterpret_cast<float *>(ws + lay.tiles_o);
+        b.part_ml = reinterpret_cast<float *>(ws + lay.tiles_ml);
+        b.join = reinterpret_cast<PagedJoin *>(ws + lay.tiles_join);
+        if (int e = launch_paged_tiles(maps, b, f16, box, stream))
+            return record_cuda_error(e, "paged attention tile launch");
+    }
     return BSM_OK;
 }
 

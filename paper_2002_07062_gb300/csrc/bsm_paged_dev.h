@@ -133,7 +133,7 @@ template <int kStep> struct PagedLine {
         s.t0 = t0;
         s.m = t1 - t0;
         s.L = L;
-        const int64_t rows = static_cast<int64_t>(s.m) * a.sub;
+        const int64_t rows = static_cast<int64_t>(s.m) * a.group;
         if (s.m == 0 || rows <= a.rows_min || rows > a.rows_max) {
             s.m = 0;
             return s;
@@ -220,14 +220,14 @@ struct PagedPiece {
     PagedRange keys;                    // keys the tile sees
     int32_t first, steps;               // first step (of kStep keys, from key 0), steps of this piece
     bool starts, ends;                  // the piece holds the tile's first, last step
-    int64_t tile_begin, tile_end;       // the tile on the line
+    int64_t tile_end;                   // end of the tile on the line
 };
 
+// The closed form finds the range's first tile; from there the walk counts on.
 template <int kStep> struct PagedWalk {
     const PagedLine<kStep> &line;
     int64_t x, end;                     // next step, end of the unit's range
-    int64_t base = 0;                   // steps before request r
-    int32_t r = 0;
+    int32_t r = 0, head = 0, tile = 0, at = 0;
     PagedSeq s;
 
     template <int kThreads>
@@ -244,45 +244,56 @@ template <int kStep> struct PagedWalk {
             else
                 hi = mid;
         }
-        base = p.pre[lo];
+        int64_t o = x - p.pre[lo];
         r = lo * ((l.a.n + kThreads - 1) / kThreads);
         s = l.seq(r, false);
+        while (o >= line.all_steps(s) && r + 1 < l.a.n) {       // (the line's end is past x: some request holds it)
+            o -= line.all_steps(s);
+            s = line.seq(++r, false);
+        }
+        head = static_cast<int32_t>(o / s.steps);
+        o -= head * s.steps;
+        int32_t t0 = 0, t1 = s.tiles;
+        while (t1 - t0 > 1) {
+            const int32_t mid = (t0 + t1) >> 1;
+            if (line.before(s, mid) <= o)
+                t0 = mid;
+            else
+                t1 = mid;
+        }
+        tile = t0;
+        at = static_cast<int32_t>(o - line.before(s, t0));
     }
 
     __device__ bool next(PagedPiece &pc)
     {
         if (x >= end)
             return false;
-        while (x - base >= line.all_steps(s)) {     // (the line's end is past x: some request holds it)
-            base += line.all_steps(s);
-            s = line.seq(++r, false);
+        if (tile == s.tiles) {
+            tile = 0;
+            if (++head == line.a.heads_kv * line.a.subs) {
+                head = 0;
+                do {
+                    if (++r >= line.a.n)
+                        return false;
+                    s = line.seq(r, false);
+                } while (s.m == 0);
+            }
         }
-        const int64_t o = x - base;
-        const int32_t head = static_cast<int32_t>(o / s.steps);
-        const int64_t in = o - head * s.steps;
-        int32_t lo = 0, hi = s.tiles;
-        while (hi - lo > 1) {
-            const int32_t mid = (lo + hi) >> 1;
-            if (line.before(s, mid) <= in)
-                lo = mid;
-            else
-                hi = mid;
-        }
-        const int64_t first = line.before(s, lo);
         pc.r = r;
         pc.head = head;
-        pc.tile = lo;
-        pc.keys = line.range(s, lo);
+        pc.tile = tile;
+        pc.keys = line.range(s, tile);
         const int32_t n = line.steps_of(pc.keys);
-        pc.tile_begin = x - (in - first);
-        pc.tile_end = pc.tile_begin + n;
-        const int32_t at = static_cast<int32_t>(in - first);
         const int64_t left = end - x;
+        pc.tile_end = x + (n - at);
         pc.steps = left < n - at ? static_cast<int32_t>(left) : n - at;
         pc.first = pc.keys.lo / kStep + at;
         pc.starts = at == 0;
         pc.ends = at + pc.steps == n;
         x += pc.steps;
+        at = 0;
+        ++tile;
         return true;
     }
 };
@@ -295,6 +306,10 @@ __device__ __forceinline__ float pg_exp2(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+
+// Probabilities are held as 2^(s - m + shift): f16 would lose those below
+// 2^-14 of the largest, so its exponents start at the top of its range.
+template <bool kF16> __device__ __forceinline__ constexpr float pg_shift(float lag) { return kF16 ? 14.0f - lag : 0.0f; }
 
 template <bool kF16> __device__ __forceinline__ uint32_t pg_pack(float lo, float hi)
 {

@@ -267,9 +267,9 @@ __global__ void __launch_bounds__(kRowThreads, 1) paged_rows(const PagedArgs a)
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
                         // a row that has seen no key yet: exponents against 0, all of them -inf
-                        const float ref = top == -INFINITY ? 0.0f : top;
+                        const float ref = top == -INFINITY ? 0.0f : top - pg_shift<kF16>(0.0f);
                         if (__any_sync(0xffffffffu, top != m[mt][i])) {
-                            const float f = pg_exp2(m[mt][i] - ref);
+                            const float f = top == m[mt][i] ? 1.0f : pg_exp2(m[mt][i] - top);
                             l[mt][i] *= f;
 #pragma unroll
                             for (int n = 0; n < DP / 8; ++n) {
@@ -315,6 +315,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) paged_rows(const PagedArgs a)
                 float sum = l[mt][i];
                 sum += __shfl_xor_sync(0xffffffffu, sum, 1);
                 sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+                const float ref = m[mt][i] - pg_shift<kF16>(0.0f);
                 const int row = mt * 16 + i * 8 + lane / 4;
                 const int32_t tt = row / a.sub, h = row - tt * a.sub;
                 if (row >= rows || h >= t.heads)
@@ -331,7 +332,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) paged_rows(const PagedArgs a)
                                 pg_pack<kF16>(o[mt][n][2 * i] * inv, o[mt][n][2 * i + 1] * inv);
                     if (a.lse && (lane & 3) == 0)
                         a.lse[static_cast<int64_t>(t.token + tt) * a.heads_q + t.head + h] =
-                            sum == 0.0f ? -INFINITY : (m[mt][i] + log2f(sum)) * 0.6931471805599453f;
+                            sum == 0.0f ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
                 } else {
                     float *dst = a.part_o + (static_cast<int64_t>(slot) * kPagedRowTile + row) * kPagedMaxDim;
 #pragma unroll
@@ -340,7 +341,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) paged_rows(const PagedArgs a)
                             make_float2(o[mt][n][2 * i], o[mt][n][2 * i + 1]);
                     if ((lane & 3) == 0)
                         *reinterpret_cast<float2 *>(a.part_ml + (static_cast<int64_t>(slot) * kPagedRowTile + row) * 2) =
-                            make_float2(m[mt][i], sum);
+                            make_float2(ref, sum);
                 }
             }
         }
@@ -444,10 +445,13 @@ int launch_paged_join(const PagedArgs &a, bool f16, int tile_rows, void *stream)
 }
 
 int paged_tables_set_smem();
+int paged_tiles_set_smem();
 
 int paged_set_smem_limit()
 {
     int e = paged_tables_set_smem();
+    if (!e)
+        e = paged_tiles_set_smem();
     auto set = [&](const void *f) {
         if (!e)
             e = static_cast<int>(cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowSmem));
