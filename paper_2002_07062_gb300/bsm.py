@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import os
 import re
+import struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -380,61 +381,95 @@ def bsm_softmax_ragged(x, y, offsets, rows, cols, dtype: int, policy: int, flags
     del keep
 
 
-_PAGED_DTYPES = {"torch.float32": F32, "torch.bfloat16": BF16, "torch.float16": F16}
+# The paged calls run once a layer and step: their descriptors are packed in one
+# go (setting a ctypes structure field by field costs 5 to 8 us a call) and the
+# tensors' types are compared as objects.
+_CODES = {ctypes.c_void_p: "Q", ctypes.c_int64: "q", ctypes.c_int32: "i", ctypes.c_uint32: "I", ctypes.c_float: "f"}
+
+
+def _packer(desc):
+    s = struct.Struct("@" + "".join(_CODES[ct] for _, ct in desc._fields_))
+    return struct.Struct(s.format + "%dx" % (ctypes.sizeof(desc) - s.size)).pack
+
+
+_pack_tables, _pack_write, _pack_paged = _packer(PagedTablesDesc), _packer(PagedWriteDesc), _packer(PagedDesc)
+_PAGED_DTYPES = {}      # torch type -> bsm_dtype, filled on first use
+_INT32 = _INT64 = _FLOAT32 = None
+
+
+def _paged_types():
+    global _INT32, _INT64, _FLOAT32
+    import torch
+    _PAGED_DTYPES.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
+    _INT32, _INT64, _FLOAT32 = torch.int32, torch.int64, torch.float32
 
 
 def _strided(t, what: str, ndim: int):
-    """Address of a CUDA tensor whose last dimension is contiguous; its other
-    strides go to the library, which checks them."""
+    """Strides of a CUDA tensor whose last dimension is contiguous (the library
+    checks the others)."""
+    st = t.stride()
+    if t.is_cuda and len(st) == ndim and (st[-1] == 1 or t.shape[-1] <= 1):
+        return st
     if not t.is_cuda:
         raise ValueError("%s must be a CUDA tensor (got one on %s)" % (what, t.device))
-    if t.dim() != ndim:
-        raise ValueError("%s must have %d dimensions, not %d" % (what, ndim, t.dim()))
-    if t.stride(-1) != 1 and t.shape[-1] > 1:
-        raise ValueError("the last dimension of %s must be contiguous" % what)
-    return t.data_ptr()
+    if len(st) != ndim:
+        raise ValueError("%s must have %d dimensions, not %d" % (what, ndim, len(st)))
+    raise ValueError("the last dimension of %s must be contiguous" % what)
 
 
-def _ints(t, what: str, size: int, n: int):
-    """Address of a contiguous CUDA tensor of at least n integers of `size` bytes."""
-    if t.element_size() != size or t.is_floating_point():
-        raise ValueError("%s must hold integers of %d bytes" % (what, size))
-    return _dptr(t, n * size, what)
+def _vec(t, what: str, dtype, n: int):
+    """Address of a contiguous CUDA tensor of at least n entries of dtype."""
+    if t.dtype is dtype and t.is_cuda and t.numel() >= n and t.is_contiguous():
+        return t.data_ptr()
+    if t.dtype is not dtype:
+        raise ValueError("%s must be %s (got %s)" % (what, dtype, t.dtype))
+    return _dptr(t, n * t.element_size(), what)
 
 
-def _paged_dtype(*tensors):
-    kinds = {str(t.dtype) for t in tensors}
-    if len(kinds) != 1 or next(iter(kinds)) not in _PAGED_DTYPES:
-        raise ValueError("tensors must share one of the types %s (got %s)"
-                         % (", ".join(sorted(_PAGED_DTYPES)), ", ".join(sorted(kinds))))
-    return _PAGED_DTYPES[next(iter(kinds))]
+def _paged_dtype(first, *others):
+    code = _PAGED_DTYPES.get(first.dtype)
+    if code is None:
+        if not _PAGED_DTYPES:
+            _paged_types()
+        code = _PAGED_DTYPES.get(first.dtype)
+    for o in others:
+        if o.dtype is not first.dtype:
+            raise ValueError("tensors must share one type (got %s and %s)" % (first.dtype, o.dtype))
+    if code is None:
+        raise ValueError("type %s is not one of %s" % (first.dtype, ", ".join(str(k) for k in _PAGED_DTYPES)))
+    return code
 
 
 def _caches(k_cache, v_cache):
-    if k_cache.shape != v_cache.shape or k_cache.stride() != v_cache.stride():
+    st = _strided(k_cache, "k_cache", 4)
+    if v_cache.shape != k_cache.shape or _strided(v_cache, "v_cache", 4) != st:
         raise ValueError("k_cache and v_cache must have the same shape and strides")
-    return _strided(k_cache, "k_cache", 4), _strided(v_cache, "v_cache", 4)
+    return st
+
+
+def _page_tables(tables, n: int):
+    """(address, row stride, width) of the page tables of n requests."""
+    st = _strided(tables, "tables", 2)
+    rows, width = tables.shape
+    if tables.dtype is not _INT32 or rows < n:
+        raise ValueError("tables must be %s, a row for each of %d requests" % (_INT32, n))
+    return tables.data_ptr(), st[0] if rows > 1 else width, width
 
 
 def bsm_paged_tables(cached, fresh, free_pages, page_size: int, tables, starts, lengths, slots, positions, owners,
                      info, stream=None):
     """Block tables and slot maps from the requests' lengths (all CUDA integer
     tensors: int64 slots and info, int32 the rest; tables [requests, width])."""
+    if _INT32 is None:
+        _paged_types()
     n, m = cached.numel(), slots.numel()
-    d = PagedTablesDesc()
-    d.cached, d.fresh = _ints(cached, "cached", 4, n), _ints(fresh, "fresh", 4, n)
-    d.free_pages = _ints(free_pages, "free_pages", 4, 0)
-    if tables.element_size() != 4 or tables.is_floating_point() or tables.shape[0] < n:
-        raise ValueError("tables must hold a row of 4-byte integers for every request")
-    d.tables = _strided(tables, "tables", 2)
-    d.starts, d.lengths = _ints(starts, "starts", 4, n + 1), _ints(lengths, "lengths", 4, n)
-    d.slots = _ints(slots, "slots", 8, m)
-    d.positions, d.owners = _ints(positions, "positions", 4, m), _ints(owners, "owners", 4, m)
-    d.info = _ints(info, "info", 8, 4)
-    d.table_stride = tables.stride(0) if n > 1 else tables.shape[1]
-    d.n_requests, d.n_free, d.page_size = n, free_pages.numel(), page_size
-    d.table_width, d.n_slots = tables.shape[1], m
-    rc = lib().bsm_paged_tables(ctypes.addressof(d), _stream(stream))
+    tab, stride, width = _page_tables(tables, n)
+    d = _pack_tables(
+        _vec(cached, "cached", _INT32, n), _vec(fresh, "fresh", _INT32, n), _vec(free_pages, "free_pages", _INT32, 0),
+        tab, _vec(starts, "starts", _INT32, n + 1), _vec(lengths, "lengths", _INT32, n), _vec(slots, "slots", _INT64, m),
+        _vec(positions, "positions", _INT32, m), _vec(owners, "owners", _INT32, m), _vec(info, "info", _INT64, 4),
+        stride, n, free_pages.numel(), page_size, width, m)
+    rc = lib().bsm_paged_tables(d, _stream(stream))
     if rc:
         _check(rc, "bsm_paged_tables")
 
@@ -442,19 +477,16 @@ def bsm_paged_tables(cached, fresh, free_pages, page_size: int, tables, starts, 
 def bsm_paged_write(k, v, k_cache, v_cache, slots, stream=None):
     """New keys and values [tokens, heads, dim] to their slots of the caches
     [pages, page_size, heads, dim] (any strides; the last dimension contiguous)."""
-    d = PagedWriteDesc()
-    d.dtype = _paged_dtype(k, v, k_cache, v_cache)
-    d.k, d.v = _strided(k, "k", 3), _strided(v, "v", 3)
-    d.k_cache, d.v_cache = _caches(k_cache, v_cache)
-    if k.shape != v.shape or k.shape[1:] != k_cache.shape[2:]:
-        raise ValueError("k and v must be [tokens, %d, %d]" % tuple(k_cache.shape[2:]))
-    d.n_tokens, d.n_heads, d.head_dim = k.shape
-    d.slots = _ints(slots, "slots", 8, d.n_tokens)
-    d.n_pages, d.page_size = k_cache.shape[:2]
-    d.k_stride_token, d.k_stride_head, _ = k.stride()
-    d.v_stride_token, d.v_stride_head, _ = v.stride()
-    d.kv_stride_page, d.kv_stride_token, d.kv_stride_head, _ = k_cache.stride()
-    rc = lib().bsm_paged_write(ctypes.addressof(d), _stream(stream))
+    dtype = _paged_dtype(k, v, k_cache, v_cache)
+    ks, vs, cs = _strided(k, "k", 3), _strided(v, "v", 3), _caches(k_cache, v_cache)
+    tokens, heads, dim = shape = k.shape
+    pages, page_size, ch, cd = k_cache.shape
+    if v.shape != shape or heads != ch or dim != cd:
+        raise ValueError("k and v must be [tokens, %d, %d]" % (ch, cd))
+    d = _pack_write(k.data_ptr(), v.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+                    _vec(slots, "slots", _INT64, tokens), ks[0], ks[1], vs[0], vs[1], cs[0], cs[1], cs[2],
+                    tokens, heads, dim, page_size, pages, dtype)
+    rc = lib().bsm_paged_write(d, _stream(stream))
     if rc:
         _check(rc, "bsm_paged_write")
 
@@ -470,31 +502,21 @@ def bsm_paged_attention(q, k_cache, v_cache, out, starts, lengths, tables, max_n
                         flags: int = 0, window: int = 0, lse=None, stream=None):
     """Attention of new tokens q [tokens, heads_q, dim] over caches [pages,
     page_size, heads_kv, dim] (any strides; the last dimension contiguous)."""
-    d = PagedDesc()
-    d.dtype = _paged_dtype(q, k_cache, v_cache, out)
-    d.q, d.out = _strided(q, "q", 3), _strided(out, "out", 3)
-    d.k_cache, d.v_cache = _caches(k_cache, v_cache)
-    if out.shape != q.shape or q.shape[2] != k_cache.shape[3]:
+    dtype = _paged_dtype(q, k_cache, v_cache, out)
+    qs, os_, cs = _strided(q, "q", 3), _strided(out, "out", 3), _caches(k_cache, v_cache)
+    tokens, heads_q, dim = shape = q.shape
+    pages, page_size, heads_kv, cd = k_cache.shape
+    if out.shape != shape or dim != cd:
         raise ValueError("out must have q's shape, and the caches its last dimension")
-    d.n_tokens, d.heads_q, d.head_dim = q.shape
-    d.n_pages, d.page_size, d.heads_kv, _ = k_cache.shape
     n = lengths.numel()
-    if tables.element_size() != 4 or tables.is_floating_point() or tables.shape[0] < n:
-        raise ValueError("tables must hold a row of 4-byte integers for every request")
-    d.starts, d.lengths = _ints(starts, "starts", 4, n + 1), _ints(lengths, "lengths", 4, n)
-    d.tables = _strided(tables, "tables", 2)
-    d.table_stride = tables.stride(0) if n > 1 else tables.shape[1]
-    d.n_requests, d.table_width, d.max_new = n, tables.shape[1], max_new
-    d.q_stride_token, d.q_stride_head, _ = q.stride()
-    d.out_stride_token, d.out_stride_head, _ = out.stride()
-    d.kv_stride_page, d.kv_stride_token, d.kv_stride_head, _ = k_cache.stride()
-    if lse is not None:
-        if str(lse.dtype) != "torch.float32":
-            raise ValueError("lse must be float32")
-        d.lse = _dptr(lse, 4 * d.n_tokens * d.heads_q, "lse")
-    d.workspace, d.workspace_bytes = _dptr(workspace, None, "workspace"), workspace.nbytes
-    d.flags, d.window, d.scale = flags, window, scale
-    rc = lib().bsm_paged_attention(ctypes.addressof(d), _stream(stream))
+    tab, stride, width = _page_tables(tables, n)
+    d = _pack_paged(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr(),
+                    0 if lse is None else _vec(lse, "lse", _FLOAT32, tokens * heads_q),
+                    _vec(starts, "starts", _INT32, n + 1), _vec(lengths, "lengths", _INT32, n), tab,
+                    _dptr(workspace, None, "workspace"), workspace.nbytes, qs[0], qs[1], os_[0], os_[1], cs[0], cs[1],
+                    cs[2], stride, n, tokens, heads_q, heads_kv, dim, page_size, pages, width, max_new, dtype, window,
+                    flags, scale)
+    rc = lib().bsm_paged_attention(d, _stream(stream))
     if rc:
         _check(rc, "bsm_paged_attention")
 

@@ -47,16 +47,16 @@ struct PagedArgs {
     int32_t group;                                  // query heads of a key/value head
     int32_t subs, sub;                              // head groups of one key/value head, heads of each
     int32_t tok;                                    // tokens of a tile
-    int32_t rows_min, rows_max;                     // takes requests of rows_min < tokens * group <= rows_max
-    int32_t units, min_steps;                       // units at most; key steps of a unit at least
-    float *part_o;                                  // units x 2 x tile rows x padded head size
-    float *part_ml;                                 // units x 2 x tile rows x 2
-    struct PagedJoin *join;                         // units
+    int32_t units;                                  // units at most
+    float *part_o;                                  // CTAs x 2 x tile rows x kPagedMaxDim
+    float *part_ml;                                 // CTAs x 2 x tile rows x 2
+    struct PagedJoin *join;                         // CTAs
+    float *warp_o, *warp_ml;                        // the row kernel's: the same for every warp
     uint32_t *status;
 };
 
-// A tile whose keys were split over units u .. u + count - 1: the first one's
-// second partial and the others' first are joined by paged_join.
+// A tile whose keys were split over CTAs c .. c + count - 1: the first one's
+// second partial and the others' first are joined.
 struct PagedJoin {
     int32_t token, head, tokens, heads;             // first token, first query head, tokens, heads of the tile
     int32_t count;                                  // 0: nothing to join
@@ -64,7 +64,7 @@ struct PagedJoin {
 };
 
 constexpr int kPagedWarps = 8;                      // of the row kernel
-constexpr int kPagedRowTile = 32;                   // most rows of its tiles
+constexpr int kPagedRowTile = 16;                   // most rows of its tiles
 constexpr int kPagedMaxDim = 128;
 constexpr int kPagedTileRows = 256;                 // of the tile kernel: two blocks of 128
 constexpr int kPagedTileKeys = 128;                 // keys of its steps
@@ -72,7 +72,6 @@ constexpr int kPagedTileKeys = 128;                 // keys of its steps
 int launch_paged_tables(const PagedTablesArgs &a, int n_sm, void *stream);
 int launch_paged_write(const PagedWriteArgs &a, int n_sm, void *stream);
 int launch_paged_rows(const PagedArgs &a, bool f16, int grid, void *stream);
-int launch_paged_join(const PagedArgs &a, bool f16, int tile_rows, void *stream);
 // maps: CUtensorMaps of q, k, v (host); box: rows of one copy of k and v
 int launch_paged_tiles(const void *maps, const PagedArgs &a, bool f16, int box, void *stream);
 int paged_set_smem_limit();

@@ -96,18 +96,20 @@ int elem_size(int dtype) { return dtype == BSM_F32 ? 4 : 2; }
 
 // Workspace: partial outputs, maxima and sums of cut tiles, and who joins them.
 struct PagedLayout {
-    int64_t rows_o, rows_ml, rows_join, tiles_o, tiles_ml, tiles_join, bytes;
+    int64_t warp_o, warp_ml, rows_o, rows_ml, rows_join, tiles_o, tiles_ml, tiles_join, bytes;
 };
 
 PagedLayout paged_layout(int n_sm)
 {
     PagedLayout l{};
     auto up = [](int64_t x) { return (x + 255) & ~int64_t(255); };
-    const int64_t units = static_cast<int64_t>(n_sm) * kPagedWarps;
-    l.rows_o = 0;
-    l.rows_ml = l.rows_o + up(units * 2 * kPagedRowTile * kPagedMaxDim * 4);
-    l.rows_join = l.rows_ml + up(units * 2 * kPagedRowTile * 8);
-    l.tiles_o = l.rows_join + up(units * static_cast<int64_t>(sizeof(PagedJoin)));
+    const int64_t row_part = static_cast<int64_t>(n_sm) * 2 * kPagedRowTile;
+    l.warp_o = 0;
+    l.warp_ml = l.warp_o + up(kPagedWarps * row_part * kPagedMaxDim * 4);
+    l.rows_o = l.warp_ml + up(kPagedWarps * row_part * 8);
+    l.rows_ml = l.rows_o + up(row_part * kPagedMaxDim * 4);
+    l.rows_join = l.rows_ml + up(row_part * 8);
+    l.tiles_o = l.rows_join + up(static_cast<int64_t>(n_sm) * static_cast<int64_t>(sizeof(PagedJoin)));
     l.tiles_ml = l.tiles_o + up(static_cast<int64_t>(n_sm) * 2 * kPagedTileRows * kPagedMaxDim * 4);
     l.tiles_join = l.tiles_ml + up(static_cast<int64_t>(n_sm) * 2 * kPagedTileRows * 8);
     l.bytes = l.tiles_join + up(static_cast<int64_t>(n_sm) * static_cast<int64_t>(sizeof(PagedJoin)));
@@ -327,14 +329,16 @@ int paged_attention(const bsm_paged_desc *d, bsm_stream_t stream)
     a.n_pages = d->n_pages;
     a.width = d->table_width;
     a.causal = (d->flags & BSM_FLAG_CAUSAL) ? 1 : 0;
-    a.window = d->window;
+    // (a window as long as any request can be hides nothing)
+    a.window = d->window < static_cast<int64_t>(d->table_width) * d->page_size ? d->window : 0;
     a.scale_log2 = d->scale * 1.4426950408889634f;
     a.group = d->heads_q / d->heads_kv;
     a.status = dev->status;
     unsigned char *ws = static_cast<unsigned char *>(d->workspace);
-    // Requests of more than 32 rows (new tokens times the heads that share a
-    // key/value head) go to the tile kernel, where pages are whole groups of
-    // eight rows (the copies' swizzle).
+    // A batch with requests of more than 16 rows (new tokens times the heads that
+    // share a key/value head) goes to the tile kernel, its single tokens too: it
+    // keeps up with the cache's bytes there, and one launch deals all the work.
+    // The tile kernel's copies want pages of whole groups of eight rows.
     int box = 1;
     while (box < kPagedTileKeys && d->page_size % (2 * box) == 0)
         box *= 2;
@@ -352,31 +356,25 @@ int paged_attention(const bsm_paged_desc *d, bsm_stream_t stream)
         tiles = paged_map(&maps[0], f16, d->q, 3, qd, qst, qb) && paged_map(&maps[1], f16, d->k_cache, 4, kd, kst, kb) &&
                 paged_map(&maps[2], f16, d->v_cache, 4, kd, kst, kb);
     }
-    split_group(a, kPagedRowTile);
-    const int64_t rows = static_cast<int64_t>(d->max_new) * a.sub;
-    a.tok = std::max(1, (rows <= 16 ? 16 : kPagedRowTile) / a.sub);
-    a.rows_min = 0;
-    a.rows_max = tiles ? kPagedRowTile : INT32_MAX;
-    a.units = dev->n_sm * kPagedWarps;
-    a.min_steps = a.d <= 64 ? 1 : 2;
-    a.part_o = reinterpret_cast<float *>(ws + lay.rows_o);
-    a.part_ml = reinterpret_cast<float *>(ws + lay.rows_ml);
-    a.join = reinterpret_cast<PagedJoin *>(ws + lay.rows_join);
-    if (int e = launch_paged_rows(a, f16, dev->n_sm, stream))
-        return record_cuda_error(e, "paged attention launch");
-    if (int e = launch_paged_join(a, f16, kPagedRowTile, stream))
-        return record_cuda_error(e, "paged attention join launch");
     if (tiles) {
-        b.rows_min = kPagedRowTile;
-        b.rows_max = INT32_MAX;
         b.units = dev->n_sm;
-        b.min_steps = 1;
         b.part_o = reinterpret_cast<float *>(ws + lay.tiles_o);
         b.part_ml = reinterpret_cast<float *>(ws + lay.tiles_ml);
         b.join = reinterpret_cast<PagedJoin *>(ws + lay.tiles_join);
         if (int e = launch_paged_tiles(maps, b, f16, box, stream))
             return record_cuda_error(e, "paged attention tile launch");
+        return BSM_OK;
     }
+    split_group(a, kPagedRowTile);
+    a.tok = std::max(1, kPagedRowTile / a.sub);
+    a.units = dev->n_sm * kPagedWarps;
+    a.warp_o = reinterpret_cast<float *>(ws + lay.warp_o);
+    a.warp_ml = reinterpret_cast<float *>(ws + lay.warp_ml);
+    a.part_o = reinterpret_cast<float *>(ws + lay.rows_o);
+    a.part_ml = reinterpret_cast<float *>(ws + lay.rows_ml);
+    a.join = reinterpret_cast<PagedJoin *>(ws + lay.rows_join);
+    if (int e = launch_paged_rows(a, f16, dev->n_sm, stream))
+        return record_cuda_error(e, "paged attention launch");
     return BSM_OK;
 }
 

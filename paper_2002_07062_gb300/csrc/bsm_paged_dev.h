@@ -23,24 +23,37 @@
 
 namespace bsm {
 
+// Quotients of counts that nearly always fit 32 bits (a 64-bit division costs
+// several hundred cycles in the one warp that needs it).
+__device__ __forceinline__ int64_t pg_div(int64_t a, int64_t b)
+{
+    if (((a | b) >> 32) == 0)
+        return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
+    return a / b;
+}
+
 // sum over i < n of (a i + b) / m, rounded down each (Euclid on the slope).
+// a n + b < 2^32.  (64-bit quotients here and a search tile by tile cost 8 to 30 us a
+// call for a few long requests.)
 __device__ __forceinline__ int64_t floor_sum(uint32_t n, uint32_t m, uint32_t a, uint32_t b)
 {
     uint64_t ans = 0;
     while (n > 0) {
         if (a >= m) {
-            ans += static_cast<uint64_t>(n) * (n - 1) / 2 * (a / m);
-            a %= m;
+            const uint32_t q = a / m;
+            ans += static_cast<uint64_t>(n) * (n - 1) / 2 * q;
+            a -= q * m;
         }
         if (b >= m) {
-            ans += static_cast<uint64_t>(n) * (b / m);
-            b %= m;
+            const uint32_t q = b / m;
+            ans += static_cast<uint64_t>(n) * q;
+            b -= q * m;
         }
-        const uint64_t y = static_cast<uint64_t>(a) * n + b;
+        const uint32_t y = a * n + b;
         if (y < m)
             break;
-        n = static_cast<uint32_t>(y / m);
-        b = static_cast<uint32_t>(y % m);
+        n = y / m;
+        b = y - n * m;
         const uint32_t t = m;
         m = a;
         a = t;
@@ -69,14 +82,11 @@ template <int kStep> struct PagedLine {
     {
         PagedRange r{0, s.L};
         if (a.causal) {
-            const int32_t end = (i + 1) * a.tok < s.m ? (i + 1) * a.tok : s.m;
-            r.hi = s.L - s.m + end;
+            const int32_t first = s.L - s.m + i * a.tok, left = s.m - i * a.tok;
+            r.hi = first + (left < a.tok ? left : a.tok);
             r.hi = r.hi < 0 ? 0 : r.hi;
-            if (a.window) {
-                const int64_t lo = static_cast<int64_t>(s.L) - s.m + i * a.tok - a.window + 1;
-                r.lo = lo < 0 ? 0 : static_cast<int32_t>(lo);
-                r.lo = r.lo < r.hi ? r.lo : r.hi;
-            }
+            if (a.window && first >= a.window)
+                r.lo = first - a.window + 1;
         }
         return r;
     }
@@ -95,28 +105,30 @@ template <int kStep> struct PagedLine {
             return 0;
         if (!a.causal)
             return static_cast<int64_t>(i) * steps_of(PagedRange{0, s.L});
-        int64_t tail = 0;
+        int32_t tail = 0;
         if (i == s.tiles) {             // the last tile may be short
             --i;
             tail = steps_of(range(s, i));
         }
-        const int64_t base = static_cast<int64_t>(s.L) - s.m;
+        const int32_t base = s.L - s.m;
+        const uint32_t tok = static_cast<uint32_t>(a.tok);
         // tiles whose last token lies before the first key see none
-        int32_t none = 0;
-        if (base < 0)
-            none = static_cast<int32_t>(-base / a.tok);
-        if (i <= none)
-            return i + tail;
-        int64_t n = none + floor_sum(i - none, kStep, a.tok, static_cast<uint32_t>(base + static_cast<int64_t>(none + 1) * a.tok + kStep - 1));
+        const uint32_t none = base < 0 ? (0u - static_cast<uint32_t>(base)) / tok : 0u;
+        if (static_cast<uint32_t>(i) <= none)
+            return static_cast<int64_t>(i) + tail;
+        int64_t n = tail + static_cast<int64_t>(none) +
+                    floor_sum(i - none, kStep, tok, static_cast<uint32_t>(base) + (none + 1) * tok + kStep - 1);
         if (a.window) {
-            // whole steps that lie left of a tile's window
-            const int64_t past = static_cast<int64_t>(a.window) - 1 - base;
-            int64_t j = past < 0 ? 0 : past / a.tok + 1;
-            j = j < none ? none : j;
-            if (j < i)
-                n -= floor_sum(static_cast<uint32_t>(i - j), kStep, a.tok, static_cast<uint32_t>(base + j * a.tok - a.window + 1));
+            // whole steps that lie left of a tile's window: of tiles j and on
+            uint32_t j = none;
+            if (base < a.window) {
+                const uint32_t past = (static_cast<uint32_t>(a.window) - 1u - static_cast<uint32_t>(base)) / tok + 1;
+                j = j < past ? past : j;
+            }
+            if (j < static_cast<uint32_t>(i))
+                n -= floor_sum(i - j, kStep, tok, static_cast<uint32_t>(base) + j * tok - static_cast<uint32_t>(a.window) + 1u);
         }
-        return n + tail;
+        return n;
     }
 
     __device__ PagedSeq seq(int32_t r, bool report) const
@@ -133,11 +145,8 @@ template <int kStep> struct PagedLine {
         s.t0 = t0;
         s.m = t1 - t0;
         s.L = L;
-        const int64_t rows = static_cast<int64_t>(s.m) * a.group;
-        if (s.m == 0 || rows <= a.rows_min || rows > a.rows_max) {
-            s.m = 0;
+        if (s.m == 0)
             return s;
-        }
         s.tiles = (s.m + a.tok - 1) / a.tok;
         s.steps = before(s, s.tiles);
         return s;
@@ -195,20 +204,30 @@ __device__ void paged_prefix(const PagedLine<kStep> &line, PagedPrefix<kThreads>
     __syncthreads();
 }
 
-// How the line is cut: `units` ranges of at least min_steps steps.
+// How the line is cut: `units` ranges, none empty; unit u begins at W u / units.
 struct PagedCut {
-    int64_t W;
-    int32_t units;
+    int64_t W, q;
+    int32_t units, rem;
     __device__ PagedCut(const PagedArgs &a, int64_t steps) : W(steps)
     {
-        const int64_t u = steps / a.min_steps;
-        units = u >= a.units ? a.units : u < 1 ? 1 : static_cast<int32_t>(u);
+        units = steps >= a.units ? a.units : steps < 1 ? 1 : static_cast<int32_t>(steps);
+        q = pg_div(W, units);
+        rem = static_cast<int32_t>(W - q * units);
     }
-    __device__ __forceinline__ int64_t begin(int32_t u) const { return W * u / units; }
-    // the unit that takes step x
+    __device__ __forceinline__ int64_t begin(int32_t u) const
+    {
+        return q * u + static_cast<uint32_t>(rem) * static_cast<uint32_t>(u) / static_cast<uint32_t>(units);
+    }
+    // the unit that takes step x: a guess in fp32, put right
     __device__ __forceinline__ int32_t owner(int64_t x) const
     {
-        return static_cast<int32_t>(((x + 1) * units - 1) / W);
+        int32_t u = static_cast<int32_t>(static_cast<float>(x) * static_cast<float>(units) / static_cast<float>(W));
+        u = u < 0 ? 0 : u >= units ? units - 1 : u;
+        while (u + 1 < units && begin(u + 1) <= x)
+            ++u;
+        while (u > 0 && begin(u) > x)
+            --u;
+        return u;
     }
 };
 
@@ -236,33 +255,32 @@ template <int kStep> struct PagedWalk {
     {
         if (x >= end)
             return;
-        int lo = 0, hi = kThreads;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (p.pre[mid] <= x)
-                lo = mid;
-            else
-                hi = mid;
-        }
+        // the whole warp searches: 32 candidates at once
+        const int lane = threadIdx.x & 31;
+        constexpr int kEach = kThreads / 32;
+        int lo = (__popc(__ballot_sync(0xffffffffu, p.pre[lane * kEach] <= x)) - 1) * kEach;
+        lo += __popc(__ballot_sync(0xffffffffu, lane < kEach && p.pre[lo + lane] <= x)) - 1;
         int64_t o = x - p.pre[lo];
-        r = lo * ((l.a.n + kThreads - 1) / kThreads);
-        s = l.seq(r, false);
-        while (o >= line.all_steps(s) && r + 1 < l.a.n) {       // (the line's end is past x: some request holds it)
-            o -= line.all_steps(s);
+        r = lo * ((l.a.n + kThreads - 1) / kThreads) - 1;
+        int64_t all = 0;
+        do {                                    // (the line's end is past x: some request holds it)
+            o -= all;
             s = line.seq(++r, false);
-        }
-        head = static_cast<int32_t>(o / s.steps);
+            all = line.all_steps(s);
+        } while (o >= all && r + 1 < l.a.n);
+        head = static_cast<int32_t>(pg_div(o, s.steps));
         o -= head * s.steps;
-        int32_t t0 = 0, t1 = s.tiles;
-        while (t1 - t0 > 1) {
-            const int32_t mid = (t0 + t1) >> 1;
-            if (line.before(s, mid) <= o)
-                t0 = mid;
-            else
-                t1 = mid;
+        int32_t left = s.tiles;
+        int64_t first = 0;
+        while (left > 1) {
+            const int32_t each = (left + 31) / 32, mine = lane * each;
+            const int64_t f = mine < left ? line.before(s, tile + mine) : 0;
+            const int k = 31 - __clz(__ballot_sync(0xffffffffu, mine < left && f <= o));
+            first = __shfl_sync(0xffffffffu, f, k);
+            tile += k * each;
+            left = each < left - k * each ? each : left - k * each;
         }
-        tile = t0;
-        at = static_cast<int32_t>(o - line.before(s, t0));
+        at = static_cast<int32_t>(o - first);
     }
 
     __device__ bool next(PagedPiece &pc)

@@ -1,5 +1,5 @@
 // bsm_paged_rows.cu -- attention of a few new tokens over a paged cache:
-// tiles of at most 32 rows (tokens times the query heads that share a
+// tiles of at most 16 rows (tokens times the query heads that share a
 // key/value head), the keys split over every warp of the device.
 //
 //   s = scale q k^T,  p = exp(s - m),  o = sum p v / sum p   (m a running maximum)
@@ -9,7 +9,7 @@
 // built for loads: every warp is on its own, with its own range of the work,
 // its own three stages of 16 keys (8 KiB of K and V at D = 128) filled by
 // 16-byte asynchronous copies, its own running maximum and sum; no barrier of
-// the block after the work is laid out.  24 stages an SM keep 128 to 192 KiB
+// the block between the layout of the work and the join of cut tiles.  24 stages an SM keep 128 to 192 KiB
 // in flight.
 #include <cuda_runtime.h>
 
@@ -31,8 +31,18 @@ template <int DP> struct RowShape {
     static constexpr int kChunks = DP / 8;              // 16-byte pieces of a row
 };
 
+// A part of a tile that a warp leaves to be joined: [0] of a tile that an
+// earlier warp started, [1] of one that it starts and does not end.
+struct RowPart {
+    int32_t token, head, tokens, heads; // of the tile
+    int32_t rows;                       // 0: no part
+    int32_t starts, ends;
+    int32_t last_cta;                   // that has part of the tile
+};
+
 struct RowSmem {
     PagedPrefix<kRowThreads> prefix;
+    RowPart part[kPagedWarps][2];
 };
 constexpr int kRowHeader = 4096;
 static_assert(sizeof(RowSmem) <= kRowHeader, "row header");
@@ -75,6 +85,37 @@ template <bool kF16> __device__ __forceinline__ void mma16(float *d, const uint3
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+constexpr float kLn2 = 0.6931471805599453f;
+
+// The sum over the parts of a row: with M the largest of their references m_i,
+// o = sum 2^(m_i - M) o_i, l = sum 2^(m_i - M) l_i.  A lane has four columns.
+struct RowSum {
+    float top = -INFINITY, sum = 0.0f;
+    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    __device__ __forceinline__ void add(const float2 &ml, const float4 &v)
+    {
+        const float f = pg_exp2(ml.x - (top == -INFINITY ? 0.0f : top));
+        sum += f * ml.y;
+        acc.x += f * v.x;
+        acc.y += f * v.y;
+        acc.z += f * v.z;
+        acc.w += f * v.w;
+    }
+    template <bool kF16> __device__ __forceinline__ void store(const PagedArgs &a, int64_t token, int32_t head, int lane) const
+    {
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        if (lane * 4 < a.d) {
+            uint2 w;
+            w.x = pg_pack<kF16>(acc.x * inv, acc.y * inv);
+            w.y = pg_pack<kF16>(acc.z * inv, acc.w * inv);
+            *reinterpret_cast<uint2 *>(static_cast<unsigned char *>(a.out) +
+                                       2 * (token * a.out_token + head * a.out_head + lane * 4)) = w;
+        }
+        if (a.lse && lane == 0)
+            a.lse[token * a.heads_q + head] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
+    }
+};
+
 // Where the rows of a tile come from and go to.
 struct RowTile {
     int32_t token, head, tokens, heads; // first token, first query head, tokens, heads
@@ -93,8 +134,8 @@ __device__ __forceinline__ RowTile row_tile(const PagedArgs &a, const PagedSeq &
     return t;
 }
 
-// DP: the head size padded to 64 or 128; MT: 16-row blocks of a tile.
-template <int DP, int MT, bool kF16>
+// DP: the head size padded to 64 or 128.
+template <int DP, bool kF16>
 __global__ void __launch_bounds__(kRowThreads, 1) paged_rows(const PagedArgs a)
 {
     using Shape = RowShape<DP>;
@@ -106,19 +147,20 @@ __global__ void __launch_bounds__(kRowThreads, 1) paged_rows(const PagedArgs a)
     RowSmem &sm = *reinterpret_cast<RowSmem *>(raw);
     const int lane = threadIdx.x & 31;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
+    const int32_t cta = blockIdx.x, unit = cta * kPagedWarps + warp;
+    if (threadIdx.x == 0)
+        a.join[cta].count = 0;
+    if (lane < 2)
+        sm.part[warp][lane].rows = 0;
     const PagedLine<kKeys> line(a);
-    paged_prefix<kKeys, kRowThreads>(line, sm.prefix, blockIdx.x == 0);
+    paged_prefix<kKeys, kRowThreads>(line, sm.prefix, cta == 0);
     const int64_t W = sm.prefix.pre[kRowThreads];
     const PagedCut cut(a, W);
-    // neighbouring units on different SMs: a small batch spreads over the device
-    const int32_t unit = warp * gridDim.x + blockIdx.x;
-    if (lane == 0)
-        a.join[unit].count = 0;
-    if (W == 0 || unit >= cut.units)
-        return;
-    const int64_t begin = cut.begin(unit), end = cut.begin(unit + 1);
+    if (W == 0 || cta * kPagedWarps >= cut.units)
+        return;                                         // (the whole CTA)
+    const int64_t begin = unit < cut.units ? cut.begin(unit) : 0, end = unit < cut.units ? cut.begin(unit + 1) : 0;
     const int32_t total = static_cast<int32_t>(end - begin);
-    PagedWalk<kKeys> fetch(line, sm.prefix, begin, end), walk(line, sm.prefix, begin, end);
+    PagedWalk<kKeys> fetch(line, sm.prefix, begin, end), walk = fetch;
 
     const uint32_t stages = pg_saddr(raw) + kRowHeader + warp * (kRowStages * kStageBytes);
     const unsigned char *kbase = static_cast<const unsigned char *>(a.k), *vbase = static_cast<const unsigned char *>(a.v);
@@ -188,39 +230,31 @@ __global__ void __launch_bounds__(kRowThreads, 1) paged_rows(const PagedArgs a)
     while (walk.next(p)) {
         const RowTile t = row_tile(a, walk.s, p);
         const int32_t rows = t.tokens * a.sub;
-        // this lane's rows: lane / 4 and lane / 4 + 8 of each 16-row block
-        int32_t lo[MT][2], hi[MT][2];
-        uint32_t q[MT][DP / 16][4];
+        // this lane's rows: lane / 4 and lane / 4 + 8
+        int32_t lo[2], hi[2];
+        uint32_t q[DP / 16][4];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
+        for (int i = 0; i < 2; ++i) {
+            const int row = i * 8 + lane / 4;
+            const int32_t tt = row / a.sub, h = row - tt * a.sub;
+            const bool live = row < rows && h < t.heads;
+            const int32_t pos = t.pos + tt;
+            hi[i] = !live ? 0 : a.causal ? (pos + 1 < p.keys.hi ? pos + 1 : p.keys.hi) : p.keys.hi;
+            lo[i] = a.window && pos >= a.window ? pos - a.window + 1 : 0;
+            const uint32_t *src = reinterpret_cast<const uint32_t *>(
+                static_cast<const unsigned char *>(a.q) + 2 * ((t.token + tt) * a.q_token + (t.head + h) * a.q_head));
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int row = mt * 16 + i * 8 + lane / 4;
-                const int32_t tt = row / a.sub, h = row - tt * a.sub;
-                const bool live = row < rows && h < t.heads;
-                const int32_t pos = t.pos + tt;
-                hi[mt][i] = !live ? 0 : a.causal ? (pos + 1 < p.keys.hi ? pos + 1 : p.keys.hi) : p.keys.hi;
-                lo[mt][i] = a.window && pos - a.window + 1 > 0 ? pos - a.window + 1 : 0;
-                const uint32_t *src = reinterpret_cast<const uint32_t *>(
-                    static_cast<const unsigned char *>(a.q) + 2 * ((t.token + tt) * a.q_token + (t.head + h) * a.q_head));
-#pragma unroll
-                for (int k = 0; k < DP / 16; ++k) {
-                    const int d0 = k * 16 + (lane & 3) * 2;
-                    q[mt][k][i] = live && d0 < a.d ? src[d0 / 2] : 0u;
-                    q[mt][k][i + 2] = live && d0 + 8 < a.d ? src[d0 / 2 + 4] : 0u;
-                }
+            for (int k = 0; k < DP / 16; ++k) {
+                const int d0 = k * 16 + (lane & 3) * 2;
+                q[k][i] = live && d0 < a.d ? src[d0 / 2] : 0u;
+                q[k][i + 2] = live && d0 + 8 < a.d ? src[d0 / 2 + 4] : 0u;
             }
         }
-        float o[MT][DP / 8][4];
-        float m[MT][2], l[MT][2];
+        float o[DP / 8][4];
+        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-            for (int n = 0; n < DP / 8; ++n)
-                o[mt][n][0] = o[mt][n][1] = o[mt][n][2] = o[mt][n][3] = 0.0f;
-            m[mt][0] = m[mt][1] = -INFINITY;
-            l[mt][0] = l[mt][1] = 0.0f;
-        }
+        for (int n = 0; n < DP / 8; ++n)
+            o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.0f;
         for (int32_t st = 0; st < p.steps; ++st) {
             cp_wait<kRowStages - 1>();
             __syncwarp();
@@ -228,198 +262,216 @@ __global__ void __launch_bounds__(kRowThreads, 1) paged_rows(const PagedArgs a)
 #pragma unroll
             for (int sb = 0; sb < kSubs; ++sb) {
                 const int32_t key0 = (p.first + st) * kKeys + sb * 16;
-                float s[MT][2][4];
+                float s[2][4];
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        s[mt][0][j] = s[mt][1][j] = 0.0f;
+                for (int j = 0; j < 4; ++j)
+                    s[0][j] = s[1][j] = 0.0f;
                 // keys 0-7 / 8-15 and halves of 8 columns: matrices of lanes 0-7, 8-15, 16-23, 24-31
                 const int krow = sb * 16 + (lane & 7) + ((lane >> 4) << 3);
 #pragma unroll
                 for (int k = 0; k < DP / 16; ++k) {
                     uint32_t b[4];
                     ldsm4(kst + krow * kRB + (((2 * k + ((lane >> 3) & 1)) ^ (krow & 7)) << 4), b);
-#pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) {
-                        if (mt * 16 < rows) {
-                            mma16<kF16>(s[mt][0], q[mt][k], b[0], b[1]);
-                            mma16<kF16>(s[mt][1], q[mt][k], b[2], b[3]);
-                        }
-                    }
+                    mma16<kF16>(s[0], q[k], b[0], b[1]);
+                    mma16<kF16>(s[1], q[k], b[2], b[3]);
                 }
-                uint32_t pa[MT][4];
+                uint32_t pa[4];
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    if (mt * 16 >= rows)
-                        continue;
+                for (int i = 0; i < 2; ++i) {
+                    float x[4];
+                    float top = m[i];
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        float x[4];
-                        float top = m[mt][i];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const int32_t key = key0 + (j >> 1) * 8 + (lane & 3) * 2 + (j & 1);
-                            const float v = s[mt][j >> 1][i * 2 + (j & 1)] * a.scale_log2;
-                            x[j] = key >= lo[mt][i] && key < hi[mt][i] ? v : -INFINITY;
-                            top = fmaxf(top, x[j]);
-                        }
-                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                        // a row that has seen no key yet: exponents against 0, all of them -inf
-                        const float ref = top == -INFINITY ? 0.0f : top - pg_shift<kF16>(0.0f);
-                        if (__any_sync(0xffffffffu, top != m[mt][i])) {
-                            const float f = top == m[mt][i] ? 1.0f : pg_exp2(m[mt][i] - top);
-                            l[mt][i] *= f;
-#pragma unroll
-                            for (int n = 0; n < DP / 8; ++n) {
-                                o[mt][n][2 * i] *= f;
-                                o[mt][n][2 * i + 1] *= f;
-                            }
-                        }
-                        m[mt][i] = top;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            x[j] = pg_exp2(x[j] - ref);
-                            l[mt][i] += x[j];
-                        }
-                        pa[mt][i] = pg_pack<kF16>(x[0], x[1]);
-                        pa[mt][i + 2] = pg_pack<kF16>(x[2], x[3]);
+                    for (int j = 0; j < 4; ++j) {
+                        const int32_t key = key0 + (j >> 1) * 8 + (lane & 3) * 2 + (j & 1);
+                        const float v = s[j >> 1][i * 2 + (j & 1)] * a.scale_log2;
+                        x[j] = key >= lo[i] && key < hi[i] ? v : -INFINITY;
+                        top = fmaxf(top, x[j]);
                     }
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                    // a row that has seen no key yet: exponents against 0, all of them -inf
+                    const float ref = top == -INFINITY ? 0.0f : top - pg_shift<kF16>(0.0f);
+                    if (__any_sync(0xffffffffu, top != m[i])) {
+                        const float f = top == m[i] ? 1.0f : pg_exp2(m[i] - top);
+                        l[i] *= f;
+#pragma unroll
+                        for (int n = 0; n < DP / 8; ++n) {
+                            o[n][2 * i] *= f;
+                            o[n][2 * i + 1] *= f;
+                        }
+                    }
+                    m[i] = top;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        x[j] = pg_exp2(x[j] - ref);
+                        l[i] += x[j];
+                    }
+                    pa[i] = pg_pack<kF16>(x[0], x[1]);
+                    pa[i + 2] = pg_pack<kF16>(x[2], x[3]);
                 }
                 const int vrow = sb * 16 + (lane & 15);
 #pragma unroll
                 for (int n = 0; n < DP / 16; ++n) {
                     uint32_t b[4];
                     ldsm4t(kst + kHalf + vrow * kRB + (((2 * n + (lane >> 4)) ^ (vrow & 7)) << 4), b);
-#pragma unroll
-                    for (int mt = 0; mt < MT; ++mt) {
-                        if (mt * 16 < rows) {
-                            mma16<kF16>(o[mt][2 * n], pa[mt], b[0], b[1]);
-                            mma16<kF16>(o[mt][2 * n + 1], pa[mt], b[2], b[3]);
-                        }
-                    }
+                    mma16<kF16>(o[2 * n], pa, b[0], b[1]);
+                    mma16<kF16>(o[2 * n + 1], pa, b[2], b[3]);
                 }
             }
             __syncwarp();
             ++done;
             issue();
         }
-        // ---- the tile's output, or this unit's part of it
+        // ---- the tile's output, or this warp's part of it
         const bool whole = p.starts && p.ends;
         const int32_t slot = 2 * unit + (p.starts ? 1 : 0);
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
+        for (int i = 0; i < 2; ++i) {
+            float sum = l[i];
+            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+            const float ref = m[i] - pg_shift<kF16>(0.0f);
+            const int row = i * 8 + lane / 4;
+            const int32_t tt = row / a.sub, h = row - tt * a.sub;
+            if (row >= rows || h >= t.heads)
+                continue;
+            if (whole) {
+                const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+                uint32_t *dst = reinterpret_cast<uint32_t *>(static_cast<unsigned char *>(a.out) +
+                                                             2 * ((t.token + tt) * a.out_token + (t.head + h) * a.out_head));
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                float sum = l[mt][i];
-                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-                const float ref = m[mt][i] - pg_shift<kF16>(0.0f);
-                const int row = mt * 16 + i * 8 + lane / 4;
-                const int32_t tt = row / a.sub, h = row - tt * a.sub;
-                if (row >= rows || h >= t.heads)
-                    continue;
-                if (whole) {
-                    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-                    uint32_t *dst = reinterpret_cast<uint32_t *>(
-                        static_cast<unsigned char *>(a.out) +
-                        2 * ((t.token + tt) * a.out_token + (t.head + h) * a.out_head));
+                for (int n = 0; n < DP / 8; ++n)
+                    if (n * 8 < a.d)
+                        dst[n * 4 + (lane & 3)] = pg_pack<kF16>(o[n][2 * i] * inv, o[n][2 * i + 1] * inv);
+                if (a.lse && (lane & 3) == 0)
+                    a.lse[static_cast<int64_t>(t.token + tt) * a.heads_q + t.head + h] =
+                        sum == 0.0f ? -INFINITY : (ref + log2f(sum)) * kLn2;
+            } else {
+                float *dst = a.warp_o + (static_cast<int64_t>(slot) * kPagedRowTile + row) * kPagedMaxDim;
 #pragma unroll
-                    for (int n = 0; n < DP / 8; ++n)
-                        if (n * 8 < a.d)
-                            dst[n * 4 + (lane & 3)] =
-                                pg_pack<kF16>(o[mt][n][2 * i] * inv, o[mt][n][2 * i + 1] * inv);
-                    if (a.lse && (lane & 3) == 0)
-                        a.lse[static_cast<int64_t>(t.token + tt) * a.heads_q + t.head + h] =
-                            sum == 0.0f ? -INFINITY : (ref + log2f(sum)) * 0.6931471805599453f;
-                } else {
-                    float *dst = a.part_o + (static_cast<int64_t>(slot) * kPagedRowTile + row) * kPagedMaxDim;
-#pragma unroll
-                    for (int n = 0; n < DP / 8; ++n)
-                        *reinterpret_cast<float2 *>(dst + n * 8 + (lane & 3) * 2) =
-                            make_float2(o[mt][n][2 * i], o[mt][n][2 * i + 1]);
-                    if ((lane & 3) == 0)
-                        *reinterpret_cast<float2 *>(a.part_ml + (static_cast<int64_t>(slot) * kPagedRowTile + row) * 2) =
-                            make_float2(ref, sum);
-                }
+                for (int n = 0; n < DP / 8; ++n)
+                    *reinterpret_cast<float2 *>(dst + n * 8 + (lane & 3) * 2) = make_float2(o[n][2 * i], o[n][2 * i + 1]);
+                if ((lane & 3) == 0)
+                    *reinterpret_cast<float2 *>(a.warp_ml + (static_cast<int64_t>(slot) * kPagedRowTile + row) * 2) =
+                        make_float2(ref, sum);
             }
         }
-        if (p.starts && !p.ends && lane == 0) {
-            PagedJoin j{};
-            j.token = t.token;
-            j.head = t.head;
-            j.tokens = t.tokens;
-            j.heads = t.heads;
-            j.count = cut.owner(p.tile_end - 1) - unit + 1;
-            a.join[unit] = j;
+        if (!whole && lane == 0) {
+            RowPart &r = sm.part[warp][p.starts ? 1 : 0];
+            r.token = t.token;
+            r.head = t.head;
+            r.tokens = t.tokens;
+            r.heads = t.heads;
+            r.rows = rows;
+            r.starts = p.starts;
+            r.ends = p.ends;
+            r.last_cta = cut.owner(p.tile_end - 1) / kPagedWarps;
         }
     }
     cp_wait<0>();
+    __syncthreads();
+
+    // ---- tiles cut between warps of this CTA: their parts, one warp a row.  A
+    // chain of parts of one tile starts with the warp that starts the tile (or
+    // with the first warp, for a tile of the previous CTA) and goes on with the
+    // first parts of the warps behind it.
+    int32_t item = 0;
+    for (int w = -1; w < kPagedWarps; ++w) {
+        const RowPart c = w < 0 ? sm.part[0][0] : sm.part[w][1];
+        if (c.rows == 0)
+            continue;
+        const int first = w < 0 ? 0 : 2 * w + 1;        // slots of the chain: first, then 2 w', w' = next ..
+        const int next = w < 0 ? 1 : w + 1;
+        int n = 1;
+        bool ends = c.ends;
+        while (!ends && next + n - 1 < kPagedWarps && sm.part[next + n - 1][0].rows) {
+            ends = sm.part[next + n - 1][0].ends;
+            ++n;
+        }
+        const bool here = c.starts && ends;             // no other CTA has part of it
+        const int32_t slot = 2 * cta + (c.starts ? 1 : 0);
+        for (int row = 0; row < c.rows; ++row, ++item) {
+            if (item % kPagedWarps != warp)
+                continue;
+            const int32_t tt = row / a.sub, h = row - tt * a.sub;
+            if (h >= c.heads)
+                continue;
+            auto at = [&](int i) {
+                return (static_cast<int64_t>(cta) * 2 * kPagedWarps + (i == 0 ? first : 2 * (next + i - 1))) * kPagedRowTile + row;
+            };
+            float2 ml[kPagedWarps];
+            float4 v[kPagedWarps];
+#pragma unroll
+            for (int i = 0; i < kPagedWarps; ++i) {
+                if (i < n) {
+                    ml[i] = *reinterpret_cast<const float2 *>(a.warp_ml + at(i) * 2);
+                    v[i] = *reinterpret_cast<const float4 *>(a.warp_o + at(i) * kPagedMaxDim + lane * 4);
+                }
+            }
+            RowSum r;
+#pragma unroll
+            for (int i = 0; i < kPagedWarps; ++i)
+                if (i < n)
+                    r.top = fmaxf(r.top, ml[i].x);
+#pragma unroll
+            for (int i = 0; i < kPagedWarps; ++i)
+                if (i < n)
+                    r.add(ml[i], v[i]);
+            if (here) {
+                r.store<kF16>(a, c.token + tt, c.head + h, lane);
+            } else {
+                const int64_t to = static_cast<int64_t>(slot) * kPagedRowTile + row;
+                *reinterpret_cast<float4 *>(a.part_o + to * kPagedMaxDim + lane * 4) = r.acc;
+                if (lane == 0)
+                    *reinterpret_cast<float2 *>(a.part_ml + to * 2) = make_float2(r.top, r.sum);
+            }
+        }
+        if (c.starts && !ends && threadIdx.x == 0) {
+            PagedJoin j{};
+            j.token = c.token;
+            j.head = c.head;
+            j.tokens = c.tokens;
+            j.heads = c.heads;
+            j.count = c.last_cta - cta + 1;
+            a.join[cta] = j;
+        }
+    }
 }
 
-// Joins the parts of every cut tile: with M the largest of the parts' maxima,
-// o = sum 2^(m_i - M) o_i / sum 2^(m_i - M) l_i, in unit order.  One CTA a unit
-// (most find nothing to do and leave), one warp a row, 16 bytes a lane.
-constexpr int kJoinThreads = 256;
+// Joins the parts of every tile cut between CTAs, in their order.  One CTA a
+// unit (those that start no such tile leave), one warp a row, 16 bytes a lane.
+constexpr int kJoinThreads = 512;
 
-template <bool kF16>
-__global__ void __launch_bounds__(kJoinThreads) paged_join(const PagedArgs a, const int tile_rows)
+template <bool kF16> __global__ void __launch_bounds__(kJoinThreads) paged_join(const PagedArgs a)
 {
     const int unit = blockIdx.x;
     const PagedJoin j = a.join[unit];
     if (j.count <= 0)
         return;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int rows = j.tokens * a.sub;
-    for (int row = warp + static_cast<int>(blockIdx.y) * (kJoinThreads / 32); row < rows;
-         row += static_cast<int>(gridDim.y) * (kJoinThreads / 32)) {
-        const int tt = row / a.sub, h = row - tt * a.sub;
-        if (h >= j.heads)
-            continue;
-        float top = -INFINITY;
-        for (int i = lane; i < j.count; i += 32) {
-            const int64_t slot = i == 0 ? 2 * unit + 1 : 2 * (unit + i);
-            top = fmaxf(top, a.part_ml[(slot * tile_rows + row) * 2]);
-        }
+    const int lane = threadIdx.x & 31, row = threadIdx.x >> 5;
+    const int tt = row / a.sub, h = row - tt * a.sub;
+    if (row >= j.tokens * a.sub || h >= j.heads)
+        return;
+    auto at = [&](int i) { return static_cast<int64_t>(i == 0 ? 2 * unit + 1 : 2 * (unit + i)) * kPagedRowTile + row; };
+    RowSum r;
+    for (int i = lane; i < j.count; i += 32)
+        r.top = fmaxf(r.top, a.part_ml[at(i) * 2]);
 #pragma unroll
-        for (int o = 16; o; o >>= 1)
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        const float ref = top == -INFINITY ? 0.0f : top;
-        float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        float sum = 0.0f;
+    for (int o = 16; o; o >>= 1)
+        r.top = fmaxf(r.top, __shfl_xor_sync(0xffffffffu, r.top, o));
 #pragma unroll 8
-        for (int i = 0; i < j.count; ++i) {
-            const int64_t slot = i == 0 ? 2 * unit + 1 : 2 * (unit + i);
-            const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + (slot * tile_rows + row) * 2);
-            const float4 v = *reinterpret_cast<const float4 *>(a.part_o + (slot * tile_rows + row) * kPagedMaxDim + lane * 4);
-            const float f = pg_exp2(ml.x - ref);
-            sum += f * ml.y;
-            acc.x += f * v.x;
-            acc.y += f * v.y;
-            acc.z += f * v.z;
-            acc.w += f * v.w;
-        }
-        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-        if (lane * 4 < a.d) {
-            uint2 w;
-            w.x = pg_pack<kF16>(acc.x * inv, acc.y * inv);
-            w.y = pg_pack<kF16>(acc.z * inv, acc.w * inv);
-            *reinterpret_cast<uint2 *>(static_cast<unsigned char *>(a.out) +
-                                       2 * ((j.token + tt) * a.out_token + (j.head + h) * a.out_head + lane * 4)) = w;
-        }
-        if (a.lse && lane == 0)
-            a.lse[static_cast<int64_t>(j.token + tt) * a.heads_q + j.head + h] =
-                sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
-    }
+    for (int i = 0; i < j.count; ++i)
+        r.add(*reinterpret_cast<const float2 *>(a.part_ml + at(i) * 2),
+              *reinterpret_cast<const float4 *>(a.part_o + at(i) * kPagedMaxDim + lane * 4));
+    r.store<kF16>(a, j.token + tt, j.head + h, lane);
 }
 
 template <int DP, bool kF16> int launch_rows(const PagedArgs &a, int grid, cudaStream_t st)
 {
-    if (a.tok * a.sub <= 16)
-        paged_rows<DP, 1, kF16><<<grid, kRowThreads, kRowSmem, st>>>(a);
-    else
-        paged_rows<DP, 2, kF16><<<grid, kRowThreads, kRowSmem, st>>>(a);
+    paged_rows<DP, kF16><<<grid, kRowThreads, kRowSmem, st>>>(a);
+    if (int e = static_cast<int>(cudaGetLastError()))
+        return e;
+    paged_join<kF16><<<grid, kJoinThreads, 0, st>>>(a);
     return static_cast<int>(cudaGetLastError());
 }
 
@@ -431,17 +483,6 @@ int launch_paged_rows(const PagedArgs &a, bool f16, int grid, void *stream)
     if (a.d <= 64)
         return f16 ? launch_rows<64, true>(a, grid, st) : launch_rows<64, false>(a, grid, st);
     return f16 ? launch_rows<128, true>(a, grid, st) : launch_rows<128, false>(a, grid, st);
-}
-
-int launch_paged_join(const PagedArgs &a, bool f16, int tile_rows, void *stream)
-{
-    const int rows = a.tok * a.sub;
-    const dim3 grid(a.units, rows <= 64 ? 1 : 4);
-    if (f16)
-        paged_join<true><<<grid, kJoinThreads, 0, static_cast<cudaStream_t>(stream)>>>(a, tile_rows);
-    else
-        paged_join<false><<<grid, kJoinThreads, 0, static_cast<cudaStream_t>(stream)>>>(a, tile_rows);
-    return static_cast<int>(cudaGetLastError());
 }
 
 int paged_tables_set_smem();
@@ -456,14 +497,10 @@ int paged_set_smem_limit()
         if (!e)
             e = static_cast<int>(cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowSmem));
     };
-    set(reinterpret_cast<const void *>(&paged_rows<64, 1, false>));
-    set(reinterpret_cast<const void *>(&paged_rows<64, 2, false>));
-    set(reinterpret_cast<const void *>(&paged_rows<64, 1, true>));
-    set(reinterpret_cast<const void *>(&paged_rows<64, 2, true>));
-    set(reinterpret_cast<const void *>(&paged_rows<128, 1, false>));
-    set(reinterpret_cast<const void *>(&paged_rows<128, 2, false>));
-    set(reinterpret_cast<const void *>(&paged_rows<128, 1, true>));
-    set(reinterpret_cast<const void *>(&paged_rows<128, 2, true>));
+    set(reinterpret_cast<const void *>(&paged_rows<64, false>));
+    set(reinterpret_cast<const void *>(&paged_rows<64, true>));
+    set(reinterpret_cast<const void *>(&paged_rows<128, false>));
+    set(reinterpret_cast<const void *>(&paged_rows<128, true>));
     return e;
 }
 

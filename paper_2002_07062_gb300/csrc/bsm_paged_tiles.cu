@@ -4,23 +4,32 @@
 //   s = scale q k^T,  p = exp(s - m),  o = sum p v / sum p   (m a running reference)
 //
 // Bound: the tensor cores (4 D operations a pair of a query row and a key) and,
-// close behind, the exponentials.  One persistent CTA per SM, 10 warps:
+// close behind, the exponentials.  One persistent CTA per SM, 11 warps:
 //   warps 0-3, 4-7  softmax of one 128-row block each: a thread owns a row, reads
-//                   its 128 scores from tensor memory, writes the probabilities
+//                   its 128 scores of a step from tensor memory, writes the probabilities
 //                   back over them as 16-bit pairs, and at the end scales and
 //                   stores its row of the output;
-//   warp 8          producer: walks its share of the work line, copies the two
-//                   query blocks and then blocks of 128 keys and values, page by
-//                   page, with TMA (128-byte swizzle) into a ring of stages;
-//   warp 9          issues tcgen05.mma: scores (both operands in shared memory),
-//                   then probabilities (tensor memory) times values (shared memory,
-//                   rows of head columns: the "N-major" form).
+//   warp 8          producer: walks its share of the work line, copies the query
+//                   blocks and then steps of 128 keys and values, page by page,
+//                   with TMA (128-byte swizzle) into a ring of stages;
+//   warps 9, 10     issue tcgen05.mma, one for each softmax group: scores (both
+//                   operands in shared memory), then probabilities (tensor memory)
+//                   times values (shared memory, rows of head columns: the
+//                   "N-major" form).  One warp for both groups was the limit: 24
+//                   instructions a step, and in order, so a group waited for the
+//                   other's probabilities.
 // The two row blocks share every stage, which halves what an SM reads from L2,
-// and alternate on the tensor cores: while one block's scores become
-// probabilities, the other's products run.  The output stays in tensor memory;
-// it is rescaled only when a row's maximum has grown by more than 2^8 since
-// its reference was taken (any reference gives the same quotient, and 2^8 is
-// far from the range of fp32 sums), so nearly all blocks skip that pass.
+// and take turns on the tensor cores.  (Steps of 64 keys with two score buffers a block would never
+// wait for scores, but a product of 128 x 64 x 16 from shared memory takes 52
+// cycles instead of 32, its operands' bytes, and the issuing warps half again as
+// many instructions: two prompts of 8192 tokens 963 us.)
+// A tile of one row block takes both
+// softmax groups all the same: one has the even key steps, the other the odd
+// ones, each with its own output and reference, and the two are added at the end.
+// Outputs stay in tensor memory; one is rescaled only when a row's maximum has
+// grown by more than 2^8 since its reference was taken (any reference gives the
+// same quotient, and 2^8 is far from the range of fp32 sums), so nearly all
+// blocks skip that pass.
 // Every wait is bounded as in the batched product.
 #include <cuda.h>
 #include <cuda_runtime.h>
@@ -33,33 +42,44 @@
 namespace bsm {
 namespace {
 
-constexpr int kTileThreads = 320;
+constexpr int kTileThreads = 352;
 constexpr int kPrefixThreads = 256;
 constexpr int kKeys = kPagedTileKeys;
-constexpr int kHalfBytes = 128 * 128;                   // 128 rows of 64 columns
-constexpr int kTileHeader = 1024;
+constexpr int kQHalf = 128 * 128;                       // 128 query rows of 64 columns
+constexpr int kHalfBytes = kKeys * 128;                 // a step's keys, 64 columns
+constexpr int kStore = 8 * 32 * 64;                     // a warp's 32 rows of 32 columns on their way out
+constexpr int kTileHeader = 2048;
 constexpr uint32_t kTileTmemCols = 512;
 constexpr int kMaxStages = 8;
 constexpr float kLag = 8.0f;                            // log2 of how far a maximum may pass its reference
 
-// columns of the tensor memory: scores of the two blocks (probabilities over
-// them), outputs of the two
+// columns of the tensor memory: scores of the two blocks (the probabilities of
+// each part over it), outputs of the two
 __device__ __forceinline__ constexpr uint32_t s_col(int sub) { return static_cast<uint32_t>(sub * 128); }
 __device__ __forceinline__ constexpr uint32_t o_col(int sub) { return static_cast<uint32_t>(256 + sub * 128); }
 
+// A step's probabilities come in two parts, the first of this many keys: its
+// product runs beside the exponentials of the second.  (96 and 32: 4 % slower.)
+constexpr int kPartKeys = 64;
+
+template <int N> struct Const {
+    static constexpr int value = N;
+};
+
 template <int DP> struct TileShape {
     static constexpr int kHalves = DP / 64;
-    static constexpr int kStageBytes = kHalves * kHalfBytes;
-    static constexpr int kStages = DP == 128 ? 5 : 8;
-    static constexpr int kQBytes = 2 * kStageBytes;
-    static constexpr int kSmem = 1024 + kTileHeader + kQBytes + kStages * kStageBytes;
+    static constexpr int kStageBytes = kHalves * kHalfBytes;    // keys, or values, of a step
+    static constexpr int kStages = DP == 128 ? 4 : 8;
+    static constexpr int kQBytes = 2 * kHalves * kQHalf;
+    static constexpr int kSmem = 1024 + kTileHeader + kStore + kQBytes + kStages * kStageBytes;
 };
 
 // What the producer tells the other warps of a piece.
 struct TilePiece {
-    int32_t blocks;                     // key blocks; 0: no more pieces
-    int32_t subs;                       // row blocks with rows (1 or 2)
-    int32_t first;                      // first key block
+    int32_t blocks;                     // key steps; 0: no more pieces
+    int32_t subs;                       // softmax groups with work (1 or 2)
+    int32_t dual;                       // one row block: key steps dealt to the two groups in turn
+    int32_t first;                      // first key step
     int32_t lo, hi, pos;                // keys of the tile; position of its first token
     int32_t token, tokens, head, heads;
     int32_t slot;                       // of its partial output; -1: the tile is whole
@@ -69,12 +89,14 @@ struct TilePiece {
 struct TileSmem {
     uint64_t full[kMaxStages], empty[kMaxStages];
     uint64_t qfull, qempty;
-    uint64_t sfull[2], pfull[2], odone[2], ofree[2];
+    uint64_t sfull[2], pfull[2][2], ohalf[2], olast[2], ofree[2];
     uint64_t pcfull[2], pcempty[2];
-    uint64_t tail, drain;
+    uint64_t turn[2];                   // the group may issue its next scores
+    uint64_t tail, drain, xfull;
     TilePiece piece[2];
+    float2 other[128];                  // reference and sum of the second group's rows (dual)
     uint32_t tmem_base;
-    int32_t abort_flag;
+    int32_t abort_flag, no_abort;       // (the second stays 0)
 };
 static_assert(sizeof(TileSmem) <= kTileHeader, "tile header");
 
@@ -145,6 +167,15 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t *r)
         "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
         : "memory");
 }
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r)
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+        "%15, %16};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // Every lane waits; true in all lanes only if none gave up.
@@ -154,9 +185,9 @@ __device__ __forceinline__ bool warp_wait(uint64_t *b, uint32_t parity, const vo
 }
 
 // The same for what is waited for whether or not another warp gave up.
-__device__ __forceinline__ bool warp_drain(uint64_t *b, uint32_t parity)
+__device__ __forceinline__ bool warp_drain(TileSmem &h, uint64_t *b, uint32_t parity)
 {
-    return __all_sync(0xffffffffu, bar_wait(b, parity, nullptr));
+    return __all_sync(0xffffffffu, bar_spin(b, parity, &h.no_abort));
 }
 
 // ------------------------------------------------------------- producer
@@ -197,7 +228,9 @@ __device__ bool produce(const PagedArgs &a, const CUtensorMap &tq, const CUtenso
         t.token = s.t0 + p.tile * a.tok;
         t.tokens = s.m - p.tile * a.tok < a.tok ? s.m - p.tile * a.tok : a.tok;
         t.pos = s.L - s.m + p.tile * a.tok;
-        t.subs = t.tokens > half_tok ? 2 : 1;
+        const int32_t blocks_q = t.tokens > half_tok ? 2 : 1;
+        t.dual = blocks_q == 1 && p.steps > 1;
+        t.subs = t.dual ? 2 : blocks_q;
         t.head = kvh * a.group + sub * a.sub;
         t.heads = a.group - sub * a.sub < a.sub ? a.group - sub * a.sub : a.sub;
         t.slot = p.starts && p.ends ? -1 : 2 * unit + (p.starts ? 1 : 0);
@@ -210,17 +243,17 @@ __device__ bool produce(const PagedArgs &a, const CUtensorMap &tq, const CUtenso
         if (!warp_wait(&h.qempty, (npc & 1u) ^ 1u, &h.abort_flag))
             return false;
         if (elect_one()) {
-            bar_expect(&h.qfull, static_cast<uint32_t>(t.subs * Shape::kHalves * half_tok * a.sub * 128));
-            for (int sb = 0; sb < t.subs; ++sb)
+            bar_expect(&h.qfull, static_cast<uint32_t>(blocks_q * Shape::kHalves * half_tok * a.sub * 128));
+            for (int sb = 0; sb < blocks_q; ++sb)
                 for (int hf = 0; hf < Shape::kHalves; ++hf)
-                    tma_load_3d_q(qs + (sb * Shape::kHalves + hf) * kHalfBytes, &tq, hf * 64, t.head,
+                    tma_load_3d_q(qs + (sb * Shape::kHalves + hf) * kQHalf, &tq, hf * 64, t.head,
                                   t.token + sb * half_tok, &h.qfull);
         }
         __syncwarp();
         ++qloads;
         // keys that some token of the request sees: the others are not read
         int32_t keep = 0;
-        if (a.window && s.L - s.m - a.window + 1 > 0)
+        if (a.window && s.L - s.m >= a.window)
             keep = s.L - s.m - a.window + 1;
         const int64_t row = p.r * a.table_stride;
         // page of this lane's piece of block b: (page, row in it); n_pages: not there, filled with zeros
@@ -237,64 +270,72 @@ __device__ bool produce(const PagedArgs &a, const CUtensorMap &tq, const CUtenso
             }
             return page;
         };
-        int32_t in = 0;
-        int32_t page = page_of(p.first, in);
-        for (int32_t i = 0; i < p.steps; ++i) {
-            const int32_t key0 = (p.first + i) * kKeys;
+        // one stage: keys (side 0) or values of step i, whose pieces lie in the pages given
+        auto load = [&](int32_t i, int side, int32_t page, int32_t in) -> bool {
             const uint32_t have = __ballot_sync(0xffffffffu, page >= 0);
-            // rows of the block that hold no key of the request: zeros for the values (0 times
-            // whatever lies there may be NaN); their scores are masked
+            // rows of the values that belong to no key of the request: zeros (0 times whatever
+            // lies there may be NaN); their scores are masked
+            const int32_t key0 = (p.first + i) * kKeys;
             const int32_t v0 = keep > key0 ? keep - key0 : 0;
             const int32_t v1 = s.L - key0 < kKeys ? (s.L > key0 ? s.L - key0 : 0) : kKeys;
-            const bool ragged = v0 > 0 || v1 < kKeys;
-            int32_t nin = 0, npage = -1;
-#pragma unroll 1
-            for (int kv = 0; kv < 2; ++kv) {
-                if (!warp_wait(&h.empty[pos.s], pos.ph ^ 1u, &h.abort_flag))
-                    return false;
-                const uint32_t st = saddr(stages) + static_cast<uint32_t>(pos.s * Shape::kStageBytes);
-                const bool hold = kv == 1 && ragged;
-                uint64_t *bar = hold ? &h.tail : &h.full[pos.s];
-                if (elect_one())
-                    bar_expect(bar, static_cast<uint32_t>(__popc(have) * box * 128 * Shape::kHalves));
+            const bool hold = side == 1 && (v0 > 0 || v1 < kKeys);
+            if (!warp_wait(&h.empty[pos.s], pos.ph ^ 1u, &h.abort_flag))
+                return false;
+            const uint32_t st = saddr(stages) + static_cast<uint32_t>(pos.s * Shape::kStageBytes);
+            uint64_t *bar = hold ? &h.tail : &h.full[pos.s];
+            if (elect_one())
+                bar_expect(bar, static_cast<uint32_t>(__popc(have) * box * 128 * Shape::kHalves));
+            __syncwarp();
+            for (int c = 0; c < boxes; ++c) {
+                const int32_t pg = __shfl_sync(0xffffffffu, page, c), rw = __shfl_sync(0xffffffffu, in, c);
+                if (!((have >> c) & 1u))
+                    continue;
+                if (elect_one()) {
+#pragma unroll
+                    for (int hf = 0; hf < Shape::kHalves; ++hf)
+                        tma_load_4d(st + hf * kHalfBytes + c * box * 128, side ? &tv : &tk, hf * 64, rw, kvh, pg, bar);
+                }
                 __syncwarp();
-                for (int c = 0; c < boxes; ++c) {
-                    const int32_t pg = __shfl_sync(0xffffffffu, page, c), rw = __shfl_sync(0xffffffffu, in, c);
-                    if (!((have >> c) & 1u))
-                        continue;
-                    if (elect_one()) {
+            }
+            if (hold) {
+                if (!warp_drain(h, &h.tail, tails & 1u))
+                    return false;
+                ++tails;
+                for (int x = lane; x < 8 * kKeys; x += 32) {
+                    const int r = x >> 3;
+                    if (r < v0 || r >= v1) {
 #pragma unroll
                         for (int hf = 0; hf < Shape::kHalves; ++hf)
-                            tma_load_4d(st + hf * kHalfBytes + c * box * 128, kv ? &tv : &tk, hf * 64, rw, kvh, pg, bar);
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(
+                                             st + hf * kHalfBytes + r * 128 + (x & 7) * 16),
+                                         "r"(0)
+                                         : "memory");
                     }
-                    __syncwarp();
                 }
-                if (kv == 0 && i + 1 < p.steps)
-                    npage = page_of(p.first + i + 1, nin);
-                if (hold) {
-                    if (!warp_drain(&h.tail, tails & 1u))
-                        return false;
-                    ++tails;
-                    for (int x = lane; x < 8 * kKeys; x += 32) {
-                        const int r = x >> 3;
-                        if (r < v0 || r >= v1) {
-#pragma unroll
-                            for (int hf = 0; hf < Shape::kHalves; ++hf)
-                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(
-                                                 st + hf * kHalfBytes + r * 128 + (x & 7) * 16),
-                                             "r"(0)
-                                             : "memory");
-                        }
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (elect_one())
-                        bar_arrive(&h.full[pos.s]);
-                    __syncwarp();
-                }
-                ++loaded;
-                pos.step(Shape::kStages);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (elect_one())
+                    bar_arrive(&h.full[pos.s]);
+                __syncwarp();
             }
+            ++loaded;
+            pos.step(Shape::kStages);
+            return true;
+        };
+        // in the order of the products: K0 V0 K1 V1 .., dual K0 K1 V0 K2 V1 ..: the keys of step i,
+        // then the values of step i - lag
+        const int32_t lag = t.dual ? 1 : 0;
+        int32_t in = 0, page = page_of(p.first, in), in1 = 0, page1 = -1;
+        for (int32_t i = 0; i < p.steps + lag; ++i) {
+            int32_t nin = 0, npage = -1;
+            if (i + 1 < p.steps)
+                npage = page_of(p.first + i + 1, nin);      // (read a step ahead)
+            if (i < p.steps && !load(i, 0, page, in))
+                return false;
+            if (i >= lag && !load(i - lag, 1, lag ? page1 : page, lag ? in1 : in))
+                return false;
+            page1 = page;
+            in1 = in;
             page = npage;
             in = nin;
         }
@@ -302,18 +343,27 @@ __device__ bool produce(const PagedArgs &a, const CUtensorMap &tq, const CUtenso
 }
 
 // ------------------------------------------------------------- tensor cores
+// The same value in every lane, for the compiler too: what addresses an MMA
+// has to lie in uniform registers, and moving it there costs more than the MMA.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __reduce_max_sync(0xffffffffu, x); }
+
+// One warp per softmax group.  Both go through all stages; of a stage that is
+// the other group's alone it only takes note.
 template <int DP, bool kF16>
-__device__ bool multiply(TileSmem &h, unsigned char *qs, unsigned char *stages, uint32_t tmem)
+__device__ bool multiply(TileSmem &h, unsigned char *qs, unsigned char *stages, uint32_t tmem_, uint32_t sub_)
 {
     using Shape = TileShape<DP>;
     constexpr uint32_t kScores = tile_idesc<kF16, kKeys, false>(), kOut = tile_idesc<kF16, DP, true>();
-    RingPos pos;                        // next stage: K of the next block, then V of this one
-    uint32_t nblk[2] = {0, 0}, npiece[2] = {0, 0};
+    const uint32_t tmem = uniform(tmem_);
+    const int sub = static_cast<int>(uniform(sub_));
+    RingPos pos;
+    uint32_t np = 0, used = 0, turns = 0;   // steps' outputs issued; pieces with work; turns taken
     for (uint32_t npc = 0;; ++npc) {
         if (!warp_wait(&h.pcfull[npc & 1u], (npc >> 1) & 1u, &h.abort_flag))
             return false;
-        const int32_t blocks = __shfl_sync(0xffffffffu, h.piece[npc & 1u].blocks, 0);
-        const int32_t subs = __shfl_sync(0xffffffffu, h.piece[npc & 1u].subs, 0);
+        const int32_t blocks = static_cast<int32_t>(uniform(static_cast<uint32_t>(h.piece[npc & 1u].blocks)));
+        const int32_t subs = static_cast<int32_t>(uniform(static_cast<uint32_t>(h.piece[npc & 1u].subs)));
+        const bool dual = uniform(static_cast<uint32_t>(h.piece[npc & 1u].dual)) != 0;
         __syncwarp();
         if (elect_one())
             bar_arrive(&h.pcempty[npc & 1u]);
@@ -322,85 +372,152 @@ __device__ bool multiply(TileSmem &h, unsigned char *qs, unsigned char *stages, 
             return true;
         if (!warp_wait(&h.qfull, npc & 1u, &h.abort_flag))
             return false;
-        auto scores = [&](int sub, int stage) {
-            const uint64_t ad = smem_desc(qs + sub * Shape::kStageBytes);
-            const uint64_t bd = smem_desc(stages + stage * Shape::kStageBytes);
-#pragma unroll
-            for (int k = 0; k < DP / 16; ++k) {
-                const uint64_t off = static_cast<uint64_t>((k / 4) * (kHalfBytes >> 4) + (k % 4) * 2);
-                mma_ss(tmem + s_col(sub), ad + off, bd + off, kScores, k != 0);
-            }
-            mma_commit(&h.sfull[sub]);
-        };
-        // K of the first block
-        if (!warp_wait(&h.full[pos.s], pos.ph, &h.abort_flag))
-            return false;
-        tc_fence_after();
-        if (elect_one()) {
-            for (int sub = 0; sub < subs; ++sub)
-                scores(sub, pos.s);
-            mma_commit(&h.empty[pos.s]);
-            if (blocks == 1)
-                mma_commit(&h.qempty);
-        }
+        const bool active = sub < subs;
+        const int32_t lead = dual ? 2 : 1;
+        const int32_t from = dual ? sub : 0;            // this group's steps: from, from + lead .. last
+        const int32_t last = dual ? blocks - 1 - ((blocks - 1 - sub) & 1) : blocks - 1;
+        const uint64_t ad = smem_desc(qs + (dual ? 0 : sub) * (Shape::kHalves * kQHalf));
+        if (!active && elect_one())
+            bar_arrive(&h.qempty);
         __syncwarp();
-        pos.step(Shape::kStages);
-        for (int32_t j = 0; j < blocks; ++j) {
-            const bool next = j + 1 < blocks;
-            const int vs = pos.s;
-            const uint32_t vph = pos.ph;
+        const uint32_t to_s = tmem + s_col(sub), to_o = tmem + o_col(sub);
+        auto scores = [&](int32_t i, int stage) {
+            const uint64_t kd = smem_desc(stages + stage * Shape::kStageBytes);
+#pragma unroll
+            for (int d = 0; d < DP / 16; ++d)
+                mma_ss(to_s, ad + (d / 4) * (kQHalf >> 4) + (d % 4) * 2, kd + (d / 4) * (kHalfBytes >> 4) + (d % 4) * 2,
+                       kScores, d != 0);
+            mma_commit(&h.sfull[sub]);
+            mma_commit(&h.empty[stage]);
+            if (i == last)
+                mma_commit(&h.qempty);
+        };
+        // scores of the first steps
+        for (int32_t i = 0; i < lead; ++i) {
+            if (!warp_wait(&h.full[pos.s], pos.ph, &h.abort_flag))
+                return false;
+            tc_fence_after();
+            const bool mine = active && (!dual || i == sub);
+            if (elect_one()) {
+                if (mine)
+                    scores(i, pos.s);
+                else
+                    bar_arrive(&h.empty[pos.s]);
+            }
+            __syncwarp();
             pos.step(Shape::kStages);
-            const int ks = pos.s;
-            const uint32_t kph = pos.ph;
-            if (next)
-                pos.step(Shape::kStages);
-            for (int sub = 0; sub < subs; ++sub) {
-                if (sub == 0 && !warp_wait(&h.full[vs], vph, &h.abort_flag))
-                    return false;
-                if (!warp_wait(&h.pfull[sub], nblk[sub] & 1u, &h.abort_flag))
-                    return false;
-                ++nblk[sub];
+        }
+        // then the output of step j and the scores of step j + lead, whose keys are waited for
+        // before the probabilities, so that nothing lies between the last product and them
+        for (int32_t j = 0; j < blocks; ++j) {
+            const bool mine = active && (!dual || (j & 1) == sub), more = j + lead < blocks;
+            if (!warp_wait(&h.full[pos.s], pos.ph, &h.abort_flag))
+                return false;
+            const int vs = pos.s;
+            pos.step(Shape::kStages);
+            if (!mine) {
+                if (elect_one())
+                    bar_arrive(&h.empty[vs]);
+                __syncwarp();
+            } else {
                 // the previous piece's output has been read
-                if (j == 0) {
-                    if (!warp_wait(&h.ofree[sub], (npiece[sub] & 1u) ^ 1u, &h.abort_flag))
-                        return false;
-                    ++npiece[sub];
-                }
-                if (sub == 0 && next && !warp_wait(&h.full[ks], kph, &h.abort_flag))
+                if (j == from && !warp_wait(&h.ofree[sub], (used++ & 1u) ^ 1u, &h.abort_flag))
+                    return false;
+            }
+            const uint64_t vd = smem_desc_n(saddr(stages) + static_cast<uint32_t>(vs * Shape::kStageBytes));
+            if (mine) {
+                if (!warp_wait(&h.pfull[sub][0], np & 1u, &h.abort_flag))
                     return false;
                 tc_fence_after();
                 if (elect_one()) {
-                    const uint64_t bd = smem_desc_n(saddr(stages) + vs * Shape::kStageBytes);
 #pragma unroll
-                    for (int k = 0; k < kKeys / 16; ++k)
-                        mma_ts(tmem + o_col(sub), tmem + s_col(sub) + k * 8, bd + k * (2048 >> 4), kOut, (j | k) != 0);
-                    mma_commit(&h.odone[sub]);
-                    if (sub == subs - 1)
-                        mma_commit(&h.empty[vs]);
-                    if (next) {
-                        scores(sub, ks);
-                        if (sub == subs - 1) {
-                            mma_commit(&h.empty[ks]);
-                            if (j + 2 == blocks)
-                                mma_commit(&h.qempty);
-                        }
-                    }
+                    for (int k = 0; k < kPartKeys / 16; ++k)
+                        mma_ts(to_o, to_s + k * 8, vd + k * (2048 >> 4), kOut, j != from || k != 0);
+                    mma_commit(&h.ohalf[sub]);
                 }
                 __syncwarp();
             }
+            const int ks = pos.s;
+            if (more) {
+                if (!warp_wait(&h.full[ks], pos.ph, &h.abort_flag))
+                    return false;
+                pos.step(Shape::kStages);
+            }
+            if (mine && !warp_wait(&h.pfull[sub][1], np++ & 1u, &h.abort_flag))
+                return false;
+            // The groups take turns: products of both, issued at once, would be done at once, and
+            // the groups' exponentials and products would go on at the same time, each leaving
+            // the other's unit idle.  (The first group's turn at the start has no barrier.)
+            if (mine && subs == 2) {
+                if ((sub == 1 || turns > 0) && !warp_wait(&h.turn[sub], (turns - (sub == 0 ? 1u : 0u)) & 1u, &h.abort_flag))
+                    return false;
+                ++turns;
+            }
+            tc_fence_after();
+            if (elect_one()) {
+                if (mine) {
+#pragma unroll
+                    for (int k = kPartKeys / 16; k < kKeys / 16; ++k)
+                        mma_ts(to_o, to_s + kPartKeys + (k - kPartKeys / 16) * 8, vd + k * (2048 >> 4), kOut, 1u);
+                    if (j == last)
+                        mma_commit(&h.olast[sub]);
+                    mma_commit(&h.empty[vs]);
+                    if (more)
+                        scores(j + lead, ks);
+                    if (subs == 2)
+                        bar_arrive(&h.turn[dual ? (j + 1 < blocks ? 1 - sub : 0) : 1 - sub]);
+                } else if (more) {
+                    bar_arrive(&h.empty[ks]);
+                }
+            }
+            __syncwarp();
         }
     }
 }
 
 // ------------------------------------------------------------- softmax
+__device__ __forceinline__ uint64_t pair(float lo, float hi)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t p, float &lo, float &hi)
+{
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(p));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// Waits for this thread's loads from tensor memory; r[0 .. N-1] are used after it.
+template <int N> __device__ __forceinline__ void tmem_landed(uint32_t *r)
+{
+    tmem_wait_ld();
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        asm volatile("" : "+r"(r[i]));
+}
+
 template <int DP, bool kF16>
-__device__ bool softmax(const PagedArgs &a, TileSmem &h, uint32_t tmem, int sub, int32_t unit)
+__device__ bool softmax(const PagedArgs &a, TileSmem &h, unsigned char *store, uint32_t tmem, int sub, int32_t unit)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quarter = warp & 3;
     const int row = quarter * 32 + lane;                // of the row block
     const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
     const int32_t tt = row / a.sub, hh = row - tt * a.sub, half_tok = a.tok / 2;
-    uint32_t nblk = 0;
+    const uint64_t scale2 = pair(a.scale_log2, a.scale_log2);
+    unsigned char *mine = store + warp * (32 * 64);
+    uint32_t n = 0, pieces = 0, pieces1 = 0, duals = 0; // steps and pieces so far; pieces of the second group
     for (uint32_t npc = 0;; ++npc) {
         if (!warp_wait(&h.pcfull[npc & 1u], (npc >> 1) & 1u, &h.abort_flag))
             return false;
@@ -412,134 +529,205 @@ __device__ bool softmax(const PagedArgs &a, TileSmem &h, uint32_t tmem, int sub,
             return true;
         if (sub >= t.subs)
             continue;
-        const int32_t tok = sub * half_tok + tt;        // of the tile
+        const int32_t tok = (t.dual ? 0 : sub * half_tok) + tt;     // of the tile
         const bool live = tt < half_tok && tok < t.tokens && hh < t.heads;
+        const bool idle = !__any_sync(0xffffffffu, live);
         // keys this row sees; rows that are not stored compute whatever comes
         int32_t lo = 0, hi = INT32_MAX;
         if (live) {
             hi = t.hi;
             if (a.causal) {
                 hi = t.pos + tok + 1 < t.hi ? t.pos + tok + 1 : t.hi;
-                if (a.window && t.pos + tok - a.window + 1 > 0)
+                if (a.window && t.pos + tok >= a.window)
                     lo = t.pos + tok - a.window + 1;
             }
         }
         float ref = -INFINITY, sum = 0.0f;              // reference (log2), sum of probabilities
-        for (int32_t j = 0; j < t.blocks; ++j, ++nblk) {
-            if (!warp_wait(&h.sfull[sub], nblk & 1u, &h.abort_flag))
+        const int32_t j0 = t.dual ? sub : 0, dj = t.dual ? 2 : 1;
+        for (int32_t j = j0; j < t.blocks; j += dj, ++n) {
+            if (!warp_wait(&h.sfull[sub], n & 1u, &h.abort_flag))
                 return false;
             tc_fence_after();
-            uint32_t r[128];
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-                tmem_ld32_nowait(lanes + s_col(sub) + c * 32, r + c * 32);
-            tmem_wait_ld();
-            float x[128];
-#pragma unroll
-            for (int c = 0; c < 128; ++c)
-                x[c] = __uint_as_float(r[c]);
-            const int32_t key0 = (t.first + j) * kKeys;
-            if (!__all_sync(0xffffffffu, lo <= key0 && hi - kKeys >= key0)) {
-                const int32_t c0 = lo - key0, c1 = hi - key0;
-#pragma unroll
-                for (int c = 0; c < 128; ++c)
-                    x[c] = c >= c0 && c < c1 ? x[c] : -INFINITY;
-            }
-            float top4[4] = {x[0], x[1], x[2], x[3]};
-#pragma unroll
-            for (int c = 4; c < 128; ++c)
-                top4[c & 3] = fmaxf(top4[c & 3], x[c]);
-            const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3])) * a.scale_log2;
-            // (a maximum of -inf moves nothing; NaN neither: it comes out in the sum)
-            const bool move = top > ref + kLag;
-            if (__any_sync(0xffffffffu, move)) {
-                const float f = !move ? 1.0f : pg_exp2(ref - top);
-                ref = move ? top : ref;
-                sum *= f;
-                if (j > 0) {
-                    // the product of the previous block still adds to the output
-                    if (!warp_wait(&h.odone[sub], (nblk & 1u) ^ 1u, &h.abort_flag))
-                        return false;
-                    tc_fence_after();
-#pragma unroll 1
-                    for (int c = 0; c < DP / 32; ++c) {
-                        uint32_t o[32];
-                        tmem_ld32_nowait(lanes + o_col(sub) + c * 32, o);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                        tmem_st32(lanes + o_col(sub) + c * 32, o);
-                    }
+            if (idle) {
+                // no row of this warp is stored: whatever lies there will do
+                __syncwarp();
+                if (lane == 0) {
+                    bar_arrive(&h.pfull[sub][0]);
+                    bar_arrive(&h.pfull[sub][1]);
                 }
+                continue;
             }
-            const float base = ref == -INFINITY ? 0.0f : ref - pg_shift<kF16>(kLag);
-            float s4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            uint32_t pr[64];
+            auto probabilities = [&](auto from_, auto cols_) -> bool {
+                constexpr int kFrom = decltype(from_)::value, kCols = decltype(cols_)::value;
+                const uint32_t sc = lanes + s_col(sub) + kFrom;
+                uint32_t r[kCols];
 #pragma unroll
-            for (int c = 0; c < 128; c += 2) {
-                const float p0 = pg_exp2(fmaf(x[c], a.scale_log2, -base));
-                const float p1 = pg_exp2(fmaf(x[c + 1], a.scale_log2, -base));
-                s4[c & 2] += p0;
-                s4[(c & 2) + 1] += p1;
-                pr[c / 2] = pg_pack<kF16>(p0, p1);
-            }
-            sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
-            tmem_st32(lanes + s_col(sub), pr);
-            tmem_st32(lanes + s_col(sub) + 32, pr + 32);
-            tmem_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0)
-                bar_arrive(&h.pfull[sub]);
-        }
-        // ---- the row's output
-        if (!warp_wait(&h.odone[sub], (nblk & 1u) ^ 1u, &h.abort_flag))
-            return false;
-        tc_fence_after();
-        const float base = ref - pg_shift<kF16>(kLag);
-        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-        const int64_t token = t.token + tok;
-        unsigned char *dst = static_cast<unsigned char *>(a.out) + 2 * (token * a.out_token + (t.head + hh) * a.out_head);
-        float *part = a.part_o + static_cast<int64_t>(t.slot) * (256 * kPagedMaxDim) + (sub * 128 + row) * 4;
+                for (int c = 0; c < kCols; c += 32)
+                    tmem_ld32_nowait(sc + c, r + c);
+                const int32_t key0 = (t.first + j) * kKeys + kFrom;
+                const bool masked = !__all_sync(0xffffffffu, lo <= key0 && hi - kCols >= key0);
+                tmem_landed<kCols>(r);
+                if (masked) {
+                    const int32_t c0 = lo - key0, c1 = hi - key0;
+#pragma unroll
+                    for (int c = 0; c < kCols; ++c)
+                        r[c] = c >= c0 && c < c1 ? r[c] : 0xFF800000u;
+                }
+                float top4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int c = 0; c < kCols; c += 2)
+                    top4[(c >> 1) & 3] =
+                        fmaxf(fmaxf(top4[(c >> 1) & 3], __uint_as_float(r[c])), __uint_as_float(r[c + 1]));
+                const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3])) * a.scale_log2;
+                // (a maximum of -inf moves nothing; NaN neither: it comes out in the sum)
+                const bool move = top > ref + kLag;
+                if (__any_sync(0xffffffffu, move)) {
+                    const float f = !move ? 1.0f : pg_exp2(ref - top);
+                    ref = move ? top : ref;
+                    sum *= f;
+                    if (j != j0 || kFrom) {
+                        // the products so far still add to the output: those of earlier steps are done
+                        // (this step's scores were issued behind them), the first part's may not be
+                        if (kFrom && !warp_wait(&h.ohalf[sub], n & 1u, &h.abort_flag))
+                            return false;
+                        tc_fence_after();
 #pragma unroll 1
-        for (int c = 0; c < DP / 32; ++c) {
-            uint32_t o[32];
-            tmem_ld32_nowait(lanes + o_col(sub) + c * 32, o);
-            tmem_wait_ld();
-            const float *f = reinterpret_cast<const float *>(o);
-            if (t.slot < 0) {
-                if (live) {
+                        for (int c = 0; c < DP / 32; ++c) {
+                            uint32_t o[32];
+                            tmem_ld32_nowait(lanes + o_col(sub) + c * 32, o);
+                            tmem_landed<32>(o);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if (c * 32 + i * 8 < a.d) {
-                            uint4 w;
-                            w.x = pg_pack<kF16>(f[8 * i] * inv, f[8 * i + 1] * inv);
-                            w.y = pg_pack<kF16>(f[8 * i + 2] * inv, f[8 * i + 3] * inv);
-                            w.z = pg_pack<kF16>(f[8 * i + 4] * inv, f[8 * i + 5] * inv);
-                            w.w = pg_pack<kF16>(f[8 * i + 6] * inv, f[8 * i + 7] * inv);
-                            *reinterpret_cast<uint4 *>(dst + (c * 32 + i * 8) * 2) = w;
+                            for (int i = 0; i < 32; ++i)
+                                o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                            tmem_st32(lanes + o_col(sub) + c * 32, o);
                         }
                     }
                 }
+                const float base = ref == -INFINITY ? 0.0f : ref - pg_shift<kF16>(kLag);
+                const uint64_t base2 = pair(-base, -base);
+                uint64_t s2[2] = {0, 0};
+                uint32_t pr[kCols / 2];
+#pragma unroll
+                for (int c = 0; c < kCols; c += 2) {
+                    float p0, p1;
+                    unpair(fma2(pair(__uint_as_float(r[c]), __uint_as_float(r[c + 1])), scale2, base2), p0, p1);
+                    p0 = pg_exp2(p0);
+                    p1 = pg_exp2(p1);
+                    s2[(c >> 1) & 1] = add2(s2[(c >> 1) & 1], pair(p0, p1));
+                    pr[c / 2] = pg_pack<kF16>(p0, p1);
+                }
+#pragma unroll
+                for (int c = 0; c < kCols / 2; c += 16)
+                    tmem_st16(sc + c, pr + c);
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0)
+                    bar_arrive(&h.pfull[sub][kFrom ? 1 : 0]);
+                float e0, e1;
+                unpair(add2(s2[0], s2[1]), e0, e1);
+                sum += e0 + e1;
+                return true;
+            };
+            if (!probabilities(Const<0>{}, Const<kPartKeys>{}) ||
+                !probabilities(Const<kPartKeys>{}, Const<kKeys - kPartKeys>{}))
+                return false;
+        }
+        // ---- the row's output
+        if (!warp_wait(&h.olast[sub], pieces++ & 1u, &h.abort_flag))
+            return false;
+        pieces1 += t.subs == 2 ? 1 : 0;
+        float base = ref - pg_shift<kF16>(kLag), f0 = 1.0f, f1 = 0.0f;
+        if (t.dual) {
+            if (sub == 1) {
+                // the first group adds and stores both outputs
+                h.other[row] = make_float2(base, sum);
+                __syncwarp();
+                if (lane == 0)
+                    bar_arrive(&h.xfull);
+                continue;
+            }
+            if (!warp_wait(&h.xfull, duals & 1u, &h.abort_flag) ||
+                !warp_wait(&h.olast[1], (pieces1 & 1u) ^ 1u, &h.abort_flag))
+                return false;
+            ++duals;
+            const float2 x = h.other[row];
+            const float both = fmaxf(base, x.x), at = both == -INFINITY ? 0.0f : both;
+            f0 = pg_exp2(base - at);
+            f1 = pg_exp2(x.x - at);
+            sum = f0 * sum + f1 * x.y;
+            base = both;
+        }
+        tc_fence_after();
+        const int64_t token = t.token + tok;
+        const int64_t off = 2 * (token * a.out_token + (t.head + hh) * a.out_head);
+        const int srow = (t.dual ? 0 : sub) * 128 + row;
+        float *part = a.part_o + static_cast<int64_t>(t.slot) * (kPagedTileRows * kPagedMaxDim) + srow * 4;
+        if (t.slot < 0) {
+            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            f0 *= inv;
+            f1 *= inv;
+        }
+#pragma unroll 1
+        for (int c = 0; c < DP / 32 && !idle; ++c) {
+            uint32_t o[32];
+            float f[32];
+            tmem_ld32_nowait(lanes + o_col(sub) + c * 32, o);
+            tmem_landed<32>(o);
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                f[i] = __uint_as_float(o[i]) * f0;
+            if (t.dual) {
+                tmem_ld32_nowait(lanes + o_col(1) + c * 32, o);
+                tmem_landed<32>(o);
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    f[i] = fmaf(__uint_as_float(o[i]), f1, f[i]);
+            }
+            if (t.slot < 0) {
+                // through shared memory, so that four lanes store 64 bytes of a row (a lane storing
+                // its own row touches 32 lines at once); 16-byte pieces swizzled over the banks
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint4 w;
+                    w.x = pg_pack<kF16>(f[8 * i], f[8 * i + 1]);
+                    w.y = pg_pack<kF16>(f[8 * i + 2], f[8 * i + 3]);
+                    w.z = pg_pack<kF16>(f[8 * i + 4], f[8 * i + 5]);
+                    w.w = pg_pack<kF16>(f[8 * i + 6], f[8 * i + 7]);
+                    *reinterpret_cast<uint4 *>(mine + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4)) = w;
+                }
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = i * 8 + (lane >> 2), k = lane & 3;
+                    const int64_t to = __shfl_sync(0xffffffffu, off, r);
+                    const bool ok = __shfl_sync(0xffffffffu, live ? 1 : 0, r) != 0;
+                    const uint4 w = *reinterpret_cast<const uint4 *>(mine + r * 64 + ((k ^ ((r >> 1) & 3)) << 4));
+                    if (ok && c * 32 + k * 8 < a.d)
+                        *reinterpret_cast<uint4 *>(static_cast<unsigned char *>(a.out) + to + (c * 32 + k * 8) * 2) = w;
+                }
+                __syncwarp();
             } else {
                 // four columns of a row together, rows side by side: a warp stores 512 bytes at once
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    *reinterpret_cast<float4 *>(part + static_cast<int64_t>(c * 8 + i) * (256 * 4)) =
+                    *reinterpret_cast<float4 *>(part + static_cast<int64_t>(c * 8 + i) * (kPagedTileRows * 4)) =
                         make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
             }
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0)
+        if (lane == 0) {
             bar_arrive(&h.ofree[sub]);
+            if (t.dual)
+                bar_arrive(&h.ofree[1]);
+        }
         if (t.slot < 0) {
             if (live && a.lse)
                 a.lse[token * a.heads_q + t.head + hh] =
                     sum == 0.0f ? -INFINITY : (base + log2f(sum)) * 0.6931471805599453f;
         } else {
-            *reinterpret_cast<float2 *>(a.part_ml + (static_cast<int64_t>(t.slot) * 256 + sub * 128 + row) * 2) =
+            *reinterpret_cast<float2 *>(a.part_ml + (static_cast<int64_t>(t.slot) * kPagedTileRows + srow) * 2) =
                 make_float2(base, sum);
         }
         if (t.join > 0 && sub == 0 && threadIdx.x == 0) {
@@ -563,27 +751,31 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     extern __shared__ __align__(1024) unsigned char raw[];
     unsigned char *smem = raw + ((1024u - (saddr(raw) & 1023u)) & 1023u);
     TileSmem &h = *reinterpret_cast<TileSmem *>(smem);
-    unsigned char *qs = smem + kTileHeader, *stages = qs + Shape::kQBytes;
+    unsigned char *store = smem + kTileHeader, *qs = store + kStore, *stages = qs + Shape::kQBytes;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
     const int32_t unit = blockIdx.x;
     if (threadIdx.x == 0) {
         for (int s = 0; s < Shape::kStages; ++s) {
             bar_init(&h.full[s], 1);
-            bar_init(&h.empty[s], 1);
+            bar_init(&h.empty[s], 2);
         }
         bar_init(&h.qfull, 1);
-        bar_init(&h.qempty, 1);
+        bar_init(&h.qempty, 2);
         for (int s = 0; s < 2; ++s) {
             bar_init(&h.sfull[s], 1);
-            bar_init(&h.pfull[s], 4);
-            bar_init(&h.odone[s], 1);
+            bar_init(&h.pfull[s][0], 4);
+            bar_init(&h.pfull[s][1], 4);
+            bar_init(&h.ohalf[s], 1);
+            bar_init(&h.olast[s], 1);
             bar_init(&h.ofree[s], 4);
+            bar_init(&h.turn[s], 1);
             bar_init(&h.pcfull[s], 1);
-            bar_init(&h.pcempty[s], 9);
+            bar_init(&h.pcempty[s], 10);
         }
         bar_init(&h.tail, 1);
-        bar_init(&h.drain, 1);
-        h.abort_flag = 0;
+        bar_init(&h.drain, 2);
+        bar_init(&h.xfull, 4);
+        h.abort_flag = h.no_abort = 0;
         a.join[unit].count = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -607,7 +799,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = h.tmem_base;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, h.tmem_base, 0);
 
     bool ok;
     if (warp == 8) {
@@ -623,11 +815,11 @@ __global__ void __launch_bounds__(kTileThreads, 1)
         // copies in flight land before the CTA leaves
         const uint32_t S = Shape::kStages;
         for (uint32_t j = loaded > S ? loaded - S : 0u; j < loaded; ++j)
-            warp_drain(&h.full[j % S], (j / S) & 1u);
+            warp_drain(h, &h.full[j % S], (j / S) & 1u);
         if (qloads)
-            warp_drain(&h.qfull, (qloads - 1) & 1u);
-    } else if (warp == 9) {
-        ok = multiply<DP, kF16>(h, qs, stages, tmem);
+            warp_drain(h, &h.qfull, (qloads - 1) & 1u);
+    } else if (warp >= 9) {
+        ok = multiply<DP, kF16>(h, qs, stages, tmem, warp - 9);
         if (elect_one()) {
             if (!ok) {
                 atomicOr(a.status, BSM_DEV_TIMEOUT);
@@ -637,9 +829,9 @@ __global__ void __launch_bounds__(kTileThreads, 1)
         }
         __syncwarp();
         // every product has finished before the tensor memory is freed
-        warp_drain(&h.drain, 0);
+        warp_drain(h, &h.drain, 0);
     } else {
-        ok = softmax<DP, kF16>(a, h, tmem, warp >> 2, unit);
+        ok = softmax<DP, kF16>(a, h, store, tmem, warp >> 2, unit);
         if (!ok) {
             if ((threadIdx.x & 31) == 0) {
                 atomicOr(a.status, BSM_DEV_TIMEOUT);
