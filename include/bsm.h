@@ -302,7 +302,8 @@ int bsm_bmm_ex(const void *a, const void *bt, void *c, int64_t B, int64_t M, int
  * gives the same answer.  Page ids are not checked here.
  * Errors: BSM_ERR_INVALID_ARG (sizes, null pointers, outputs that overlap each
  * other or an input), BSM_ERR_MISALIGNED (8 bytes for slots and info, 4 for the
- * rest), BSM_ERR_CUDA.
+ * rest), BSM_ERR_UNSUPPORTED (tables of 2^20 entries a request and wider),
+ * BSM_ERR_CUDA.
  */
 #define BSM_PAGED_PAGES 1u      /* free_pages ran out */
 #define BSM_PAGED_WIDTH 2u      /* a request needs more than table_width pages: the rest has no slot */

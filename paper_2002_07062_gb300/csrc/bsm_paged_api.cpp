@@ -154,6 +154,8 @@ int paged_tables(const bsm_paged_tables_desc *d, bsm_stream_t stream)
     if (!d || d->n_requests < 0 || d->n_free < 0 || d->page_size < 1 || d->table_width < 1 || d->n_slots < 0 ||
         d->table_stride < d->table_width)
         return BSM_ERR_INVALID_ARG;
+    if (d->table_width >= (1 << 20))
+        return BSM_ERR_UNSUPPORTED;
     if (!d->starts || !d->info || (d->n_requests > 0 && (!d->cached || !d->fresh || !d->tables || !d->lengths)) ||
         (d->n_free > 0 && !d->free_pages) || (d->n_slots > 0 && (!d->slots || !d->positions || !d->owners)))
         return BSM_ERR_INVALID_ARG;
@@ -209,6 +211,8 @@ int paged_write(const bsm_paged_write_desc *d, bsm_stream_t stream)
         return BSM_OK;
     if (!d->k || !d->v || !d->k_cache || !d->v_cache || !d->slots || d->n_pages == 0)
         return BSM_ERR_INVALID_ARG;
+    if (static_cast<int64_t>(d->n_heads) * d->head_dim >= (int64_t(1) << 31))
+        return BSM_ERR_UNSUPPORTED;
     const int es = elem_size(d->dtype);
     const int64_t row = static_cast<int64_t>(d->head_dim) * es;
     const int64_t ks = extent2(d->n_tokens, d->k_stride_token, d->n_heads, d->k_stride_head, d->head_dim, es);

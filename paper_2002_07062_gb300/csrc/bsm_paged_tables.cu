@@ -18,14 +18,15 @@ constexpr int kTabPer = 4;                              // requests of a thread
 constexpr int kTabTile = kTabThreads * kTabPer;         // requests scanned at once
 
 struct TabSmem {
-    int64_t tok[kTabTile + 1];      // tokens before each request of the tile
-    int64_t pg[kTabTile + 1];       // new pages before it
-    int64_t warp_tok[kTabThreads / 32], warp_pg[kTabThreads / 32];
+    int32_t tok[kTabTile + 1];      // tokens of the tile before each request
+    int32_t pg[kTabTile + 1];       // new pages of the tile before it
+    int64_t warp_tok[kTabThreads / 32];
+    int32_t warp_pg[kTabThreads / 32];
     int32_t cached[kTabTile], have[kTabTile];
 };
 
 // Largest i with pre[i] <= x, pre[0] <= x < pre[n] ascending.
-__device__ __forceinline__ int find_last(const int64_t *pre, int n, int64_t x)
+__device__ __forceinline__ int find_last(const int32_t *pre, int n, int32_t x)
 {
     int lo = 0, hi = n;
     while (hi - lo > 1) {
@@ -38,13 +39,18 @@ __device__ __forceinline__ int find_last(const int64_t *pre, int n, int64_t x)
     return lo;
 }
 
+__device__ __forceinline__ uint32_t pages_of(uint32_t tokens, uint32_t page) { return tokens / page + (tokens % page ? 1u : 0u); }
+
 // Prefix sums of the requests' tokens and of the pages they take, then every
 // token's owner, position and slot, and the new table entries.  Each CTA scans
 // all requests (two loads of 4 bytes each, 2048 requests at a time) instead of
 // waiting for another's sums, and writes its own range of tokens and entries;
 // a token finds its owner by bisection in the shared prefix.  One launch, no
 // scratch, no order between CTAs: a page of a new token comes from the free
-// list, not from the table entry another CTA writes.
+// list, not from the table entry another CTA writes.  Bound by latency: loads,
+// scan, search and stores follow one another.  Everything per token and request
+// is 32-bit (a tile's new pages fit, tables being less than 2^20 wide; its
+// tokens are cut at 2^31, past any slot); only running totals are 64-bit.
 __global__ void __launch_bounds__(kTabThreads) paged_tables(const PagedTablesArgs a)
 {
     extern __shared__ __align__(16) unsigned char raw[];
@@ -53,43 +59,45 @@ __global__ void __launch_bounds__(kTabThreads) paged_tables(const PagedTablesArg
     // this CTA's tokens
     const int64_t t_lo = static_cast<int64_t>(a.n_slots) * blockIdx.x / gridDim.x;
     const int64_t t_hi = static_cast<int64_t>(a.n_slots) * (blockIdx.x + 1) / gridDim.x;
-    const int64_t stride = static_cast<int64_t>(gridDim.x) * kTabThreads;
+    const uint32_t stride = gridDim.x * kTabThreads;
     const int64_t limit = static_cast<int64_t>(a.width) * a.page;
+    const uint32_t page_size = static_cast<uint32_t>(a.page), width = static_cast<uint32_t>(a.width);
     int64_t tok_base = 0, pg_base = 0;
     uint32_t flags = 0;
 
     for (int r0 = 0; r0 < a.n; r0 += kTabTile) {
-        int64_t tok[kTabPer], pg[kTabPer];
-        int64_t tsum = 0, psum = 0;
+        int64_t tok[kTabPer], tsum = 0;
+        int32_t pg[kTabPer], psum = 0;
+        int32_t cs[kTabPer], fs[kTabPer];
 #pragma unroll
         for (int i = 0; i < kTabPer; ++i) {
-            const int j = tid * kTabPer + i, r = r0 + j;
-            int64_t c = 0, f = 0;
-            if (r < a.n) {
-                c = a.cached[r];
-                f = a.fresh[r];
-                if (c < 0 || f < 0) {
-                    flags |= BSM_PAGED_NEGATIVE;
-                    c = c < 0 ? 0 : c;
-                    f = f < 0 ? 0 : f;
-                }
-                if (c + f > limit)
-                    flags |= BSM_PAGED_WIDTH;
-            }
-            const int64_t have_all = (c + a.page - 1) / a.page, need_all = (c + f + a.page - 1) / a.page;
-            const int64_t have = have_all < a.width ? have_all : a.width;
-            const int64_t need = need_all < a.width ? need_all : a.width;
+            const int r = r0 + tid * kTabPer + i;
+            cs[i] = r < a.n ? a.cached[r] : 0;
+            fs[i] = r < a.n ? a.fresh[r] : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < kTabPer; ++i) {
+            const int j = tid * kTabPer + i;
+            if (cs[i] < 0 || fs[i] < 0)
+                flags |= BSM_PAGED_NEGATIVE;
+            const uint32_t c = cs[i] < 0 ? 0u : static_cast<uint32_t>(cs[i]);
+            const uint32_t f = fs[i] < 0 ? 0u : static_cast<uint32_t>(fs[i]);
+            if (static_cast<int64_t>(c) + f > limit)
+                flags |= BSM_PAGED_WIDTH;
+            const uint32_t have = min(pages_of(c, page_size), width), need = min(pages_of(c + f, page_size), width);
             tok[i] = tsum;
             pg[i] = psum;
             tsum += f;
-            psum += need - have;
+            psum += static_cast<int32_t>(need - have);
             s.cached[j] = static_cast<int32_t>(c);
             s.have[j] = static_cast<int32_t>(have);
         }
-        int64_t ti = tsum, pi = psum;
+        int64_t ti = tsum;
+        int32_t pi = psum;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int64_t tv = __shfl_up_sync(0xffffffffu, ti, o), pv = __shfl_up_sync(0xffffffffu, pi, o);
+            const int64_t tv = __shfl_up_sync(0xffffffffu, ti, o);
+            const int32_t pv = __shfl_up_sync(0xffffffffu, pi, o);
             if (lane >= o) {
                 ti += tv;
                 pi += pv;
@@ -100,10 +108,12 @@ __global__ void __launch_bounds__(kTabThreads) paged_tables(const PagedTablesArg
             s.warp_pg[warp] = pi;
         }
         __syncthreads();
-        int64_t tw = 0, pw = 0, tall = 0, pall = 0;
+        int64_t tw = 0, tall = 0;
+        int32_t pw = 0, pall = 0;
 #pragma unroll
         for (int w = 0; w < kTabThreads / 32; ++w) {
-            const int64_t tv = s.warp_tok[w], pv = s.warp_pg[w];
+            const int64_t tv = s.warp_tok[w];
+            const int32_t pv = s.warp_pg[w];
             if (w < warp) {
                 tw += tv;
                 pw += pv;
@@ -111,55 +121,59 @@ __global__ void __launch_bounds__(kTabThreads) paged_tables(const PagedTablesArg
             tall += tv;
             pall += pv;
         }
-        const int64_t tb = tok_base + tw + ti - tsum, pb = pg_base + pw + pi - psum;
-        const bool mine = (r0 / kTabTile) % gridDim.x == blockIdx.x;
+        const int64_t tb = tw + ti - tsum;              // of the tile, before this thread
+        const int32_t pb = pw + pi - psum;
+        const bool mine = static_cast<uint32_t>(r0 / kTabTile) % gridDim.x == blockIdx.x;
 #pragma unroll
         for (int i = 0; i < kTabPer; ++i) {
             const int j = tid * kTabPer + i, r = r0 + j;
-            s.tok[j] = tb + tok[i];
+            const int64_t at = tb + tok[i];
+            s.tok[j] = static_cast<int32_t>(at < INT_MAX ? at : INT_MAX);
             s.pg[j] = pb + pg[i];
             if (mine && r < a.n) {
-                const int64_t end = s.cached[j] + (i + 1 < kTabPer ? tok[i + 1] : tsum) - tok[i];
-                a.starts[r] = static_cast<int32_t>(tb + tok[i] < INT_MAX ? tb + tok[i] : INT_MAX);
-                a.lengths[r] = static_cast<int32_t>(end < INT_MAX ? end : INT_MAX);
+                const int64_t start = tok_base + at;
+                const uint32_t len = static_cast<uint32_t>(s.cached[j]) + (fs[i] < 0 ? 0u : static_cast<uint32_t>(fs[i]));
+                a.starts[r] = static_cast<int32_t>(start < INT_MAX ? start : INT_MAX);
+                a.lengths[r] = static_cast<int32_t>(len < INT_MAX ? len : INT_MAX);
             }
         }
         if (tid == 0) {
-            s.tok[kTabTile] = tok_base + tall;
-            s.pg[kTabTile] = pg_base + pall;
+            s.tok[kTabTile] = static_cast<int32_t>(tall < INT_MAX ? tall : INT_MAX);
+            s.pg[kTabTile] = pall;
         }
         __syncthreads();
         // tokens of these requests that are this CTA's
         const int64_t lo = tok_base > t_lo ? tok_base : t_lo;
         const int64_t hi = tok_base + tall < t_hi ? tok_base + tall : t_hi;
         for (int64_t t = lo + tid; t < hi; t += kTabThreads) {
-            const int j = find_last(s.tok, kTabTile, t);
-            const int64_t pos = s.cached[j] + (t - s.tok[j]);
-            const int64_t e = pos / a.page;
+            const int32_t rel = static_cast<int32_t>(t - tok_base);
+            const int j = find_last(s.tok, kTabTile, rel);
+            const uint32_t pos = static_cast<uint32_t>(s.cached[j]) + static_cast<uint32_t>(rel - s.tok[j]);
+            const uint32_t e = pos / page_size;
             int32_t page = -1;
-            if (e < a.width) {
-                if (e < s.have[j]) {
+            if (e < width) {
+                if (e < static_cast<uint32_t>(s.have[j])) {
                     page = a.tables[(r0 + j) * a.table_stride + e];
                 } else {
-                    const int64_t k = s.pg[j] + (e - s.have[j]);
+                    const int64_t k = pg_base + s.pg[j] + (e - static_cast<uint32_t>(s.have[j]));
                     page = k < a.n_free ? a.free_pages[k] : -1;
                 }
             }
-            a.slots[t] = page >= 0 ? static_cast<int64_t>(page) * a.page + (pos - e * a.page) : -1;
+            a.slots[t] = page >= 0 ? static_cast<int64_t>(page) * page_size + (pos - e * page_size) : -1;
             a.positions[t] = static_cast<int32_t>(pos < INT_MAX ? pos : INT_MAX);
             a.owners[t] = r0 + j;
         }
-        // new entries, dealt over all threads of the launch by their place in the free list
-        const int64_t me = static_cast<int64_t>(blockIdx.x) * kTabThreads + tid;
-        int64_t k = pg_base - pg_base % stride + me;
-        k += k < pg_base ? stride : 0;
-        for (; k < pg_base + pall; k += stride) {
-            const int j = find_last(s.pg, kTabTile, k);
-            a.tables[(r0 + j) * a.table_stride + s.have[j] + (k - s.pg[j])] = k < a.n_free ? a.free_pages[k] : -1;
+        // new entries, dealt over all threads of the launch
+        for (uint32_t k = blockIdx.x * kTabThreads + tid; k < static_cast<uint32_t>(pall); k += stride) {
+            const int j = find_last(s.pg, kTabTile, static_cast<int32_t>(k));
+            const int64_t from = pg_base + k;
+            a.tables[(r0 + j) * a.table_stride + s.have[j] + (static_cast<int32_t>(k) - s.pg[j])] =
+                from < a.n_free ? a.free_pages[from] : -1;
         }
         tok_base += tall;
         pg_base += pall;
-        __syncthreads();
+        if (r0 + kTabTile < a.n)
+            __syncthreads();
     }
     for (int64_t t = (tok_base > t_lo ? tok_base : t_lo) + tid; t < t_hi; t += kTabThreads) {
         a.slots[t] = -1;
@@ -185,45 +199,61 @@ __global__ void __launch_bounds__(kTabThreads) paged_tables(const PagedTablesArg
     }
 }
 
-// The copy: 16 bytes a thread and step, kWriteAhead of them in flight.
+// The copy, bound by its bytes.  A thread keeps its place in the row of a
+// token (16 bytes of one head) and goes from token to token, eight loads in
+// flight; the divisions that find a slot's page are one a token.
 constexpr int kWriteThreads = 256;
 constexpr int kWriteAhead = 4;
 
 __global__ void __launch_bounds__(kWriteThreads) paged_write(const PagedWriteArgs a)
 {
-    const int64_t per_token = static_cast<int64_t>(a.heads) * a.chunks;
-    const int64_t total = 2 * a.n_tokens * per_token;
-    const int64_t step = static_cast<int64_t>(gridDim.x) * kWriteThreads;
-    for (int64_t i0 = static_cast<int64_t>(blockIdx.x) * kWriteThreads + threadIdx.x; i0 < total;
-         i0 += step * kWriteAhead) {
-        uint4 val[kWriteAhead];
-        unsigned char *dst[kWriteAhead];
+    const uint32_t per = static_cast<uint32_t>(a.heads) * static_cast<uint32_t>(a.chunks);
+    const uint32_t at_once = per < kWriteThreads ? kWriteThreads / per : 1u;     // tokens of a block and pass
+    const uint32_t sub = at_once > 1 ? threadIdx.x / per : 0u;
+    if (sub >= at_once)
+        return;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * at_once;
+    for (uint32_t y = threadIdx.x - sub * per; y < per; y += kWriteThreads) {
+        const uint32_t head = y / static_cast<uint32_t>(a.chunks), piece = y - head * static_cast<uint32_t>(a.chunks);
+        const unsigned char *src[2];
+        unsigned char *dst[2];
 #pragma unroll
-        for (int u = 0; u < kWriteAhead; ++u) {
-            const int64_t i = i0 + u * step;
-            dst[u] = nullptr;
-            if (i >= total)
-                continue;
-            const int kv = i >= total / 2;
-            const int64_t x = kv ? i - total / 2 : i;
-            const int64_t t = x / per_token;
-            const int32_t y = static_cast<int32_t>(x - t * per_token);
-            const int32_t h = y / a.chunks, c = y - h * a.chunks;
-            const int64_t slot = a.slots[t];
-            if (slot < 0)
-                continue;
-            if (slot >= a.n_slots_cache) {
-                atomicOr(a.status, BSM_DEV_BOUNDS);
-                continue;
-            }
-            const int64_t page = slot / a.page;
-            val[u] = *reinterpret_cast<const uint4 *>(a.src[kv] + t * a.src_token[kv] + h * a.src_head[kv] + c * 16);
-            dst[u] = a.dst[kv] + page * a.dst_page + (slot - page * a.page) * a.dst_token + h * a.dst_head + c * 16;
+        for (int kv = 0; kv < 2; ++kv) {
+            src[kv] = a.src[kv] + head * a.src_head[kv] + piece * 16;
+            dst[kv] = a.dst[kv] + head * a.dst_head + piece * 16;
         }
+        for (int64_t t0 = blockIdx.x * static_cast<int64_t>(at_once) + sub; t0 < a.n_tokens; t0 += step * kWriteAhead) {
+            int64_t to[kWriteAhead];
+            uint4 val[kWriteAhead][2];
 #pragma unroll
-        for (int u = 0; u < kWriteAhead; ++u)
-            if (dst[u])
-                *reinterpret_cast<uint4 *>(dst[u]) = val[u];
+            for (int u = 0; u < kWriteAhead; ++u) {
+                const int64_t t = t0 + u * step;
+                to[u] = t < a.n_tokens ? a.slots[t] : -1;
+            }
+#pragma unroll
+            for (int u = 0; u < kWriteAhead; ++u) {
+                if (to[u] < 0)
+                    continue;
+                if (to[u] >= a.n_slots_cache) {
+                    atomicOr(a.status, BSM_DEV_BOUNDS);
+                    to[u] = -1;
+                    continue;
+                }
+                const int64_t t = t0 + u * step;
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv)
+                    val[u][kv] = __ldg(reinterpret_cast<const uint4 *>(src[kv] + t * a.src_token[kv]));
+                const int64_t page = to[u] >> 32 ? to[u] / a.page
+                                                 : static_cast<int64_t>(static_cast<uint32_t>(to[u]) / static_cast<uint32_t>(a.page));
+                to[u] = page * a.dst_page + (to[u] - page * a.page) * a.dst_token;
+            }
+#pragma unroll
+            for (int u = 0; u < kWriteAhead; ++u)
+                if (to[u] >= 0)
+#pragma unroll
+                    for (int kv = 0; kv < 2; ++kv)
+                        *reinterpret_cast<uint4 *>(dst[kv] + to[u]) = val[u][kv];
+        }
     }
 }
 
@@ -239,8 +269,8 @@ int launch_paged_tables(const PagedTablesArgs &a, int n_sm, void *stream)
 
 int launch_paged_write(const PagedWriteArgs &a, int n_sm, void *stream)
 {
-    const int64_t total = 2 * a.n_tokens * a.heads * a.chunks;
-    const int64_t want = (total + kWriteThreads - 1) / kWriteThreads;
+    const int64_t per = static_cast<int64_t>(a.heads) * a.chunks, at_once = per < kWriteThreads ? kWriteThreads / per : 1;
+    const int64_t want = (a.n_tokens + at_once - 1) / at_once;
     const int64_t most = static_cast<int64_t>(n_sm) * 8;
     paged_write<<<static_cast<int>(want < most ? want : most), kWriteThreads, 0, static_cast<cudaStream_t>(stream)>>>(a);
     return static_cast<int>(cudaGetLastError());

@@ -53,18 +53,10 @@ constexpr uint32_t kTileTmemCols = 512;
 constexpr int kMaxStages = 8;
 constexpr float kLag = 8.0f;                            // log2 of how far a maximum may pass its reference
 
-// columns of the tensor memory: scores of the two blocks (the probabilities of
-// each part over it), outputs of the two
+// columns of the tensor memory: scores of the two blocks (the probabilities
+// over them), outputs of the two
 __device__ __forceinline__ constexpr uint32_t s_col(int sub) { return static_cast<uint32_t>(sub * 128); }
 __device__ __forceinline__ constexpr uint32_t o_col(int sub) { return static_cast<uint32_t>(256 + sub * 128); }
-
-// A step's probabilities come in two parts, the first of this many keys: its
-// product runs beside the exponentials of the second.  (96 and 32: 4 % slower.)
-constexpr int kPartKeys = 64;
-
-template <int N> struct Const {
-    static constexpr int value = N;
-};
 
 template <int DP> struct TileShape {
     static constexpr int kHalves = DP / 64;
@@ -89,7 +81,7 @@ struct TilePiece {
 struct TileSmem {
     uint64_t full[kMaxStages], empty[kMaxStages];
     uint64_t qfull, qempty;
-    uint64_t sfull[2], pfull[2][2], ohalf[2], olast[2], ofree[2];
+    uint64_t sfull[2], pfull[2], olast[2], ofree[2];
     uint64_t pcfull[2], pcempty[2];
     uint64_t turn[2];                   // the group may issue its next scores
     uint64_t tail, drain, xfull;
@@ -156,16 +148,15 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
         : "memory");
 }
 
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t *r)
+// 16 columns
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t *r)
 {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
-        "%15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
-        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
-        "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
-        "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-        : "memory");
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+        "%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr));
 }
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r)
 {
@@ -425,26 +416,12 @@ __device__ bool multiply(TileSmem &h, unsigned char *qs, unsigned char *stages, 
                     return false;
             }
             const uint64_t vd = smem_desc_n(saddr(stages) + static_cast<uint32_t>(vs * Shape::kStageBytes));
-            if (mine) {
-                if (!warp_wait(&h.pfull[sub][0], np & 1u, &h.abort_flag))
-                    return false;
-                tc_fence_after();
-                if (elect_one()) {
-#pragma unroll
-                    for (int k = 0; k < kPartKeys / 16; ++k)
-                        mma_ts(to_o, to_s + k * 8, vd + k * (2048 >> 4), kOut, j != from || k != 0);
-                    mma_commit(&h.ohalf[sub]);
-                }
-                __syncwarp();
-            }
             const int ks = pos.s;
             if (more) {
                 if (!warp_wait(&h.full[ks], pos.ph, &h.abort_flag))
                     return false;
                 pos.step(Shape::kStages);
             }
-            if (mine && !warp_wait(&h.pfull[sub][1], np++ & 1u, &h.abort_flag))
-                return false;
             // The groups take turns: products of both, issued at once, would be done at once, and
             // the groups' exponentials and products would go on at the same time, each leaving
             // the other's unit idle.  (The first group's turn at the start has no barrier.)
@@ -453,12 +430,14 @@ __device__ bool multiply(TileSmem &h, unsigned char *qs, unsigned char *stages, 
                     return false;
                 ++turns;
             }
+            if (mine && !warp_wait(&h.pfull[sub], np++ & 1u, &h.abort_flag))
+                return false;
             tc_fence_after();
             if (elect_one()) {
                 if (mine) {
 #pragma unroll
-                    for (int k = kPartKeys / 16; k < kKeys / 16; ++k)
-                        mma_ts(to_o, to_s + kPartKeys + (k - kPartKeys / 16) * 8, vd + k * (2048 >> 4), kOut, 1u);
+                    for (int k = 0; k < kKeys / 16; ++k)
+                        mma_ts(to_o, to_s + k * 8, vd + k * (2048 >> 4), kOut, j != from || k != 0);
                     if (j == last)
                         mma_commit(&h.olast[sub]);
                     mma_commit(&h.empty[vs]);
@@ -552,86 +531,81 @@ __device__ bool softmax(const PagedArgs &a, TileSmem &h, unsigned char *store, u
                 // no row of this warp is stored: whatever lies there will do
                 __syncwarp();
                 if (lane == 0) {
-                    bar_arrive(&h.pfull[sub][0]);
-                    bar_arrive(&h.pfull[sub][1]);
+                    bar_arrive(&h.pfull[sub]);
                 }
                 continue;
             }
-            auto probabilities = [&](auto from_, auto cols_) -> bool {
-                constexpr int kFrom = decltype(from_)::value, kCols = decltype(cols_)::value;
-                const uint32_t sc = lanes + s_col(sub) + kFrom;
-                uint32_t r[kCols];
+            const uint32_t sc = lanes + s_col(sub);
+            uint32_t r[kKeys];
+            tmem_ld32_nowait(sc, r);
+            tmem_ld32_nowait(sc + 32, r + 32);
+            const int32_t key0 = (t.first + j) * kKeys;
+            const bool masked = !__all_sync(0xffffffffu, lo <= key0 && hi - kKeys >= key0);
+            const int32_t c0 = lo - key0, c1 = hi - key0;
+            float top4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int c = 0; c < kCols; c += 32)
-                    tmem_ld32_nowait(sc + c, r + c);
-                const int32_t key0 = (t.first + j) * kKeys + kFrom;
-                const bool masked = !__all_sync(0xffffffffu, lo <= key0 && hi - kCols >= key0);
-                tmem_landed<kCols>(r);
+            for (int q = 0; q < kKeys; q += 64) {
+                tmem_landed<64>(r + q);
+                if (q == 0) {
+                    tmem_ld32_nowait(sc + 64, r + 64);
+                    tmem_ld32_nowait(sc + 96, r + 96);
+                }
                 if (masked) {
-                    const int32_t c0 = lo - key0, c1 = hi - key0;
 #pragma unroll
-                    for (int c = 0; c < kCols; ++c)
+                    for (int c = q; c < q + 64; ++c)
                         r[c] = c >= c0 && c < c1 ? r[c] : 0xFF800000u;
                 }
-                float top4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int c = 0; c < kCols; c += 2)
+                for (int c = q; c < q + 64; c += 2)
                     top4[(c >> 1) & 3] =
                         fmaxf(fmaxf(top4[(c >> 1) & 3], __uint_as_float(r[c])), __uint_as_float(r[c + 1]));
-                const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3])) * a.scale_log2;
-                // (a maximum of -inf moves nothing; NaN neither: it comes out in the sum)
-                const bool move = top > ref + kLag;
-                if (__any_sync(0xffffffffu, move)) {
-                    const float f = !move ? 1.0f : pg_exp2(ref - top);
-                    ref = move ? top : ref;
-                    sum *= f;
-                    if (j != j0 || kFrom) {
-                        // the products so far still add to the output: those of earlier steps are done
-                        // (this step's scores were issued behind them), the first part's may not be
-                        if (kFrom && !warp_wait(&h.ohalf[sub], n & 1u, &h.abort_flag))
-                            return false;
-                        tc_fence_after();
+            }
+            const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3])) * a.scale_log2;
+            // (a maximum of -inf moves nothing; NaN neither: it comes out in the sum)
+            const bool move = top > ref + kLag;
+            if (__any_sync(0xffffffffu, move)) {
+                const float f = !move ? 1.0f : pg_exp2(ref - top);
+                ref = move ? top : ref;
+                sum *= f;
+                if (j != j0) {
+                    // the products of earlier steps are done: this step's scores were issued behind them
 #pragma unroll 1
-                        for (int c = 0; c < DP / 32; ++c) {
-                            uint32_t o[32];
-                            tmem_ld32_nowait(lanes + o_col(sub) + c * 32, o);
-                            tmem_landed<32>(o);
+                    for (int c = 0; c < DP / 16; ++c) {
+                        uint32_t o[16];
+                        tmem_ld16(lanes + o_col(sub) + c * 16, o);
+                        tmem_landed<16>(o);
 #pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                            tmem_st32(lanes + o_col(sub) + c * 32, o);
-                        }
+                        for (int i = 0; i < 16; ++i)
+                            o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                        tmem_st16(lanes + o_col(sub) + c * 16, o);
                     }
                 }
-                const float base = ref == -INFINITY ? 0.0f : ref - pg_shift<kF16>(kLag);
-                const uint64_t base2 = pair(-base, -base);
-                uint64_t s2[2] = {0, 0};
-                uint32_t pr[kCols / 2];
+            }
+            const float base = ref == -INFINITY ? 0.0f : ref - pg_shift<kF16>(kLag);
+            const uint64_t base2 = pair(-base, -base);
+            uint64_t s2[2] = {0, 0};
 #pragma unroll
-                for (int c = 0; c < kCols; c += 2) {
+            for (int q = 0; q < kKeys; q += 32) {
+                uint32_t pr[16];
+#pragma unroll
+                for (int c = q; c < q + 32; c += 2) {
                     float p0, p1;
                     unpair(fma2(pair(__uint_as_float(r[c]), __uint_as_float(r[c + 1])), scale2, base2), p0, p1);
                     p0 = pg_exp2(p0);
                     p1 = pg_exp2(p1);
                     s2[(c >> 1) & 1] = add2(s2[(c >> 1) & 1], pair(p0, p1));
-                    pr[c / 2] = pg_pack<kF16>(p0, p1);
+                    pr[(c - q) / 2] = pg_pack<kF16>(p0, p1);
                 }
-#pragma unroll
-                for (int c = 0; c < kCols / 2; c += 16)
-                    tmem_st16(sc + c, pr + c);
-                tmem_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0)
-                    bar_arrive(&h.pfull[sub][kFrom ? 1 : 0]);
-                float e0, e1;
-                unpair(add2(s2[0], s2[1]), e0, e1);
-                sum += e0 + e1;
-                return true;
-            };
-            if (!probabilities(Const<0>{}, Const<kPartKeys>{}) ||
-                !probabilities(Const<kPartKeys>{}, Const<kKeys - kPartKeys>{}))
-                return false;
+                tmem_st16(sc + q / 2, pr);
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0)
+                bar_arrive(&h.pfull[sub]);
+            float e0, e1;
+            unpair(add2(s2[0], s2[1]), e0, e1);
+            sum += e0 + e1;
         }
         // ---- the row's output
         if (!warp_wait(&h.olast[sub], pieces++ & 1u, &h.abort_flag))
@@ -763,9 +737,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
         bar_init(&h.qempty, 2);
         for (int s = 0; s < 2; ++s) {
             bar_init(&h.sfull[s], 1);
-            bar_init(&h.pfull[s][0], 4);
-            bar_init(&h.pfull[s][1], 4);
-            bar_init(&h.ohalf[s], 1);
+            bar_init(&h.pfull[s], 4);
             bar_init(&h.olast[s], 1);
             bar_init(&h.ofree[s], 4);
             bar_init(&h.turn[s], 1);

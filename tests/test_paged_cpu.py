@@ -52,7 +52,7 @@ INV, MIS, UNS = bsm.ERR_INVALID_ARG, bsm.ERR_MISALIGNED, bsm.ERR_UNSUPPORTED
 
 @pytest.mark.parametrize("kw,code", [
     (dict(n_requests=-1), INV), (dict(n_free=-1), INV), (dict(page_size=0), INV), (dict(table_width=0), INV),
-    (dict(n_slots=-1), INV), (dict(table_stride=7), INV), (dict(starts=None), INV), (dict(info=None), INV),
+    (dict(n_slots=-1), INV), (dict(table_stride=7), INV), (dict(table_width=1 << 20, table_stride=1 << 20), UNS), (dict(starts=None), INV), (dict(info=None), INV),
     (dict(cached=None), INV), (dict(fresh=None), INV), (dict(tables=None), INV), (dict(lengths=None), INV),
     (dict(free_pages=None), INV), (dict(slots=None), INV), (dict(owners=None), INV),
     (dict(slots=(1 << 40) + 4), MIS), (dict(cached=(1 << 40) + 2), MIS),
@@ -69,6 +69,7 @@ def test_tables_refusals(kw, code):
     (dict(k_stride_token=64), INV),                             # tokens overlap
     (dict(kv_stride_page=1024), INV), (dict(kv_stride_head=-64), INV),
     (dict(head_dim=60), MIS), (dict(k=(1 << 40) + 8), MIS), (dict(kv_stride_page=2052), MIS),
+    (dict(n_heads=1 << 20, head_dim=1 << 12), UNS),
     (dict(k=1 << 40, k_cache=(1 << 40) + 256), INV), (dict(k_cache=1 << 40, v_cache=1 << 40), INV),
     (dict(n_tokens=0, k=None), bsm.OK),
 ])
