@@ -47,15 +47,14 @@ struct PagedArgs {
     int32_t group;                                  // query heads of a key/value head
     int32_t subs, sub;                              // head groups of one key/value head, heads of each
     int32_t tok;                                    // tokens of a tile
-    int32_t units;                                  // units at most
-    float *part_o;                                  // CTAs x 2 x tile rows x kPagedMaxDim
-    float *part_ml;                                 // CTAs x 2 x tile rows x 2
-    struct PagedJoin *join;                         // CTAs
-    float *warp_o, *warp_ml;                        // the row kernel's: the same for every warp
+    int32_t units, min_steps;                       // units at most; key steps of a unit at least
+    float *part_o;                                  // units x 2 x tile rows x kPagedMaxDim
+    float *part_ml;                                 // units x 2 x tile rows x 2
+    struct PagedJoin *join;                         // units
     uint32_t *status;
 };
 
-// A tile whose keys were split over CTAs c .. c + count - 1: the first one's
+// A tile whose keys were split over units u .. u + count - 1: the first one's
 // second partial and the others' first are joined.
 struct PagedJoin {
     int32_t token, head, tokens, heads;             // first token, first query head, tokens, heads of the tile

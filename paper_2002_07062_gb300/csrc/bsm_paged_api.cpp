@@ -96,20 +96,18 @@ int elem_size(int dtype) { return dtype == BSM_F32 ? 4 : 2; }
 
 // Workspace: partial outputs, maxima and sums of cut tiles, and who joins them.
 struct PagedLayout {
-    int64_t warp_o, warp_ml, rows_o, rows_ml, rows_join, tiles_o, tiles_ml, tiles_join, bytes;
+    int64_t rows_o, rows_ml, rows_join, tiles_o, tiles_ml, tiles_join, bytes;
 };
 
 PagedLayout paged_layout(int n_sm)
 {
     PagedLayout l{};
     auto up = [](int64_t x) { return (x + 255) & ~int64_t(255); };
-    const int64_t row_part = static_cast<int64_t>(n_sm) * 2 * kPagedRowTile;
-    l.warp_o = 0;
-    l.warp_ml = l.warp_o + up(kPagedWarps * row_part * kPagedMaxDim * 4);
-    l.rows_o = l.warp_ml + up(kPagedWarps * row_part * 8);
-    l.rows_ml = l.rows_o + up(row_part * kPagedMaxDim * 4);
-    l.rows_join = l.rows_ml + up(row_part * 8);
-    l.tiles_o = l.rows_join + up(static_cast<int64_t>(n_sm) * static_cast<int64_t>(sizeof(PagedJoin)));
+    const int64_t units = static_cast<int64_t>(n_sm) * kPagedWarps, parts = units * 2 * kPagedRowTile;
+    l.rows_o = 0;
+    l.rows_ml = l.rows_o + up(parts * kPagedMaxDim * 4);
+    l.rows_join = l.rows_ml + up(parts * 8);
+    l.tiles_o = l.rows_join + up(units * static_cast<int64_t>(sizeof(PagedJoin)));
     l.tiles_ml = l.tiles_o + up(static_cast<int64_t>(n_sm) * 2 * kPagedTileRows * kPagedMaxDim * 4);
     l.tiles_join = l.tiles_ml + up(static_cast<int64_t>(n_sm) * 2 * kPagedTileRows * 8);
     l.bytes = l.tiles_join + up(static_cast<int64_t>(n_sm) * static_cast<int64_t>(sizeof(PagedJoin)));
@@ -362,6 +360,7 @@ int paged_attention(const bsm_paged_desc *d, bsm_stream_t stream)
     }
     if (tiles) {
         b.units = dev->n_sm;
+        b.min_steps = 1;
         b.part_o = reinterpret_cast<float *>(ws + lay.tiles_o);
         b.part_ml = reinterpret_cast<float *>(ws + lay.tiles_ml);
         b.join = reinterpret_cast<PagedJoin *>(ws + lay.tiles_join);
@@ -372,8 +371,7 @@ int paged_attention(const bsm_paged_desc *d, bsm_stream_t stream)
     split_group(a, kPagedRowTile);
     a.tok = std::max(1, kPagedRowTile / a.sub);
     a.units = dev->n_sm * kPagedWarps;
-    a.warp_o = reinterpret_cast<float *>(ws + lay.warp_o);
-    a.warp_ml = reinterpret_cast<float *>(ws + lay.warp_ml);
+    a.min_steps = a.d <= 64 ? 2 : 4;
     a.part_o = reinterpret_cast<float *>(ws + lay.rows_o);
     a.part_ml = reinterpret_cast<float *>(ws + lay.rows_ml);
     a.join = reinterpret_cast<PagedJoin *>(ws + lay.rows_join);

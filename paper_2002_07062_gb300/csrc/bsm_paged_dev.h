@@ -131,7 +131,8 @@ template <int kStep> struct PagedLine {
         return n;
     }
 
-    __device__ PagedSeq seq(int32_t r, bool report) const
+    // known >= 0: the request's steps, all head groups
+    __device__ PagedSeq seq(int32_t r, bool report, int64_t known = -1) const
     {
         PagedSeq s;
         const int32_t raw0 = a.starts[r], raw1 = a.starts[r + 1], rawL = a.lengths[r];
@@ -148,7 +149,7 @@ template <int kStep> struct PagedLine {
         if (s.m == 0)
             return s;
         s.tiles = (s.m + a.tok - 1) / a.tok;
-        s.steps = before(s, s.tiles);
+        s.steps = known >= 0 ? pg_div(known, static_cast<int64_t>(a.heads_kv) * a.subs) : before(s, s.tiles);
         return s;
     }
 
@@ -204,13 +205,15 @@ __device__ void paged_prefix(const PagedLine<kStep> &line, PagedPrefix<kThreads>
     __syncthreads();
 }
 
-// How the line is cut: `units` ranges, none empty; unit u begins at W u / units.
+// How the line is cut: `units` ranges of at least min_steps steps (the line may be
+// shorter: one range); unit u begins at W u / units.
 struct PagedCut {
     int64_t W, q;
     int32_t units, rem;
     __device__ PagedCut(const PagedArgs &a, int64_t steps) : W(steps)
     {
-        units = steps >= a.units ? a.units : steps < 1 ? 1 : static_cast<int32_t>(steps);
+        const int64_t most = pg_div(steps, a.min_steps);
+        units = most >= a.units ? a.units : most < 1 ? 1 : static_cast<int32_t>(most);
         q = pg_div(W, units);
         rem = static_cast<int32_t>(W - q * units);
     }
@@ -265,7 +268,9 @@ template <int kStep> struct PagedWalk {
         int64_t all = 0;
         do {                                    // (the line's end is past x: some request holds it)
             o -= all;
-            s = line.seq(++r, false);
+            // (a thread's sum over one request is that request's steps)
+            const int64_t known = l.a.n <= kThreads ? p.pre[r + 2] - p.pre[r + 1] : -1;
+            s = line.seq(++r, false, known);
             all = line.all_steps(s);
         } while (o >= all && r + 1 < l.a.n);
         head = static_cast<int32_t>(pg_div(o, s.steps));
@@ -279,6 +284,13 @@ template <int kStep> struct PagedWalk {
             first = __shfl_sync(0xffffffffu, f, k);
             tile += k * each;
             left = each < left - k * each ? each : left - k * each;
+            if (each <= 8) {                    // the rest one by one
+                for (int32_t n; left > 1 && first + (n = line.steps_of(line.range(s, tile))) <= o; --left) {
+                    first += n;
+                    ++tile;
+                }
+                break;
+            }
         }
         at = static_cast<int32_t>(o - first);
     }
@@ -315,6 +327,24 @@ template <int kStep> struct PagedWalk {
         return true;
     }
 };
+
+// Launches a kernel that may start while the one before it in the stream ends
+// (it waits for that one's writes itself).
+template <typename... Ks, typename... As>
+inline int launch_early(void (*kernel)(Ks...), dim3 grid, int threads, size_t smem, cudaStream_t st, const As &...args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(static_cast<unsigned>(threads));
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return static_cast<int>(cudaLaunchKernelEx(&cfg, kernel, args...));
+}
 
 __device__ __forceinline__ uint32_t pg_saddr(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 

@@ -9,13 +9,14 @@
 // built for loads: every warp is on its own, with its own range of the work,
 // its own three stages of 16 keys (8 KiB of K and V at D = 128) filled by
 // 16-byte asynchronous copies, its own running maximum and sum; no barrier of
-// the block between the layout of the work and the join of cut tiles.  24 stages an SM keep 128 to 192 KiB
+// the block after the work is laid out.  24 stages an SM keep 128 to 192 KiB
 // in flight.
 #include <cuda_runtime.h>
 
 #include <cstdint>
 
 #include "bsm_paged_dev.h"
+#include "bsm_tc.h"
 
 namespace bsm {
 namespace {
@@ -31,18 +32,8 @@ template <int DP> struct RowShape {
     static constexpr int kChunks = DP / 8;              // 16-byte pieces of a row
 };
 
-// A part of a tile that a warp leaves to be joined: [0] of a tile that an
-// earlier warp started, [1] of one that it starts and does not end.
-struct RowPart {
-    int32_t token, head, tokens, heads; // of the tile
-    int32_t rows;                       // 0: no part
-    int32_t starts, ends;
-    int32_t last_cta;                   // that has part of the tile
-};
-
 struct RowSmem {
     PagedPrefix<kRowThreads> prefix;
-    RowPart part[kPagedWarps][2];
 };
 constexpr int kRowHeader = 4096;
 static_assert(sizeof(RowSmem) <= kRowHeader, "row header");
@@ -147,18 +138,19 @@ __global__ void __launch_bounds__(kRowThreads, 1) paged_rows(const PagedArgs a)
     RowSmem &sm = *reinterpret_cast<RowSmem *>(raw);
     const int lane = threadIdx.x & 31;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
-    const int32_t cta = blockIdx.x, unit = cta * kPagedWarps + warp;
-    if (threadIdx.x == 0)
-        a.join[cta].count = 0;
-    if (lane < 2)
-        sm.part[warp][lane].rows = 0;
+    // neighbouring units on different SMs: a small batch spreads over the device
+    const int32_t unit = warp * gridDim.x + blockIdx.x;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    if (lane == 0)
+        a.join[unit].count = 0;
     const PagedLine<kKeys> line(a);
-    paged_prefix<kKeys, kRowThreads>(line, sm.prefix, cta == 0);
+    paged_prefix<kKeys, kRowThreads>(line, sm.prefix, blockIdx.x == 0);
     const int64_t W = sm.prefix.pre[kRowThreads];
     const PagedCut cut(a, W);
-    if (W == 0 || cta * kPagedWarps >= cut.units)
-        return;                                         // (the whole CTA)
-    const int64_t begin = unit < cut.units ? cut.begin(unit) : 0, end = unit < cut.units ? cut.begin(unit + 1) : 0;
+    if (W == 0 || unit >= cut.units)
+        return;
+    const int64_t begin = cut.begin(unit), end = cut.begin(unit + 1);
     const int32_t total = static_cast<int32_t>(end - begin);
     PagedWalk<kKeys> fetch(line, sm.prefix, begin, end), walk = fetch;
 
@@ -322,9 +314,9 @@ __global__ void __launch_bounds__(kRowThreads, 1) paged_rows(const PagedArgs a)
             ++done;
             issue();
         }
-        // ---- the tile's output, or this warp's part of it
+        // ---- the tile's output, or this unit's part of it
         const bool whole = p.starts && p.ends;
-        const int32_t slot = 2 * unit + (p.starts ? 1 : 0);
+        const int64_t slot = static_cast<int64_t>(2 * unit + (p.starts ? 1 : 0)) * kPagedRowTile;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             float sum = l[i];
@@ -347,132 +339,92 @@ __global__ void __launch_bounds__(kRowThreads, 1) paged_rows(const PagedArgs a)
                     a.lse[static_cast<int64_t>(t.token + tt) * a.heads_q + t.head + h] =
                         sum == 0.0f ? -INFINITY : (ref + log2f(sum)) * kLn2;
             } else {
-                float *dst = a.warp_o + (static_cast<int64_t>(slot) * kPagedRowTile + row) * kPagedMaxDim;
 #pragma unroll
                 for (int n = 0; n < DP / 8; ++n)
-                    *reinterpret_cast<float2 *>(dst + n * 8 + (lane & 3) * 2) = make_float2(o[n][2 * i], o[n][2 * i + 1]);
+                    *reinterpret_cast<float2 *>(a.part_o + (slot + row) * kPagedMaxDim + n * 8 + (lane & 3) * 2) =
+                        make_float2(o[n][2 * i], o[n][2 * i + 1]);
                 if ((lane & 3) == 0)
-                    *reinterpret_cast<float2 *>(a.warp_ml + (static_cast<int64_t>(slot) * kPagedRowTile + row) * 2) =
-                        make_float2(ref, sum);
+                    *reinterpret_cast<float2 *>(a.part_ml + (slot + row) * 2) = make_float2(ref, sum);
             }
         }
-        if (!whole && lane == 0) {
-            RowPart &r = sm.part[warp][p.starts ? 1 : 0];
-            r.token = t.token;
-            r.head = t.head;
-            r.tokens = t.tokens;
-            r.heads = t.heads;
-            r.rows = rows;
-            r.starts = p.starts;
-            r.ends = p.ends;
-            r.last_cta = cut.owner(p.tile_end - 1) / kPagedWarps;
+        if (p.starts && !p.ends && lane == 0) {
+            PagedJoin j{};
+            j.token = t.token;
+            j.head = t.head;
+            j.tokens = t.tokens;
+            j.heads = t.heads;
+            j.count = cut.owner(p.tile_end - 1) - unit + 1;
+            a.join[unit] = j;
         }
     }
     cp_wait<0>();
-    __syncthreads();
-
-    // ---- tiles cut between warps of this CTA: their parts, one warp a row.  A
-    // chain of parts of one tile starts with the warp that starts the tile (or
-    // with the first warp, for a tile of the previous CTA) and goes on with the
-    // first parts of the warps behind it.
-    int32_t item = 0;
-    for (int w = -1; w < kPagedWarps; ++w) {
-        const RowPart c = w < 0 ? sm.part[0][0] : sm.part[w][1];
-        if (c.rows == 0)
-            continue;
-        const int first = w < 0 ? 0 : 2 * w + 1;        // slots of the chain: first, then 2 w', w' = next ..
-        const int next = w < 0 ? 1 : w + 1;
-        int n = 1;
-        bool ends = c.ends;
-        while (!ends && next + n - 1 < kPagedWarps && sm.part[next + n - 1][0].rows) {
-            ends = sm.part[next + n - 1][0].ends;
-            ++n;
-        }
-        const bool here = c.starts && ends;             // no other CTA has part of it
-        const int32_t slot = 2 * cta + (c.starts ? 1 : 0);
-        for (int row = 0; row < c.rows; ++row, ++item) {
-            if (item % kPagedWarps != warp)
-                continue;
-            const int32_t tt = row / a.sub, h = row - tt * a.sub;
-            if (h >= c.heads)
-                continue;
-            auto at = [&](int i) {
-                return (static_cast<int64_t>(cta) * 2 * kPagedWarps + (i == 0 ? first : 2 * (next + i - 1))) * kPagedRowTile + row;
-            };
-            float2 ml[kPagedWarps];
-            float4 v[kPagedWarps];
-#pragma unroll
-            for (int i = 0; i < kPagedWarps; ++i) {
-                if (i < n) {
-                    ml[i] = *reinterpret_cast<const float2 *>(a.warp_ml + at(i) * 2);
-                    v[i] = *reinterpret_cast<const float4 *>(a.warp_o + at(i) * kPagedMaxDim + lane * 4);
-                }
-            }
-            RowSum r;
-#pragma unroll
-            for (int i = 0; i < kPagedWarps; ++i)
-                if (i < n)
-                    r.top = fmaxf(r.top, ml[i].x);
-#pragma unroll
-            for (int i = 0; i < kPagedWarps; ++i)
-                if (i < n)
-                    r.add(ml[i], v[i]);
-            if (here) {
-                r.store<kF16>(a, c.token + tt, c.head + h, lane);
-            } else {
-                const int64_t to = static_cast<int64_t>(slot) * kPagedRowTile + row;
-                *reinterpret_cast<float4 *>(a.part_o + to * kPagedMaxDim + lane * 4) = r.acc;
-                if (lane == 0)
-                    *reinterpret_cast<float2 *>(a.part_ml + to * 2) = make_float2(r.top, r.sum);
-            }
-        }
-        if (c.starts && !ends && threadIdx.x == 0) {
-            PagedJoin j{};
-            j.token = c.token;
-            j.head = c.head;
-            j.tokens = c.tokens;
-            j.heads = c.heads;
-            j.count = c.last_cta - cta + 1;
-            a.join[cta] = j;
-        }
-    }
 }
 
-// Joins the parts of every tile cut between CTAs, in their order.  One CTA a
-// unit (those that start no such tile leave), one warp a row, 16 bytes a lane.
-constexpr int kJoinThreads = 512;
+// Joins the parts of every cut tile, in unit order.  One CTA a unit (those that
+// start no such tile leave); its warps are dealt to the rows, and where there are
+// fewer rows than warps, several share a row's parts.  128 requests: 353 us in
+// all; joining the parts of a CTA's warps in shared memory first 367 (a row after
+// another there, in code run once), by the CTA that arrives last 372.
+constexpr int kJoinWarps = 8;
 
-template <bool kF16> __global__ void __launch_bounds__(kJoinThreads) paged_join(const PagedArgs a)
+template <bool kF16> __global__ void __launch_bounds__(kJoinWarps * 32) paged_join(const PagedArgs a)
 {
+    __shared__ float4 part[kJoinWarps][32];
+    __shared__ float2 part_ml[kJoinWarps];
+    grid_dependency_wait();
+    grid_launch_dependents();
     const int unit = blockIdx.x;
     const PagedJoin j = a.join[unit];
     if (j.count <= 0)
         return;
-    const int lane = threadIdx.x & 31, row = threadIdx.x >> 5;
-    const int tt = row / a.sub, h = row - tt * a.sub;
-    if (row >= j.tokens * a.sub || h >= j.heads)
-        return;
-    auto at = [&](int i) { return static_cast<int64_t>(i == 0 ? 2 * unit + 1 : 2 * (unit + i)) * kPagedRowTile + row; };
-    RowSum r;
-    for (int i = lane; i < j.count; i += 32)
-        r.top = fmaxf(r.top, a.part_ml[at(i) * 2]);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int rows = j.tokens * a.sub;
+    // warps of a row: a power of two, so that a row's lie side by side
+    int each = 1;
+    while (2 * each * rows <= kJoinWarps && 2 * each <= j.count)
+        each *= 2;
+    auto at = [&](int i) { return static_cast<int64_t>(i == 0 ? 2 * unit + 1 : 2 * (unit + i)) * kPagedRowTile; };
+    for (int row0 = 0; row0 < rows; row0 += kJoinWarps / each) {
+        const int row = row0 + warp / each, share = warp % each;
+        const int tt = row / a.sub, h = row - tt * a.sub;
+        const bool live = row < rows && h < j.heads;
+        RowSum r;
+        if (live) {
+            const int from = j.count * share / each, to = j.count * (share + 1) / each;
+            for (int i = from + lane; i < to; i += 32)
+                r.top = fmaxf(r.top, a.part_ml[(at(i) + row) * 2]);
 #pragma unroll
-    for (int o = 16; o; o >>= 1)
-        r.top = fmaxf(r.top, __shfl_xor_sync(0xffffffffu, r.top, o));
+            for (int o = 16; o; o >>= 1)
+                r.top = fmaxf(r.top, __shfl_xor_sync(0xffffffffu, r.top, o));
 #pragma unroll 8
-    for (int i = 0; i < j.count; ++i)
-        r.add(*reinterpret_cast<const float2 *>(a.part_ml + at(i) * 2),
-              *reinterpret_cast<const float4 *>(a.part_o + at(i) * kPagedMaxDim + lane * 4));
-    r.store<kF16>(a, j.token + tt, j.head + h, lane);
+            for (int i = from; i < to; ++i)
+                r.add(*reinterpret_cast<const float2 *>(a.part_ml + (at(i) + row) * 2),
+                      *reinterpret_cast<const float4 *>(a.part_o + (at(i) + row) * kPagedMaxDim + lane * 4));
+        }
+        if (each > 1) {
+            part[warp][lane] = r.acc;
+            if (lane == 0)
+                part_ml[warp] = make_float2(r.top, r.sum);
+            __syncthreads();
+            if (live && share == 0) {
+                r = RowSum{};
+                for (int i = 0; i < each; ++i)
+                    r.top = fmaxf(r.top, part_ml[warp + i].x);
+                for (int i = 0; i < each; ++i)
+                    r.add(part_ml[warp + i], part[warp + i][lane]);
+            }
+            __syncthreads();
+        }
+        if (live && share == 0)
+            r.store<kF16>(a, j.token + tt, j.head + h, lane);
+    }
 }
 
 template <int DP, bool kF16> int launch_rows(const PagedArgs &a, int grid, cudaStream_t st)
 {
-    paged_rows<DP, kF16><<<grid, kRowThreads, kRowSmem, st>>>(a);
-    if (int e = static_cast<int>(cudaGetLastError()))
+    if (int e = launch_early(paged_rows<DP, kF16>, dim3(grid), kRowThreads, kRowSmem, st, a))
         return e;
-    paged_join<kF16><<<grid, kJoinThreads, 0, st>>>(a);
-    return static_cast<int>(cudaGetLastError());
+    return launch_early(paged_join<kF16>, dim3(a.units), kJoinWarps * 32, 0, st, a);
 }
 
 }  // namespace

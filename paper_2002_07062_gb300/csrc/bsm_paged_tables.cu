@@ -8,7 +8,8 @@
 #include <climits>
 #include <cstdint>
 
-#include "bsm_paged.h"
+#include "bsm_paged_dev.h"
+#include "bsm_tc.h"
 
 namespace bsm {
 namespace {
@@ -64,6 +65,8 @@ __global__ void __launch_bounds__(kTabThreads) paged_tables(const PagedTablesArg
     const uint32_t page_size = static_cast<uint32_t>(a.page), width = static_cast<uint32_t>(a.width);
     int64_t tok_base = 0, pg_base = 0;
     uint32_t flags = 0;
+    grid_dependency_wait();
+    grid_launch_dependents();
 
     for (int r0 = 0; r0 < a.n; r0 += kTabTile) {
         int64_t tok[kTabPer], tsum = 0;
@@ -207,6 +210,8 @@ constexpr int kWriteAhead = 4;
 
 __global__ void __launch_bounds__(kWriteThreads) paged_write(const PagedWriteArgs a)
 {
+    grid_dependency_wait();
+    grid_launch_dependents();
     const uint32_t per = static_cast<uint32_t>(a.heads) * static_cast<uint32_t>(a.chunks);
     const uint32_t at_once = per < kWriteThreads ? kWriteThreads / per : 1u;     // tokens of a block and pass
     const uint32_t sub = at_once > 1 ? threadIdx.x / per : 0u;
@@ -263,8 +268,7 @@ int launch_paged_tables(const PagedTablesArgs &a, int n_sm, void *stream)
 {
     const int64_t want = (static_cast<int64_t>(a.n_slots) + kTabThreads - 1) / kTabThreads;
     const int grid = static_cast<int>(want < 1 ? 1 : want > n_sm ? n_sm : want);
-    paged_tables<<<grid, kTabThreads, sizeof(TabSmem), static_cast<cudaStream_t>(stream)>>>(a);
-    return static_cast<int>(cudaGetLastError());
+    return launch_early(paged_tables, dim3(grid), kTabThreads, sizeof(TabSmem), static_cast<cudaStream_t>(stream), a);
 }
 
 int launch_paged_write(const PagedWriteArgs &a, int n_sm, void *stream)
@@ -272,8 +276,8 @@ int launch_paged_write(const PagedWriteArgs &a, int n_sm, void *stream)
     const int64_t per = static_cast<int64_t>(a.heads) * a.chunks, at_once = per < kWriteThreads ? kWriteThreads / per : 1;
     const int64_t want = (a.n_tokens + at_once - 1) / at_once;
     const int64_t most = static_cast<int64_t>(n_sm) * 8;
-    paged_write<<<static_cast<int>(want < most ? want : most), kWriteThreads, 0, static_cast<cudaStream_t>(stream)>>>(a);
-    return static_cast<int>(cudaGetLastError());
+    return launch_early(paged_write, dim3(static_cast<unsigned>(want < most ? want : most)), kWriteThreads, 0,
+                        static_cast<cudaStream_t>(stream), a);
 }
 
 int paged_tables_set_smem()

@@ -4,14 +4,15 @@
 //   s = scale q k^T,  p = exp(s - m),  o = sum p v / sum p   (m a running reference)
 //
 // Bound: the tensor cores (4 D operations a pair of a query row and a key) and,
-// close behind, the exponentials.  One persistent CTA per SM, 11 warps:
+// close behind, the exponentials.  One persistent CTA per SM, 12 warps:
 //   warps 0-3, 4-7  softmax of one 128-row block each: a thread owns a row, reads
 //                   its 128 scores of a step from tensor memory, writes the probabilities
 //                   back over them as 16-bit pairs, and at the end scales and
 //                   stores its row of the output;
 //   warp 8          producer: walks its share of the work line, copies the query
-//                   blocks and then steps of 128 keys and values, page by page,
+//                   and steps of 128 keys and values, page by page,
 //                   with TMA (128-byte swizzle) into a ring of stages;
+//   warp 11         copies each piece's query blocks;
 //   warps 9, 10     issue tcgen05.mma, one for each softmax group: scores (both
 //                   operands in shared memory), then probabilities (tensor memory)
 //                   times values (shared memory, rows of head columns: the
@@ -42,7 +43,8 @@
 namespace bsm {
 namespace {
 
-constexpr int kTileThreads = 352;
+constexpr int kTileThreads = 384;
+constexpr int kPieces = 4;                              // told ahead at most
 constexpr int kPrefixThreads = 256;
 constexpr int kKeys = kPagedTileKeys;
 constexpr int kQHalf = 128 * 128;                       // 128 query rows of 64 columns
@@ -82,10 +84,10 @@ struct TileSmem {
     uint64_t full[kMaxStages], empty[kMaxStages];
     uint64_t qfull, qempty;
     uint64_t sfull[2], pfull[2], olast[2], ofree[2];
-    uint64_t pcfull[2], pcempty[2];
+    uint64_t pcfull[kPieces], pcempty[kPieces];
     uint64_t turn[2];                   // the group may issue its next scores
     uint64_t tail, drain, xfull;
-    TilePiece piece[2];
+    TilePiece piece[kPieces];
     float2 other[128];                  // reference and sum of the second group's rows (dual)
     uint32_t tmem_base;
     int32_t abort_flag, no_abort;       // (the second stays 0)
@@ -187,9 +189,8 @@ __device__ __forceinline__ bool warp_drain(TileSmem &h, uint64_t *b, uint32_t pa
 // box of `box` rows lies in one page); the copies themselves are issued by one
 // elected lane.
 template <int DP>
-__device__ bool produce(const PagedArgs &a, const CUtensorMap &tq, const CUtensorMap &tk, const CUtensorMap &tv, int box,
-                        TileSmem &h, unsigned char *qs, unsigned char *stages, const PagedLine<kKeys> &line,
-                        PagedWalk<kKeys> &walk, const PagedCut &cut, int32_t unit, uint32_t &loaded, uint32_t &qloads)
+__device__ bool produce(const PagedArgs &a, const CUtensorMap &tk, const CUtensorMap &tv, int box, TileSmem &h,
+                        unsigned char *stages, PagedWalk<kKeys> &walk, const PagedCut &cut, int32_t unit, uint32_t &loaded)
 {
     using Shape = TileShape<DP>;
     const int lane = threadIdx.x & 31;
@@ -199,12 +200,12 @@ __device__ bool produce(const PagedArgs &a, const CUtensorMap &tq, const CUtenso
     for (;; ++npc) {
         PagedPiece p{};
         const bool more = walk.next(p);
-        if (!warp_wait(&h.pcempty[npc & 1u], ((npc >> 1) & 1u) ^ 1u, &h.abort_flag))
+        if (!warp_wait(&h.pcempty[npc % kPieces], ((npc / kPieces) & 1u) ^ 1u, &h.abort_flag))
             return false;
         if (!more) {
             if (elect_one()) {
-                h.piece[npc & 1u].blocks = 0;
-                bar_arrive(&h.pcfull[npc & 1u]);
+                h.piece[npc % kPieces].blocks = 0;
+                bar_arrive(&h.pcfull[npc % kPieces]);
             }
             __syncwarp();
             return true;
@@ -227,21 +228,10 @@ __device__ bool produce(const PagedArgs &a, const CUtensorMap &tq, const CUtenso
         t.slot = p.starts && p.ends ? -1 : 2 * unit + (p.starts ? 1 : 0);
         t.join = p.starts && !p.ends ? cut.owner(p.tile_end - 1) - unit + 1 : 0;
         if (elect_one()) {
-            h.piece[npc & 1u] = t;
-            bar_arrive(&h.pcfull[npc & 1u]);
+            h.piece[npc % kPieces] = t;
+            bar_arrive(&h.pcfull[npc % kPieces]);
         }
         __syncwarp();
-        if (!warp_wait(&h.qempty, (npc & 1u) ^ 1u, &h.abort_flag))
-            return false;
-        if (elect_one()) {
-            bar_expect(&h.qfull, static_cast<uint32_t>(blocks_q * Shape::kHalves * half_tok * a.sub * 128));
-            for (int sb = 0; sb < blocks_q; ++sb)
-                for (int hf = 0; hf < Shape::kHalves; ++hf)
-                    tma_load_3d_q(qs + (sb * Shape::kHalves + hf) * kQHalf, &tq, hf * 64, t.head,
-                                  t.token + sb * half_tok, &h.qfull);
-        }
-        __syncwarp();
-        ++qloads;
         // keys that some token of the request sees: the others are not read
         int32_t keep = 0;
         if (a.window && s.L - s.m >= a.window)
@@ -333,6 +323,39 @@ __device__ bool produce(const PagedArgs &a, const CUtensorMap &tq, const CUtenso
     }
 }
 
+// The query blocks of each piece, as soon as the one before it has its scores
+// (in a warp of its own, so that keys and values of the next piece come
+// meanwhile).
+template <int DP>
+__device__ bool produce_q(const PagedArgs &a, const CUtensorMap &tq, TileSmem &h, unsigned char *qs, uint32_t &loaded)
+{
+    using Shape = TileShape<DP>;
+    const int32_t half_tok = a.tok / 2;
+    for (uint32_t npc = 0;; ++npc) {
+        if (!warp_wait(&h.pcfull[npc % kPieces], (npc / kPieces) & 1u, &h.abort_flag))
+            return false;
+        const TilePiece t = h.piece[npc % kPieces];
+        __syncwarp();
+        if (elect_one())
+            bar_arrive(&h.pcempty[npc % kPieces]);
+        __syncwarp();
+        if (t.blocks == 0)
+            return true;
+        if (!warp_wait(&h.qempty, (npc & 1u) ^ 1u, &h.abort_flag))
+            return false;
+        const int32_t blocks_q = t.tokens > half_tok ? 2 : 1;
+        if (elect_one()) {
+            bar_expect(&h.qfull, static_cast<uint32_t>(blocks_q * Shape::kHalves * half_tok * a.sub * 128));
+            for (int sb = 0; sb < blocks_q; ++sb)
+                for (int hf = 0; hf < Shape::kHalves; ++hf)
+                    tma_load_3d_q(qs + (sb * Shape::kHalves + hf) * kQHalf, &tq, hf * 64, t.head,
+                                  t.token + sb * half_tok, &h.qfull);
+        }
+        __syncwarp();
+        ++loaded;
+    }
+}
+
 // ------------------------------------------------------------- tensor cores
 // The same value in every lane, for the compiler too: what addresses an MMA
 // has to lie in uniform registers, and moving it there costs more than the MMA.
@@ -350,14 +373,14 @@ __device__ bool multiply(TileSmem &h, unsigned char *qs, unsigned char *stages, 
     RingPos pos;
     uint32_t np = 0, used = 0, turns = 0;   // steps' outputs issued; pieces with work; turns taken
     for (uint32_t npc = 0;; ++npc) {
-        if (!warp_wait(&h.pcfull[npc & 1u], (npc >> 1) & 1u, &h.abort_flag))
+        if (!warp_wait(&h.pcfull[npc % kPieces], (npc / kPieces) & 1u, &h.abort_flag))
             return false;
-        const int32_t blocks = static_cast<int32_t>(uniform(static_cast<uint32_t>(h.piece[npc & 1u].blocks)));
-        const int32_t subs = static_cast<int32_t>(uniform(static_cast<uint32_t>(h.piece[npc & 1u].subs)));
-        const bool dual = uniform(static_cast<uint32_t>(h.piece[npc & 1u].dual)) != 0;
+        const int32_t blocks = static_cast<int32_t>(uniform(static_cast<uint32_t>(h.piece[npc % kPieces].blocks)));
+        const int32_t subs = static_cast<int32_t>(uniform(static_cast<uint32_t>(h.piece[npc % kPieces].subs)));
+        const bool dual = uniform(static_cast<uint32_t>(h.piece[npc % kPieces].dual)) != 0;
         __syncwarp();
         if (elect_one())
-            bar_arrive(&h.pcempty[npc & 1u]);
+            bar_arrive(&h.pcempty[npc % kPieces]);
         __syncwarp();
         if (blocks == 0)
             return true;
@@ -498,12 +521,12 @@ __device__ bool softmax(const PagedArgs &a, TileSmem &h, unsigned char *store, u
     unsigned char *mine = store + warp * (32 * 64);
     uint32_t n = 0, pieces = 0, pieces1 = 0, duals = 0; // steps and pieces so far; pieces of the second group
     for (uint32_t npc = 0;; ++npc) {
-        if (!warp_wait(&h.pcfull[npc & 1u], (npc >> 1) & 1u, &h.abort_flag))
+        if (!warp_wait(&h.pcfull[npc % kPieces], (npc / kPieces) & 1u, &h.abort_flag))
             return false;
-        const TilePiece t = h.piece[npc & 1u];
+        const TilePiece t = h.piece[npc % kPieces];
         __syncwarp();
         if (lane == 0)
-            bar_arrive(&h.pcempty[npc & 1u]);
+            bar_arrive(&h.pcempty[npc % kPieces]);
         if (t.blocks == 0)
             return true;
         if (sub >= t.subs)
@@ -741,16 +764,21 @@ __global__ void __launch_bounds__(kTileThreads, 1)
             bar_init(&h.olast[s], 1);
             bar_init(&h.ofree[s], 4);
             bar_init(&h.turn[s], 1);
+        }
+        for (int s = 0; s < kPieces; ++s) {
             bar_init(&h.pcfull[s], 1);
-            bar_init(&h.pcempty[s], 10);
+            bar_init(&h.pcempty[s], 11);
         }
         bar_init(&h.tail, 1);
         bar_init(&h.drain, 2);
         bar_init(&h.xfull, 4);
         h.abort_flag = h.no_abort = 0;
-        a.join[unit].count = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    grid_dependency_wait();
+    grid_launch_dependents();
+    if (threadIdx.x == 0)
+        a.join[unit].count = 0;
     // the line of work; its prefix lies where the stages will be
     PagedPrefix<kPrefixThreads> &prefix = *reinterpret_cast<PagedPrefix<kPrefixThreads> *>(stages);
     const PagedLine<kKeys> line(a);
@@ -775,8 +803,8 @@ __global__ void __launch_bounds__(kTileThreads, 1)
 
     bool ok;
     if (warp == 8) {
-        uint32_t loaded = 0, qloads = 0;
-        ok = produce<DP>(a, tq, tk, tv, box, h, qs, stages, line, walk, cut, unit, loaded, qloads);
+        uint32_t loaded = 0;
+        ok = produce<DP>(a, tk, tv, box, h, stages, walk, cut, unit, loaded);
         if (!ok) {
             if (elect_one()) {
                 atomicOr(a.status, BSM_DEV_TIMEOUT);
@@ -788,8 +816,18 @@ __global__ void __launch_bounds__(kTileThreads, 1)
         const uint32_t S = Shape::kStages;
         for (uint32_t j = loaded > S ? loaded - S : 0u; j < loaded; ++j)
             warp_drain(h, &h.full[j % S], (j / S) & 1u);
-        if (qloads)
-            warp_drain(h, &h.qfull, (qloads - 1) & 1u);
+    } else if (warp == 11) {
+        uint32_t loaded = 0;
+        ok = produce_q<DP>(a, tq, h, qs, loaded);
+        if (!ok) {
+            if (elect_one()) {
+                atomicOr(a.status, BSM_DEV_TIMEOUT);
+                h.abort_flag = 1;
+            }
+            __syncwarp();
+        }
+        if (loaded)
+            warp_drain(h, &h.qfull, (loaded - 1) & 1u);
     } else if (warp >= 9) {
         ok = multiply<DP, kF16>(h, qs, stages, tmem, warp - 9);
         if (elect_one()) {
@@ -820,13 +858,16 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     }
 }
 
-// Joins the parts of every cut tile (see paged_join of the row kernel): a
-// thread a row, eight columns a CTA.
+// Joins the parts of every cut tile (the sums of the row kernel's RowSum): a
+// thread a row, 32 columns a CTA.
 constexpr int kTileJoinThreads = 128;
+constexpr int kJoinCols = 32;
 
 template <bool kF16> __global__ void __launch_bounds__(kTileJoinThreads) paged_tile_join(const PagedArgs a)
 {
     const int unit = blockIdx.x, sub = blockIdx.y;
+    grid_dependency_wait();
+    grid_launch_dependents();
     const PagedJoin j = a.join[unit];
     if (j.count <= 0)
         return;
@@ -843,35 +884,38 @@ template <bool kF16> __global__ void __launch_bounds__(kTileJoinThreads) paged_t
         top = fmaxf(top, ml[slot * 256 + row].x);
     }
     const float ref = top == -INFINITY ? 0.0f : top;
-    float acc[8] = {};
+    float4 acc[kJoinCols / 4] = {};
     float sum = 0.0f;
-    const int c = blockIdx.z * 2;
-#pragma unroll 4
+    const int c = blockIdx.z * (kJoinCols / 4);
+#pragma unroll 2
     for (int i = 0; i < j.count; ++i) {
         const int64_t slot = i == 0 ? 2 * unit + 1 : 2 * (unit + i);
         const float2 m = ml[slot * 256 + row];
-        const float4 u = po[(slot * (kPagedMaxDim / 4) + c) * 256 + row];
-        const float4 v = po[(slot * (kPagedMaxDim / 4) + c + 1) * 256 + row];
         const float f = pg_exp2(m.x - ref);
         sum += f * m.y;
-        acc[0] += f * u.x;
-        acc[1] += f * u.y;
-        acc[2] += f * u.z;
-        acc[3] += f * u.w;
-        acc[4] += f * v.x;
-        acc[5] += f * v.y;
-        acc[6] += f * v.z;
-        acc[7] += f * v.w;
+#pragma unroll
+        for (int k = 0; k < kJoinCols / 4; ++k) {
+            const float4 v = po[(slot * (kPagedMaxDim / 4) + c + k) * 256 + row];
+            acc[k].x += f * v.x;
+            acc[k].y += f * v.y;
+            acc[k].z += f * v.z;
+            acc[k].w += f * v.w;
+        }
     }
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    uint4 w;
-    w.x = pg_pack<kF16>(acc[0] * inv, acc[1] * inv);
-    w.y = pg_pack<kF16>(acc[2] * inv, acc[3] * inv);
-    w.z = pg_pack<kF16>(acc[4] * inv, acc[5] * inv);
-    w.w = pg_pack<kF16>(acc[6] * inv, acc[7] * inv);
     const int64_t token = j.token + tok;
-    *reinterpret_cast<uint4 *>(static_cast<unsigned char *>(a.out) +
-                               2 * (token * a.out_token + (j.head + h) * a.out_head + blockIdx.z * 8)) = w;
+    unsigned char *out = static_cast<unsigned char *>(a.out) + 2 * (token * a.out_token + (j.head + h) * a.out_head);
+#pragma unroll
+    for (int k = 0; k < kJoinCols / 4; k += 2) {
+        const int col = blockIdx.z * kJoinCols + k * 4;
+        uint4 w;
+        w.x = pg_pack<kF16>(acc[k].x * inv, acc[k].y * inv);
+        w.y = pg_pack<kF16>(acc[k].z * inv, acc[k].w * inv);
+        w.z = pg_pack<kF16>(acc[k + 1].x * inv, acc[k + 1].y * inv);
+        w.w = pg_pack<kF16>(acc[k + 1].z * inv, acc[k + 1].w * inv);
+        if (col < a.d)
+            *reinterpret_cast<uint4 *>(out + col * 2) = w;
+    }
     if (a.lse && blockIdx.z == 0)
         a.lse[token * a.heads_q + j.head + h] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
 }
@@ -879,11 +923,10 @@ template <bool kF16> __global__ void __launch_bounds__(kTileJoinThreads) paged_t
 template <int DP, bool kF16>
 int launch(const CUtensorMap *m, const PagedArgs &a, int box, cudaStream_t st)
 {
-    paged_tiles<DP, kF16><<<a.units, kTileThreads, TileShape<DP>::kSmem, st>>>(m[0], m[1], m[2], a, box);
-    if (int e = static_cast<int>(cudaGetLastError()))
+    if (int e = launch_early(paged_tiles<DP, kF16>, dim3(a.units), kTileThreads, TileShape<DP>::kSmem, st, m[0], m[1], m[2],
+                             a, box))
         return e;
-    paged_tile_join<kF16><<<dim3(a.units, 2, a.d / 8), kTileJoinThreads, 0, st>>>(a);
-    return static_cast<int>(cudaGetLastError());
+    return launch_early(paged_tile_join<kF16>, dim3(a.units, 2, (a.d + kJoinCols - 1) / kJoinCols), kTileJoinThreads, 0, st, a);
 }
 
 }  // namespace
