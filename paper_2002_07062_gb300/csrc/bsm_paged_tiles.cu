@@ -574,9 +574,20 @@ __device__ bool softmax(const PagedArgs &a, TileSmem &h, unsigned char *store, u
                     tmem_ld32_nowait(sc + 96, r + 96);
                 }
                 if (masked) {
+                    // 32 columns at a time, and only the side that cuts them
 #pragma unroll
-                    for (int c = q; c < q + 64; ++c)
-                        r[c] = c >= c0 && c < c1 ? r[c] : 0xFF800000u;
+                    for (int g = q; g < q + 64; g += 32) {
+                        if (__any_sync(0xffffffffu, c1 < g + 32)) {
+#pragma unroll
+                            for (int c = g; c < g + 32; ++c)
+                                r[c] = c < c1 ? r[c] : 0xFF800000u;
+                        }
+                        if (__any_sync(0xffffffffu, c0 > g)) {
+#pragma unroll
+                            for (int c = g; c < g + 32; ++c)
+                                r[c] = c >= c0 ? r[c] : 0xFF800000u;
+                        }
+                    }
                 }
 #pragma unroll
                 for (int c = q; c < q + 64; c += 2)

@@ -156,6 +156,61 @@ def test_attention(name, mask):
     b.check(**MASKS[mask])
 
 
+LONG = {
+    # several steps and tiles a CTA, both row blocks of a tile
+    "tiles": dict(lens=[3000, 2500, 1800], fresh=[700, 1, 400], hq=16, hkv=8, d=128, page=16),
+    "tiles, head size 64": dict(lens=[3100, 2500, 77], fresh=[900, 300, 1], hq=16, hkv=16, d=64, page=64),
+    "tiles, f16": dict(lens=[2900, 2100], fresh=[333, 500], hq=24, hkv=8, d=128, page=32, dtype="f16"),
+    # tiles of one row block: the key steps of both softmax groups
+    "few rows": dict(lens=[60000, 33], fresh=[3, 5], hq=16, hkv=2, d=128, page=16),
+    "few rows, head size 64, f16": dict(lens=[50000], fresh=[9], hq=16, hkv=4, d=64, page=128, dtype="f16"),
+    "single tokens beside a prompt": dict(lens=[900 + 37 * i for i in range(20)] + [700], fresh=[1] * 20 + [700], hq=8,
+                                          hkv=8, d=128, page=8),
+    # the row kernel, several steps a warp
+    "single tokens": dict(lens=[1 + 511 * i for i in range(30)], fresh=[1] * 30, hq=16, hkv=8, d=128, page=16),
+    "single tokens, head size 64": dict(lens=[9000 - 511 * i for i in range(17)], fresh=[1] * 17, hq=12, hkv=4, d=64,
+                                        page=48, dtype="f16"),
+    "prompts in pages of 4": dict(lens=[700, 900], fresh=[150, 1], hq=8, hkv=4, d=96, page=4),
+}
+
+
+@pytest.mark.parametrize("keys", ["even", "growing", "falling"])
+@pytest.mark.parametrize("mask", ["causal", "full", "window 300"])
+@pytest.mark.parametrize("name", LONG)
+def test_long_runs(name, mask, keys):
+    """Many steps a unit.  Keys that grow (or fall) along the request make every
+    row's maximum rise step after step (or lie in its first step)."""
+    import torch
+    b = Batch(**LONG[name], seed=len(name) + len(mask))
+    if keys != "even":
+        for r, L in enumerate(b.lens):
+            for e in range(-(-int(L) // b.page)):
+                f = e * b.page / max(1, int(L))
+                b.kc[int(b.tables[r, e])] *= 0.2 + 6 * (f if keys == "growing" else 1 - f)
+    b.poison()
+    b.run(**MASKS[mask])
+    b.check(**MASKS[mask])
+
+
+def test_drawn_batches():
+    """Shapes drawn over the whole range, every mask and type."""
+    rng = np.random.default_rng(11)
+    for i in range(40):
+        n = int(rng.integers(1, 9))
+        fresh = np.where(rng.random(n) < 0.5, 1, rng.integers(0, 260, n))
+        lens = np.maximum(0, fresh + rng.integers(-20, 900, n) * (rng.random(n) < 0.8))
+        hkv, g = int(rng.choice([1, 2, 3])), int(rng.choice([1, 2, 3, 5, 8, 17, 33]))
+        b = Batch(lens, fresh, hkv * g, hkv, int(rng.choice([8, 24, 64, 80, 112, 128])),
+                  int(rng.choice([1, 2, 8, 16, 24, 64, 200])), dtype=str(rng.choice(["bf16", "f16"])), seed=100 + i,
+                  layout=str(rng.choice(["nhd", "hnd"])), pad=int(rng.integers(0, 5)))
+        if b.T == 0:
+            continue
+        m = MASKS[str(rng.choice(list(MASKS)))]
+        b.poison()
+        b.run(**m)
+        b.check(**m)
+
+
 def test_many_requests():
     rng = np.random.default_rng(1)
     lens = rng.integers(0, 60, 3000)
