@@ -1812,6 +1812,6 @@ const char *bsm_status_string(int status)
     }
 }
 
-int bsm_version(void) { return (1 << 16) | 0; }
+int bsm_version(void) { return (1 << 16) | 1; }
 
 }  // extern "C"

@@ -62,6 +62,7 @@ struct PagedJoin {
     int32_t pad[3];
 };
 
+constexpr int32_t kPagedMostKeys = INT32_MAX - 255; // of a request: a step past them is still a 32-bit number
 constexpr int kPagedWarps = 8;                      // of the row kernel
 constexpr int kPagedRowTile = 16;                   // most rows of its tiles
 constexpr int kPagedMaxDim = 128;

@@ -56,7 +56,14 @@ int paged_device(int device, PagedDev **out)
                 return BSM_ERR_NO_DEVICE;
             g_paged_encode = reinterpret_cast<EncodeTiled>(fn);
         }
-        if (int e = paged_set_smem_limit())
+        // (the kernels' attributes belong to the current device)
+        int prev = -1;
+        if (cudaGetDevice(&prev) != cudaSuccess || (prev != device && cudaSetDevice(device) != cudaSuccess))
+            return BSM_ERR_NO_DEVICE;
+        const int e = paged_set_smem_limit();
+        if (prev != device)
+            cudaSetDevice(prev);
+        if (e)
             return record_cuda_error(e, "cudaFuncSetAttribute(paged)");
         d.ready = true;
     }
@@ -74,22 +81,36 @@ struct Span {
 
 Span span(const void *p, int64_t bytes) { return Span{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes}; }
 
-// Bytes from the first element to the end of the last of n0 x n1 rows of `row`
-// elements; -1 when the strides make rows overlap or overflow.
-int64_t extent2(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t row, int es)
+// A dimension of a strided array, in elements.  The stride of a dimension of one
+// entry is never used and may be anything.
+struct Dim {
+    int64_t n, stride;
+};
+
+// Bytes from the first element to the end of the last row (`row` contiguous
+// elements) of an array with these dimensions, in any order; -1 when its rows
+// overlap or the strides overflow.
+template <size_t N> int64_t extent(Dim (&&d)[N], int64_t row, int es)
 {
     constexpr int64_t kMost = int64_t(1) << 60;
-    if (s0 < 0 || s1 < 0 || (n0 > 1 && s0 > kMost / n0) || (n1 > 1 && s1 > kMost / n1))
-        return -1;
-    // (rows of one token must not overlap, nor those of neighbouring tokens)
-    if ((n1 > 1 && s1 < row) || (n0 > 1 && s0 < row))
-        return -1;
-    if (n0 > 1 && n1 > 1) {
-        const bool inner1 = s0 >= (n1 - 1) * s1 + row, inner0 = s1 >= (n0 - 1) * s0 + row;
-        if (!inner1 && !inner0)
+    std::sort(d, d + N, [](const Dim &a, const Dim &b) { return a.stride < b.stride; });
+    int64_t cur = row;
+    for (const Dim &x : d) {
+        if (x.n <= 1)
+            continue;
+        if (x.stride < cur || x.stride > kMost / x.n)
             return -1;
+        cur += (x.n - 1) * x.stride;
     }
-    return ((n0 - 1) * s0 + (n1 - 1) * s1 + row) * es;
+    return cur < kMost ? cur * es : -1;
+}
+
+template <size_t N> bool unaligned(Dim (&&d)[N], int es)
+{
+    for (const Dim &x : d)
+        if (x.n > 1 && x.stride * es % 16)
+            return true;
+    return false;
 }
 
 int elem_size(int dtype) { return dtype == BSM_F32 ? 4 : 2; }
@@ -213,18 +234,20 @@ int paged_write(const bsm_paged_write_desc *d, bsm_stream_t stream)
         return BSM_ERR_UNSUPPORTED;
     const int es = elem_size(d->dtype);
     const int64_t row = static_cast<int64_t>(d->head_dim) * es;
-    const int64_t ks = extent2(d->n_tokens, d->k_stride_token, d->n_heads, d->k_stride_head, d->head_dim, es);
-    const int64_t vs = extent2(d->n_tokens, d->v_stride_token, d->n_heads, d->v_stride_head, d->head_dim, es);
-    const int64_t one = extent2(d->page_size, d->kv_stride_token, d->n_heads, d->kv_stride_head, d->head_dim, es);
-    if (ks < 0 || vs < 0 || one < 0 || d->kv_stride_page < 0 ||
-        (d->n_pages > 1 && (d->kv_stride_page * es < one || d->kv_stride_page > (int64_t(1) << 60) / d->n_pages)))
+    const int64_t ks = extent({Dim{d->n_tokens, d->k_stride_token}, Dim{d->n_heads, d->k_stride_head}}, d->head_dim, es);
+    const int64_t vs = extent({Dim{d->n_tokens, d->v_stride_token}, Dim{d->n_heads, d->v_stride_head}}, d->head_dim, es);
+    const int64_t all = extent({Dim{d->n_pages, d->kv_stride_page}, Dim{d->page_size, d->kv_stride_token},
+                                Dim{d->n_heads, d->kv_stride_head}},
+                               d->head_dim, es);
+    if (ks < 0 || vs < 0 || all < 0)
         return BSM_ERR_INVALID_ARG;
     if (row % 16 || misaligned(d->k, 16) || misaligned(d->v, 16) || misaligned(d->k_cache, 16) ||
-        misaligned(d->v_cache, 16) || misaligned(d->slots, 8) || (d->k_stride_token * es) % 16 ||
-        (d->k_stride_head * es) % 16 || (d->v_stride_token * es) % 16 || (d->v_stride_head * es) % 16 ||
-        (d->kv_stride_page * es) % 16 || (d->kv_stride_token * es) % 16 || (d->kv_stride_head * es) % 16)
+        misaligned(d->v_cache, 16) || misaligned(d->slots, 8) ||
+        unaligned({Dim{d->n_tokens, d->k_stride_token}, Dim{d->n_heads, d->k_stride_head},
+                   Dim{d->n_tokens, d->v_stride_token}, Dim{d->n_heads, d->v_stride_head}, Dim{d->n_pages, d->kv_stride_page},
+                   Dim{d->page_size, d->kv_stride_token}, Dim{d->n_heads, d->kv_stride_head}},
+                  es))
         return BSM_ERR_MISALIGNED;
-    const int64_t all = (d->n_pages - 1) * d->kv_stride_page * es + one;
     const Span kc = span(d->k_cache, all), vc = span(d->v_cache, all), k = span(d->k, ks), v = span(d->v, vs),
                sl = span(d->slots, 8ll * d->n_tokens);
     // (keys and values may be interleaved in one allocation: only equal places clash)
@@ -276,18 +299,23 @@ int paged_attention(const bsm_paged_desc *d, bsm_stream_t stream)
     if (!d->q || !d->k_cache || !d->v_cache || !d->out || !d->starts || !d->lengths || !d->tables || !d->workspace ||
         d->n_pages == 0)
         return BSM_ERR_INVALID_ARG;
-    const int64_t qs = extent2(d->n_tokens, d->q_stride_token, d->heads_q, d->q_stride_head, d->head_dim, 2);
-    const int64_t os = extent2(d->n_tokens, d->out_stride_token, d->heads_q, d->out_stride_head, d->head_dim, 2);
-    const int64_t one = extent2(d->page_size, d->kv_stride_token, d->heads_kv, d->kv_stride_head, d->head_dim, 2);
-    if (qs < 0 || os < 0 || one < 0 || d->kv_stride_page < 0 ||
-        (d->n_pages > 1 && (d->kv_stride_page * 2 < one || d->kv_stride_page > (int64_t(1) << 60) / d->n_pages)))
+    const int64_t qs = extent({Dim{d->n_tokens, d->q_stride_token}, Dim{d->heads_q, d->q_stride_head}}, d->head_dim, 2);
+    const int64_t os = extent({Dim{d->n_tokens, d->out_stride_token}, Dim{d->heads_q, d->out_stride_head}}, d->head_dim, 2);
+    const int64_t all = extent({Dim{d->n_pages, d->kv_stride_page}, Dim{d->page_size, d->kv_stride_token},
+                                Dim{d->heads_kv, d->kv_stride_head}},
+                               d->head_dim, 2);
+    if (qs < 0 || os < 0 || all < 0)
         return BSM_ERR_INVALID_ARG;
     if (misaligned(d->q, 16) || misaligned(d->k_cache, 16) || misaligned(d->v_cache, 16) || misaligned(d->out, 16) ||
         misaligned(d->lse, 4) || misaligned(d->starts, 4) || misaligned(d->lengths, 4) || misaligned(d->tables, 4) ||
-        misaligned(d->workspace, 256) || d->q_stride_token % 8 || d->q_stride_head % 8 || d->out_stride_token % 8 ||
-        d->out_stride_head % 8 || d->kv_stride_page % 8 || d->kv_stride_token % 8 || d->kv_stride_head % 8)
+        misaligned(d->workspace, 256) ||
+        unaligned({Dim{d->n_tokens, d->q_stride_token}, Dim{d->heads_q, d->q_stride_head},
+                   Dim{d->n_tokens, d->out_stride_token}, Dim{d->heads_q, d->out_stride_head},
+                   Dim{d->n_pages, d->kv_stride_page}, Dim{d->page_size, d->kv_stride_token},
+                   Dim{d->heads_kv, d->kv_stride_head}},
+                  2))
         return BSM_ERR_MISALIGNED;
-    const int64_t all = (d->n_pages - 1) * d->kv_stride_page * 2 + one, n = d->n_requests;
+    const int64_t n = d->n_requests;
     const Span o = span(d->out, os), w = span(d->workspace, d->workspace_bytes),
                ls = span(d->lse, d->lse ? 4ll * d->n_tokens * d->heads_q : 0);
     const Span in[6] = {span(d->q, qs), span(d->k_cache, all), span(d->v_cache, all), span(d->starts, 4 * (n + 1)),

@@ -149,7 +149,7 @@ template <int kStep> struct PagedLine {
         PagedSeq s;
         const int32_t raw0 = a.starts[r], raw1 = a.starts[r + 1], rawL = a.lengths[r];
         const int64_t cap = static_cast<int64_t>(a.width) * a.page;
-        const int32_t most = cap < INT32_MAX ? static_cast<int32_t>(cap) : INT32_MAX;
+        const int32_t most = cap < kPagedMostKeys ? static_cast<int32_t>(cap) : kPagedMostKeys;
         const int32_t t0 = raw0 < 0 ? 0 : raw0 > a.n_tokens ? a.n_tokens : raw0;
         const int32_t t1 = raw1 < t0 ? t0 : raw1 > a.n_tokens ? a.n_tokens : raw1;
         const int32_t L = rawL < 0 ? 0 : rawL > most ? most : rawL;

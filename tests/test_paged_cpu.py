@@ -67,7 +67,8 @@ def test_tables_refusals(kw, code):
     (dict(n_tokens=-1), INV), (dict(n_heads=0), INV), (dict(head_dim=0), INV), (dict(page_size=0), INV),
     (dict(n_pages=0), INV), (dict(dtype=9), INV), (dict(k=None), INV), (dict(slots=None), INV),
     (dict(k_stride_token=64), INV),                             # tokens overlap
-    (dict(kv_stride_page=1024), INV), (dict(kv_stride_head=-64), INV),
+    (dict(kv_stride_page=1024), INV), (dict(kv_stride_head=-64), INV), (dict(kv_stride_page=1 << 60), INV),
+    (dict(n_tokens=1, k_stride_token=3, k=(1 << 40) + 8), MIS),
     (dict(head_dim=60), MIS), (dict(k=(1 << 40) + 8), MIS), (dict(kv_stride_page=2052), MIS),
     (dict(n_heads=1 << 20, head_dim=1 << 12), UNS),
     (dict(k=1 << 40, k_cache=(1 << 40) + 256), INV), (dict(k_cache=1 << 40, v_cache=1 << 40), INV),

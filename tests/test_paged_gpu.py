@@ -261,6 +261,42 @@ def test_fused_projection_strides_and_strided_out():
     b.kc, b.vc = both[:, 0], both[:, 1]
     b.run()
     b.check()
+    # heads outermost, pages between heads and tokens
+    far = both.permute(1, 3, 0, 2, 4).contiguous()
+    b.kc, b.vc = far[0].permute(1, 2, 0, 3), far[1].permute(1, 2, 0, 3)
+    b.run()
+    b.check()
+
+
+def test_tables_inside_a_wider_array():
+    import torch
+    b = Batch([300, 45, 700], [130, 1, 5], 8, 2, 64, 16, seed=8)
+    st, ln, tab = b.dev()
+    wide = torch.full((3, tab.shape[1] + 9), -1, dtype=torch.int32, device="cuda")
+    wide[:, 4:4 + tab.shape[1]] = tab
+    b.dev = lambda: [st, ln, wide[:, 4:4 + tab.shape[1]]]
+    for hint in (130, 0):
+        b.run(max_new=hint)
+        b.check()
+
+
+def test_two_streams_at_once():
+    """Calls on two streams with a workspace each."""
+    import torch
+    bs = [Batch([5000, 700], [1, 400], 8, 2, 128, 16, seed=20), Batch([3000, 900, 4], [1, 1, 1], 8, 2, 128, 16, seed=21)]
+    streams = [torch.cuda.Stream() for _ in bs]
+    ws = [torch.full((bsm.bsm_paged_workspace_bytes(8, 2, 128, 400),), 255, dtype=torch.uint8, device="cuda") for _ in bs]
+    args = [b.dev() for b in bs]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for b, s, w, x in zip(bs, streams, ws, args):
+            bsm.bsm_paged_attention(b.q, b.kc, b.vc, b.out, *x, int(b.fresh.max()), 128 ** -0.5, w, flags=bsm.FLAG_CAUSAL,
+                                    lse=b.lse, stream=s)
+    torch.cuda.synchronize()
+    for b in bs:
+        b.scale = 128 ** -0.5
+        b.check()
+    assert bsm.bsm_device_status() == 0
 
 
 def test_offsets_past_32_bits():
@@ -299,10 +335,11 @@ def test_bad_tables_and_lengths_are_reported():
             b.starts = np.array([0, 140, 170], np.int32)
         nb = bsm.bsm_paged_workspace_bytes(8, 2, 128, 140)
         ws = torch.zeros(nb, dtype=torch.uint8, device="cuda")
-        bsm.bsm_paged_attention(b.q, b.kc, b.vc, b.out, *b.dev(), 140, 0.1, ws, flags=bsm.FLAG_CAUSAL)
-        torch.cuda.synchronize()
-        assert bsm.bsm_device_status() == bsm.DEV_BOUNDS, case
-        bsm.bsm_device_status_clear()
+        for hint in (140, 0):           # the tile kernel, the row kernel
+            bsm.bsm_paged_attention(b.q, b.kc, b.vc, b.out, *b.dev(), hint, 0.1, ws, flags=bsm.FLAG_CAUSAL)
+            torch.cuda.synchronize()
+            assert bsm.bsm_device_status() == bsm.DEV_BOUNDS, (case, hint)
+            bsm.bsm_device_status_clear()
 
 
 def _tables_case(cached, fresh, page, width=None, n_free=None, n_slots=None, seed=0):
@@ -455,3 +492,14 @@ def test_step_on_a_side_stream_and_in_a_graph():
     graph.replay()
     check(22)
     assert bsm.bsm_device_status() == 0
+
+
+def test_serving_example():
+    """The example's steps against its own recomputation: prompts in chunks, then single tokens, four layers.
+    An output is a mean of values under rounded weights: half a unit of 8 bits twice, of the largest value."""
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import paged_serving
+    worst = paged_serving.main(["--requests", "5", "--prompt", "300", "--chunk", "128", "--steps", "6", "--check"])
+    assert worst <= 2 * 2.0 ** -8 * 4       # (means of values up to 4 times the largest output)
