@@ -10,7 +10,8 @@
 // its own three stages of 16 keys (8 KiB of K and V at D = 128) filled by
 // 16-byte asynchronous copies, its own running maximum and sum; no barrier of
 // the block after the work is laid out.  24 stages an SM keep 128 to 192 KiB
-// in flight.
+// in flight.  GB300: 128 requests of up to 8192 keys, 32/8 heads of 128, 2.25 GB:
+// 353 to 363 us, 0.91 to 0.94 of the copy rate; one request of 2000 keys 14 us.
 #include <cuda_runtime.h>
 
 #include <cstdint>
@@ -25,6 +26,8 @@ constexpr int kRowThreads = kPagedWarps * 32;
 constexpr int kRowStages = 3;
 constexpr int kStageBytes = 8192;                       // of one warp: K and V of a step
 
+// Tiles of 32 rows (two 16-row blocks a warp) spilled and ran at 0.45 of the copy
+// rate; such batches go to the tile kernel.
 // keys of a step: 16 rows of 256 bytes, or 32 of 128
 template <int DP> struct RowShape {
     static constexpr int kKeys = DP == 128 ? 16 : 32;

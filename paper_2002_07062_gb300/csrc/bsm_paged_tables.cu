@@ -49,7 +49,8 @@ __device__ __forceinline__ uint32_t pages_of(uint32_t tokens, uint32_t page) { r
 // a token finds its owner by bisection in the shared prefix.  One launch, no
 // scratch, no order between CTAs: a page of a new token comes from the free
 // list, not from the table entry another CTA writes.  Bound by latency: loads,
-// scan, search and stores follow one another.  Everything per token and request
+// scan, search and stores follow one another (64 requests 4.5 us, 4096 requests
+// with 224 thousand tokens 9.5 us on a GB300; with 64-bit quotients 6.5 and 12.2).  Everything per token and request
 // is 32-bit (a tile's new pages fit, tables being less than 2^20 wide; its
 // tokens are cut at 2^31, past any slot); only running totals are 64-bit.
 __global__ void __launch_bounds__(kTabThreads) paged_tables(const PagedTablesArgs a)
@@ -204,7 +205,8 @@ __global__ void __launch_bounds__(kTabThreads) paged_tables(const PagedTablesArg
 
 // The copy, bound by its bytes.  A thread keeps its place in the row of a
 // token (16 bytes of one head) and goes from token to token, eight loads in
-// flight; the divisions that find a slot's page are one a token.
+// flight; the divisions that find a slot's page are one a token.  237 MB: 38.3 us,
+// 0.91 of the copy rate (57 with the place divided out for every piece).
 constexpr int kWriteThreads = 256;
 constexpr int kWriteAhead = 4;
 

@@ -4,33 +4,39 @@
 //   s = scale q k^T,  p = exp(s - m),  o = sum p v / sum p   (m a running reference)
 //
 // Bound: the tensor cores (4 D operations a pair of a query row and a key) and,
-// close behind, the exponentials.  One persistent CTA per SM, 12 warps:
-//   warps 0-3, 4-7  softmax of one 128-row block each: a thread owns a row, reads
-//                   its 128 scores of a step from tensor memory, writes the probabilities
-//                   back over them as 16-bit pairs, and at the end scales and
-//                   stores its row of the output;
-//   warp 8          producer: walks its share of the work line, copies the query
-//                   and steps of 128 keys and values, page by page,
-//                   with TMA (128-byte swizzle) into a ring of stages;
-//   warp 11         copies each piece's query blocks;
-//   warps 9, 10     issue tcgen05.mma, one for each softmax group: scores (both
-//                   operands in shared memory), then probabilities (tensor memory)
-//                   times values (shared memory, rows of head columns: the
-//                   "N-major" form).  One warp for both groups was the limit: 24
-//                   instructions a step, and in order, so a group waited for the
-//                   other's probabilities.
-// The two row blocks share every stage, which halves what an SM reads from L2,
-// and take turns on the tensor cores.  (Steps of 64 keys with two score buffers a block would never
-// wait for scores, but a product of 128 x 64 x 16 from shared memory takes 52
-// cycles instead of 32, its operands' bytes, and the issuing warps half again as
-// many instructions: two prompts of 8192 tokens 963 us.)
-// A tile of one row block takes both
-// softmax groups all the same: one has the even key steps, the other the odd
-// ones, each with its own output and reference, and the two are added at the end.
+// close behind, the softmax between a row block's two products.  One persistent
+// CTA per SM, 12 warps:
+//   warps 0-3, 4-7  two softmax groups, each with one block of 128 rows: a thread
+//                   owns a row, reads its 128 scores of a step from tensor memory,
+//                   writes the probabilities back over them as 16-bit pairs, and at
+//                   the end scales and stores its row of the output;
+//   warp 8          walks its CTA's share of the work line and copies steps of 128
+//                   keys and values, page by page, with TMA (128-byte swizzle) into a
+//                   ring of stages;
+//   warps 9, 10     issue tcgen05.mma, one for each group: scores (both operands in
+//                   shared memory), then probabilities (tensor memory) times values
+//                   (shared memory, rows of head columns: the "N-major" form);
+//   warp 11         copies each tile's query blocks.
+// The row blocks share every stage, which halves what an SM reads from L2.  They
+// take turns at the tensor cores: while one block's scores become
+// probabilities, the other's products run.  A tile of one row block takes both
+// groups all the same: one has the even key steps, the other the odd ones, each
+// with its own output and reference, and the two are added at the end.
 // Outputs stay in tensor memory; one is rescaled only when a row's maximum has
 // grown by more than 2^8 since its reference was taken (any reference gives the
 // same quotient, and 2^8 is far from the range of fp32 sums), so nearly all
-// blocks skip that pass.
+// steps skip that pass.
+//
+// GB300: two prompts of 8192 tokens, 32/8 heads of 128: 722 us (1.52 PFLOP/s; a
+// plain bf16 product 1.95), tensor pipe 69 % active on 2048 tokens over 6100;
+// 4 tokens over 131 thousand keys, 1.02 GB: 172 us.  Without the softmax the first
+// runs in 548 us.  Tried and slower for it: steps of 64 keys with two score
+// buffers a block, which never wait for scores (963 us: a product of 128 x 64 x 16
+// takes 52 cycles instead of 32, the bytes of its operands in shared memory);
+// probabilities in two parts, the first one's product beside the second's
+// exponentials (787); two softmax warps a row (917: 96 registers, and the two
+// have to meet every step); one issuing warp (849 to 1025); a warp each for keys and
+// values (759).
 // Every wait is bounded as in the batched product.
 #include <cuda.h>
 #include <cuda_runtime.h>
@@ -74,7 +80,7 @@ struct TilePiece {
     int32_t subs;                       // softmax groups with work (1 or 2)
     int32_t dual;                       // one row block: key steps dealt to the two groups in turn
     int32_t first;                      // first key step
-    int32_t lo, hi, pos;                // keys of the tile; position of its first token
+    int32_t hi, pos;                    // end of the tile's keys; position of its first token
     int32_t token, tokens, head, heads;
     int32_t slot;                       // of its partial output; -1: the tile is whole
     int32_t join;                       // units that share the tile, if this one is the first
@@ -215,7 +221,6 @@ __device__ bool produce(const PagedArgs &a, const CUtensorMap &tk, const CUtenso
         TilePiece t;
         t.blocks = p.steps;
         t.first = p.first;
-        t.lo = p.keys.lo;
         t.hi = p.keys.hi;
         t.token = s.t0 + p.tile * a.tok;
         t.tokens = s.m - p.tile * a.tok < a.tok ? s.m - p.tile * a.tok : a.tok;
