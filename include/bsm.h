@@ -364,6 +364,9 @@ int bsm_paged_write(const bsm_paged_write_desc *d, bsm_stream_t stream);
  *   lse       n_tokens x heads_q fp32, or null.
  *   max_new   the most new tokens of any request, as the host knows it.  A hint:
  *             it selects kernels; a wrong one costs time, not the answer.
+ *   page_size any; multiples of 16 are fastest (with more than 16 rows, new tokens
+ *             times heads_q / heads_kv, pages that are no multiple of 8 cost about
+ *             twice the time).
  *   workspace bsm_paged_workspace_bytes bytes, 256-byte aligned, for this call
  *             alone until its work is done; its contents need no preparation.
  * The result depends on the batch (the keys are split by what the whole batch

@@ -72,7 +72,8 @@ constexpr int kPagedTileKeys = 128;                 // keys of its steps
 int launch_paged_tables(const PagedTablesArgs &a, int n_sm, void *stream);
 int launch_paged_write(const PagedWriteArgs &a, int n_sm, void *stream);
 int launch_paged_rows(const PagedArgs &a, bool f16, int grid, void *stream);
-// maps: CUtensorMaps of q, k, v (host); box: rows of one copy of k and v
+// maps: CUtensorMaps of q, k, v (host); box: rows of one copy of k and v (below 8:
+// those maps are not used)
 int launch_paged_tiles(const void *maps, const PagedArgs &a, bool f16, int box, void *stream);
 int paged_set_smem_limit();
 

@@ -368,23 +368,25 @@ int paged_attention(const bsm_paged_desc *d, bsm_stream_t stream)
     // A batch with requests of more than 16 rows (new tokens times the heads that
     // share a key/value head) goes to the tile kernel, its single tokens too: it
     // keeps up with the cache's bytes there, and one launch deals all the work.
-    // The tile kernel's copies want pages of whole groups of eight rows.
+    // Pages of whole groups of eight rows come by TMA (box >= 8), others row by row.
     int box = 1;
     while (box < kPagedTileKeys && d->page_size % (2 * box) == 0)
         box *= 2;
     PagedArgs b = a;
     split_group(b, kPagedTileRows / 2);
     b.tok = 2 * (kPagedTileRows / 2 / b.sub);
-    CUtensorMap maps[3];
-    bool tiles = box >= 8 && static_cast<int64_t>(d->max_new) * a.group > kPagedRowTile;
+    CUtensorMap maps[3] = {};
+    bool tiles = static_cast<int64_t>(d->max_new) * a.group > kPagedRowTile;
     if (tiles) {
         const int64_t qd[3] = {d->head_dim, d->heads_q, d->n_tokens}, qst[3] = {1, d->q_stride_head, d->q_stride_token};
         const int qb[3] = {64, b.sub, b.tok / 2};
         const int64_t kd[4] = {d->head_dim, d->page_size, d->heads_kv, d->n_pages};
         const int64_t kst[4] = {1, d->kv_stride_token, d->kv_stride_head, d->kv_stride_page};
         const int kb[4] = {64, box, 1, 1};
-        tiles = paged_map(&maps[0], f16, d->q, 3, qd, qst, qb) && paged_map(&maps[1], f16, d->k_cache, 4, kd, kst, kb) &&
-                paged_map(&maps[2], f16, d->v_cache, 4, kd, kst, kb);
+        tiles = paged_map(&maps[0], f16, d->q, 3, qd, qst, qb);
+        if (box >= 8 && !(paged_map(&maps[1], f16, d->k_cache, 4, kd, kst, kb) &&
+                          paged_map(&maps[2], f16, d->v_cache, 4, kd, kst, kb)))
+            box = 0;
     }
     if (tiles) {
         b.units = dev->n_sm;

@@ -56,7 +56,7 @@ constexpr int kKeys = kPagedTileKeys;
 constexpr int kQHalf = 128 * 128;                       // 128 query rows of 64 columns
 constexpr int kHalfBytes = kKeys * 128;                 // a step's keys, 64 columns
 constexpr int kStore = 8 * 32 * 64;                     // a warp's 32 rows of 32 columns on their way out
-constexpr int kTileHeader = 2048;
+constexpr int kTileHeader = 4096;
 constexpr uint32_t kTileTmemCols = 512;
 constexpr int kMaxStages = 8;
 constexpr float kLag = 8.0f;                            // log2 of how far a maximum may pass its reference
@@ -82,6 +82,7 @@ struct TilePiece {
     int32_t first;                      // first key step
     int32_t hi, pos;                    // end of the tile's keys; position of its first token
     int32_t token, tokens, head, heads;
+    int32_t r, kvh, keep, len;          // request, key/value head; keys [keep, len) may be read
     int32_t slot;                       // of its partial output; -1: the tile is whole
     int32_t join;                       // units that share the tile, if this one is the first
 };
@@ -95,6 +96,7 @@ struct TileSmem {
     uint64_t tail, drain, xfull;
     TilePiece piece[kPieces];
     float2 other[128];                  // reference and sum of the second group's rows (dual)
+    int64_t where[2][kKeys];            // of odd pages: byte offset of a step's rows (-1: not read)
     uint32_t tmem_base;
     int32_t abort_flag, no_abort;       // (the second stays 0)
 };
@@ -177,6 +179,20 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r)
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// Whether the phase is over, without waiting.
+__device__ __forceinline__ bool bar_done(uint64_t *b, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(saddr(b)), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+
 // Every lane waits; true in all lanes only if none gave up.
 __device__ __forceinline__ bool warp_wait(uint64_t *b, uint32_t parity, const volatile int32_t *abort)
 {
@@ -187,6 +203,31 @@ __device__ __forceinline__ bool warp_wait(uint64_t *b, uint32_t parity, const vo
 __device__ __forceinline__ bool warp_drain(TileSmem &h, uint64_t *b, uint32_t parity)
 {
     return __all_sync(0xffffffffu, bar_spin(b, parity, &h.no_abort));
+}
+
+__device__ TilePiece tile_piece(const PagedArgs &a, const PagedSeq &s, const PagedPiece &p, const PagedCut &cut, int32_t unit)
+{
+    const int32_t kvh = p.head / a.subs, sub = p.head - kvh * a.subs;
+    TilePiece t;
+    t.blocks = p.steps;
+    t.first = p.first;
+    t.hi = p.keys.hi;
+    t.token = s.t0 + p.tile * a.tok;
+    t.tokens = s.m - p.tile * a.tok < a.tok ? s.m - p.tile * a.tok : a.tok;
+    t.pos = s.L - s.m + p.tile * a.tok;
+    const int32_t blocks_q = t.tokens > a.tok / 2 ? 2 : 1;
+    t.dual = blocks_q == 1 && p.steps > 1;
+    t.subs = t.dual ? 2 : blocks_q;
+    t.r = p.r;
+    t.kvh = kvh;
+    t.len = s.L;
+    // (keys before the first that some token of the request sees are not read)
+    t.keep = a.window && s.L - s.m >= a.window ? s.L - s.m - a.window + 1 : 0;
+    t.head = kvh * a.group + sub * a.sub;
+    t.heads = a.group - sub * a.sub < a.sub ? a.group - sub * a.sub : a.sub;
+    t.slot = p.starts && p.ends ? -1 : 2 * unit + (p.starts ? 1 : 0);
+    t.join = p.starts && !p.ends ? cut.owner(p.tile_end - 1) - unit + 1 : 0;
+    return t;
 }
 
 // ------------------------------------------------------------- producer
@@ -217,30 +258,13 @@ __device__ bool produce(const PagedArgs &a, const CUtensorMap &tk, const CUtenso
             return true;
         }
         const PagedSeq &s = walk.s;
-        const int32_t kvh = p.head / a.subs, sub = p.head - kvh * a.subs, half_tok = a.tok / 2;
-        TilePiece t;
-        t.blocks = p.steps;
-        t.first = p.first;
-        t.hi = p.keys.hi;
-        t.token = s.t0 + p.tile * a.tok;
-        t.tokens = s.m - p.tile * a.tok < a.tok ? s.m - p.tile * a.tok : a.tok;
-        t.pos = s.L - s.m + p.tile * a.tok;
-        const int32_t blocks_q = t.tokens > half_tok ? 2 : 1;
-        t.dual = blocks_q == 1 && p.steps > 1;
-        t.subs = t.dual ? 2 : blocks_q;
-        t.head = kvh * a.group + sub * a.sub;
-        t.heads = a.group - sub * a.sub < a.sub ? a.group - sub * a.sub : a.sub;
-        t.slot = p.starts && p.ends ? -1 : 2 * unit + (p.starts ? 1 : 0);
-        t.join = p.starts && !p.ends ? cut.owner(p.tile_end - 1) - unit + 1 : 0;
+        const TilePiece t = tile_piece(a, s, p, cut, unit);
         if (elect_one()) {
             h.piece[npc % kPieces] = t;
             bar_arrive(&h.pcfull[npc % kPieces]);
         }
         __syncwarp();
-        // keys that some token of the request sees: the others are not read
-        int32_t keep = 0;
-        if (a.window && s.L - s.m >= a.window)
-            keep = s.L - s.m - a.window + 1;
+        const int32_t kvh = t.kvh, keep = t.keep;
         const int64_t row = p.r * a.table_stride;
         // page of this lane's piece of block b: (page, row in it); n_pages: not there, filled with zeros
         auto page_of = [&](int32_t b, int32_t &in) -> int32_t {
@@ -328,14 +352,31 @@ __device__ bool produce(const PagedArgs &a, const CUtensorMap &tk, const CUtenso
     }
 }
 
+// The query blocks of piece npc, once the one before it has its scores.
+template <int DP>
+__device__ bool load_q(const PagedArgs &a, const CUtensorMap &tq, TileSmem &h, unsigned char *qs, const TilePiece &t, uint32_t npc)
+{
+    using Shape = TileShape<DP>;
+    const int32_t half_tok = a.tok / 2, blocks_q = t.tokens > half_tok ? 2 : 1;
+    if (!warp_wait(&h.qempty, (npc & 1u) ^ 1u, &h.abort_flag))
+        return false;
+    if (elect_one()) {
+        bar_expect(&h.qfull, static_cast<uint32_t>(blocks_q * Shape::kHalves * half_tok * a.sub * 128));
+        for (int sb = 0; sb < blocks_q; ++sb)
+            for (int hf = 0; hf < Shape::kHalves; ++hf)
+                tma_load_3d_q(qs + (sb * Shape::kHalves + hf) * kQHalf, &tq, hf * 64, t.head, t.token + sb * half_tok,
+                              &h.qfull);
+    }
+    __syncwarp();
+    return true;
+}
+
 // The query blocks of each piece, as soon as the one before it has its scores
 // (in a warp of its own, so that keys and values of the next piece come
 // meanwhile).
 template <int DP>
 __device__ bool produce_q(const PagedArgs &a, const CUtensorMap &tq, TileSmem &h, unsigned char *qs, uint32_t &loaded)
 {
-    using Shape = TileShape<DP>;
-    const int32_t half_tok = a.tok / 2;
     for (uint32_t npc = 0;; ++npc) {
         if (!warp_wait(&h.pcfull[npc % kPieces], (npc / kPieces) & 1u, &h.abort_flag))
             return false;
@@ -346,18 +387,150 @@ __device__ bool produce_q(const PagedArgs &a, const CUtensorMap &tq, TileSmem &h
         __syncwarp();
         if (t.blocks == 0)
             return true;
-        if (!warp_wait(&h.qempty, (npc & 1u) ^ 1u, &h.abort_flag))
+        if (!load_q<DP>(a, tq, h, qs, t, npc))
             return false;
-        const int32_t blocks_q = t.tokens > half_tok ? 2 : 1;
-        if (elect_one()) {
-            bar_expect(&h.qfull, static_cast<uint32_t>(blocks_q * Shape::kHalves * half_tok * a.sub * 128));
-            for (int sb = 0; sb < blocks_q; ++sb)
-                for (int hf = 0; hf < Shape::kHalves; ++hf)
-                    tma_load_3d_q(qs + (sb * Shape::kHalves + hf) * kQHalf, &tq, hf * 64, t.head,
-                                  t.token + sb * half_tok, &h.qfull);
-        }
-        __syncwarp();
         ++loaded;
+    }
+}
+
+// Pages that are no whole groups of eight rows (the swizzle of the copies above):
+// 16 bytes a lane by plain asynchronous copies, to the swizzled places, rows that
+// are not read filled with zeros.  Up to three stages of this warp's are in flight;
+// a stage is handed on when its copies have landed, at the latest before this warp
+// waits for anything (so no one waits for a stage that only this warp could hand
+// on).  Warp 8 fills the stages of keys, warp 11 those of values: bound by their
+// instructions.  Two prompts of 8192 tokens in pages of 1: 1.67 ms (2.18 with one
+// warp, 12.1 on the row kernel; in pages of 64, by TMA, 0.76).
+struct Pending {
+    int count = 0;                      // stages not handed on yet
+    int at[3];                          // which, the oldest first
+};
+
+template <int kLeft> __device__ __forceinline__ void hand_on(TileSmem &h, Pending &q)
+{
+    if (q.count <= kLeft)
+        return;
+    asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    while (q.count > kLeft) {
+        if (elect_one())
+            bar_arrive(&h.full[q.at[0]]);
+        __syncwarp();
+        q.at[0] = q.at[1];
+        q.at[1] = q.at[2];
+        --q.count;
+    }
+}
+
+template <int DP>
+__device__ bool produce_odd(const PagedArgs &a, const CUtensorMap &tq, TileSmem &h, unsigned char *qs, unsigned char *stages,
+                            PagedWalk<kKeys> &walk, const PagedCut &cut, int32_t unit, int side, uint32_t &queries)
+{
+    using Shape = TileShape<DP>;
+    constexpr int S = Shape::kStages;
+    const int lane = threadIdx.x & 31;
+    const unsigned char *base = static_cast<const unsigned char *>(side ? a.v : a.k);
+    RingPos pos;
+    Pending q;
+    for (uint32_t npc = 0;; ++npc) {
+        TilePiece t;
+        if (side == 0) {
+            PagedPiece p{};
+            const bool more = walk.next(p);
+            t.blocks = 0;
+            if (more)
+                t = tile_piece(a, walk.s, p, cut, unit);
+            hand_on<0>(h, q);
+            if (!warp_wait(&h.pcempty[npc % kPieces], ((npc / kPieces) & 1u) ^ 1u, &h.abort_flag))
+                return false;
+            if (elect_one()) {
+                h.piece[npc % kPieces] = t;
+                bar_arrive(&h.pcfull[npc % kPieces]);
+            }
+            __syncwarp();
+        } else {
+            hand_on<0>(h, q);
+            if (!warp_wait(&h.pcfull[npc % kPieces], (npc / kPieces) & 1u, &h.abort_flag))
+                return false;
+            t = h.piece[npc % kPieces];
+            __syncwarp();
+            if (elect_one())
+                bar_arrive(&h.pcempty[npc % kPieces]);
+            __syncwarp();
+        }
+        if (t.blocks == 0)
+            return true;
+        if (side == 1) {
+            if (!load_q<DP>(a, tq, h, qs, t, npc))
+                return false;
+            ++queries;
+        }
+        const int64_t row0 = t.r * a.table_stride, head = t.kvh * a.kv_head;
+        // byte offsets of the rows of step i, four a lane: read a step ahead
+        int64_t off[kKeys / 32];
+        auto locate = [&](int32_t i) {
+#pragma unroll
+            for (int x = 0; x < kKeys / 32; ++x) {
+                const int32_t key = (t.first + i) * kKeys + x * 32 + lane;
+                off[x] = -1;
+                if (i < t.blocks && key >= t.keep && key < t.len) {
+                    const int32_t e = key / a.page, page = a.tables[row0 + e];
+                    if (page >= 0 && page < a.n_pages)
+                        off[x] = 2 * (page * a.kv_page + (key - e * a.page) * a.kv_token + head);
+                    else
+                        atomicOr(a.status, BSM_DEV_BOUNDS);
+                }
+            }
+        };
+        auto load = [&]() -> bool {
+            if (!__all_sync(0xffffffffu, bar_done(&h.empty[pos.s], pos.ph ^ 1u))) {
+                hand_on<0>(h, q);
+                if (!warp_wait(&h.empty[pos.s], pos.ph ^ 1u, &h.abort_flag))
+                    return false;
+            }
+            const uint32_t st = saddr(stages) + static_cast<uint32_t>(pos.s * Shape::kStageBytes);
+            const int c = lane & 7;
+#pragma unroll 4
+            for (int r4 = 0; r4 < kKeys; r4 += 4) {
+                const int row = r4 + (lane >> 3);
+                const int64_t at = h.where[side][row];
+#pragma unroll
+                for (int hf = 0; hf < Shape::kHalves; ++hf) {
+                    const bool in = at >= 0 && hf * 64 + c * 8 < a.d;
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                                     st + hf * kHalfBytes + row * 128 + ((c ^ (row & 7)) << 4)),
+                                 "l"(base + (in ? at + (hf * 64 + c * 8) * 2 : 0)), "r"(in ? 16u : 0u)
+                                 : "memory");
+                }
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            q.at[q.count == 0 ? 0 : q.count == 1 ? 1 : 2] = pos.s;
+            ++q.count;
+            hand_on<2>(h, q);
+            return true;
+        };
+        // K0 V0 K1 V1 .., dual K0 K1 V0 K2 V1 ..
+        const int32_t lag = t.dual ? 1 : 0;
+        locate(0);
+        for (int32_t i = 0; i < t.blocks + lag; ++i) {
+            for (int sd = 0; sd < 2; ++sd) {
+                const int32_t step = sd ? i - lag : i;
+                if (step < 0 || step >= t.blocks)
+                    continue;
+                if (sd == side) {
+                    __syncwarp();           // the rows of the step before have been read
+#pragma unroll
+                    for (int x = 0; x < kKeys / 32; ++x)
+                        h.where[side][x * 32 + lane] = off[x];
+                    __syncwarp();
+                    locate(step + 1);
+                    if (!load())
+                        return false;
+                }
+                pos.step(S);
+            }
+        }
     }
 }
 
@@ -755,7 +928,9 @@ __device__ bool softmax(const PagedArgs &a, TileSmem &h, unsigned char *store, u
     }
 }
 
-template <int DP, bool kF16>
+// kOdd: pages that the TMA copies cannot take (an instance of its own, so that its
+// registers cost the other nothing).
+template <int DP, bool kF16, bool kOdd>
 __global__ void __launch_bounds__(kTileThreads, 1)
     paged_tiles(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk,
                 const __grid_constant__ CUtensorMap tv, const PagedArgs a, const int box)
@@ -820,7 +995,11 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     bool ok;
     if (warp == 8) {
         uint32_t loaded = 0;
-        ok = produce<DP>(a, tk, tv, box, h, stages, walk, cut, unit, loaded);
+        uint32_t none = 0;
+        if (kOdd)
+            ok = produce_odd<DP>(a, tq, h, qs, stages, walk, cut, unit, 0, none);
+        else
+            ok = produce<DP>(a, tk, tv, box, h, stages, walk, cut, unit, loaded);
         if (!ok) {
             if (elect_one()) {
                 atomicOr(a.status, BSM_DEV_TIMEOUT);
@@ -829,12 +1008,17 @@ __global__ void __launch_bounds__(kTileThreads, 1)
             __syncwarp();
         }
         // copies in flight land before the CTA leaves
+        if (kOdd)
+            asm volatile("cp.async.wait_all;" ::: "memory");
         const uint32_t S = Shape::kStages;
         for (uint32_t j = loaded > S ? loaded - S : 0u; j < loaded; ++j)
             warp_drain(h, &h.full[j % S], (j / S) & 1u);
     } else if (warp == 11) {
         uint32_t loaded = 0;
-        ok = produce_q<DP>(a, tq, h, qs, loaded);
+        if (kOdd)
+            ok = produce_odd<DP>(a, tq, h, qs, stages, walk, cut, unit, 1, loaded);
+        else
+            ok = produce_q<DP>(a, tq, h, qs, loaded);
         if (!ok) {
             if (elect_one()) {
                 atomicOr(a.status, BSM_DEV_TIMEOUT);
@@ -842,6 +1026,8 @@ __global__ void __launch_bounds__(kTileThreads, 1)
             }
             __syncwarp();
         }
+        if (kOdd)
+            asm volatile("cp.async.wait_all;" ::: "memory");
         if (loaded)
             warp_drain(h, &h.qfull, (loaded - 1) & 1u);
     } else if (warp >= 9) {
@@ -939,8 +1125,8 @@ template <bool kF16> __global__ void __launch_bounds__(kTileJoinThreads) paged_t
 template <int DP, bool kF16>
 int launch(const CUtensorMap *m, const PagedArgs &a, int box, cudaStream_t st)
 {
-    if (int e = launch_early(paged_tiles<DP, kF16>, dim3(a.units), kTileThreads, TileShape<DP>::kSmem, st, m[0], m[1], m[2],
-                             a, box))
+    const auto kernel = box >= 8 ? paged_tiles<DP, kF16, false> : paged_tiles<DP, kF16, true>;
+    if (int e = launch_early(kernel, dim3(a.units), kTileThreads, TileShape<DP>::kSmem, st, m[0], m[1], m[2], a, box))
         return e;
     return launch_early(paged_tile_join<kF16>, dim3(a.units, 2, (a.d + kJoinCols - 1) / kJoinCols), kTileJoinThreads, 0, st, a);
 }
@@ -963,10 +1149,14 @@ int paged_tiles_set_smem()
         if (!e)
             e = static_cast<int>(cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
     };
-    set(reinterpret_cast<const void *>(&paged_tiles<64, false>), TileShape<64>::kSmem);
-    set(reinterpret_cast<const void *>(&paged_tiles<64, true>), TileShape<64>::kSmem);
-    set(reinterpret_cast<const void *>(&paged_tiles<128, false>), TileShape<128>::kSmem);
-    set(reinterpret_cast<const void *>(&paged_tiles<128, true>), TileShape<128>::kSmem);
+    set(reinterpret_cast<const void *>(&paged_tiles<64, false, false>), TileShape<64>::kSmem);
+    set(reinterpret_cast<const void *>(&paged_tiles<64, true, false>), TileShape<64>::kSmem);
+    set(reinterpret_cast<const void *>(&paged_tiles<128, false, false>), TileShape<128>::kSmem);
+    set(reinterpret_cast<const void *>(&paged_tiles<128, true, false>), TileShape<128>::kSmem);
+    set(reinterpret_cast<const void *>(&paged_tiles<64, false, true>), TileShape<64>::kSmem);
+    set(reinterpret_cast<const void *>(&paged_tiles<64, true, true>), TileShape<64>::kSmem);
+    set(reinterpret_cast<const void *>(&paged_tiles<128, false, true>), TileShape<128>::kSmem);
+    set(reinterpret_cast<const void *>(&paged_tiles<128, true, true>), TileShape<128>::kSmem);
     return e;
 }
 
