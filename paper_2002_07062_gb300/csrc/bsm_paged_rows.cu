@@ -363,63 +363,68 @@ __global__ void __launch_bounds__(kRowThreads, 1) paged_rows(const PagedArgs a)
     cp_wait<0>();
 }
 
-// Joins the parts of every cut tile, in unit order.  One CTA a unit (those that
-// start no such tile leave); its warps are dealt to the rows, and where there are
-// fewer rows than warps, several share a row's parts.  128 requests: 353 us in
+// Joins the parts of every cut tile, in unit order.  CTA (x, y) has units 8 x ..
+// 8 x + 7 (one a warp) and the rows y, y + grid: a warp joins its unit's few parts
+// alone, many parts are split over the CTA's warps.  128 requests: 353 us in
 // all; joining the parts of a CTA's warps in shared memory first 367 (a row after
-// another there, in code run once), by the CTA that arrives last 372.
+// another there, in code run once), by the CTA that arrives last 372.  One request
+// of 100 thousand keys and one key/value head is one tile in 1216 parts: 40 us
+// in all, 357 with one CTA for all its rows.  8 requests of 300 keys and less take
+// 15.4 us so, 13.0 with a CTA a unit.
 constexpr int kJoinWarps = 8;
+constexpr int kJoinAlone = 16;          // parts a warp joins alone
 
 template <bool kF16> __global__ void __launch_bounds__(kJoinWarps * 32) paged_join(const PagedArgs a)
 {
+    __shared__ PagedJoin join[kJoinWarps];
     __shared__ float4 part[kJoinWarps][32];
     __shared__ float2 part_ml[kJoinWarps];
     grid_dependency_wait();
     grid_launch_dependents();
-    const int unit = blockIdx.x;
-    const PagedJoin j = a.join[unit];
-    if (j.count <= 0)
-        return;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int rows = j.tokens * a.sub;
-    // warps of a row: a power of two, so that a row's lie side by side
-    int each = 1;
-    while (2 * each * rows <= kJoinWarps && 2 * each <= j.count)
-        each *= 2;
-    auto at = [&](int i) { return static_cast<int64_t>(i == 0 ? 2 * unit + 1 : 2 * (unit + i)) * kPagedRowTile; };
-    for (int row0 = 0; row0 < rows; row0 += kJoinWarps / each) {
-        const int row = row0 + warp / each, share = warp % each;
-        const int tt = row / a.sub, h = row - tt * a.sub;
-        const bool live = row < rows && h < j.heads;
+    const int first = blockIdx.x * kJoinWarps, mine = first + warp;
+    if (lane == 0)
+        join[warp] = a.join[mine];
+    __syncthreads();
+    // parts [from, to) of a row of the tile that unit `unit` starts
+    auto sum = [&](int unit, int row, int from, int to) {
+        auto at = [&](int i) { return static_cast<int64_t>(i == 0 ? 2 * unit + 1 : 2 * (unit + i)) * kPagedRowTile + row; };
         RowSum r;
-        if (live) {
-            const int from = j.count * share / each, to = j.count * (share + 1) / each;
-            for (int i = from + lane; i < to; i += 32)
-                r.top = fmaxf(r.top, a.part_ml[(at(i) + row) * 2]);
+        for (int i = from + lane; i < to; i += 32)
+            r.top = fmaxf(r.top, a.part_ml[at(i) * 2]);
 #pragma unroll
-            for (int o = 16; o; o >>= 1)
-                r.top = fmaxf(r.top, __shfl_xor_sync(0xffffffffu, r.top, o));
+        for (int o = 16; o; o >>= 1)
+            r.top = fmaxf(r.top, __shfl_xor_sync(0xffffffffu, r.top, o));
 #pragma unroll 8
-            for (int i = from; i < to; ++i)
-                r.add(*reinterpret_cast<const float2 *>(a.part_ml + (at(i) + row) * 2),
-                      *reinterpret_cast<const float4 *>(a.part_o + (at(i) + row) * kPagedMaxDim + lane * 4));
-        }
-        if (each > 1) {
+        for (int i = from; i < to; ++i)
+            r.add(*reinterpret_cast<const float2 *>(a.part_ml + at(i) * 2),
+                  *reinterpret_cast<const float4 *>(a.part_o + at(i) * kPagedMaxDim + lane * 4));
+        return r;
+    };
+    for (int row = blockIdx.y; row < kPagedRowTile; row += gridDim.y) {
+        const int tt = row / a.sub, h = row - tt * a.sub;
+        const PagedJoin &j = join[warp];
+        if (j.count > 0 && j.count <= kJoinAlone && tt < j.tokens && h < j.heads)
+            sum(mine, row, 0, j.count).template store<kF16>(a, j.token + tt, j.head + h, lane);
+        for (int w = 0; w < kJoinWarps; ++w) {
+            const PagedJoin &c = join[w];
+            if (c.count <= kJoinAlone || tt >= c.tokens || h >= c.heads)
+                continue;
+            RowSum r = sum(first + w, row, c.count * warp / kJoinWarps, c.count * (warp + 1) / kJoinWarps);
             part[warp][lane] = r.acc;
             if (lane == 0)
                 part_ml[warp] = make_float2(r.top, r.sum);
             __syncthreads();
-            if (live && share == 0) {
+            if (warp == 0) {
                 r = RowSum{};
-                for (int i = 0; i < each; ++i)
-                    r.top = fmaxf(r.top, part_ml[warp + i].x);
-                for (int i = 0; i < each; ++i)
-                    r.add(part_ml[warp + i], part[warp + i][lane]);
+                for (int i = 0; i < kJoinWarps; ++i)
+                    r.top = fmaxf(r.top, part_ml[i].x);
+                for (int i = 0; i < kJoinWarps; ++i)
+                    r.add(part_ml[i], part[i][lane]);
+                r.store<kF16>(a, c.token + tt, c.head + h, lane);
             }
             __syncthreads();
         }
-        if (live && share == 0)
-            r.store<kF16>(a, j.token + tt, j.head + h, lane);
     }
 }
 
@@ -427,7 +432,9 @@ template <int DP, bool kF16> int launch_rows(const PagedArgs &a, int grid, cudaS
 {
     if (int e = launch_early(paged_rows<DP, kF16>, dim3(grid), kRowThreads, kRowSmem, st, a))
         return e;
-    return launch_early(paged_join<kF16>, dim3(a.units), kJoinWarps * 32, 0, st, a);
+    static_assert(kJoinWarps == kPagedWarps, "a unit a warp");
+    const int rows = a.tok * a.sub;
+    return launch_early(paged_join<kF16>, dim3(grid, rows < kPagedRowTile ? rows : kPagedRowTile), kJoinWarps * 32, 0, st, a);
 }
 
 }  // namespace

@@ -1061,55 +1061,100 @@ __global__ void __launch_bounds__(kTileThreads, 1)
 }
 
 // Joins the parts of every cut tile (the sums of the row kernel's RowSum): a
-// thread a row, 32 columns a CTA.
-constexpr int kTileJoinThreads = 128;
-constexpr int kJoinCols = 32;
-
-template <bool kF16> __global__ void __launch_bounds__(kTileJoinThreads) paged_tile_join(const PagedArgs a)
+// thread a row and kCols columns, kShares threads a row where there are many parts
+// (few tiles), each with its share of them.
+template <bool kF16, int kCols, int kShares> __global__ void __launch_bounds__(128 * kShares) paged_tile_join(const PagedArgs a)
 {
+    __shared__ float other[kShares > 1 ? (kShares - 1) * 128 * (kCols + 2) : 1];
     const int unit = blockIdx.x, sub = blockIdx.y;
     grid_dependency_wait();
     grid_launch_dependents();
     const PagedJoin j = a.join[unit];
     if (j.count <= 0)
         return;
-    const int half_tok = a.tok / 2;
-    const int tt = threadIdx.x / a.sub, h = threadIdx.x - tt * a.sub, tok = sub * half_tok + tt;
-    if (tt >= half_tok || tok >= j.tokens || h >= j.heads)
-        return;
-    const int row = sub * 128 + threadIdx.x;
+    const int half_tok = a.tok / 2, lane_row = threadIdx.x & 127, share = threadIdx.x >> 7;
+    const int tt = lane_row / a.sub, h = lane_row - tt * a.sub, tok = sub * half_tok + tt;
+    const bool live = tt < half_tok && tok < j.tokens && h < j.heads;
+    const int row = sub * 128 + lane_row;
     const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml);
     const float4 *po = reinterpret_cast<const float4 *>(a.part_o);
-    float top = -INFINITY;
-    for (int i = 0; i < j.count; ++i) {
-        const int64_t slot = i == 0 ? 2 * unit + 1 : 2 * (unit + i);
-        top = fmaxf(top, ml[slot * 256 + row].x);
-    }
-    const float ref = top == -INFINITY ? 0.0f : top;
-    float4 acc[kJoinCols / 4] = {};
-    float sum = 0.0f;
-    const int c = blockIdx.z * (kJoinCols / 4);
-#pragma unroll 2
-    for (int i = 0; i < j.count; ++i) {
-        const int64_t slot = i == 0 ? 2 * unit + 1 : 2 * (unit + i);
-        const float2 m = ml[slot * 256 + row];
-        const float f = pg_exp2(m.x - ref);
-        sum += f * m.y;
+    auto slot = [&](int i) { return static_cast<int64_t>(i == 0 ? 2 * unit + 1 : 2 * (unit + i)); };
+    const int from = j.count * share / kShares, to = j.count * (share + 1) / kShares;
+    float4 acc[kCols / 4] = {};
+    float sum = 0.0f, top = -INFINITY;
+    if (live) {
+#pragma unroll 8
+        for (int i = from; i < to; ++i)
+            top = fmaxf(top, ml[slot(i) * kPagedTileRows + row].x);
+        const float ref = top == -INFINITY ? 0.0f : top;
+        const int c = blockIdx.z * (kCols / 4);
+#pragma unroll(kCols == 32 ? 2 : 8)
+        for (int i = from; i < to; ++i) {
+            const float2 m = ml[slot(i) * kPagedTileRows + row];
+            const float f = pg_exp2(m.x - ref);
+            sum += f * m.y;
 #pragma unroll
-        for (int k = 0; k < kJoinCols / 4; ++k) {
-            const float4 v = po[(slot * (kPagedMaxDim / 4) + c + k) * 256 + row];
-            acc[k].x += f * v.x;
-            acc[k].y += f * v.y;
-            acc[k].z += f * v.z;
-            acc[k].w += f * v.w;
+            for (int k = 0; k < kCols / 4; ++k) {
+                const float4 v = po[(slot(i) * (kPagedMaxDim / 4) + c + k) * kPagedTileRows + row];
+                acc[k].x += f * v.x;
+                acc[k].y += f * v.y;
+                acc[k].z += f * v.z;
+                acc[k].w += f * v.w;
+            }
         }
     }
+    if (kShares > 1) {
+        // [share - 1][column, then sum and top][row]
+        float *mine = other + (share - 1) * 128 * (kCols + 2) + lane_row;
+        if (share > 0) {
+#pragma unroll
+            for (int k = 0; k < kCols / 4; ++k) {
+                mine[(4 * k) * 128] = acc[k].x;
+                mine[(4 * k + 1) * 128] = acc[k].y;
+                mine[(4 * k + 2) * 128] = acc[k].z;
+                mine[(4 * k + 3) * 128] = acc[k].w;
+            }
+            mine[kCols * 128] = sum;
+            mine[(kCols + 1) * 128] = top;
+        }
+        __syncthreads();
+        if (share > 0)
+            return;
+        float all = top;
+        for (int s = 0; s < kShares - 1; ++s)
+            all = fmaxf(all, other[(s * (kCols + 2) + kCols + 1) * 128 + lane_row]);
+        const float ref = all == -INFINITY ? 0.0f : all;
+        const float f0 = pg_exp2(top - ref);
+        sum *= f0;
+#pragma unroll
+        for (int k = 0; k < kCols / 4; ++k) {
+            acc[k].x *= f0;
+            acc[k].y *= f0;
+            acc[k].z *= f0;
+            acc[k].w *= f0;
+        }
+        for (int s = 0; s < kShares - 1; ++s) {
+            const float *o = other + s * 128 * (kCols + 2) + lane_row;
+            const float f = pg_exp2(o[(kCols + 1) * 128] - ref);
+            sum += f * o[kCols * 128];
+#pragma unroll
+            for (int k = 0; k < kCols / 4; ++k) {
+                acc[k].x += f * o[(4 * k) * 128];
+                acc[k].y += f * o[(4 * k + 1) * 128];
+                acc[k].z += f * o[(4 * k + 2) * 128];
+                acc[k].w += f * o[(4 * k + 3) * 128];
+            }
+        }
+        top = all;
+    }
+    if (!live)
+        return;
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     const int64_t token = j.token + tok;
     unsigned char *out = static_cast<unsigned char *>(a.out) + 2 * (token * a.out_token + (j.head + h) * a.out_head);
 #pragma unroll
-    for (int k = 0; k < kJoinCols / 4; k += 2) {
-        const int col = blockIdx.z * kJoinCols + k * 4;
+    for (int k = 0; k < kCols / 4; k += 2) {
+        const int col = blockIdx.z * kCols + k * 4;
         uint4 w;
         w.x = pg_pack<kF16>(acc[k].x * inv, acc[k].y * inv);
         w.y = pg_pack<kF16>(acc[k].z * inv, acc[k].w * inv);
@@ -1122,13 +1167,22 @@ template <bool kF16> __global__ void __launch_bounds__(kTileJoinThreads) paged_t
         a.lse[token * a.heads_q + j.head + h] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
 }
 
+template <bool kF16, int kCols, int kShares> int launch_join(const PagedArgs &a, cudaStream_t st)
+{
+    return launch_early(paged_tile_join<kF16, kCols, kShares>, dim3(a.units, 2, (a.d + kCols - 1) / kCols), 128 * kShares, 0,
+                        st, a);
+}
+
 template <int DP, bool kF16>
-int launch(const CUtensorMap *m, const PagedArgs &a, int box, cudaStream_t st)
+int launch(const CUtensorMap *m, const PagedArgs &a, int box, int64_t tiles, cudaStream_t st)
 {
     const auto kernel = box >= 8 ? paged_tiles<DP, kF16, false> : paged_tiles<DP, kF16, true>;
     if (int e = launch_early(kernel, dim3(a.units), kTileThreads, TileShape<DP>::kSmem, st, m[0], m[1], m[2], a, box))
         return e;
-    return launch_early(paged_tile_join<kF16>, dim3(a.units, 2, (a.d + kJoinCols - 1) / kJoinCols), kTileJoinThreads, 0, st, a);
+    // Tiles of ten parts and more: more CTAs, four threads to a row's parts.  16 tokens
+    // over 100 thousand keys, one key/value head: 41.6 us in all, 112 the other way; 64
+    // tokens over 8000 keys, 8 key/value heads: 28 and 33.
+    return tiles * 10 <= a.units ? launch_join<kF16, 8, 4>(a, st) : launch_join<kF16, 32, 1>(a, st);
 }
 
 }  // namespace
@@ -1137,9 +1191,11 @@ int launch_paged_tiles(const void *maps, const PagedArgs &a, bool f16, int box, 
 {
     const CUtensorMap *m = static_cast<const CUtensorMap *>(maps);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    // tiles of the batch, each request having one at least
+    const int64_t tiles = static_cast<int64_t>(a.n > a.n_tokens / a.tok ? a.n : a.n_tokens / a.tok) * a.heads_kv * a.subs;
     if (a.d <= 64)
-        return f16 ? launch<64, true>(m, a, box, st) : launch<64, false>(m, a, box, st);
-    return f16 ? launch<128, true>(m, a, box, st) : launch<128, false>(m, a, box, st);
+        return f16 ? launch<64, true>(m, a, box, tiles, st) : launch<64, false>(m, a, box, tiles, st);
+    return f16 ? launch<128, true>(m, a, box, tiles, st) : launch<128, false>(m, a, box, tiles, st);
 }
 
 int paged_tiles_set_smem()

@@ -170,6 +170,11 @@ LONG = {
     "single tokens": dict(lens=[1 + 511 * i for i in range(30)], fresh=[1] * 30, hq=16, hkv=8, d=128, page=16),
     "single tokens, head size 64": dict(lens=[9000 - 511 * i for i in range(17)], fresh=[1] * 17, hq=12, hkv=4, d=64,
                                         page=48, dtype="f16"),
+    # one tile in many parts
+    "one token, one key/value head": dict(lens=[70000], fresh=[1], hq=16, hkv=1, d=128, page=16),
+    "a few tokens, one key/value head": dict(lens=[20, 40000], fresh=[1, 3], hq=5, hkv=1, d=64, page=64, dtype="f16"),
+    "40 tokens, one key/value head": dict(lens=[60000], fresh=[40], hq=4, hkv=1, d=64, page=16),
+    "20 tokens beside others": dict(lens=[50000, 2000], fresh=[20, 1], hq=3, hkv=1, d=120, page=12, dtype="f16"),
     "prompts in pages of 4": dict(lens=[700, 900], fresh=[150, 1], hq=8, hkv=4, d=96, page=4),
 }
 
