@@ -32,45 +32,24 @@ __device__ __forceinline__ int64_t pg_div(int64_t a, int64_t b)
     return a / b;
 }
 
-// a / b: in fp32 and put right where both are small (the common case), which has
-// half the latency of the integer division.
-__device__ __forceinline__ uint32_t pg_udiv(uint32_t a, uint32_t b)
+// sum over i < n of (a i + b) / kStep, rounded down each: the sum of a i + b less that of
+// the remainders, which repeat every P = kStep / gcd(a, kStep) terms and in a period
+// are (b mod g), (b mod g) + g, ...; those of the last part of a period are added up one by
+// one (fewer than P).  a n + b < 2^32.  Needs no division: three prompts under a window
+// of 1024 take 152.5 us with Euclid's steps on the slope, 148 so.
+template <int kStep> __device__ __forceinline__ int64_t floor_sum(uint32_t n, uint32_t a, uint32_t b)
 {
-    if (a >= 1u << 22)
-        return a / b;
-    uint32_t q = static_cast<uint32_t>(__fdividef(static_cast<float>(a), static_cast<float>(b)));
-    q -= q * b > a ? 1u : 0u;           // (off by one at most: a < 2^22, the quotient's relative error 2^-22)
-    q += a - q * b >= b ? 1u : 0u;
-    return q;
-}
-
-// sum over i < n of (a i + b) / m, rounded down each (Euclid on the slope).
-// a n + b < 2^32.  (64-bit quotients here and a search tile by tile cost 8 to 30 us a
-// call for a few long requests.)
-__device__ __forceinline__ int64_t floor_sum(uint32_t n, uint32_t m, uint32_t a, uint32_t b)
-{
-    uint64_t ans = 0;
-    while (n > 0) {
-        if (a >= m) {
-            const uint32_t q = pg_udiv(a, m);
-            ans += static_cast<uint64_t>(n) * (n - 1) / 2 * q;
-            a -= q * m;
-        }
-        if (b >= m) {
-            const uint32_t q = pg_udiv(b, m);
-            ans += static_cast<uint64_t>(n) * q;
-            b -= q * m;
-        }
-        const uint32_t y = a * n + b;
-        if (y < m)
-            break;
-        n = pg_udiv(y, m);
-        b = y - n * m;
-        const uint32_t t = m;
-        m = a;
-        a = t;
-    }
-    return static_cast<int64_t>(ans);
+    static_assert((kStep & (kStep - 1)) == 0, "steps are powers of two");
+    const uint32_t low = a & (0u - a), g = low < kStep ? low : kStep, lg = 31 - __clz(g);
+    const uint32_t P = static_cast<uint32_t>(kStep) >> lg;
+    const uint32_t rest = n & (P - 1);
+    uint32_t part = 0, x = b;
+    for (uint32_t i = 0; i < rest; ++i, x += a)
+        part += x & (kStep - 1);
+    const uint64_t periods = (n - rest) * static_cast<uint64_t>(g) / kStep;
+    const uint64_t mods = periods * (P * (b & (g - 1)) + kStep * (P - 1) / 2) + part;
+    const uint64_t all = static_cast<uint64_t>(n) * (n - 1) / 2 * a + static_cast<uint64_t>(n) * b;
+    return static_cast<int64_t>((all - mods) / kStep);
 }
 
 // One request as the kernels see it: lengths and offsets outside the buffers
@@ -129,7 +108,7 @@ template <int kStep> struct PagedLine {
         if (static_cast<uint32_t>(i) <= none)
             return static_cast<int64_t>(i) + tail;
         int64_t n = tail + static_cast<int64_t>(none) +
-                    floor_sum(i - none, kStep, tok, static_cast<uint32_t>(base) + (none + 1) * tok + kStep - 1);
+                    floor_sum<kStep>(i - none, tok, static_cast<uint32_t>(base) + (none + 1) * tok + kStep - 1);
         if (a.window) {
             // whole steps that lie left of a tile's window: of tiles j and on
             uint32_t j = none;
@@ -138,7 +117,7 @@ template <int kStep> struct PagedLine {
                 j = j < past ? past : j;
             }
             if (j < static_cast<uint32_t>(i))
-                n -= floor_sum(i - j, kStep, tok, static_cast<uint32_t>(base) + j * tok - static_cast<uint32_t>(a.window) + 1u);
+                n -= floor_sum<kStep>(i - j, tok, static_cast<uint32_t>(base) + j * tok - static_cast<uint32_t>(a.window) + 1u);
         }
         return n;
     }
