@@ -113,12 +113,12 @@ __device__ __forceinline__ void tma_load_3d_q(void *dst, const CUtensorMap *map,
 }
 
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map, int32_t c0, int32_t c1, int32_t c2,
-                                            int32_t c3, uint64_t *bar)
+                                            int32_t c3, uint32_t bar)
 {
     asm volatile(
         "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, "
         "%5}], [%6];" ::"r"(dst),
-        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(saddr(bar))
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar)
         : "memory");
 }
 
@@ -230,11 +230,17 @@ __device__ TilePiece tile_piece(const PagedArgs &a, const PagedSeq &s, const Pag
     return t;
 }
 
+// The same value in every lane, for the compiler too: what addresses an MMA or a tensor
+// copy has to lie in uniform registers, and moving it there costs more than the MMA.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __reduce_max_sync(0xffffffffu, x); }
+
 // ------------------------------------------------------------- producer
 // Copies stage after stage in the order the products read them: K and V of one
 // block after another.  Lane c looks up the page of the block's c-th piece (a
 // box of `box` rows lies in one page); the copies themselves are issued by one
-// elected lane.
+// elected lane.  The warp's instructions bound the small pages: with coordinates the
+// compiler does not know to be uniform, two prompts of 8192 tokens in pages of 16 take
+// 829 us, 770 so; in pages of 8 1106 and 928.
 template <int DP>
 __device__ bool produce(const PagedArgs &a, const CUtensorMap &tk, const CUtensorMap &tv, int box, TileSmem &h,
                         unsigned char *stages, PagedWalk<kKeys> &walk, const PagedCut &cut, int32_t unit, uint32_t &loaded)
@@ -264,7 +270,7 @@ __device__ bool produce(const PagedArgs &a, const CUtensorMap &tk, const CUtenso
             bar_arrive(&h.pcfull[npc % kPieces]);
         }
         __syncwarp();
-        const int32_t kvh = t.kvh, keep = t.keep;
+        const int32_t kvh = static_cast<int32_t>(uniform(t.kvh)), keep = t.keep;
         const int64_t row = p.r * a.table_stride;
         // page of this lane's piece of block b: (page, row in it); n_pages: not there, filled with zeros
         auto page_of = [&](int32_t b, int32_t &in) -> int32_t {
@@ -291,15 +297,16 @@ __device__ bool produce(const PagedArgs &a, const CUtensorMap &tk, const CUtenso
             const bool hold = side == 1 && (v0 > 0 || v1 < kKeys);
             if (!warp_wait(&h.empty[pos.s], pos.ph ^ 1u, &h.abort_flag))
                 return false;
-            const uint32_t st = saddr(stages) + static_cast<uint32_t>(pos.s * Shape::kStageBytes);
-            uint64_t *bar = hold ? &h.tail : &h.full[pos.s];
+            const uint32_t st = uniform(saddr(stages) + static_cast<uint32_t>(pos.s * Shape::kStageBytes));
+            const uint32_t bar = uniform(saddr(hold ? &h.tail : &h.full[pos.s]));
             if (elect_one())
-                bar_expect(bar, static_cast<uint32_t>(__popc(have) * box * 128 * Shape::kHalves));
+                bar_expect(hold ? &h.tail : &h.full[pos.s], static_cast<uint32_t>(__popc(have) * box * 128 * Shape::kHalves));
             __syncwarp();
             for (int c = 0; c < boxes; ++c) {
-                const int32_t pg = __shfl_sync(0xffffffffu, page, c), rw = __shfl_sync(0xffffffffu, in, c);
                 if (!((have >> c) & 1u))
                     continue;
+                const int32_t pg = static_cast<int32_t>(uniform(lane == c ? page : 0));
+                const int32_t rw = static_cast<int32_t>(uniform(lane == c ? in : 0));
                 if (elect_one()) {
 #pragma unroll
                     for (int hf = 0; hf < Shape::kHalves; ++hf)
@@ -535,10 +542,6 @@ __device__ bool produce_odd(const PagedArgs &a, const CUtensorMap &tq, TileSmem 
 }
 
 // ------------------------------------------------------------- tensor cores
-// The same value in every lane, for the compiler too: what addresses an MMA
-// has to lie in uniform registers, and moving it there costs more than the MMA.
-__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __reduce_max_sync(0xffffffffu, x); }
-
 // One warp per softmax group.  Both go through all stages; of a stage that is
 // the other group's alone it only takes note.
 template <int DP, bool kF16>

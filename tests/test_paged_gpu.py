@@ -273,6 +273,38 @@ def test_fused_projection_strides_and_strided_out():
     b.check()
 
 
+@pytest.mark.parametrize("d,page", [(128, 16), (128, 8), (128, 256), (64, 16), (96, 32)])
+@pytest.mark.parametrize("order", ["4 rows more a page", "8 rows more a page", "24 rows more a page", "pages inside tokens",
+                                   "heads first", "one page", "a wider row"])
+def test_cache_strides(order, d, page):
+    """Caches whose pages lie whole groups of eight rows apart, or not."""
+    import torch
+    lens, fresh = ([page - 1], [page - 2]) if order == "one page" else ([700, 90, 2 * page], [300, 1, 40])
+    b = Batch(lens=lens, fresh=fresh, hq=4, hkv=2, d=d, page=page, seed=d + page, spare=0 if order == "one page" else 3,
+              qscale=2.0)
+    for name in ("kc", "vc"):
+        c = getattr(b, name)
+        n = c.shape[0]
+        if "more" in order:
+            w = torch.full((n, page + int(order.split()[0]), 2, d), float("nan"), device="cuda", dtype=c.dtype)[:, :page]
+        elif order == "pages inside tokens":
+            w = torch.empty((page, n, 2, d), device="cuda", dtype=c.dtype).transpose(0, 1)
+        elif order == "heads first":
+            w = torch.empty((2, n, page, d), device="cuda", dtype=c.dtype).permute(1, 2, 0, 3)
+        elif order == "a wider row":
+            w = torch.full((n, page, 3, d + 8), float("nan"), device="cuda", dtype=c.dtype)[:, :, 1:, :d]
+        else:
+            w = torch.empty_like(c)
+        w.copy_(c)
+        setattr(b, name, w)
+    b.poison()
+    for mask in ("causal", "full", "window 300"):
+        b.out.fill_(7.0)
+        b.lse.fill_(7.0)
+        b.run(**MASKS[mask])
+        b.check(**MASKS[mask])
+
+
 def test_tables_inside_a_wider_array():
     import torch
     b = Batch([300, 45, 700], [130, 1, 5], 8, 2, 64, 16, seed=8)
