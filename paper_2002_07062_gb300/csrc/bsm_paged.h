@@ -73,8 +73,9 @@ int launch_paged_tables(const PagedTablesArgs &a, int n_sm, void *stream);
 int launch_paged_write(const PagedWriteArgs &a, int n_sm, void *stream);
 int launch_paged_rows(const PagedArgs &a, bool f16, int grid, void *stream);
 // maps: CUtensorMaps of q, k, v (host); box: rows of one copy of k and v (below 8:
-// those maps are not used)
-int launch_paged_tiles(const void *maps, const PagedArgs &a, bool f16, int box, void *stream);
+// those maps are not used); per_page: 0, or whole rows a copy, with the maps' fourth
+// dimension counting groups of eight rows, per_page of them from page to page
+int launch_paged_tiles(const void *maps, const PagedArgs &a, bool f16, int box, int per_page, void *stream);
 int paged_set_smem_limit();
 
 }  // namespace bsm

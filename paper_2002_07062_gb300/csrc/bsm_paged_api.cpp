@@ -141,8 +141,8 @@ PagedLayout paged_layout(int n_sm)
 bool paged_map(CUtensorMap *m, bool f16, const void *base, int rank, const int64_t *dims, const int64_t *strides,
                const int *box)
 {
-    cuuint64_t d[4], s[3];
-    cuuint32_t b[4], e[4] = {1u, 1u, 1u, 1u};
+    cuuint64_t d[5], s[4];
+    cuuint32_t b[5], e[5] = {1u, 1u, 1u, 1u, 1u};
     for (int i = 0; i < rank; ++i) {
         d[i] = static_cast<cuuint64_t>(dims[i]);
         b[i] = static_cast<cuuint32_t>(box[i]);
@@ -376,16 +376,33 @@ int paged_attention(const bsm_paged_desc *d, bsm_stream_t stream)
     split_group(b, kPagedTileRows / 2);
     b.tok = 2 * (kPagedTileRows / 2 / b.sub);
     CUtensorMap maps[3] = {};
+    int per_page = 0;
     bool tiles = static_cast<int64_t>(d->max_new) * a.group > kPagedRowTile;
     if (tiles) {
         const int64_t qd[3] = {d->head_dim, d->heads_q, d->n_tokens}, qst[3] = {1, d->q_stride_head, d->q_stride_token};
         const int qb[3] = {64, b.sub, b.tok / 2};
+        // Whole rows of 128 columns a copy, the 64-column halves of eight rows side by
+        // side: a map of groups of eight rows, where pages lie whole groups apart.
+        const int64_t token = d->kv_stride_token, each = d->page_size / 8;
+        if (box >= 8 && d->head_dim == 128 && token > 0) {
+            const int64_t apart = d->n_pages == 1 ? each : d->kv_stride_page / (8 * token);
+            const int64_t groups = (d->n_pages - 1) * apart + each;
+            if (apart >= each && (d->n_pages == 1 || d->kv_stride_page == apart * 8 * token) &&
+                groups + apart <= INT32_MAX) {
+                const int64_t gd[5] = {64, 8, 2, groups, d->heads_kv};
+                const int64_t gst[5] = {1, token, 64, 8 * token, d->kv_stride_head};
+                const int gb[5] = {64, 8, 2, box / 8, 1};
+                if (paged_map(&maps[1], f16, d->k_cache, 5, gd, gst, gb) &&
+                    paged_map(&maps[2], f16, d->v_cache, 5, gd, gst, gb))
+                    per_page = static_cast<int>(apart);
+            }
+        }
         const int64_t kd[4] = {d->head_dim, d->page_size, d->heads_kv, d->n_pages};
         const int64_t kst[4] = {1, d->kv_stride_token, d->kv_stride_head, d->kv_stride_page};
         const int kb[4] = {64, box, 1, 1};
         tiles = paged_map(&maps[0], f16, d->q, 3, qd, qst, qb);
-        if (box >= 8 && !(paged_map(&maps[1], f16, d->k_cache, 4, kd, kst, kb) &&
-                          paged_map(&maps[2], f16, d->v_cache, 4, kd, kst, kb)))
+        if (box >= 8 && !per_page &&
+            !(paged_map(&maps[1], f16, d->k_cache, 4, kd, kst, kb) && paged_map(&maps[2], f16, d->v_cache, 4, kd, kst, kb)))
             box = 0;
     }
     if (tiles) {
@@ -394,7 +411,7 @@ int paged_attention(const bsm_paged_desc *d, bsm_stream_t stream)
         b.part_o = reinterpret_cast<float *>(ws + lay.tiles_o);
         b.part_ml = reinterpret_cast<float *>(ws + lay.tiles_ml);
         b.join = reinterpret_cast<PagedJoin *>(ws + lay.tiles_join);
-        if (int e = launch_paged_tiles(maps, b, f16, box, stream))
+        if (int e = launch_paged_tiles(maps, b, f16, box, per_page, stream))
             return record_cuda_error(e, "paged attention tile launch");
         return BSM_OK;
     }

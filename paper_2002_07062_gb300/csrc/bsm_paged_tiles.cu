@@ -74,6 +74,19 @@ template <int DP> struct TileShape {
     static constexpr int kSmem = 1024 + kTileHeader + kStore + kQBytes + kStages * kStageBytes;
 };
 
+// How the stages are filled: by TMA, the two halves of the columns apart (a copy each);
+// by TMA with whole rows a copy, the halves of eight rows side by side; row by row.
+// (An instance of the kernel each: descriptors stay constants, and the last one's
+// registers cost the others nothing.)  Whole rows halve the copies: two prompts of 8192
+// tokens in pages of 16 take 757 us, 770 with halves apart; in pages of 8 876 and 926;
+// a chunk of 2048 over 6100 keys in pages of 64 161 and 164.
+enum Fill { kByHalves, kByRows, kOddPages };
+
+template <int kFill> struct StageSteps {
+    static constexpr int kHalf = kFill == kByRows ? 1024 : kHalfBytes;  // bytes to the other 64 columns
+    static constexpr int kGroup = kFill == kByRows ? 2048 : 1024;       // to the next eight rows
+};
+
 // What the producer tells the other warps of a piece.
 struct TilePiece {
     int32_t blocks;                     // key steps; 0: no more pieces
@@ -122,13 +135,29 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map
         : "memory");
 }
 
-// Descriptor of a tile whose rows are the reduction dimension and whose
-// columns (64 of them a 128-byte row) are N: groups of 8 rows 1024 bytes apart,
-// the next 64 columns kHalfBytes on; 128-byte swizzle.
-__device__ __forceinline__ uint64_t smem_desc_n(uint32_t addr)
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *map, int32_t c0, int32_t c1, int32_t c2,
+                                            int32_t c3, int32_t c4, uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, "
+        "%5, %6}], [%7];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "r"(bar)
+        : "memory");
+}
+
+// Descriptors of a stage, 128-byte swizzle.  Keys: the columns are the reduction
+// dimension; groups of eight rows kGroup bytes apart.  Values: the rows are, and the
+// columns (64 of them a 128-byte row) are N; the next 64 kHalf bytes on.
+template <int kFill> __device__ __forceinline__ uint64_t stage_desc_k(uint32_t addr)
 {
     const uint64_t a = (addr & 0x3FFFFu) >> 4;
-    return a | (uint64_t(kHalfBytes >> 4) << 16) | (uint64_t(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+    return a | (1ull << 16) | (uint64_t(StageSteps<kFill>::kGroup >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+template <int kFill> __device__ __forceinline__ uint64_t stage_desc_v(uint32_t addr)
+{
+    const uint64_t a = (addr & 0x3FFFFu) >> 4;
+    return a | (uint64_t(StageSteps<kFill>::kHalf >> 4) << 16) | (uint64_t(StageSteps<kFill>::kGroup >> 4) << 32) |
+           (1ull << 46) | (2ull << 61);
 }
 
 // kind::f16, fp32 accumulator, A and B both f16 or both bf16, M = 128.
@@ -241,8 +270,8 @@ __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __reduce_max_sy
 // elected lane.  The warp's instructions bound the small pages: with coordinates the
 // compiler does not know to be uniform, two prompts of 8192 tokens in pages of 16 take
 // 829 us, 770 so; in pages of 8 1106 and 928.
-template <int DP>
-__device__ bool produce(const PagedArgs &a, const CUtensorMap &tk, const CUtensorMap &tv, int box, TileSmem &h,
+template <int DP, int kFill>
+__device__ bool produce(const PagedArgs &a, const CUtensorMap &tk, const CUtensorMap &tv, int box, int per_page, TileSmem &h,
                         unsigned char *stages, PagedWalk<kKeys> &walk, const PagedCut &cut, int32_t unit, uint32_t &loaded)
 {
     using Shape = TileShape<DP>;
@@ -302,15 +331,20 @@ __device__ bool produce(const PagedArgs &a, const CUtensorMap &tk, const CUtenso
             if (elect_one())
                 bar_expect(hold ? &h.tail : &h.full[pos.s], static_cast<uint32_t>(__popc(have) * box * 128 * Shape::kHalves));
             __syncwarp();
+            const int32_t at = kFill == kByRows ? page * per_page + in / 8 : page;  // (of this lane's piece)
             for (int c = 0; c < boxes; ++c) {
                 if (!((have >> c) & 1u))
                     continue;
-                const int32_t pg = static_cast<int32_t>(uniform(lane == c ? page : 0));
-                const int32_t rw = static_cast<int32_t>(uniform(lane == c ? in : 0));
+                const int32_t pg = static_cast<int32_t>(uniform(lane == c ? at : 0));
+                const int32_t rw = kFill == kByRows ? 0 : static_cast<int32_t>(uniform(lane == c ? in : 0));
                 if (elect_one()) {
+                    if (kFill == kByRows) {
+                        tma_load_5d(st + c * box * 256, side ? &tv : &tk, 0, 0, 0, pg, kvh, bar);
+                    } else {
 #pragma unroll
-                    for (int hf = 0; hf < Shape::kHalves; ++hf)
-                        tma_load_4d(st + hf * kHalfBytes + c * box * 128, side ? &tv : &tk, hf * 64, rw, kvh, pg, bar);
+                        for (int hf = 0; hf < Shape::kHalves; ++hf)
+                            tma_load_4d(st + hf * kHalfBytes + c * box * 128, side ? &tv : &tk, hf * 64, rw, kvh, pg, bar);
+                    }
                 }
                 __syncwarp();
             }
@@ -324,7 +358,8 @@ __device__ bool produce(const PagedArgs &a, const CUtensorMap &tk, const CUtenso
 #pragma unroll
                         for (int hf = 0; hf < Shape::kHalves; ++hf)
                             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(
-                                             st + hf * kHalfBytes + r * 128 + (x & 7) * 16),
+                                             st + hf * StageSteps<kFill>::kHalf + (r >> 3) * StageSteps<kFill>::kGroup +
+                                             (r & 7) * 128 + (x & 7) * 16),
                                          "r"(0)
                                          : "memory");
                     }
@@ -544,10 +579,11 @@ __device__ bool produce_odd(const PagedArgs &a, const CUtensorMap &tq, TileSmem 
 // ------------------------------------------------------------- tensor cores
 // One warp per softmax group.  Both go through all stages; of a stage that is
 // the other group's alone it only takes note.
-template <int DP, bool kF16>
+template <int DP, bool kF16, int kFill>
 __device__ bool multiply(TileSmem &h, unsigned char *qs, unsigned char *stages, uint32_t tmem_, uint32_t sub_)
 {
     using Shape = TileShape<DP>;
+    using Steps = StageSteps<kFill>;
     constexpr uint32_t kScores = tile_idesc<kF16, kKeys, false>(), kOut = tile_idesc<kF16, DP, true>();
     const uint32_t tmem = uniform(tmem_);
     const int sub = static_cast<int>(uniform(sub_));
@@ -577,10 +613,10 @@ __device__ bool multiply(TileSmem &h, unsigned char *qs, unsigned char *stages, 
         __syncwarp();
         const uint32_t to_s = tmem + s_col(sub), to_o = tmem + o_col(sub);
         auto scores = [&](int32_t i, int stage) {
-            const uint64_t kd = smem_desc(stages + stage * Shape::kStageBytes);
+            const uint64_t kd = stage_desc_k<kFill>(saddr(stages) + static_cast<uint32_t>(stage * Shape::kStageBytes));
 #pragma unroll
             for (int d = 0; d < DP / 16; ++d)
-                mma_ss(to_s, ad + (d / 4) * (kQHalf >> 4) + (d % 4) * 2, kd + (d / 4) * (kHalfBytes >> 4) + (d % 4) * 2,
+                mma_ss(to_s, ad + (d / 4) * (kQHalf >> 4) + (d % 4) * 2, kd + (d / 4) * (Steps::kHalf >> 4) + (d % 4) * 2,
                        kScores, d != 0);
             mma_commit(&h.sfull[sub]);
             mma_commit(&h.empty[stage]);
@@ -619,7 +655,7 @@ __device__ bool multiply(TileSmem &h, unsigned char *qs, unsigned char *stages, 
                 if (j == from && !warp_wait(&h.ofree[sub], (used++ & 1u) ^ 1u, &h.abort_flag))
                     return false;
             }
-            const uint64_t vd = smem_desc_n(saddr(stages) + static_cast<uint32_t>(vs * Shape::kStageBytes));
+            const uint64_t vd = stage_desc_v<kFill>(saddr(stages) + static_cast<uint32_t>(vs * Shape::kStageBytes));
             const int ks = pos.s;
             if (more) {
                 if (!warp_wait(&h.full[ks], pos.ph, &h.abort_flag))
@@ -641,7 +677,7 @@ __device__ bool multiply(TileSmem &h, unsigned char *qs, unsigned char *stages, 
                 if (mine) {
 #pragma unroll
                     for (int k = 0; k < kKeys / 16; ++k)
-                        mma_ts(to_o, to_s + k * 8, vd + k * (2048 >> 4), kOut, j != from || k != 0);
+                        mma_ts(to_o, to_s + k * 8, vd + k * (2 * Steps::kGroup >> 4), kOut, j != from || k != 0);
                     if (j == last)
                         mma_commit(&h.olast[sub]);
                     mma_commit(&h.empty[vs]);
@@ -931,12 +967,10 @@ __device__ bool softmax(const PagedArgs &a, TileSmem &h, unsigned char *store, u
     }
 }
 
-// kOdd: pages that the TMA copies cannot take (an instance of its own, so that its
-// registers cost the other nothing).
-template <int DP, bool kF16, bool kOdd>
+template <int DP, bool kF16, int kFill>
 __global__ void __launch_bounds__(kTileThreads, 1)
     paged_tiles(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk,
-                const __grid_constant__ CUtensorMap tv, const PagedArgs a, const int box)
+                const __grid_constant__ CUtensorMap tv, const PagedArgs a, const int box, const int per_page)
 {
     using Shape = TileShape<DP>;
     extern __shared__ __align__(1024) unsigned char raw[];
@@ -999,10 +1033,10 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     if (warp == 8) {
         uint32_t loaded = 0;
         uint32_t none = 0;
-        if (kOdd)
+        if (kFill == kOddPages)
             ok = produce_odd<DP>(a, tq, h, qs, stages, walk, cut, unit, 0, none);
         else
-            ok = produce<DP>(a, tk, tv, box, h, stages, walk, cut, unit, loaded);
+            ok = produce<DP, kFill>(a, tk, tv, box, per_page, h, stages, walk, cut, unit, loaded);
         if (!ok) {
             if (elect_one()) {
                 atomicOr(a.status, BSM_DEV_TIMEOUT);
@@ -1011,14 +1045,14 @@ __global__ void __launch_bounds__(kTileThreads, 1)
             __syncwarp();
         }
         // copies in flight land before the CTA leaves
-        if (kOdd)
+        if (kFill == kOddPages)
             asm volatile("cp.async.wait_all;" ::: "memory");
         const uint32_t S = Shape::kStages;
         for (uint32_t j = loaded > S ? loaded - S : 0u; j < loaded; ++j)
             warp_drain(h, &h.full[j % S], (j / S) & 1u);
     } else if (warp == 11) {
         uint32_t loaded = 0;
-        if (kOdd)
+        if (kFill == kOddPages)
             ok = produce_odd<DP>(a, tq, h, qs, stages, walk, cut, unit, 1, loaded);
         else
             ok = produce_q<DP>(a, tq, h, qs, loaded);
@@ -1029,12 +1063,12 @@ __global__ void __launch_bounds__(kTileThreads, 1)
             }
             __syncwarp();
         }
-        if (kOdd)
+        if (kFill == kOddPages)
             asm volatile("cp.async.wait_all;" ::: "memory");
         if (loaded)
             warp_drain(h, &h.qfull, (loaded - 1) & 1u);
     } else if (warp >= 9) {
-        ok = multiply<DP, kF16>(h, qs, stages, tmem, warp - 9);
+        ok = multiply<DP, kF16, kFill>(h, qs, stages, tmem, warp - 9);
         if (elect_one()) {
             if (!ok) {
                 atomicOr(a.status, BSM_DEV_TIMEOUT);
@@ -1177,10 +1211,14 @@ template <bool kF16, int kCols, int kShares> int launch_join(const PagedArgs &a,
 }
 
 template <int DP, bool kF16>
-int launch(const CUtensorMap *m, const PagedArgs &a, int box, int64_t tiles, cudaStream_t st)
+int launch(const CUtensorMap *m, const PagedArgs &a, int box, int per_page, int64_t tiles, cudaStream_t st)
 {
-    const auto kernel = box >= 8 ? paged_tiles<DP, kF16, false> : paged_tiles<DP, kF16, true>;
-    if (int e = launch_early(kernel, dim3(a.units), kTileThreads, TileShape<DP>::kSmem, st, m[0], m[1], m[2], a, box))
+    // (halves side by side: heads of 128 only)
+    const auto kernel = box < 8 ? paged_tiles<DP, kF16, kOddPages>
+                        : DP == 128 && per_page ? paged_tiles<DP, kF16, DP == 128 ? kByRows : kByHalves>
+                                                : paged_tiles<DP, kF16, kByHalves>;
+    if (int e = launch_early(kernel, dim3(a.units), kTileThreads, TileShape<DP>::kSmem, st, m[0], m[1], m[2], a, box,
+                             per_page))
         return e;
     // Tiles of ten parts and more: more CTAs, four threads to a row's parts.  16 tokens
     // over 100 thousand keys, one key/value head: 41.6 us in all, 112 the other way; 64
@@ -1190,15 +1228,15 @@ int launch(const CUtensorMap *m, const PagedArgs &a, int box, int64_t tiles, cud
 
 }  // namespace
 
-int launch_paged_tiles(const void *maps, const PagedArgs &a, bool f16, int box, void *stream)
+int launch_paged_tiles(const void *maps, const PagedArgs &a, bool f16, int box, int per_page, void *stream)
 {
     const CUtensorMap *m = static_cast<const CUtensorMap *>(maps);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     // tiles of the batch, each request having one at least
     const int64_t tiles = static_cast<int64_t>(a.n > a.n_tokens / a.tok ? a.n : a.n_tokens / a.tok) * a.heads_kv * a.subs;
     if (a.d <= 64)
-        return f16 ? launch<64, true>(m, a, box, tiles, st) : launch<64, false>(m, a, box, tiles, st);
-    return f16 ? launch<128, true>(m, a, box, tiles, st) : launch<128, false>(m, a, box, tiles, st);
+        return f16 ? launch<64, true>(m, a, box, per_page, tiles, st) : launch<64, false>(m, a, box, per_page, tiles, st);
+    return f16 ? launch<128, true>(m, a, box, per_page, tiles, st) : launch<128, false>(m, a, box, per_page, tiles, st);
 }
 
 int paged_tiles_set_smem()
@@ -1208,14 +1246,16 @@ int paged_tiles_set_smem()
         if (!e)
             e = static_cast<int>(cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
     };
-    set(reinterpret_cast<const void *>(&paged_tiles<64, false, false>), TileShape<64>::kSmem);
-    set(reinterpret_cast<const void *>(&paged_tiles<64, true, false>), TileShape<64>::kSmem);
-    set(reinterpret_cast<const void *>(&paged_tiles<128, false, false>), TileShape<128>::kSmem);
-    set(reinterpret_cast<const void *>(&paged_tiles<128, true, false>), TileShape<128>::kSmem);
-    set(reinterpret_cast<const void *>(&paged_tiles<64, false, true>), TileShape<64>::kSmem);
-    set(reinterpret_cast<const void *>(&paged_tiles<64, true, true>), TileShape<64>::kSmem);
-    set(reinterpret_cast<const void *>(&paged_tiles<128, false, true>), TileShape<128>::kSmem);
-    set(reinterpret_cast<const void *>(&paged_tiles<128, true, true>), TileShape<128>::kSmem);
+    set(reinterpret_cast<const void *>(&paged_tiles<64, false, kByHalves>), TileShape<64>::kSmem);
+    set(reinterpret_cast<const void *>(&paged_tiles<64, true, kByHalves>), TileShape<64>::kSmem);
+    set(reinterpret_cast<const void *>(&paged_tiles<64, false, kOddPages>), TileShape<64>::kSmem);
+    set(reinterpret_cast<const void *>(&paged_tiles<64, true, kOddPages>), TileShape<64>::kSmem);
+    set(reinterpret_cast<const void *>(&paged_tiles<128, false, kByHalves>), TileShape<128>::kSmem);
+    set(reinterpret_cast<const void *>(&paged_tiles<128, true, kByHalves>), TileShape<128>::kSmem);
+    set(reinterpret_cast<const void *>(&paged_tiles<128, false, kByRows>), TileShape<128>::kSmem);
+    set(reinterpret_cast<const void *>(&paged_tiles<128, true, kByRows>), TileShape<128>::kSmem);
+    set(reinterpret_cast<const void *>(&paged_tiles<128, false, kOddPages>), TileShape<128>::kSmem);
+    set(reinterpret_cast<const void *>(&paged_tiles<128, true, kOddPages>), TileShape<128>::kSmem);
     return e;
 }
 
