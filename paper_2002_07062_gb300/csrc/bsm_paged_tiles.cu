@@ -27,8 +27,8 @@
 // same quotient, and 2^8 is far from the range of fp32 sums), so nearly all
 // steps skip that pass.
 //
-// GB300: two prompts of 8192 tokens, 32/8 heads of 128: 722 us (1.52 PFLOP/s; a
-// plain bf16 product 1.95), tensor pipe 69 % active on 2048 tokens over 6100;
+// GB300: two prompts of 8192 tokens, 32/8 heads of 128: 714 us (1.54 PFLOP/s; a
+// plain bf16 product 1.95), tensor pipe 71 % active on 2048 tokens over 6100;
 // 4 tokens over 131 thousand keys, 1.02 GB: 172 us.  Without the softmax the first
 // runs in 548 us.  Tried and slower for it: steps of 64 keys with two score
 // buffers a block, which never wait for scores (963 us: a product of 128 x 64 x 16
@@ -443,8 +443,8 @@ __device__ bool produce_q(const PagedArgs &a, const CUtensorMap &tq, TileSmem &h
 // a stage is handed on when its copies have landed, at the latest before this warp
 // waits for anything (so no one waits for a stage that only this warp could hand
 // on).  Warp 8 fills the stages of keys, warp 11 those of values: bound by their
-// instructions.  Two prompts of 8192 tokens in pages of 1: 1.67 ms (2.18 with one
-// warp, 12.1 on the row kernel; in pages of 64, by TMA, 0.76).
+// instructions.  Two prompts of 8192 tokens in pages of 1: 1.66 ms (2.18 with one
+// warp, 12.1 on the row kernel; in pages of 64, by TMA, 0.72).
 struct Pending {
     int count = 0;                      // stages not handed on yet
     int at[3];                          // which, the oldest first
