@@ -371,8 +371,10 @@ int bsm_paged_write(const bsm_paged_write_desc *d, bsm_stream_t stream);
  *             alone until its work is done; its contents need no preparation.
  * The result depends on the batch (the keys are split by what the whole batch
  * needs) and is the same every time for the same batch.
- * Lengths, offsets and page ids that lie outside the buffers are cut or skipped
- * and set BSM_DEV_BOUNDS; nothing outside the buffers is touched.
+ * Lengths and offsets that lie outside the buffers are cut to them; a key whose
+ * page id lies outside the cache (-1 where bsm_paged_tables ran out of pages)
+ * takes no part, as if it were masked.  Both set BSM_DEV_BOUNDS; nothing outside
+ * the buffers is touched.
  * Pointers 16-byte aligned, strides multiples of 8 (else BSM_ERR_MISALIGNED).
  * out, lse and workspace must not overlap each other or an input.
  * Errors: BSM_ERR_INVALID_ARG, BSM_ERR_MISALIGNED, BSM_ERR_UNSUPPORTED,

@@ -65,6 +65,24 @@ struct PagedRange {
     int32_t lo, hi;
 };
 
+// Its tokens and keys.
+__device__ __forceinline__ PagedSeq paged_request(const PagedArgs &a, int32_t r, bool report)
+{
+    PagedSeq s;
+    const int32_t raw0 = a.starts[r], raw1 = a.starts[r + 1], rawL = a.lengths[r];
+    const int64_t cap = static_cast<int64_t>(a.width) * a.page;
+    const int32_t most = cap < kPagedMostKeys ? static_cast<int32_t>(cap) : kPagedMostKeys;
+    const int32_t t0 = raw0 < 0 ? 0 : raw0 > a.n_tokens ? a.n_tokens : raw0;
+    const int32_t t1 = raw1 < t0 ? t0 : raw1 > a.n_tokens ? a.n_tokens : raw1;
+    const int32_t L = rawL < 0 ? 0 : rawL > most ? most : rawL;
+    if (report && (t0 != raw0 || t1 != raw1 || L != rawL))
+        atomicOr(a.status, BSM_DEV_BOUNDS);
+    s.t0 = t0;
+    s.m = t1 - t0;
+    s.L = L;
+    return s;
+}
+
 template <int kStep> struct PagedLine {
     const PagedArgs &a;
     __device__ explicit PagedLine(const PagedArgs &args) : a(args) {}
@@ -125,18 +143,7 @@ template <int kStep> struct PagedLine {
     // known >= 0: the request's steps, all head groups
     __device__ PagedSeq seq(int32_t r, bool report, int64_t known = -1) const
     {
-        PagedSeq s;
-        const int32_t raw0 = a.starts[r], raw1 = a.starts[r + 1], rawL = a.lengths[r];
-        const int64_t cap = static_cast<int64_t>(a.width) * a.page;
-        const int32_t most = cap < kPagedMostKeys ? static_cast<int32_t>(cap) : kPagedMostKeys;
-        const int32_t t0 = raw0 < 0 ? 0 : raw0 > a.n_tokens ? a.n_tokens : raw0;
-        const int32_t t1 = raw1 < t0 ? t0 : raw1 > a.n_tokens ? a.n_tokens : raw1;
-        const int32_t L = rawL < 0 ? 0 : rawL > most ? most : rawL;
-        if (report && (t0 != raw0 || t1 != raw1 || L != rawL))
-            atomicOr(a.status, BSM_DEV_BOUNDS);
-        s.t0 = t0;
-        s.m = t1 - t0;
-        s.L = L;
+        PagedSeq s = paged_request(a, r, report);
         if (s.m == 0)
             return s;
         s.tiles = (s.m + a.tok - 1) / a.tok;

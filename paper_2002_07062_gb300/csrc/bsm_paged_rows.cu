@@ -188,9 +188,14 @@ __global__ void __launch_bounds__(kRowThreads, 1) paged_rows(const PagedArgs a)
     };
     int64_t off = -1;
     int32_t issued = 0;
+    uint32_t there[kRowStages];         // of the stages in order: the keys of the tile that have a page
     advance();
     off = key_offset();
     auto issue = [&]() {
+#pragma unroll
+        for (int i = 0; i + 1 < kRowStages; ++i)
+            there[i] = there[i + 1];
+        there[kRowStages - 1] = __ballot_sync(0xffffffffu, off >= 0);
         if (issued < total) {
             const uint32_t st = stages + (issued % kRowStages) * kStageBytes;
             constexpr int kRowsAtOnce = 32 / kChunks;
@@ -270,6 +275,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) paged_rows(const PagedArgs a)
                     mma16<kF16>(s[0], q[k], b[0], b[1]);
                     mma16<kF16>(s[1], q[k], b[2], b[3]);
                 }
+                const uint32_t have = there[0] >> (sb * 16 + (lane & 3) * 2);
                 uint32_t pa[4];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
@@ -279,7 +285,8 @@ __global__ void __launch_bounds__(kRowThreads, 1) paged_rows(const PagedArgs a)
                     for (int j = 0; j < 4; ++j) {
                         const int32_t key = key0 + (j >> 1) * 8 + (lane & 3) * 2 + (j & 1);
                         const float v = s[j >> 1][i * 2 + (j & 1)] * a.scale_log2;
-                        x[j] = key >= lo[i] && key < hi[i] ? v : -INFINITY;
+                        const bool in = key >= lo[i] && key < hi[i] && (have >> ((j >> 1) * 8 + (j & 1)) & 1u);
+                        x[j] = in ? v : -INFINITY;
                         top = fmaxf(top, x[j]);
                     }
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));

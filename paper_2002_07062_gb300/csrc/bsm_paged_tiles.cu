@@ -43,6 +43,7 @@
 
 #include <cstdint>
 
+#include "bsm_paged_again.h"
 #include "bsm_paged_dev.h"
 #include "bsm_tc.h"
 
@@ -274,7 +275,8 @@ __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __reduce_max_sy
 // 829 us, 770 so; in pages of 8 1106 and 928.
 template <int DP, int kFill>
 __device__ bool produce(const PagedArgs &a, const CUtensorMap &tk, const CUtensorMap &tv, int box, int per_page, TileSmem &h,
-                        unsigned char *stages, PagedWalk<kKeys> &walk, const PagedCut &cut, int32_t unit, uint32_t &loaded)
+                        unsigned char *stages, PagedWalk<kKeys> &walk, const PagedCut &cut, int32_t unit, uint32_t &loaded,
+                        PagedSeen &seen)
 {
     using Shape = TileShape<DP>;
     const int lane = threadIdx.x & 31;
@@ -296,6 +298,7 @@ __device__ bool produce(const PagedArgs &a, const CUtensorMap &tk, const CUtenso
         }
         const PagedSeq &s = walk.s;
         const TilePiece t = tile_piece(a, s, p, cut, unit);
+        seen.note(p);
         if (elect_one()) {
             h.piece[npc % kPieces] = t;
             bar_arrive(&h.pcfull[npc % kPieces]);
@@ -303,7 +306,7 @@ __device__ bool produce(const PagedArgs &a, const CUtensorMap &tk, const CUtenso
         __syncwarp();
         const int32_t kvh = static_cast<int32_t>(uniform(t.kvh)), keep = t.keep;
         const int64_t row = p.r * a.table_stride;
-        // page of this lane's piece of block b: (page, row in it); n_pages: not there, filled with zeros
+        // page of this lane's piece of block b: (page, row in it); n_pages: not there, filled with zeros (see the join)
         auto page_of = [&](int32_t b, int32_t &in) -> int32_t {
             const int32_t key = b * kKeys + lane * box;
             if (lane >= boxes || key >= s.L || key + box <= keep)
@@ -319,6 +322,7 @@ __device__ bool produce(const PagedArgs &a, const CUtensorMap &tk, const CUtenso
         };
         // one stage: keys (side 0) or values of step i, whose pieces lie in the pages given
         auto load = [&](int32_t i, int side, int32_t page, int32_t in) -> bool {
+            seen.gone |= page == a.n_pages;
             const uint32_t have = __ballot_sync(0xffffffffu, page >= 0);
             // rows of the values that belong to no key of the request: zeros (0 times whatever
             // lies there may be NaN); their scores are masked
@@ -469,7 +473,7 @@ template <int kLeft> __device__ __forceinline__ void hand_on(TileSmem &h, Pendin
 
 template <int DP>
 __device__ bool produce_odd(const PagedArgs &a, const CUtensorMap &tq, TileSmem &h, unsigned char *qs, unsigned char *stages,
-                            PagedWalk<kKeys> &walk, const PagedCut &cut, int32_t unit, int side, uint32_t &queries)
+                            PagedWalk<kKeys> &walk, const PagedCut &cut, int32_t unit, int side, uint32_t &queries, PagedSeen &seen)
 {
     using Shape = TileShape<DP>;
     constexpr int S = Shape::kStages;
@@ -483,8 +487,10 @@ __device__ bool produce_odd(const PagedArgs &a, const CUtensorMap &tq, TileSmem 
             PagedPiece p{};
             const bool more = walk.next(p);
             t.blocks = 0;
-            if (more)
+            if (more) {
                 t = tile_piece(a, walk.s, p, cut, unit);
+                seen.note(p);
+            }
             hand_on<0>(h, q);
             if (!warp_wait(&h.pcempty[npc % kPieces], ((npc / kPieces) & 1u) ^ 1u, &h.abort_flag))
                 return false;
@@ -520,10 +526,12 @@ __device__ bool produce_odd(const PagedArgs &a, const CUtensorMap &tq, TileSmem 
                 off[x] = -1;
                 if (i < t.blocks && key >= t.keep && key < t.len) {
                     const int32_t e = key / a.page, page = a.tables[row0 + e];
-                    if (page >= 0 && page < a.n_pages)
+                    const bool in = page >= 0 && page < a.n_pages;
+                    if (in)
                         off[x] = 2 * (page * a.kv_page + (key - e * a.page) * a.kv_token + head);
                     else
                         atomicOr(a.status, BSM_DEV_BOUNDS);
+                    seen.gone |= !in;
                 }
             }
         };
@@ -957,19 +965,18 @@ __device__ bool softmax(const PagedArgs &a, TileSmem &h, unsigned char *store, u
         if (t.slot < 0) {
             if (live && a.lse)
                 a.lse[token * a.heads_q + t.head + hh] =
-                    sum == 0.0f ? -INFINITY : (base + log2f(sum)) * 0.6931471805599453f;
+                    sum == 0.0f ? -INFINITY : (base + log2f(sum)) * kPagedLn2;
         } else {
             *reinterpret_cast<float2 *>(a.part_ml + (static_cast<int64_t>(t.slot) * kPagedTileRows + srow) * 2) =
                 make_float2(base, sum);
         }
         if (t.join > 0 && sub == 0 && threadIdx.x == 0) {
-            PagedJoin j{};
+            PagedJoin &j = a.join[unit];                // (its flags are others')
             j.token = t.token;
             j.head = t.head;
             j.tokens = t.tokens;
             j.heads = t.heads;
             j.count = t.join;
-            a.join[unit] = j;
         }
     }
 }
@@ -1012,8 +1019,10 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     }
     grid_dependency_wait();
     grid_launch_dependents();
-    if (threadIdx.x == 0)
+    if (threadIdx.x == 0) {
         a.join[unit].count = 0;
+        a.join[unit].flags = 0;
+    }
     // the line of work; its prefix lies where the stages will be
     PagedPrefix<kPrefixThreads> &prefix = *reinterpret_cast<PagedPrefix<kPrefixThreads> *>(stages);
     const PagedLine<kKeys> line(a);
@@ -1040,10 +1049,13 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     if (warp == 8) {
         uint32_t loaded = 0;
         uint32_t none = 0;
+        PagedSeen seen;
         if (kFill == kOddPages)
-            ok = produce_odd<DP>(a, tq, h, qs, stages, walk, cut, unit, 0, none);
+            ok = produce_odd<DP>(a, tq, h, qs, stages, walk, cut, unit, 0, none, seen);
         else
-            ok = produce<DP, kFill>(a, tk, tv, box, per_page, h, stages, walk, cut, unit, loaded);
+            ok = produce<DP, kFill>(a, tk, tv, box, per_page, h, stages, walk, cut, unit, loaded, seen);
+        seen.store(a.join[unit]);
+        __syncwarp();
         if (!ok) {
             if (elect_one()) {
                 atomicOr(a.status, BSM_DEV_TIMEOUT);
@@ -1059,8 +1071,9 @@ __global__ void __launch_bounds__(kTileThreads, 1)
             warp_drain(h, &h.full[j % S], (j / S) & 1u);
     } else if (warp == 11) {
         uint32_t loaded = 0;
+        PagedSeen seen;                 // (the warp of the keys tells)
         if (kFill == kOddPages)
-            ok = produce_odd<DP>(a, tq, h, qs, stages, walk, cut, unit, 1, loaded);
+            ok = produce_odd<DP>(a, tq, h, qs, stages, walk, cut, unit, 1, loaded, seen);
         else
             ok = produce_q<DP>(a, tq, h, qs, loaded);
         if (!ok) {
@@ -1107,15 +1120,9 @@ __global__ void __launch_bounds__(kTileThreads, 1)
 // Joins the parts of every cut tile (the sums of the row kernel's RowSum): a
 // thread a row and kCols columns, kShares threads a row where there are many parts
 // (few tiles), each with its share of them.
-template <bool kF16, int kCols, int kShares> __global__ void __launch_bounds__(128 * kShares) paged_tile_join(const PagedArgs a)
+template <bool kF16, int kCols, int kShares>
+__device__ __forceinline__ void tile_join(const PagedArgs &a, const PagedJoin &j, int unit, int sub, float *other)
 {
-    __shared__ float other[kShares > 1 ? (kShares - 1) * 128 * (kCols + 2) : 1];
-    const int unit = blockIdx.x, sub = blockIdx.y;
-    grid_dependency_wait();
-    grid_launch_dependents();
-    const PagedJoin j = a.join[unit];
-    if (j.count <= 0)
-        return;
     const int half_tok = a.tok / 2, lane_row = threadIdx.x & 127, share = threadIdx.x >> 7;
     const int tt = lane_row / a.sub, h = lane_row - tt * a.sub, tok = sub * half_tok + tt;
     const bool live = tt < half_tok && tok < j.tokens && h < j.heads;
@@ -1208,7 +1215,33 @@ template <bool kF16, int kCols, int kShares> __global__ void __launch_bounds__(1
             *reinterpret_cast<uint4 *>(out + col * 2) = w;
     }
     if (a.lse && blockIdx.z == 0)
-        a.lse[token * a.heads_q + j.head + h] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+        a.lse[token * a.heads_q + j.head + h] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kPagedLn2;
+}
+
+// The join, then what the units' flags ask for: rows that see a key without a page once more.
+// (CTAs an SM: with what the compiler takes by itself the join's loads go through spilled
+// addresses; 2 tokens over 131 thousand keys 179 us, 170 so.)
+template <bool kF16, int kCols, int kShares>
+__global__ void __launch_bounds__(128 * kShares, kShares > 1 ? 2 : 5) paged_tile_join(const PagedArgs a)
+{
+    __shared__ float other[kShares > 1 ? (kShares - 1) * 128 * (kCols + 2) : 1];
+    const int unit = blockIdx.x, sub = blockIdx.y;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const PagedJoin j = a.join[unit];
+    if (j.count > 0)
+        tile_join<kF16, kCols, kShares>(a, j, unit, sub, other);
+    bool parts = false;                                 // a flag of any unit with a part of the cut tile
+    for (int i = threadIdx.x; i < j.count; i += 128 * kShares)
+        parts |= a.join[unit + i].flags != 0;
+    parts = __syncthreads_or(parts);
+    if (parts || j.flags) {
+        constexpr int kWarps = 4 * kShares;
+        const int warp = threadIdx.x >> 5, half_tok = a.tok / 2;
+        paged_unit_again<kF16>(a, j, j.flags != 0, parts, (blockIdx.z * gridDim.y + sub) * kWarps + warp,
+                               gridDim.z * gridDim.y * kWarps, blockIdx.z * kCols, (blockIdx.z + 1) * kCols,
+                               [&](int32_t t, int32_t h) { return t / half_tok == sub && (t * a.sub + h) % kWarps == warp; });
+    }
 }
 
 template <bool kF16, int kCols, int kShares> int launch_join(const PagedArgs &a, cudaStream_t st)

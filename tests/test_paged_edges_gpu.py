@@ -1,0 +1,164 @@
+"""Paged attention where a key must take no part: pages that are not there, keys
+a mask hides whose values are not finite, values near the end of the type's
+range; and pages that several requests share.
+
+The reference is the definition in 64 bits, the sum over the visible keys alone
+(no product with a weight of 0).  Tolerances are those derived in
+test_paged_gpu.py; infinities have to be equal and NaN has to meet NaN.
+"""
+import numpy as np
+import pytest
+
+from paper_2002_07062_gb300 import bsm
+from test_paged_gpu import Batch, MASKS, _types
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def setup():
+    import torch
+    import __graft_entry__ as g
+    g.build()
+    torch.cuda.set_device(0)
+    bsm.bsm_device_status_clear()
+
+
+def exact(b, causal=True, window=0):
+    """out, lse, sum_j p_j |v_j| and the largest scale * sum_d |q_d k_d| of every row."""
+    import torch
+    T, hq, d = b.q.shape
+    g, P = hq // b.hkv, b.page
+    f64 = dict(dtype=torch.float64, device="cuda")
+    out, mass = torch.zeros((T, hq, d), **f64), torch.zeros((T, hq, d), **f64)
+    lse, size = torch.full((T, hq), -float("inf"), **f64), torch.zeros((T, hq), **f64)
+    for r, L in enumerate(int(x) for x in b.lens):
+        t0, t1 = int(b.starts[r]), int(b.starts[r + 1])
+        if t0 == t1 or L == 0:
+            continue
+        ids = torch.from_numpy(np.array(b.tables[r][:-(-L // P)], np.int64)).cuda()
+        there = (ids >= 0) & (ids < b.kc.shape[0])
+        ids = torch.where(there, ids, 0)
+        k, v = (c[ids].reshape(-1, b.hkv, d)[:L].double() for c in (b.kc, b.vc))
+        there = there.repeat_interleave(P)[:L]
+        k, v = (torch.where(there[:, None, None], z, 0.0) for z in (k, v))
+        key = torch.arange(L, device="cuda")
+        pos = L - (t1 - t0) + torch.arange(t1 - t0, device="cuda")
+        see = there[None, :].expand(t1 - t0, L)
+        if causal:
+            see = see & (key[None, :] <= pos[:, None])
+            if window:
+                see = see & (key[None, :] > pos[:, None] - window)
+        for h in range(hq):
+            x = torch.where(see, b.q[t0:t1, h].double() @ k[:, h // g].t() * b.scale, -float("inf"))
+            top = x.amax(1, keepdim=True)
+            top = torch.where(top == -float("inf"), 0.0, top)
+            e = torch.exp(x - top)
+            s = e.sum(1, keepdim=True)
+            p = e / torch.where(s == 0, 1.0, s)
+            vh = v[:, h // g]
+            good = torch.where(torch.isfinite(vh), vh, 0.0)
+            o = p @ good
+            for j in (~torch.isfinite(vh)).any(1).nonzero().view(-1).tolist():
+                o += torch.where(see[:, j, None] & ~torch.isfinite(vh[j]), vh[j], 0.0)
+            out[t0:t1, h], mass[t0:t1, h] = o, p @ good.abs()
+            lse[t0:t1, h] = (top + torch.log(s))[:, 0]
+            kf = torch.nan_to_num(k[:, h // g], 0.0, 0.0, 0.0)
+            size[t0:t1, h] = (b.q[t0:t1, h].double().abs() @ kf.abs().t() * b.scale).amax(1)
+    return out, lse, mass, size
+
+
+def check(b, causal=True, window=0):
+    import torch
+    out, lse, mass, size = exact(b, causal, window)
+    _, u, tiny = _types()[b.dtype]
+    e = b.d * 2.0 ** -24 * size + 2.0 ** -20 * (1 + size)
+    bound = (u + 2 * e[..., None]) * mass + u * out.abs() + tiny
+    got = b.out.double()
+    ok = (torch.isnan(out) & torch.isnan(got)) | (out == got) | ((got - out).abs() <= bound) & torch.isfinite(out)
+    assert ok.all(), (int((~ok).sum()), (~ok).nonzero()[:4].tolist(), out[~ok][:4].tolist(), got[~ok][:4].tolist())
+    ls = b.lse.double()
+    ok = (torch.isnan(lse) & torch.isnan(ls)) | (lse == ls) | ((ls - lse).abs() <= 2 * e + 2.0 ** -22 * lse.abs())
+    assert ok.all(), (int((~ok).sum()), (~ok).nonzero()[:4].tolist(), lse[~ok][:4].tolist(), ls[~ok][:4].tolist())
+
+
+def run(b, hint, causal=True, window=0, status=0):
+    """One call with the given hint (None: the true one) into outputs filled with 7; the status word after it."""
+    import torch
+    b.out.fill_(7.0)
+    b.lse.fill_(7.0)
+    b.scale = b.d ** -0.5
+    most = int(b.fresh.max(initial=0))
+    ws = torch.full((bsm.bsm_paged_workspace_bytes(b.hq, b.hkv, b.d, most),), 255, dtype=torch.uint8, device="cuda")
+    bsm.bsm_paged_attention(b.q, b.kc, b.vc, b.out, *b.dev(), most if hint is None else hint, b.scale, ws,
+                            flags=bsm.FLAG_CAUSAL if causal else 0, window=window, lse=b.lse)
+    torch.cuda.synchronize()
+    got = bsm.bsm_device_status()
+    bsm.bsm_device_status_clear()
+    assert got == status
+
+
+HINTS = [1 << 20, 0]        # the tile kernel, the row kernel
+
+
+GONE = {
+    "whole rows a copy": dict(lens=[700, 300, 90, 513], fresh=[130, 300, 1, 3], hq=8, hkv=2, d=128, page=16),
+    "halves apart": dict(lens=[700, 300, 90, 513], fresh=[130, 300, 1, 3], hq=8, hkv=2, d=64, page=16),
+    "halves apart, f16": dict(lens=[500, 300, 90, 400], fresh=[130, 300, 1, 3], hq=6, hkv=2, d=80, page=32, dtype="f16"),
+    "large pages": dict(lens=[1700, 900, 300, 513], fresh=[130, 300, 1, 3], hq=4, hkv=1, d=128, page=256),
+    "odd pages": dict(lens=[300, 200, 90, 213], fresh=[130, 200, 1, 3], hq=4, hkv=2, d=96, page=3),
+    "pages of 1": dict(lens=[300, 200, 90, 213], fresh=[130, 200, 1, 3], hq=4, hkv=2, d=128, page=1, dtype="f16"),
+    "long": dict(lens=[20000, 300, 9000, 4000], fresh=[2, 40, 1, 1], hq=8, hkv=1, d=128, page=16),
+}
+
+
+@pytest.mark.parametrize("hint", HINTS)
+@pytest.mark.parametrize("mask", ["causal", "full", "window 300"])
+@pytest.mark.parametrize("name", GONE)
+def test_keys_on_missing_pages_take_no_part(name, mask, hint):
+    """Page ids outside the cache, as a table has them where pages ran out: their keys have no weight, whatever the
+    scores of the others; a request without any page gets zeros and -inf; the others' answers are the same bits."""
+    import torch
+    b = Batch(**GONE[name], seed=len(name))
+    # scores of the keys that are there far below 0, the score of a key of zeros
+    b.q.copy_(-b.q.abs())
+    b.kc.copy_(b.kc.abs())
+    b.poison()
+    run(b, hint, **MASKS[mask])
+    whole, lse = b.out.clone(), b.lse.clone()
+    need = -(-b.lens // b.page)
+    b.tables = b.tables.copy()
+    b.tables[0, [0, need[0] // 2]] = [b.kc.shape[0], -1]
+    b.tables[0, need[0] - 1:need[0]] = 1 << 30
+    b.tables[2, :need[2]] = -1
+    run(b, hint, status=bsm.DEV_BOUNDS, **MASKS[mask])
+    check(b, **MASKS[mask])
+    for r in (1, 3):
+        rows = slice(int(b.starts[r]), int(b.starts[r + 1]))
+        assert torch.equal(whole[rows].view(torch.int16), b.out[rows].view(torch.int16))
+        assert torch.equal(lse[rows], b.lse[rows])
+    rows = slice(int(b.starts[2]), int(b.starts[3]))
+    assert not b.out[rows].any() and bool((b.lse[rows] == -float("inf")).all())
+
+
+def test_pages_that_ran_out():
+    """The step of a server whose pool is empty: tables writes -1, attention goes over the keys that have a page."""
+    import torch
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")
+    b = Batch([40, 90, 33], [8, 50, 1], 8, 2, 128, 16, seed=1)
+    tab, st, ln = i32(b.tables), i32([0] * 4), i32([0] * 3)
+    tab[0, 2:], tab[1, 3:], tab[2, 2:] = -7, -7, -7
+    n = b.T
+    slots, pos, own = torch.zeros(n, dtype=torch.int64, device="cuda"), i32([0] * n), i32([0] * n)
+    info = torch.zeros(4, dtype=torch.int64, device="cuda")
+    free = i32([int(b.tables[0, 2]), int(b.tables[1, 3])])
+    bsm.bsm_paged_tables(i32(b.lens - b.fresh), i32(b.fresh), free, 16, tab, st, ln, slots, pos, own, info)
+    assert info.tolist() == [59, 2, 3, bsm.PAGED_PAGES]
+    k, v = torch.randn(n, 2, 128, device="cuda").bfloat16(), torch.randn(n, 2, 128, device="cuda").bfloat16()
+    bsm.bsm_paged_write(k, v, b.kc, b.vc, slots)
+    b.tables = tab.cpu().numpy()
+    for hint in HINTS:
+        run(b, hint, status=bsm.DEV_BOUNDS)
+        check(b)
+
+
