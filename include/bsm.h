@@ -351,10 +351,9 @@ int bsm_paged_write(const bsm_paged_write_desc *d, bsm_stream_t stream);
  *     out = sum_j exp(s_j) v_j / sum_j exp(s_j),  lse = log sum_j exp(s_j)
  * A token that sees no key (an empty request, a position below 0) gets zeros
  * and lse = -inf.  Rows of q past starts[n_requests] are not read and theirs of
- * out not written.  A masked key of the request takes part with weight 0, so an
- * infinity or a NaN among its values may show; keys that no token of the call
- * may see (past lengths[r], left of every window) are never used, whatever their
- * pages hold.
+ * out not written.  A key that a token does not see takes no part in its output,
+ * whatever it holds (outputs that an infinity or NaN of a hidden key got into on
+ * the way are computed once more, slowly).
  *   dtype     BF16 or F16 for q, caches and out (BSM_ERR_UNSUPPORTED: F32);
  *             products accumulate in fp32, the softmax is fp32, probabilities
  *             are rounded to dtype for the second product.
@@ -363,7 +362,8 @@ int bsm_paged_write(const bsm_paged_write_desc *d, bsm_stream_t stream);
  *   scale     > 0 and finite; window >= 0, > 0 only with BSM_FLAG_CAUSAL.
  *   lse       n_tokens x heads_q fp32, or null.
  *   max_new   the most new tokens of any request, as the host knows it.  A hint:
- *             it selects kernels; a wrong one costs time, not the answer.
+ *             it selects kernels; a wrong one costs time and may round
+ *             otherwise, the answer is the same.
  *   page_size any; multiples of 16 are fastest (with more than 16 rows, new tokens
  *             times heads_q / heads_kv, pages that are no multiple of 8 cost about
  *             twice the time).

@@ -59,12 +59,13 @@ struct PagedArgs {
 struct PagedJoin {
     int32_t token, head, tokens, heads;             // first token, first query head, tokens, heads of the tile
     int32_t count;                                  // 0: nothing to join
-    // of the whole unit (the tile kernel's): the first tile that it starts, the tiles that it has whole from there
+    // of the whole unit: the first tile that it starts, the tiles that it has whole from there
     uint32_t flags;                                 // kPaged*
     int32_t r, head0, tile, whole;
     int32_t pad[2];
 };
 constexpr uint32_t kPagedGone = 1;                  // it met a key whose page is not there
+constexpr uint32_t kPagedOdd = 2;                   // an output that it stored is not finite
 
 constexpr int32_t kPagedMostKeys = INT32_MAX - 255; // of a request: a step past them is still a 32-bit number
 constexpr int kPagedWarps = 8;                      // of the row kernel

@@ -1,13 +1,16 @@
 // bsm_paged_again.h -- rows of paged attention computed once more, from the
-// definition, where the tile kernel's answer does not hold.
+// definition, where the kernels' answer does not hold.
 //
 //   o = sum p_j v_j / sum p_j over the visible keys whose pages are there, in fp32
 //
-// The tile kernel's copies fill a key whose page is not there with zeros, and its
-// products cannot leave a single key out, so such a key would enter with score 0.
-// Its producer notes that it met one and which tiles it went through; the join launch,
-// which follows anyway, takes their rows that see one again: a warp a row, four
-// columns a lane, 32 keys at a time.  Where all pages are there it reads a flag a unit.
+// A product of a block of rows with a block of keys cannot leave a key out for some of
+// the rows: a masked key has weight 0 there, and 0 times an infinity or NaN among its
+// values is NaN.  And the tile kernel's copies fill a key whose page is not there with
+// zeros, so that it would enter with score 0.  The kernels note that a row of theirs is
+// not finite, or that they met such a page, and which tiles they went through; the join
+// launch, which follows anyway, looks at those tiles' rows and computes again what a hidden
+// key got into: a warp a row, four columns a lane, 32 keys at a time.  Where all is finite
+// and there it reads a flag a unit.
 // (Masking such keys in the tile kernel's own softmax cost every call 1 to 4 %.  The code is
 // kept short because its size costs too: with the walk along the work line in it, 80 KB
 // instead of 23, a chunk of 2048 tokens over 6100 keys took 163 us instead of 156.)
@@ -50,6 +53,14 @@ struct PagedSeen {
     }
 };
 
+// The kernels add up their outputs to see whether all are finite (a sum that overflows has their
+// rows looked at for nothing).
+__device__ __forceinline__ bool pg_finite(float x) { return fabsf(x) < INFINITY; }
+__device__ __forceinline__ float pg_total(const float4 &v) { return (v.x + v.y) + (v.z + v.w); }
+
+// Whether any of four is an infinity or NaN.
+__device__ __forceinline__ bool pg_odd(const float4 &v) { return v.x * 0.0f + v.y * 0.0f + v.z * 0.0f + v.w * 0.0f != 0.0f; }
+
 // Four 16-bit elements as fp32.
 template <bool kF16> __device__ __forceinline__ float4 pg_load4(const void *base, int64_t at)
 {
@@ -63,87 +74,101 @@ template <bool kF16> __device__ __forceinline__ float4 pg_load4(const void *base
                        __uint_as_float(w.y & 0xFFFF0000u));
 }
 
-__device__ __forceinline__ float pg_warp_sum(float x)
-{
-#pragma unroll 1
-    for (int w = 16; w; w >>= 1)
-        x += __shfl_xor_sync(0xffffffffu, x, w);
-    return x;
-}
+// A row's keys, and those that took part in its tile's products.
+struct PagedAgain {
+    int32_t r, pos;                     // request, position of the token
+    int32_t k0, k1;                     // keys of the tile's steps
+    int32_t len;
+    bool gone;                          // some page may not be there
+};
 
-// A token at position pos of request r and one query head: columns [c0, c1) of its output (and
-// lse where c0 is 0), by the whole warp.  Nothing is done where every key that it sees is there.
+// One token (by its place in q) and query head: columns [c0, c1) of its output (and lse where c0 is 0),
+// by the whole warp, if it sees a key that is not there, or if its output is not finite and a key that it
+// does not see has values that are not.
 template <bool kF16>
-__device__ __forceinline__ void paged_row_again(const PagedArgs &a, int32_t r, int32_t len, int32_t pos, int64_t token,
-                                                int32_t head, int32_t c0, int32_t c1)
+__device__ __forceinline__ void paged_row_again(const PagedArgs &a, const PagedAgain &w, int64_t token, int32_t head, int32_t c0,
+                                                int32_t c1)
 {
     const int lane = threadIdx.x & 31, col = lane * 4;
-    const bool live = col < a.d;
-    const int32_t hi = !a.causal ? len : pos < 0 ? 0 : pos + 1;
-    const int32_t lo = a.window && pos >= a.window ? pos - a.window + 1 : 0;
-    const int64_t kvh = head / a.group * a.kv_head;
-    const float4 q = live ? pg_load4<kF16>(a.q, token * a.q_token + head * a.q_head + col) : make_float4(0, 0, 0, 0);
+    const bool live = col < a.d, mine = live && col >= c0 && col < c1;
+    const int32_t hi = !a.causal ? w.len : w.pos < 0 ? 0 : w.pos + 1;
+    const int32_t lo = a.window && w.pos >= a.window ? w.pos - a.window + 1 : 0;
+    const int64_t kvh = head / a.group * a.kv_head, q = token * a.q_token + head * a.q_head;
+    const int64_t to = token * a.out_token + head * a.out_head + col;
+    const float4 zero = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    const bool odd = __any_sync(0xffffffffu, mine && pg_odd(pg_load4<kF16>(a.out, mine ? to : 0)));
+    if (!odd && !w.gone)
+        return;
     bool again = false;
     float top = -INFINITY, sum = 0.0f;
-    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    // the first pass looks for a key that is not there, the second computes
+    float4 acc = zero;
+    // the first pass looks at the values of hidden keys (0 times them) and for pages, the second computes
 #pragma unroll 1
     for (int pass = 0; pass < 2; ++pass) {
+        const int32_t from = pass ? lo : w.k0, end = pass ? hi : w.k1;
 #pragma unroll 1
-        for (int32_t base = lo; base < hi; base += 32) {
+        for (int32_t base = from; base < end; base += 32) {
+            if (!pass && !w.gone && base >= lo && base < hi - 32) {
+                base += (hi - base) / 32 * 32 - 32;     // (visible keys)
+                continue;
+            }
             const int32_t key = base + lane, e = key / a.page;
+            const bool seen = key >= lo && key < hi;
             int64_t off = -1;           // of this lane's key
-            if (key < hi) {
-                const int32_t page = a.tables[r * a.table_stride + e];
+            if (key < end) {
+                const int32_t page = a.tables[w.r * a.table_stride + e];
                 if (page >= 0 && page < a.n_pages)
                     off = page * a.kv_page + (key - e * a.page) * a.kv_token + kvh;
             }
-            if (pass == 0) {
-                again = __any_sync(0xffffffffu, key < hi && off < 0);
-                if (again)
+            float p = 0.0f;
+            if (pass) {
+                float x = 0.0f;         // its score
+#pragma unroll 2
+                for (int32_t c = 0; c < a.d; c += 4) {
+                    const float4 qv = pg_load4<kF16>(a.q, q + c), k = off >= 0 ? pg_load4<kF16>(a.k, off + c) : zero;
+                    x += qv.x * k.x + qv.y * k.y + qv.z * k.z + qv.w * k.w;
+                }
+                x = off >= 0 ? x * a.scale_log2 : -INFINITY;
+                float most = fmaxf(x, top);
+#pragma unroll 1
+                for (int s = 16; s; s >>= 1)
+                    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, s));
+                const float f = most == top ? 1.0f : pg_exp2(top - most);
+                top = most;
+                p = pg_exp2(x - (top == -INFINITY ? 0.0f : top));
+                float all = p;
+#pragma unroll 1
+                for (int s = 16; s; s >>= 1)
+                    all += __shfl_xor_sync(0xffffffffu, all, s);
+                sum = sum * f + all;
+                acc = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
+                if (sum != sum)         // NaN from here on
                     break;
-                continue;
+            } else {
+                again |= __any_sync(0xffffffffu, seen && off < 0);
+                off = seen || !odd ? -1 : off;
             }
-            float x = -INFINITY;        // its score
-#pragma unroll 1
-            for (int c = 0; c < 32; ++c) {
-                const int64_t o = __shfl_sync(0xffffffffu, off, c);
-                if (o < 0)
-                    continue;
-                const float4 k = live ? pg_load4<kF16>(a.k, o + col) : make_float4(0, 0, 0, 0);
-                const float dot = pg_warp_sum(q.x * k.x + q.y * k.y + q.z * k.z + q.w * k.w);
-                x = lane == c ? dot * a.scale_log2 : x;
-            }
-            float most = fmaxf(x, top);
-#pragma unroll 1
-            for (int w = 16; w; w >>= 1)
-                most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, w));
-            const float f = most == top ? 1.0f : pg_exp2(top - most);
-            top = most;
-            const float p = pg_exp2(x - (top == -INFINITY ? 0.0f : top));
-            sum = sum * f + pg_warp_sum(p);
-            acc = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
-#pragma unroll 1
+#pragma unroll 2
             for (int c = 0; c < 32; ++c) {
                 const int64_t o = __shfl_sync(0xffffffffu, off, c);
                 const float pc = __shfl_sync(0xffffffffu, p, c);
-                if (o < 0 || !live)
-                    continue;
-                const float4 v = pg_load4<kF16>(a.v, o + col);
+                const float4 v = o >= 0 && live ? pg_load4<kF16>(a.v, o + col) : zero;
                 acc = make_float4(acc.x + pc * v.x, acc.y + pc * v.y, acc.z + pc * v.z, acc.w + pc * v.w);
             }
-            if (sum != sum)             // NaN from here on
-                break;
         }
-        if (!again)
-            return;
+        if (!pass) {
+            again |= __any_sync(0xffffffffu, pg_odd(acc));
+            acc = zero;
+            if (!again)
+                return;
+        }
     }
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    if (col >= c0 && col < c1 && live) {
-        uint2 w;
-        w.x = pg_pack<kF16>(acc.x * inv, acc.y * inv);
-        w.y = pg_pack<kF16>(acc.z * inv, acc.w * inv);
-        *reinterpret_cast<uint2 *>(static_cast<unsigned char *>(a.out) + 2 * (token * a.out_token + head * a.out_head + col)) = w;
+    if (mine) {
+        uint2 o;
+        o.x = pg_pack<kF16>(acc.x * inv, acc.y * inv);
+        o.y = pg_pack<kF16>(acc.z * inv, acc.w * inv);
+        *reinterpret_cast<uint2 *>(static_cast<unsigned char *>(a.out) + 2 * to) = o;
     }
     if (a.lse && c0 == 0 && lane == 0)
         a.lse[token * a.heads_q + head] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kPagedLn2;
@@ -154,8 +179,8 @@ __device__ __forceinline__ void paged_row_again(const PagedArgs &a, int32_t r, i
 // and others end: columns [c0, c1) of the rows mine(token of the tile, head of the tile), after the
 // join has stored them.
 template <bool kF16, class Mine>
-__device__ __forceinline__ void paged_unit_again(const PagedArgs &a, const PagedJoin &j, bool whole, bool cut, int32_t first,
-                                                 int32_t stride, int32_t c0, int32_t c1, const Mine &mine)
+__device__ __forceinline__ void paged_unit_again(const PagedArgs &a, const PagedJoin &j, bool whole, bool cut, bool gone,
+                                                 int32_t first, int32_t stride, int32_t c0, int32_t c1, const Mine &mine)
 {
     int32_t r = j.r, group = j.head0, tile = j.tile;
 #pragma unroll 1
@@ -177,6 +202,15 @@ __device__ __forceinline__ void paged_unit_again(const PagedArgs &a, const Paged
         const int32_t kvh = group / a.subs, sub = group - kvh * a.subs;
         const int32_t tokens = s.m - i0 < a.tok ? s.m - i0 : a.tok;
         const int32_t heads = a.group - sub * a.sub < a.sub ? a.group - sub * a.sub : a.sub;
+        const int32_t pos = s.L - s.m + i0, past = pos + tokens < 0 ? 0 : pos + tokens;
+        PagedAgain w;
+        w.r = r;
+        w.len = s.L;
+        w.gone = gone;
+        // (the longer steps of the two kernels)
+        w.k0 = a.window && pos >= a.window ? (pos - a.window + 1) / kPagedTileKeys * kPagedTileKeys : 0;
+        w.k1 = a.causal ? (past + kPagedTileKeys - 1) / kPagedTileKeys * kPagedTileKeys : s.L;
+        w.k1 = w.k1 < s.L ? w.k1 : s.L;
         int32_t at = first;             // rows until this warp's next
 #pragma unroll 1
         for (int32_t t = 0; t < tokens; ++t)
@@ -185,8 +219,9 @@ __device__ __forceinline__ void paged_unit_again(const PagedArgs &a, const Paged
                 if (last ? !mine(t, h) : at != 0)
                     continue;
                 at += stride;
-                paged_row_again<kF16>(a, r, s.L, s.L - s.m + i0 + t, s.t0 + i0 + t, kvh * a.group + sub * a.sub + h,
-                                      last ? c0 : 0, last ? c1 : kPagedMaxDim);
+                w.pos = pos + t;
+                paged_row_again<kF16>(a, w, s.t0 + i0 + t, kvh * a.group + sub * a.sub + h, last ? c0 : 0,
+                                      last ? c1 : kPagedMaxDim);
             }
     }
 }

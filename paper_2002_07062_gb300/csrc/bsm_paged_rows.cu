@@ -16,6 +16,7 @@
 
 #include <cstdint>
 
+#include "bsm_paged_again.h"
 #include "bsm_paged_dev.h"
 #include "bsm_tc.h"
 
@@ -79,8 +80,6 @@ template <bool kF16> __device__ __forceinline__ void mma16(float *d, const uint3
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-constexpr float kLn2 = 0.6931471805599453f;
-
 // The sum over the parts of a row: with M the largest of their references m_i,
 // o = sum 2^(m_i - M) o_i, l = sum 2^(m_i - M) l_i.  A lane has four columns.
 struct RowSum {
@@ -95,18 +94,20 @@ struct RowSum {
         acc.z += f * v.z;
         acc.w += f * v.w;
     }
-    template <bool kF16> __device__ __forceinline__ void store(const PagedArgs &a, int64_t token, int32_t head, int lane) const
+    template <bool kF16>
+    __device__ __forceinline__ void store(const PagedArgs &a, int64_t token, int32_t head, int lane, float &odd) const
     {
         const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
         if (lane * 4 < a.d) {
             uint2 w;
             w.x = pg_pack<kF16>(acc.x * inv, acc.y * inv);
             w.y = pg_pack<kF16>(acc.z * inv, acc.w * inv);
+            odd += pg_total(acc);
             *reinterpret_cast<uint2 *>(static_cast<unsigned char *>(a.out) +
                                        2 * (token * a.out_token + head * a.out_head + lane * 4)) = w;
         }
         if (a.lse && lane == 0)
-            a.lse[token * a.heads_q + head] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
+            a.lse[token * a.heads_q + head] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kPagedLn2;
     }
 };
 
@@ -145,8 +146,10 @@ __global__ void __launch_bounds__(kRowThreads, 1) paged_rows(const PagedArgs a)
     const int32_t unit = warp * gridDim.x + blockIdx.x;
     grid_dependency_wait();
     grid_launch_dependents();
-    if (lane == 0)
+    if (lane == 0) {
         a.join[unit].count = 0;
+        a.join[unit].flags = 0;
+    }
     const PagedLine<kKeys> line(a);
     paged_prefix<kKeys, kRowThreads>(line, sm.prefix, blockIdx.x == 0);
     const int64_t W = sm.prefix.pre[kRowThreads];
@@ -226,8 +229,11 @@ __global__ void __launch_bounds__(kRowThreads, 1) paged_rows(const PagedArgs a)
 
     // ---- one piece after another
     PagedPiece p{};
+    PagedSeen passed;
+    float odd = 0.0f;                   // sum of the outputs: not finite if one of them is not
     int32_t done = 0;
     while (walk.next(p)) {
+        passed.note(p);
         const RowTile t = row_tile(a, walk.s, p);
         const int32_t rows = t.tokens * a.sub;
         // this lane's rows: lane / 4 and lane / 4 + 8
@@ -343,11 +349,14 @@ __global__ void __launch_bounds__(kRowThreads, 1) paged_rows(const PagedArgs a)
                                                              2 * ((t.token + tt) * a.out_token + (t.head + h) * a.out_head));
 #pragma unroll
                 for (int n = 0; n < DP / 8; ++n)
-                    if (n * 8 < a.d)
-                        dst[n * 4 + (lane & 3)] = pg_pack<kF16>(o[n][2 * i] * inv, o[n][2 * i + 1] * inv);
+                    if (n * 8 < a.d) {
+                        const float x = o[n][2 * i] * inv, y = o[n][2 * i + 1] * inv;
+                        odd += x + y;
+                        dst[n * 4 + (lane & 3)] = pg_pack<kF16>(x, y);
+                    }
                 if (a.lse && (lane & 3) == 0)
                     a.lse[static_cast<int64_t>(t.token + tt) * a.heads_q + t.head + h] =
-                        sum == 0.0f ? -INFINITY : (ref + log2f(sum)) * kLn2;
+                        sum == 0.0f ? -INFINITY : (ref + log2f(sum)) * kPagedLn2;
             } else {
 #pragma unroll
                 for (int n = 0; n < DP / 8; ++n)
@@ -358,16 +367,18 @@ __global__ void __launch_bounds__(kRowThreads, 1) paged_rows(const PagedArgs a)
             }
         }
         if (p.starts && !p.ends && lane == 0) {
-            PagedJoin j{};
+            PagedJoin &j = a.join[unit];
             j.token = t.token;
             j.head = t.head;
             j.tokens = t.tokens;
             j.heads = t.heads;
             j.count = cut.owner(p.tile_end - 1) - unit + 1;
-            a.join[unit] = j;
         }
     }
     cp_wait<0>();
+    passed.store(a.join[unit]);
+    if (!pg_finite(odd))
+        atomicOr(&a.join[unit].flags, kPagedOdd);
 }
 
 // Joins the parts of every cut tile, in unit order.  CTA (x, y) has units 8 x ..
@@ -381,7 +392,9 @@ __global__ void __launch_bounds__(kRowThreads, 1) paged_rows(const PagedArgs a)
 constexpr int kJoinWarps = 8;
 constexpr int kJoinAlone = 16;          // parts a warp joins alone
 
-template <bool kF16> __global__ void __launch_bounds__(kJoinWarps * 32) paged_join(const PagedArgs a)
+// (Five CTAs an SM, the registers of the join itself: with what the rows to be computed again
+// would take, three fit, and one token over 2000 keys takes 17.1 us instead of 14.6.)
+template <bool kF16> __global__ void __launch_bounds__(kJoinWarps * 32, 5) paged_join(const PagedArgs a)
 {
     __shared__ PagedJoin join[kJoinWarps];
     __shared__ float4 part[kJoinWarps][32];
@@ -408,11 +421,12 @@ template <bool kF16> __global__ void __launch_bounds__(kJoinWarps * 32) paged_jo
                   *reinterpret_cast<const float4 *>(a.part_o + at(i) * kPagedMaxDim + lane * 4));
         return r;
     };
+    float odd = 0.0f, odd_many = 0.0f;  // of this warp's rows; of those of tiles in many parts
     for (int row = blockIdx.y; row < kPagedRowTile; row += gridDim.y) {
         const int tt = row / a.sub, h = row - tt * a.sub;
         const PagedJoin &j = join[warp];
         if (j.count > 0 && j.count <= kJoinAlone && tt < j.tokens && h < j.heads)
-            sum(mine, row, 0, j.count).template store<kF16>(a, j.token + tt, j.head + h, lane);
+            sum(mine, row, 0, j.count).template store<kF16>(a, j.token + tt, j.head + h, lane, odd);
         for (int w = 0; w < kJoinWarps; ++w) {
             const PagedJoin &c = join[w];
             if (c.count <= kJoinAlone || tt >= c.tokens || h >= c.heads)
@@ -428,10 +442,20 @@ template <bool kF16> __global__ void __launch_bounds__(kJoinWarps * 32) paged_jo
                     r.top = fmaxf(r.top, part_ml[i].x);
                 for (int i = 0; i < kJoinWarps; ++i)
                     r.add(part_ml[i], part[i][lane]);
-                r.store<kF16>(a, c.token + tt, c.head + h, lane);
+                r.store<kF16>(a, c.token + tt, c.head + h, lane, odd_many);
             }
             __syncthreads();
         }
+    }
+    // rows once more, of this warp's unit (its cut tile after all have stored)
+    const PagedJoin &j = join[warp];
+    if (__syncthreads_or(!pg_finite(odd + odd_many) || j.flags)) {
+        const bool many = __syncthreads_or(!pg_finite(odd_many)) && j.count > kJoinAlone;
+        const bool cut = many || __any_sync(0xffffffffu, !pg_finite(odd));
+        const int32_t y = blockIdx.y, ny = gridDim.y;
+        if (cut || j.flags)
+            paged_unit_again<kF16>(a, j, j.flags != 0, cut, false, y, ny, 0, kPagedMaxDim,
+                                   [&](int32_t t, int32_t h) { return (t * a.sub + h) % ny == y; });
     }
 }
 

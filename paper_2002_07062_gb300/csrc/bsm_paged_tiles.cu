@@ -113,6 +113,7 @@ struct TileSmem {
     int64_t where[2][kKeys];            // of odd pages: byte offset of a step's rows (-1: not read)
     uint32_t tmem_base;
     int32_t abort_flag, no_abort;       // (the second stays 0)
+    int32_t odd;                        // an output that was stored is not finite
 };
 static_assert(sizeof(TileSmem) <= kTileHeader, "tile header");
 
@@ -908,6 +909,7 @@ __device__ bool softmax(const PagedArgs &a, TileSmem &h, unsigned char *store, u
             f0 *= inv;
             f1 *= inv;
         }
+        uint64_t odd[2] = {0, 0};                       // sums of the outputs: not finite if one of them is not
 #pragma unroll 1
         for (int c = 0; c < DP / 32 && !idle; ++c) {
             uint32_t o[32];
@@ -925,6 +927,9 @@ __device__ bool softmax(const PagedArgs &a, TileSmem &h, unsigned char *store, u
                     f[i] = fmaf(__uint_as_float(o[i]), f1, f[i]);
             }
             if (t.slot < 0) {
+#pragma unroll
+                for (int i = 0; i < 32; i += 2)
+                    odd[(i >> 1) & 1] = add2(odd[(i >> 1) & 1], pair(f[i], f[i + 1]));
                 // through shared memory, so that four lanes store 64 bytes of a row (a lane storing
                 // its own row touches 32 lines at once); 16-byte pieces swizzled over the banks
 #pragma unroll
@@ -962,6 +967,10 @@ __device__ bool softmax(const PagedArgs &a, TileSmem &h, unsigned char *store, u
             if (t.dual)
                 bar_arrive(&h.ofree[1]);
         }
+        float odd0, odd1;
+        unpair(add2(odd[0], odd[1]), odd0, odd1);
+        if (live && !pg_finite(odd0 + odd1))
+            *static_cast<volatile int32_t *>(&h.odd) = 1;
         if (t.slot < 0) {
             if (live && a.lse)
                 a.lse[token * a.heads_q + t.head + hh] =
@@ -1014,7 +1023,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
         bar_init(&h.tail, 1);
         bar_init(&h.drain, 2);
         bar_init(&h.xfull, 4);
-        h.abort_flag = h.no_abort = 0;
+        h.abort_flag = h.no_abort = h.odd = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     grid_dependency_wait();
@@ -1111,6 +1120,8 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     }
     tc_fence_before();
     __syncthreads();
+    if (threadIdx.x == 0 && h.odd)
+        atomicOr(&a.join[unit].flags, kPagedOdd);
     if (warp == 9) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTileTmemCols) : "memory");
@@ -1120,8 +1131,9 @@ __global__ void __launch_bounds__(kTileThreads, 1)
 // Joins the parts of every cut tile (the sums of the row kernel's RowSum): a
 // thread a row and kCols columns, kShares threads a row where there are many parts
 // (few tiles), each with its share of them.
+// Whether an output of this thread is not finite comes back.
 template <bool kF16, int kCols, int kShares>
-__device__ __forceinline__ void tile_join(const PagedArgs &a, const PagedJoin &j, int unit, int sub, float *other)
+__device__ __forceinline__ bool tile_join(const PagedArgs &a, const PagedJoin &j, int unit, int sub, float *other)
 {
     const int half_tok = a.tok / 2, lane_row = threadIdx.x & 127, share = threadIdx.x >> 7;
     const int tt = lane_row / a.sub, h = lane_row - tt * a.sub, tok = sub * half_tok + tt;
@@ -1170,7 +1182,7 @@ __device__ __forceinline__ void tile_join(const PagedArgs &a, const PagedJoin &j
         }
         __syncthreads();
         if (share > 0)
-            return;
+            return false;
         float all = top;
         for (int s = 0; s < kShares - 1; ++s)
             all = fmaxf(all, other[(s * (kCols + 2) + kCols + 1) * 128 + lane_row]);
@@ -1199,8 +1211,9 @@ __device__ __forceinline__ void tile_join(const PagedArgs &a, const PagedJoin &j
         top = all;
     }
     if (!live)
-        return;
+        return false;
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    float odd = 0.0f;
     const int64_t token = j.token + tok;
     unsigned char *out = static_cast<unsigned char *>(a.out) + 2 * (token * a.out_token + (j.head + h) * a.out_head);
 #pragma unroll
@@ -1211,16 +1224,18 @@ __device__ __forceinline__ void tile_join(const PagedArgs &a, const PagedJoin &j
         w.y = pg_pack<kF16>(acc[k].z * inv, acc[k].w * inv);
         w.z = pg_pack<kF16>(acc[k + 1].x * inv, acc[k + 1].y * inv);
         w.w = pg_pack<kF16>(acc[k + 1].z * inv, acc[k + 1].w * inv);
+        odd += pg_total(acc[k]) + pg_total(acc[k + 1]);
         if (col < a.d)
             *reinterpret_cast<uint4 *>(out + col * 2) = w;
     }
     if (a.lse && blockIdx.z == 0)
         a.lse[token * a.heads_q + j.head + h] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kPagedLn2;
+    return !pg_finite(odd);
 }
 
-// The join, then what the units' flags ask for: rows that see a key without a page once more.
+// The join, then what the units' flags ask for: rows once more.
 // (CTAs an SM: with what the compiler takes by itself the join's loads go through spilled
-// addresses; 2 tokens over 131 thousand keys 179 us, 170 so.)
+// addresses; 2 x 4 tokens over 131 thousand keys 179 us, 170 so.)
 template <bool kF16, int kCols, int kShares>
 __global__ void __launch_bounds__(128 * kShares, kShares > 1 ? 2 : 5) paged_tile_join(const PagedArgs a)
 {
@@ -1229,16 +1244,17 @@ __global__ void __launch_bounds__(128 * kShares, kShares > 1 ? 2 : 5) paged_tile
     grid_dependency_wait();
     grid_launch_dependents();
     const PagedJoin j = a.join[unit];
-    if (j.count > 0)
-        tile_join<kF16, kCols, kShares>(a, j, unit, sub, other);
-    bool parts = false;                                 // a flag of any unit with a part of the cut tile
+    uint32_t flags = 0;                                 // a page missing in a part of the cut tile; its own rows odd
     for (int i = threadIdx.x; i < j.count; i += 128 * kShares)
-        parts |= a.join[unit + i].flags != 0;
-    parts = __syncthreads_or(parts);
+        flags |= a.join[unit + i].flags & kPagedGone;
+    if (j.count > 0 && tile_join<kF16, kCols, kShares>(a, j, unit, sub, other))
+        flags |= kPagedOdd;
+    const bool parts = __syncthreads_or(flags != 0);
     if (parts || j.flags) {
+        const bool gone = __syncthreads_or((flags | j.flags) & kPagedGone);
         constexpr int kWarps = 4 * kShares;
         const int warp = threadIdx.x >> 5, half_tok = a.tok / 2;
-        paged_unit_again<kF16>(a, j, j.flags != 0, parts, (blockIdx.z * gridDim.y + sub) * kWarps + warp,
+        paged_unit_again<kF16>(a, j, j.flags != 0, parts, gone, (blockIdx.z * gridDim.y + sub) * kWarps + warp,
                                gridDim.z * gridDim.y * kWarps, blockIdx.z * kCols, (blockIdx.z + 1) * kCols,
                                [&](int32_t t, int32_t h) { return t / half_tok == sub && (t * a.sub + h) % kWarps == warp; });
     }

@@ -162,3 +162,54 @@ def test_pages_that_ran_out():
         check(b)
 
 
+BAD = {
+    "chunk": dict(lens=[700, 90], fresh=[300, 1], hq=8, hkv=2, d=128, page=16),
+    "chunk, head size 64, f16": dict(lens=[700, 300], fresh=[300, 300], hq=4, hkv=4, d=64, page=64, dtype="f16"),
+    "chunk, odd pages": dict(lens=[400, 90], fresh=[200, 1], hq=6, hkv=2, d=96, page=5),
+    "a few tokens": dict(lens=[200, 41, 8, 77], fresh=[4, 7, 8, 1], hq=8, hkv=4, d=128, page=16),
+    "a few tokens, head size 40, f16": dict(lens=[200, 41, 8], fresh=[4, 7, 8], hq=2, hkv=2, d=40, page=16, dtype="f16"),
+    "long": dict(lens=[9000], fresh=[700], hq=4, hkv=1, d=128, page=16),
+    "long, a few tokens": dict(lens=[30000, 500], fresh=[6, 3], hq=2, hkv=1, d=128, page=16),
+    "more tokens than keys": dict(lens=[30, 5], fresh=[90, 8], hq=4, hkv=2, d=64, page=16),
+}
+
+
+@pytest.mark.parametrize("hint", HINTS)
+@pytest.mark.parametrize("mask", ["causal", "full", "window 37", "window 300"])
+@pytest.mark.parametrize("name", BAD)
+def test_values_of_hidden_keys_do_not_show(name, mask, hint):
+    """Infinities and NaN among a request's own keys and values, at its last tokens and scattered: they show in the
+    tokens that see them and in no other."""
+    import torch
+    b = Batch(**BAD[name], seed=len(name))
+    rng = np.random.default_rng(len(name) + len(mask))
+    bad = [float("inf"), -float("inf"), float("nan")]
+    for r, (L, m) in enumerate(zip(b.lens.tolist(), b.fresh.tolist())):
+        # the last tokens, whole rows and single columns; some of the tokens before; and a key
+        places = [L - 1, L - 2, L - max(1, m // 2)] + rng.integers(max(0, L - m - 40), L, 3).tolist()
+        for i, at in enumerate(x for x in places if x >= 0):
+            page, row = int(b.tables[r, at // b.page]), at % b.page
+            if i == 0:
+                b.vc[page, row] = float("nan")
+            else:
+                b.vc[page, row, int(rng.integers(b.hkv)), int(rng.integers(b.d))] = bad[i % 3]
+        if m > 1:
+            at = L - 1
+            b.kc[int(b.tables[r, at // b.page]), at % b.page, 0, 0] = float("nan")
+    b.poison()
+    run(b, hint, **MASKS[mask])
+    check(b, **MASKS[mask])
+
+
+@pytest.mark.parametrize("hint", HINTS)
+def test_requests_of_nothing_but_nan(hint):
+    import torch
+    b = Batch([3000, 300, 50], [900, 20, 1], 8, 2, 128, 16, seed=3)
+    for e in range(-(-3000 // 16)):
+        b.kc[int(b.tables[0, e])] = float("nan")
+        b.vc[int(b.tables[0, e])] = float("nan")
+    b.poison()
+    run(b, hint)
+    check(b)
+
+
