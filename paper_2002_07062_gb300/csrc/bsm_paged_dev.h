@@ -353,9 +353,11 @@ __device__ __forceinline__ float pg_exp2(float x)
     return y;
 }
 
-// Probabilities are held as 2^(s - m + shift): f16 would lose those below
-// 2^-14 of the largest, so its exponents start at the top of its range.
-template <bool kF16> __device__ __forceinline__ constexpr float pg_shift(float lag) { return kF16 ? 14.0f - lag : 0.0f; }
+// Probabilities are held as 2^(s - m + shift), s at most `lag` above the reference m: f16 would
+// lose those below 2^-14 of the largest, so its exponents start at the top of its range (its
+// values are below 2^16, far from where fp32 sums end); bf16 has values up to the end of
+// that range, so its probabilities stay at 1 or less.
+template <bool kF16> __device__ __forceinline__ constexpr float pg_shift(float lag) { return (kF16 ? 14.0f : 0.0f) - lag; }
 
 template <bool kF16> __device__ __forceinline__ uint32_t pg_pack(float lo, float hi)
 {

@@ -24,7 +24,7 @@
 // with its own output and reference, and the two are added at the end.
 // Outputs stay in tensor memory; one is rescaled only when a row's maximum has
 // grown by more than 2^8 since its reference was taken (any reference gives the
-// same quotient, and 2^8 is far from the range of fp32 sums), so nearly all
+// same quotient, and probabilities are held 2^8 lower for it), so nearly all
 // steps skip that pass.
 //
 // GB300: two prompts of 8192 tokens, 32/8 heads of 128: 714 us (1.54 PFLOP/s; a

@@ -213,3 +213,26 @@ def test_requests_of_nothing_but_nan(hint):
     check(b)
 
 
+@pytest.mark.parametrize("hint", HINTS)
+@pytest.mark.parametrize("fresh", [1, 200, 300])
+def test_large_values_under_growing_scores(fresh, hint):
+    """A value near the end of bf16's range at a key whose score, in base 2, lies 7.9 above those of all steps before
+    (many requests, so that a CTA has all steps of a tile): its weight is less than 1, and so must be what it is
+    multiplied by."""
+    import torch
+    n = 40
+    b = Batch([700] * n, [fresh] * 2 + [1] * (n - 2), 8, 8, 64, 16, seed=4)
+    b.q.zero_()
+    b.q[..., 0] = 1.0
+    b.kc.zero_()
+    b.vc.normal_()
+    for r in range(n):
+        for at in (300, 450, 600):
+            page = int(b.tables[r, at // 16])
+            b.kc[page, at % 16, :, 0] = 7.9 * 8 / 1.4426950408889634
+            b.vc[page, at % 16, 0, 5] = 3e38 if at == 450 else 1.0
+            b.vc[page, at % 16, 1, 9] = -2e38 if at == 600 else 1.0
+    run(b, hint)
+    check(b)
+
+
