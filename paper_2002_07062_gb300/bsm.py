@@ -394,33 +394,50 @@ def _packer(desc):
 
 _pack_tables, _pack_write, _pack_paged = _packer(PagedTablesDesc), _packer(PagedWriteDesc), _packer(PagedDesc)
 _PAGED_DTYPES = {}      # torch type -> bsm_dtype, filled on first use
-_INT32 = _INT64 = _FLOAT32 = None
+_INT32 = _INT64 = _FLOAT32 = _cuda = None
 
 
 def _paged_types():
-    global _INT32, _INT64, _FLOAT32
+    global _INT32, _INT64, _FLOAT32, _cuda
     import torch
+    _cuda = torch.cuda
     _PAGED_DTYPES.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
     _INT32, _INT64, _FLOAT32 = torch.int32, torch.int64, torch.float32
 
 
-def _strided(t, what: str, ndim: int):
-    """Strides of a CUDA tensor whose last dimension is contiguous (the library
-    checks the others)."""
-    st = t.stride()
-    if t.is_cuda and len(st) == ndim and (st[-1] == 1 or t.shape[-1] <= 1):
-        return st
-    if not t.is_cuda:
+def _device(t, what: str) -> int:
+    """The current device, which the tensor lies on: the library launches there
+    and sees bare addresses, so the call's other tensors have to lie there too."""
+    dev = t.get_device()
+    if dev < 0:
         raise ValueError("%s must be a CUDA tensor (got one on %s)" % (what, t.device))
+    if dev != _cuda.current_device():
+        raise ValueError("%s is on cuda:%d, the current device is cuda:%d" % (what, dev, _cuda.current_device()))
+    return dev
+
+
+def _elsewhere(t, what: str, dev: int):
+    if t.get_device() != dev:
+        raise ValueError("%s is on %s, the call's other tensors on cuda:%d" % (what, t.device, dev))
+
+
+def _strided(t, what: str, ndim: int, dev: int):
+    """Strides of a tensor on device dev whose last dimension is contiguous (the
+    library checks the others)."""
+    st = t.stride()
+    if t.get_device() == dev and len(st) == ndim and (st[-1] == 1 or t.shape[-1] <= 1):
+        return st
+    _elsewhere(t, what, dev)
     if len(st) != ndim:
         raise ValueError("%s must have %d dimensions, not %d" % (what, ndim, len(st)))
     raise ValueError("the last dimension of %s must be contiguous" % what)
 
 
-def _vec(t, what: str, dtype, n: int):
-    """Address of a contiguous CUDA tensor of at least n entries of dtype."""
-    if t.dtype is dtype and t.is_cuda and t.numel() >= n and t.is_contiguous():
+def _vec(t, what: str, dtype, n: int, dev: int):
+    """Address of a contiguous tensor on device dev of at least n entries of dtype."""
+    if t.dtype is dtype and t.get_device() == dev and t.numel() >= n and t.is_contiguous():
         return t.data_ptr()
+    _elsewhere(t, what, dev)
     if t.dtype is not dtype:
         raise ValueError("%s must be %s (got %s)" % (what, dtype, t.dtype))
     return _dptr(t, n * t.element_size(), what)
@@ -440,16 +457,16 @@ def _paged_dtype(first, *others):
     return code
 
 
-def _caches(k_cache, v_cache):
-    st = _strided(k_cache, "k_cache", 4)
-    if v_cache.shape != k_cache.shape or _strided(v_cache, "v_cache", 4) != st:
+def _caches(k_cache, v_cache, dev: int):
+    st = _strided(k_cache, "k_cache", 4, dev)
+    if v_cache.shape != k_cache.shape or _strided(v_cache, "v_cache", 4, dev) != st:
         raise ValueError("k_cache and v_cache must have the same shape and strides")
     return st
 
 
-def _page_tables(tables, n: int):
+def _page_tables(tables, n: int, dev: int):
     """(address, row stride, width) of the page tables of n requests."""
-    st = _strided(tables, "tables", 2)
+    st = _strided(tables, "tables", 2, dev)
     rows, width = tables.shape
     if tables.dtype is not _INT32 or rows < n:
         raise ValueError("tables must be %s, a row for each of %d requests" % (_INT32, n))
@@ -462,12 +479,14 @@ def bsm_paged_tables(cached, fresh, free_pages, page_size: int, tables, starts, 
     tensors: int64 slots and info, int32 the rest; tables [requests, width])."""
     if _INT32 is None:
         _paged_types()
-    n, m = cached.numel(), slots.numel()
-    tab, stride, width = _page_tables(tables, n)
+    n, m, dev = cached.numel(), slots.numel(), _device(cached, "cached")
+    tab, stride, width = _page_tables(tables, n, dev)
     d = _pack_tables(
-        _vec(cached, "cached", _INT32, n), _vec(fresh, "fresh", _INT32, n), _vec(free_pages, "free_pages", _INT32, 0),
-        tab, _vec(starts, "starts", _INT32, n + 1), _vec(lengths, "lengths", _INT32, n), _vec(slots, "slots", _INT64, m),
-        _vec(positions, "positions", _INT32, m), _vec(owners, "owners", _INT32, m), _vec(info, "info", _INT64, 4),
+        _vec(cached, "cached", _INT32, n, dev), _vec(fresh, "fresh", _INT32, n, dev),
+        _vec(free_pages, "free_pages", _INT32, 0, dev), tab, _vec(starts, "starts", _INT32, n + 1, dev),
+        _vec(lengths, "lengths", _INT32, n, dev), _vec(slots, "slots", _INT64, m, dev),
+        _vec(positions, "positions", _INT32, m, dev), _vec(owners, "owners", _INT32, m, dev),
+        _vec(info, "info", _INT64, 4, dev),
         stride, n, free_pages.numel(), page_size, width, m)
     rc = lib().bsm_paged_tables(d, _stream(stream))
     if rc:
@@ -478,13 +497,14 @@ def bsm_paged_write(k, v, k_cache, v_cache, slots, stream=None):
     """New keys and values [tokens, heads, dim] to their slots of the caches
     [pages, page_size, heads, dim] (any strides; the last dimension contiguous)."""
     dtype = _paged_dtype(k, v, k_cache, v_cache)
-    ks, vs, cs = _strided(k, "k", 3), _strided(v, "v", 3), _caches(k_cache, v_cache)
+    dev = _device(k, "k")
+    ks, vs, cs = _strided(k, "k", 3, dev), _strided(v, "v", 3, dev), _caches(k_cache, v_cache, dev)
     tokens, heads, dim = shape = k.shape
     pages, page_size, ch, cd = k_cache.shape
     if v.shape != shape or heads != ch or dim != cd:
         raise ValueError("k and v must be [tokens, %d, %d]" % (ch, cd))
     d = _pack_write(k.data_ptr(), v.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
-                    _vec(slots, "slots", _INT64, tokens), ks[0], ks[1], vs[0], vs[1], cs[0], cs[1], cs[2],
+                    _vec(slots, "slots", _INT64, tokens, dev), ks[0], ks[1], vs[0], vs[1], cs[0], cs[1], cs[2],
                     tokens, heads, dim, page_size, pages, dtype)
     rc = lib().bsm_paged_write(d, _stream(stream))
     if rc:
@@ -503,16 +523,18 @@ def bsm_paged_attention(q, k_cache, v_cache, out, starts, lengths, tables, max_n
     """Attention of new tokens q [tokens, heads_q, dim] over caches [pages,
     page_size, heads_kv, dim] (any strides; the last dimension contiguous)."""
     dtype = _paged_dtype(q, k_cache, v_cache, out)
-    qs, os_, cs = _strided(q, "q", 3), _strided(out, "out", 3), _caches(k_cache, v_cache)
+    dev = _device(q, "q")
+    qs, os_, cs = _strided(q, "q", 3, dev), _strided(out, "out", 3, dev), _caches(k_cache, v_cache, dev)
     tokens, heads_q, dim = shape = q.shape
     pages, page_size, heads_kv, cd = k_cache.shape
     if out.shape != shape or dim != cd:
         raise ValueError("out must have q's shape, and the caches its last dimension")
     n = lengths.numel()
-    tab, stride, width = _page_tables(tables, n)
+    tab, stride, width = _page_tables(tables, n, dev)
+    _elsewhere(workspace, "workspace", dev)
     d = _pack_paged(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr(),
-                    0 if lse is None else _vec(lse, "lse", _FLOAT32, tokens * heads_q),
-                    _vec(starts, "starts", _INT32, n + 1), _vec(lengths, "lengths", _INT32, n), tab,
+                    0 if lse is None else _vec(lse, "lse", _FLOAT32, tokens * heads_q, dev),
+                    _vec(starts, "starts", _INT32, n + 1, dev), _vec(lengths, "lengths", _INT32, n, dev), tab,
                     _dptr(workspace, None, "workspace"), workspace.nbytes, qs[0], qs[1], os_[0], os_[1], cs[0], cs[1],
                     cs[2], stride, n, tokens, heads_q, heads_kv, dim, page_size, pages, width, max_new, dtype, window,
                     flags, scale)

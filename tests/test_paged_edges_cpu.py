@@ -1,0 +1,95 @@
+"""Refusals of the paged-cache operators that need no GPU: tensors of several
+devices, caches that overlap, counts and scales past what the kernels hold; and
+layouts that must not be refused."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2002_07062_gb300 import bsm
+from test_paged_cpu import INV, UNS, _attention, _tables, _write, built  # noqa: F401
+
+
+class On:
+    """A CPU tensor that says it lies on a GPU."""
+
+    is_cuda = True
+
+    def __init__(self, t, device=0):
+        self._t, self._device = t, device
+
+    def __getattr__(self, name):
+        return getattr(self._t, name)
+
+    def get_device(self):
+        return self._device
+
+    @property
+    def device(self):
+        return "cuda:%d" % self._device
+
+
+class Library:
+    """Takes every call and answers OK."""
+
+    def __init__(self):
+        self.calls = 0
+
+    def __getattr__(self, name):
+        def call(*a):
+            self.calls += 1
+            return 0
+        return call
+
+
+@pytest.fixture
+def library(monkeypatch):
+    lib = Library()
+    monkeypatch.setattr(bsm, "lib", lambda: lib)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    return lib
+
+
+I32 = dict(dtype=torch.int32)
+
+
+def _args(name):
+    half = lambda *s: On(torch.zeros(s, dtype=torch.bfloat16))
+    i32 = lambda *s: On(torch.zeros(s, **I32))
+    i64 = lambda *s: On(torch.zeros(s, dtype=torch.int64))
+    if name == "tables":
+        return dict(cached=i32(3), fresh=i32(3), free_pages=i32(9), page_size=16, tables=i32(3, 4), starts=i32(4),
+                    lengths=i32(3), slots=i64(5), positions=i32(5), owners=i32(5), info=i64(4))
+    if name == "write":
+        return dict(k=half(5, 2, 64), v=half(5, 2, 64), k_cache=half(9, 16, 2, 64), v_cache=half(9, 16, 2, 64),
+                    slots=i64(5))
+    return dict(q=half(5, 4, 64), k_cache=half(9, 16, 2, 64), v_cache=half(9, 16, 2, 64), out=half(5, 4, 64),
+                starts=i32(4), lengths=i32(3), tables=i32(3, 4), max_new=2, scale=0.125,
+                workspace=On(torch.zeros(4096, dtype=torch.uint8)), lse=On(torch.zeros(5, 4)))
+
+
+CALLS = {"tables": bsm.bsm_paged_tables, "write": bsm.bsm_paged_write, "attention": bsm.bsm_paged_attention}
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_tensors_of_one_current_device(name, library, monkeypatch):
+    """Every tensor of a call lies on the current device: the library launches there with bare addresses."""
+    args = _args(name)
+    CALLS[name](**args)
+    assert library.calls == 1
+    for key, value in args.items():
+        if not isinstance(value, On):
+            continue
+        value._device = 1
+        with pytest.raises(ValueError, match="cuda:1"):
+            CALLS[name](**args)
+        value._device = 0
+    for value in args.values():
+        if isinstance(value, On):
+            value._device = 1
+    with pytest.raises(ValueError, match="cuda:1"):
+        CALLS[name](**args)
+    assert library.calls == 1
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    CALLS[name](**args)
+    assert library.calls == 2
