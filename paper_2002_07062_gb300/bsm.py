@@ -458,8 +458,9 @@ def _paged_dtype(first, *others):
 
 
 def _caches(k_cache, v_cache, dev: int):
-    st = _strided(k_cache, "k_cache", 4, dev)
-    if v_cache.shape != k_cache.shape or _strided(v_cache, "v_cache", 4, dev) != st:
+    st, shape = _strided(k_cache, "k_cache", 4, dev), k_cache.shape
+    sv = _strided(v_cache, "v_cache", 4, dev)
+    if v_cache.shape != shape or (sv != st and any(x != y and n > 1 for x, y, n in zip(st, sv, shape))):
         raise ValueError("k_cache and v_cache must have the same shape and strides")
     return st
 

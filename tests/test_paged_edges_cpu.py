@@ -93,3 +93,19 @@ def test_tensors_of_one_current_device(name, library, monkeypatch):
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
     CALLS[name](**args)
     assert library.calls == 2
+
+
+@pytest.mark.parametrize("name", ["write", "attention"])
+def test_strides_of_single_entries_do_not_matter(name, library):
+    """Keys and values with one head, or one page: the stride of that dimension is never used and may differ."""
+    args = _args(name)
+    args["k_cache"] = On(torch.zeros(1, 16, 3, 64, dtype=torch.bfloat16)[:, :, :1])
+    args["v_cache"] = On(torch.as_strided(args["k_cache"]._t, (1, 16, 1, 64), (5, 192, 8, 1)))
+    for key in ("k", "v"):
+        if key in args:
+            args[key] = On(torch.zeros(5, 1, 64, dtype=torch.bfloat16))
+    CALLS[name](**args)
+    assert library.calls == 1
+    args["v_cache"] = On(torch.zeros(1, 16, 1, 64, dtype=torch.bfloat16))
+    with pytest.raises(ValueError, match="same shape and strides"):
+        CALLS[name](**args)
