@@ -327,7 +327,8 @@ int bsm_paged_tables(const bsm_paged_tables_desc *d, bsm_stream_t stream);
  * head, bit for bit.  A negative slot is skipped, one past the cache is skipped
  * and sets BSM_DEV_BOUNDS; two tokens with the same slot leave either.  dtype
  * F32, BF16 or F16.  Rows of a multiple of 16 bytes, pointers and strides too
- * (else BSM_ERR_MISALIGNED); caches must not overlap the other arguments.
+ * (else BSM_ERR_MISALIGNED).  The caches must not overlap the other arguments and
+ * may lie in one another's gaps, but have no place in common.
  */
 typedef struct {
     const void *k, *v;                  /* n_tokens x n_heads x head_dim */

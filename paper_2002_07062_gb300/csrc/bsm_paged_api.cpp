@@ -105,6 +105,23 @@ template <size_t N> int64_t extent(Dim (&&d)[N], int64_t row, int es)
     return cur < kMost ? cur * es : -1;
 }
 
+// Whether two arrays of these dimensions (the first k, by stride; rows apart as extent() asks)
+// whose first elements lie `delta` elements apart have a place in common: of the largest stride
+// only the two multiples around delta can bring the rest of it within reach.
+bool share_a_place(const Dim *d, int k, int64_t row, int64_t delta)
+{
+    if (k == 0)
+        return delta < row && -delta < row;
+    const Dim &x = d[k - 1];
+    if (x.n <= 1)
+        return share_a_place(d, k - 1, row, delta);
+    const int64_t at = delta / x.stride - (delta % x.stride < 0);
+    for (int64_t i = at; i <= at + 1; ++i)
+        if (i < x.n && -i < x.n && share_a_place(d, k - 1, row, delta - i * x.stride))
+            return true;
+    return false;
+}
+
 template <size_t N> bool unaligned(Dim (&&d)[N], int es)
 {
     for (const Dim &x : d)
@@ -251,7 +268,10 @@ int paged_write(const bsm_paged_write_desc *d, bsm_stream_t stream)
     const Span kc = span(d->k_cache, all), vc = span(d->v_cache, all), k = span(d->k, ks), v = span(d->v, vs),
                sl = span(d->slots, 8ll * d->n_tokens);
     // (keys and values may be interleaved in one allocation: only equal places clash)
-    if (d->k_cache == d->v_cache || kc.meets(k) || kc.meets(v) || kc.meets(sl) || vc.meets(k) || vc.meets(v) ||
+    Dim dims[3] = {Dim{d->n_pages, d->kv_stride_page}, Dim{d->page_size, d->kv_stride_token}, Dim{d->n_heads, d->kv_stride_head}};
+    std::sort(dims, dims + 3, [](const Dim &a, const Dim &b) { return a.stride < b.stride; });
+    if ((kc.meets(vc) && share_a_place(dims, 3, d->head_dim, (static_cast<int64_t>(vc.lo) - static_cast<int64_t>(kc.lo)) / es)) ||
+        kc.meets(k) || kc.meets(v) || kc.meets(sl) || vc.meets(k) || vc.meets(v) ||
         vc.meets(sl))
         return BSM_ERR_INVALID_ARG;
     PagedDev *dev = nullptr;

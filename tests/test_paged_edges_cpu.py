@@ -109,3 +109,49 @@ def test_strides_of_single_entries_do_not_matter(name, library):
     args["v_cache"] = On(torch.zeros(1, 16, 1, 64, dtype=torch.bfloat16))
     with pytest.raises(ValueError, match="same shape and strides"):
         CALLS[name](**args)
+
+
+def _write_code(**kw):
+    d = _write(**kw)        # (kept until the call is over)
+    return bsm.lib().bsm_paged_write(ctypes.addressof(d), None)
+
+
+# pages of 16 tokens, 2 heads of 64 bf16: strides 2048, 128, 64 elements
+@pytest.mark.parametrize("delta,strides,clash", [
+    (64, {}, True),                             # values begin at the keys' second head
+    (128, {}, True), (2048, {}, True), (9 * 2048, {}, True),            # second token, second page, last page
+    (-64, {}, True), (-9 * 2048 - 15 * 128 - 64, {}, True),
+    (10 * 2048, {}, False), (-10 * 2048, {}, False),                    # one behind the other
+    (2048, dict(kv_stride_page=4096), False), (4096, dict(kv_stride_page=4096), True),      # pages in turn
+    (6144, dict(kv_stride_page=4096), False),                           # ... three apart
+    (64, dict(kv_stride_token=256, kv_stride_head=128, kv_stride_page=4096), False),        # rows in turn
+    (32, dict(kv_stride_token=256, kv_stride_head=128, kv_stride_page=4096), True),         # ... half a row
+    (128, dict(kv_stride_token=256, kv_stride_page=4096), False),       # all heads of a token, then the values'
+    (10 * 64, dict(kv_stride_head=10 * 64 * 16, kv_stride_page=64, kv_stride_token=640), True),
+    (20 * 64 * 16, dict(kv_stride_head=10 * 64 * 16, kv_stride_page=64, kv_stride_token=640), False),
+])
+def test_caches_that_share_a_place_are_refused(delta, strides, clash):
+    """Keys and values may lie in one another's gaps; a place of both would get either."""
+    at = 1 << 44
+    code = _write_code(k_cache=at, v_cache=at + 2 * delta, **strides)
+    assert (code == INV) == clash, code
+
+
+def test_caches_that_share_a_place_against_counting():
+    import random
+    rng = random.Random(5)
+    for _ in range(400):
+        n = dict(page=rng.randint(1, 4), token=rng.randint(1, 4), head=rng.randint(1, 3))
+        stride, cur = {}, 8
+        for k in rng.sample(list(n), 3):
+            stride[k] = cur + 8 * rng.choice([0, 0, 1, 2, 8])
+            cur = stride[k] * n[k]
+        places = {p * stride["page"] + t * stride["token"] + h * stride["head"] + x
+                  for p in range(n["page"]) for t in range(n["token"]) for h in range(n["head"]) for x in range(8)}
+        delta = 8 * rng.randint(-cur // 8 - 1, cur // 8 + 1)
+        at = 1 << 44
+        code = _write_code(k_cache=at, v_cache=at + 2 * delta, n_heads=n["head"], head_dim=8, page_size=n["token"],
+                           n_pages=n["page"], kv_stride_page=stride["page"], kv_stride_token=stride["token"],
+                           kv_stride_head=stride["head"], k_stride_token=8 * n["head"], k_stride_head=8,
+                           v_stride_token=8 * n["head"], v_stride_head=8)
+        assert (code == INV) == any(x + delta in places for x in places), (n, stride, delta, code)
