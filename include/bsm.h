@@ -360,7 +360,7 @@ int bsm_paged_write(const bsm_paged_write_desc *d, bsm_stream_t stream);
  *             are rounded to dtype for the second product.
  *   heads_q   a multiple of heads_kv; head_dim a multiple of 8 up to 128 (else
  *             BSM_ERR_UNSUPPORTED).
- *   scale     > 0 and finite; window >= 0, > 0 only with BSM_FLAG_CAUSAL.
+ *   scale     > 0, scale * log2(e) finite in fp32; window >= 0, > 0 only with BSM_FLAG_CAUSAL.
  *   lse       n_tokens x heads_q fp32, or null.
  *   max_new   the most new tokens of any request, as the host knows it.  A hint:
  *             it selects kernels; a wrong one costs time and may round

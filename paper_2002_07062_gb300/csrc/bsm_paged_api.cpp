@@ -308,7 +308,8 @@ int paged_attention(const bsm_paged_desc *d, bsm_stream_t stream)
         d->table_stride < d->table_width || d->max_new < 0 || d->window < 0 || (d->flags & ~BSM_FLAG_CAUSAL) ||
         (d->dtype != BSM_F32 && d->dtype != BSM_BF16 && d->dtype != BSM_F16))
         return BSM_ERR_INVALID_ARG;
-    if (!(d->scale > 0.0f) || std::isinf(d->scale) || (d->window > 0 && !(d->flags & BSM_FLAG_CAUSAL)))
+    const float scale_log2 = d->scale * 1.4426950408889634f;
+    if (!(d->scale > 0.0f) || std::isinf(scale_log2) || (d->window > 0 && !(d->flags & BSM_FLAG_CAUSAL)))
         return BSM_ERR_INVALID_ARG;
     if (d->heads_kv < 1 || d->heads_q < d->heads_kv || d->heads_q % d->heads_kv || d->head_dim < 1)
         return BSM_ERR_INVALID_ARG;
@@ -381,7 +382,7 @@ int paged_attention(const bsm_paged_desc *d, bsm_stream_t stream)
     a.causal = (d->flags & BSM_FLAG_CAUSAL) ? 1 : 0;
     // (a window as long as any request can be hides nothing)
     a.window = d->window < static_cast<int64_t>(d->table_width) * d->page_size ? d->window : 0;
-    a.scale_log2 = d->scale * 1.4426950408889634f;
+    a.scale_log2 = scale_log2;
     a.group = d->heads_q / d->heads_kv;
     a.status = dev->status;
     unsigned char *ws = static_cast<unsigned char *>(d->workspace);

@@ -155,3 +155,10 @@ def test_caches_that_share_a_place_against_counting():
                            kv_stride_head=stride["head"], k_stride_token=8 * n["head"], k_stride_head=8,
                            v_stride_token=8 * n["head"], v_stride_head=8)
         assert (code == INV) == any(x + delta in places for x in places), (n, stride, delta, code)
+
+
+@pytest.mark.parametrize("scale,refused", [(2.3e38, False), (2.4e38, True), (3.4e38, True), (1e-45, False)])
+def test_scales_that_the_kernels_cannot_hold(scale, refused):
+    """Scores are computed in base 2: scale * log2(e) has to be finite too."""
+    d = _attention(scale=scale)
+    assert (bsm.lib().bsm_paged_attention(ctypes.addressof(d), None) == INV) == refused
