@@ -302,8 +302,8 @@ int bsm_bmm_ex(const void *a, const void *bt, void *c, int64_t B, int64_t M, int
  * gives the same answer.  Page ids are not checked here.
  * Errors: BSM_ERR_INVALID_ARG (sizes, null pointers, outputs that overlap each
  * other or an input), BSM_ERR_MISALIGNED (8 bytes for slots and info, 4 for the
- * rest), BSM_ERR_UNSUPPORTED (tables of 2^20 entries a request and wider),
- * BSM_ERR_CUDA.
+ * rest), BSM_ERR_UNSUPPORTED (tables of 2^20 entries a request and wider, more
+ * than 2^31 - 4096 requests), BSM_ERR_CUDA.
  */
 #define BSM_PAGED_PAGES 1u      /* free_pages ran out */
 #define BSM_PAGED_WIDTH 2u      /* a request needs more than table_width pages: the rest has no slot */
@@ -378,8 +378,9 @@ int bsm_paged_write(const bsm_paged_write_desc *d, bsm_stream_t stream);
  * the buffers is touched.
  * Pointers 16-byte aligned, strides multiples of 8 (else BSM_ERR_MISALIGNED).
  * out, lse and workspace must not overlap each other or an input.
- * Errors: BSM_ERR_INVALID_ARG, BSM_ERR_MISALIGNED, BSM_ERR_UNSUPPORTED,
- * BSM_ERR_CUDA.  No requests or tokens: BSM_OK, nothing launched.
+ * Errors: BSM_ERR_INVALID_ARG, BSM_ERR_MISALIGNED, BSM_ERR_UNSUPPORTED (also more
+ * than 2^31 - 4096 requests or tokens), BSM_ERR_CUDA.  No requests or tokens:
+ * BSM_OK, nothing launched.
  */
 typedef struct {
     const void *q;                      /* n_tokens x heads_q x head_dim */

@@ -68,6 +68,7 @@ constexpr uint32_t kPagedGone = 1;                  // it met a key whose page i
 constexpr uint32_t kPagedOdd = 2;                   // an output that it stored is not finite
 
 constexpr int32_t kPagedMostKeys = INT32_MAX - 255; // of a request: a step past them is still a 32-bit number
+constexpr int32_t kPagedMostCount = INT32_MAX - 4095;   // requests, and tokens of attention: a block past them likewise
 constexpr int kPagedWarps = 8;                      // of the row kernel
 constexpr int kPagedRowTile = 16;                   // most rows of its tiles
 constexpr int kPagedMaxDim = 128;

@@ -190,7 +190,7 @@ int paged_tables(const bsm_paged_tables_desc *d, bsm_stream_t stream)
     if (!d || d->n_requests < 0 || d->n_free < 0 || d->page_size < 1 || d->table_width < 1 || d->n_slots < 0 ||
         d->table_stride < d->table_width)
         return BSM_ERR_INVALID_ARG;
-    if (d->table_width >= (1 << 20))
+    if (d->table_width >= (1 << 20) || d->n_requests > kPagedMostCount)
         return BSM_ERR_UNSUPPORTED;
     if (!d->starts || !d->info || (d->n_requests > 0 && (!d->cached || !d->fresh || !d->tables || !d->lengths)) ||
         (d->n_free > 0 && !d->free_pages) || (d->n_slots > 0 && (!d->slots || !d->positions || !d->owners)))
@@ -313,7 +313,8 @@ int paged_attention(const bsm_paged_desc *d, bsm_stream_t stream)
         return BSM_ERR_INVALID_ARG;
     if (d->heads_kv < 1 || d->heads_q < d->heads_kv || d->heads_q % d->heads_kv || d->head_dim < 1)
         return BSM_ERR_INVALID_ARG;
-    if (d->dtype == BSM_F32 || !paged_heads_ok(d->heads_q, d->heads_kv, d->head_dim))
+    if (d->dtype == BSM_F32 || !paged_heads_ok(d->heads_q, d->heads_kv, d->head_dim) ||
+        d->n_requests > kPagedMostCount || d->n_tokens > kPagedMostCount)
         return BSM_ERR_UNSUPPORTED;
     if (d->n_requests == 0 || d->n_tokens == 0)
         return BSM_OK;

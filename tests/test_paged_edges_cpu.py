@@ -111,6 +111,13 @@ def test_strides_of_single_entries_do_not_matter(name, library):
         CALLS[name](**args)
 
 
+@pytest.fixture
+def no_device():
+    """These calls pass bare addresses that nothing lies at: one that is not refused must stop for want of a device."""
+    if torch.cuda.is_available():
+        pytest.skip("a call that is not refused would be launched")
+
+
 def _write_code(**kw):
     d = _write(**kw)        # (kept until the call is over)
     return bsm.lib().bsm_paged_write(ctypes.addressof(d), None)
@@ -130,14 +137,14 @@ def _write_code(**kw):
     (10 * 64, dict(kv_stride_head=10 * 64 * 16, kv_stride_page=64, kv_stride_token=640), True),
     (20 * 64 * 16, dict(kv_stride_head=10 * 64 * 16, kv_stride_page=64, kv_stride_token=640), False),
 ])
-def test_caches_that_share_a_place_are_refused(delta, strides, clash):
+def test_caches_that_share_a_place_are_refused(delta, strides, clash, no_device):
     """Keys and values may lie in one another's gaps; a place of both would get either."""
     at = 1 << 44
     code = _write_code(k_cache=at, v_cache=at + 2 * delta, **strides)
     assert (code == INV) == clash, code
 
 
-def test_caches_that_share_a_place_against_counting():
+def test_caches_that_share_a_place_against_counting(no_device):
     import random
     rng = random.Random(5)
     for _ in range(400):
@@ -158,7 +165,19 @@ def test_caches_that_share_a_place_against_counting():
 
 
 @pytest.mark.parametrize("scale,refused", [(2.3e38, False), (2.4e38, True), (3.4e38, True), (1e-45, False)])
-def test_scales_that_the_kernels_cannot_hold(scale, refused):
+def test_scales_that_the_kernels_cannot_hold(scale, refused, no_device):
     """Scores are computed in base 2: scale * log2(e) has to be finite too."""
     d = _attention(scale=scale)
     assert (bsm.lib().bsm_paged_attention(ctypes.addressof(d), None) == INV) == refused
+
+
+@pytest.mark.parametrize("make,call,field", [(_tables, "bsm_paged_tables", "n_requests"),
+                                             (_attention, "bsm_paged_attention", "n_requests"),
+                                             (_attention, "bsm_paged_attention", "n_tokens")])
+def test_counts_that_32_bits_cannot_step_over(make, call, field, no_device):
+    """Requests are scanned and tokens tiled in blocks: a count whose last block ends past 2^31 is refused before any
+    launch (its loops would wrap)."""
+    most = (1 << 31) - 1 - 4095
+    for n, refused in ((most, False), (most + 1, True), ((1 << 31) - 1, True)):
+        d = make(**{field: n})
+        assert (getattr(bsm.lib(), call)(ctypes.addressof(d), None) == UNS) == refused, n
