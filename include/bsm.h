@@ -279,9 +279,12 @@ int bsm_bmm_ex(const void *a, const void *bt, void *c, int64_t B, int64_t M, int
  * request r lies in slot tables[r, p / page_size] * page_size + p % page_size.
  * One step of a program that serves requests is bsm_paged_tables (where the
  * step's new tokens go), bsm_paged_write and bsm_paged_attention, the last two
- * once per layer.  Lengths, tables and slots stay on the device; no call
- * synchronises or allocates.  Calls share nothing but their arguments, so they
- * may run on several streams at once, each with its own workspace.
+ * once per layer.  Lengths, tables and slots stay on the device, the current one;
+ * no call synchronises or allocates, but for the library's first on a device,
+ * which sets it up and must not fall into a stream capture:
+ * bsm_paged_workspace_bytes is such a call.  Calls share nothing but their
+ * arguments, so they may run on several streams at once, each with its own
+ * workspace.
  * All strides are in elements; every row of head_dim elements is contiguous. */
 
 /*

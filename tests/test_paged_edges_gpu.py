@@ -236,3 +236,45 @@ def test_large_values_under_growing_scores(fresh, hint):
     check(b)
 
 
+_FIRST = """
+import torch
+from paper_2002_07062_gb300 import bsm
+torch.manual_seed(0)
+ws = torch.zeros(bsm.bsm_paged_workspace_bytes(8, 2, 64, 60), dtype=torch.uint8, device="cuda")
+i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+cached, fresh, free = i32([0, 0]), i32([60, 33]), torch.randperm(16, device="cuda", dtype=torch.int32)
+tab, st, ln, pos, own = torch.zeros((2, 4), dtype=torch.int32, device="cuda"), i32([0] * 3), i32([0] * 2), i32([0] * 93), i32([0] * 93)
+slots, info = torch.zeros(93, dtype=torch.int64, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda")
+q, k, v = (torch.randn(93, h, 64, device="cuda").bfloat16() for h in (8, 2, 2))
+kc, vc = torch.zeros(2, 16, 16, 2, 64, device="cuda").bfloat16()
+out = torch.zeros_like(q)
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    s = torch.cuda.current_stream()
+    bsm.bsm_paged_tables(cached, fresh, free, 16, tab, st, ln, slots, pos, own, info, stream=s)
+    bsm.bsm_paged_write(k, v, kc, vc, slots, stream=s)
+    bsm.bsm_paged_attention(q, kc, vc, out, st, ln, tab, 60, 0.125, ws, flags=bsm.FLAG_CAUSAL, stream=s)
+graph.replay()
+torch.cuda.synchronize()
+for a, b in ((0, 60), (60, 93)):
+    kk, vv = (z[a:b].double().repeat_interleave(4, 1) for z in (k, v))
+    x = torch.einsum("ihd,jhd->hij", q[a:b].double(), kk) * 0.125
+    x = x.masked_fill(torch.ones_like(x[0], dtype=torch.bool).triu(1), -float("inf"))
+    ref = torch.einsum("hij,jhd->ihd", x.softmax(-1), vv)
+    assert float((out[a:b] - ref).abs().max()) <= 3 * 2.0 ** -8 * float(vv.abs().max())
+assert info.tolist() == [93, 7, 0, 0] and bsm.bsm_device_status() == 0
+print("captured first")
+"""
+
+
+def test_first_launches_of_a_process_may_be_captured():
+    """After bsm_paged_workspace_bytes the library's first launches can be a capture."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", _FIRST], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "captured first" in r.stdout, r.stderr[-2000:]
+
+
