@@ -205,7 +205,8 @@ __global__ void __launch_bounds__(kTabThreads) paged_tables(const PagedTablesArg
 
 // The copy, bound by its bytes.  A thread keeps its place in the row of a
 // token (16 bytes of one head) and goes from token to token, eight loads in
-// flight; the divisions that find a slot's page are one a token.  237 MB: 38.3 us,
+// flight; the divisions that find a slot's page are one a token.  (Plain loads: the kernel before
+// this one may still write the keys while this one starts.)  237 MB: 38.3 us,
 // 0.91 of the copy rate (57 with the place divided out for every piece).
 constexpr int kWriteThreads = 256;
 constexpr int kWriteAhead = 4;
@@ -249,7 +250,7 @@ __global__ void __launch_bounds__(kWriteThreads) paged_write(const PagedWriteArg
                 const int64_t t = t0 + u * step;
 #pragma unroll
                 for (int kv = 0; kv < 2; ++kv)
-                    val[u][kv] = __ldg(reinterpret_cast<const uint4 *>(src[kv] + t * a.src_token[kv]));
+                    val[u][kv] = *reinterpret_cast<const uint4 *>(src[kv] + t * a.src_token[kv]);
                 const int64_t page = to[u] >> 32 ? to[u] / a.page
                                                  : static_cast<int64_t>(static_cast<uint32_t>(to[u]) / static_cast<uint32_t>(a.page));
                 to[u] = page * a.dst_page + (to[u] - page * a.page) * a.dst_token;

@@ -278,3 +278,17 @@ def test_first_launches_of_a_process_may_be_captured():
     assert r.returncode == 0 and "captured first" in r.stdout, r.stderr[-2000:]
 
 
+def test_write_reads_what_the_kernel_before_it_wrote():
+    """Launches overlap: a write follows, without a pause, the kernel that makes its keys."""
+    import torch
+    T, H, d = 4096, 8, 128
+    kc, vc = torch.zeros(2, T // 16, 16, H, d, device="cuda", dtype=torch.bfloat16)
+    slots = torch.randperm(T, device="cuda")
+    k, v, back = (torch.zeros(T, H, d, device="cuda", dtype=torch.bfloat16) for _ in range(3))
+    st = torch.cuda.current_stream()
+    for i in range(1, 60):
+        # what the second write reads, the first has stored (and lets the second start early)
+        k.fill_(i)
+        bsm.bsm_paged_write(k, k, back.view(T // 16, 16, H, d), v.view(T // 16, 16, H, d), slots, stream=st)
+        bsm.bsm_paged_write(v, back, kc, vc, slots, stream=st)
+        assert bool((kc == i).all()) and bool((vc == i).all()), i
