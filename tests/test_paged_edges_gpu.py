@@ -292,3 +292,18 @@ def test_write_reads_what_the_kernel_before_it_wrote():
         bsm.bsm_paged_write(k, k, back.view(T // 16, 16, H, d), v.view(T // 16, 16, H, d), slots, stream=st)
         bsm.bsm_paged_write(v, back, kc, vc, slots, stream=st)
         assert bool((kc == i).all()) and bool((vc == i).all()), i
+
+
+@pytest.mark.parametrize("hint", HINTS)
+@pytest.mark.parametrize("d,page", [(128, 16), (64, 16), (128, 3)])
+def test_requests_that_share_pages(d, page, hint):
+    """A common prefix lies in the cache once: its pages stand in every request's table."""
+    b = Batch([700, 650, 90, 480], [130, 1, 3, 300], 8, 2, d, page, seed=5)
+    b.tables = b.tables.copy()
+    b.tables[1, :400 // page] = b.tables[0, :400 // page]
+    b.tables[3, :160 // page] = b.tables[0, :160 // page]
+    b.tables[2, :90 // page] = b.tables[3, :90 // page]
+    b.poison()
+    for mask in ("causal", "window 300"):
+        run(b, hint, **MASKS[mask])
+        check(b, **MASKS[mask])
