@@ -11,9 +11,14 @@
 // launch, which follows anyway, looks at those tiles' rows and computes again what a hidden
 // key got into: a warp a row, four columns a lane, 32 keys at a time.  Where all is finite
 // and there it reads a flag a unit.
-// (Masking such keys in the tile kernel's own softmax cost every call 1 to 4 %.  The code is
-// kept short because its size costs too: with the walk along the work line in it, 80 KB
-// instead of 23, a chunk of 2048 tokens over 6100 keys took 163 us instead of 156.)
+// Slow, bound by the latency of its loads: of a chunk of 2048 tokens over 6100 keys (0.17 ms) with a
+// NaN among the values of its last token, the 63 tokens before it in their tile take 52 ms; all
+// of them where one page of the request is missing 143 ms; a row whose sum or outputs are NaN
+// for good ends there (all values NaN: 2.5 ms).  The rest is for the calls that need none of it:
+// leaving such keys out in the tile kernel (its query warp looking at the values of keys that
+// some rows do not see, its softmax masking keys without a page) cost every call 4 to 15 %.
+// Nor is the code made longer than this: its size alone costs, even unexecuted.  With the walk
+// along the work line in it (80 KB) that chunk took 163 us, with 39 KB 158.5, with 31 157.4.
 #pragma once
 
 #include <cuda_runtime.h>
@@ -25,6 +30,7 @@
 namespace bsm {
 
 constexpr float kPagedLn2 = 0.6931471805599453f;
+constexpr int kAgainKeys = 2, kAgainValues = 4;     // pieces of a key's row, rows of values, loaded ahead
 
 // What a unit's producer went through: the first tile that it starts, how many it has whole
 // from there on.
@@ -61,10 +67,26 @@ __device__ __forceinline__ float pg_total(const float4 &v) { return (v.x + v.y) 
 // Whether any of four is an infinity or NaN.
 __device__ __forceinline__ bool pg_odd(const float4 &v) { return v.x * 0.0f + v.y * 0.0f + v.z * 0.0f + v.w * 0.0f != 0.0f; }
 
-// Four 16-bit elements as fp32.
-template <bool kF16> __device__ __forceinline__ float4 pg_load4(const void *base, int64_t at)
+__device__ __forceinline__ bool pg_all_nan(const float4 &v)
 {
-    const uint2 w = *reinterpret_cast<const uint2 *>(static_cast<const unsigned char *>(base) + 2 * at);
+    return v.x != v.x && v.y != v.y && v.z != v.z && v.w != v.w;
+}
+
+// <(two 16-bit elements), (two more)> in fp32.
+template <bool kF16> __device__ __forceinline__ float pg_dot2(uint32_t a, uint32_t b)
+{
+    if (kF16) {
+        const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(&a));
+        const float2 y = __half22float2(*reinterpret_cast<const __half2 *>(&b));
+        return x.x * y.x + x.y * y.y;
+    }
+    return __uint_as_float(a << 16) * __uint_as_float(b << 16) +
+           __uint_as_float(a & 0xFFFF0000u) * __uint_as_float(b & 0xFFFF0000u);
+}
+
+// Four 16-bit elements as fp32.
+template <bool kF16> __device__ __forceinline__ float4 pg_wide(const uint2 &w)
+{
     if (kF16) {
         const float2 lo = __half22float2(*reinterpret_cast<const __half2 *>(&w.x));
         const float2 hi = __half22float2(*reinterpret_cast<const __half2 *>(&w.y));
@@ -72,6 +94,10 @@ template <bool kF16> __device__ __forceinline__ float4 pg_load4(const void *base
     }
     return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16),
                        __uint_as_float(w.y & 0xFFFF0000u));
+}
+template <bool kF16> __device__ __forceinline__ float4 pg_load4(const void *base, int64_t at)
+{
+    return pg_wide<kF16>(*reinterpret_cast<const uint2 *>(static_cast<const unsigned char *>(base) + 2 * at));
 }
 
 // A row's keys, and those that took part in its tile's products.
@@ -99,6 +125,8 @@ __device__ __forceinline__ void paged_row_again(const PagedArgs &a, const PagedA
     const bool odd = __any_sync(0xffffffffu, mine && pg_odd(pg_load4<kF16>(a.out, mine ? to : 0)));
     if (!odd && !w.gone)
         return;
+    // (values that are not finite do not touch lse: the kernels' holds unless a page is missing)
+    const bool wants = a.lse && w.gone && c0 == 0;
     bool again = false;
     float top = -INFINITY, sum = 0.0f;
     float4 acc = zero;
@@ -123,10 +151,20 @@ __device__ __forceinline__ void paged_row_again(const PagedArgs &a, const PagedA
             float p = 0.0f;
             if (pass) {
                 float x = 0.0f;         // its score
-#pragma unroll 2
-                for (int32_t c = 0; c < a.d; c += 4) {
-                    const float4 qv = pg_load4<kF16>(a.q, q + c), k = off >= 0 ? pg_load4<kF16>(a.k, off + c) : zero;
-                    x += qv.x * k.x + qv.y * k.y + qv.z * k.z + qv.w * k.w;
+                const unsigned char *kr = static_cast<const unsigned char *>(a.k) + 2 * (off < 0 ? 0 : off);
+                const unsigned char *qr = static_cast<const unsigned char *>(a.q) + 2 * q;
+#pragma unroll 1
+                for (int32_t c = 0; c < 2 * a.d; c += 16 * kAgainKeys) {
+                    uint4 kw[kAgainKeys];           // (loads ahead of their use)
+#pragma unroll
+                    for (int i = 0; i < kAgainKeys; ++i)
+                        kw[i] = c + 16 * i < 2 * a.d ? *reinterpret_cast<const uint4 *>(kr + c + 16 * i) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < kAgainKeys; ++i) {
+                        const uint4 qw = *reinterpret_cast<const uint4 *>(qr + (c + 16 * i < 2 * a.d ? c + 16 * i : 0));
+                        x += pg_dot2<kF16>(qw.x, kw[i].x) + pg_dot2<kF16>(qw.y, kw[i].y) + pg_dot2<kF16>(qw.z, kw[i].z) +
+                             pg_dot2<kF16>(qw.w, kw[i].w);
+                    }
                 }
                 x = off >= 0 ? x * a.scale_log2 : -INFINITY;
                 float most = fmaxf(x, top);
@@ -142,18 +180,31 @@ __device__ __forceinline__ void paged_row_again(const PagedArgs &a, const PagedA
                     all += __shfl_xor_sync(0xffffffffu, all, s);
                 sum = sum * f + all;
                 acc = make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f);
-                if (sum != sum)         // NaN from here on
+                // (NaN from here on; not before lse is known)
+                if (sum != sum || (!wants && __all_sync(0xffffffffu, !mine || pg_all_nan(acc))))
                     break;
             } else {
                 again |= __any_sync(0xffffffffu, seen && off < 0);
                 off = seen || !odd ? -1 : off;
             }
-#pragma unroll 2
-            for (int c = 0; c < 32; ++c) {
-                const int64_t o = __shfl_sync(0xffffffffu, off, c);
-                const float pc = __shfl_sync(0xffffffffu, p, c);
-                const float4 v = o >= 0 && live ? pg_load4<kF16>(a.v, o + col) : zero;
-                acc = make_float4(acc.x + pc * v.x, acc.y + pc * v.y, acc.z + pc * v.z, acc.w + pc * v.w);
+            if (!__any_sync(0xffffffffu, off >= 0))
+                continue;
+#pragma unroll 1
+            for (int c = 0; c < 32; c += kAgainValues) {
+                uint2 w[kAgainValues];
+#pragma unroll
+                for (int i = 0; i < kAgainValues; ++i) {
+                    const int64_t o = __shfl_sync(0xffffffffu, off, c + i);
+                    w[i] = *reinterpret_cast<const uint2 *>(static_cast<const unsigned char *>(a.v) +
+                                                            2 * (o >= 0 && live ? o + col : 0));
+                }
+#pragma unroll
+                for (int i = 0; i < kAgainValues; ++i) {
+                    const bool in = __shfl_sync(0xffffffffu, off, c + i) >= 0 && live;
+                    const float pc = __shfl_sync(0xffffffffu, p, c + i);
+                    const float4 v = in ? pg_wide<kF16>(w[i]) : zero;
+                    acc = make_float4(acc.x + pc * v.x, acc.y + pc * v.y, acc.z + pc * v.z, acc.w + pc * v.w);
+                }
             }
         }
         if (!pass) {
@@ -170,7 +221,7 @@ __device__ __forceinline__ void paged_row_again(const PagedArgs &a, const PagedA
         o.y = pg_pack<kF16>(acc.z * inv, acc.w * inv);
         *reinterpret_cast<uint2 *>(static_cast<unsigned char *>(a.out) + 2 * to) = o;
     }
-    if (a.lse && c0 == 0 && lane == 0)
+    if (wants && lane == 0)
         a.lse[token * a.heads_q + head] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kPagedLn2;
 }
 

@@ -307,3 +307,18 @@ def test_requests_that_share_pages(d, page, hint):
     for mask in ("causal", "window 300"):
         run(b, hint, **MASKS[mask])
         check(b, **MASKS[mask])
+
+
+@pytest.mark.parametrize("hint", HINTS)
+@pytest.mark.parametrize("gone", [False, True])
+def test_lse_beside_values_of_nothing_but_nan(gone, hint):
+    """The values have no part in lse: it is right where all outputs are NaN, also with a page missing."""
+    b = Batch([3000, 300, 50], [900, 20, 1], 8, 2, 128, 16, seed=7)
+    for r in (0, 1):
+        for e in range(-(-int(b.lens[r]) // 16)):
+            b.vc[int(b.tables[r, e])] = float("nan")
+    if gone:
+        b.tables = b.tables.copy()
+        b.tables[0, 2], b.tables[1, 1] = -1, -1
+    run(b, hint, status=bsm.DEV_BOUNDS if gone else 0)
+    check(b)
