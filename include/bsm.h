@@ -329,7 +329,8 @@ int bsm_paged_tables(const bsm_paged_tables_desc *d, bsm_stream_t stream);
  * k_cache[slots[t]] = k[t] and v_cache[slots[t]] = v[t] for every token t and
  * head, bit for bit.  A negative slot is skipped, one past the cache is skipped
  * and sets BSM_DEV_BOUNDS; two tokens with the same slot leave either.  dtype
- * F32, BF16 or F16.  Rows of a multiple of 16 bytes, pointers and strides too
+ * F32, BF16 or F16 (an F32 cache is for a reader of its own:
+ * bsm_paged_attention takes the 16-bit types alone).  Rows of a multiple of 16 bytes, pointers and strides too
  * (else BSM_ERR_MISALIGNED).  The caches must not overlap the other arguments and
  * may lie in one another's gaps, but have no place in common.
  */
@@ -360,7 +361,8 @@ int bsm_paged_write(const bsm_paged_write_desc *d, bsm_stream_t stream);
  * the way are computed once more, slowly).
  *   dtype     BF16 or F16 for q, caches and out (BSM_ERR_UNSUPPORTED: F32);
  *             products accumulate in fp32, the softmax is fp32, probabilities
- *             are rounded to dtype for the second product.
+ *             are rounded to dtype for the second product (the largest one too:
+ *             they are taken against a maximum that may lag behind).
  *   heads_q   a multiple of heads_kv; head_dim a multiple of 8 up to 128 (else
  *             BSM_ERR_UNSUPPORTED).
  *   scale     > 0, scale * log2(e) finite in fp32; window >= 0, > 0 only with BSM_FLAG_CAUSAL.

@@ -8,7 +8,8 @@
 // a line of W steps; unit u of U (a warp or a CTA) takes steps
 // [W u / U, W (u + 1) / U).  Every unit gets the same amount whatever the
 // lengths are, and a tile is cut at most where two units meet; the parts of a
-// cut tile are joined by paged_join in unit order.  The line is never stored:
+// cut tile are joined in unit order by a second launch (paged_join,
+// paged_tile_join).  The line is never stored:
 // the steps before tile i of a request have a closed form (floor sums), so a
 // unit finds its place by bisection.
 #pragma once

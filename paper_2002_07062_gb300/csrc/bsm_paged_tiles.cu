@@ -27,15 +27,16 @@
 // same quotient, and probabilities are held 2^8 lower for it), so nearly all
 // steps skip that pass.
 //
-// GB300: two prompts of 8192 tokens, 32/8 heads of 128: 714 us (1.54 PFLOP/s; a
-// plain bf16 product 1.95), tensor pipe 71 % active on 2048 tokens over 6100;
-// 4 tokens over 131 thousand keys, 1.02 GB: 172 us.  Without the softmax the first
-// runs in 548 us.  Tried and slower for it: steps of 64 keys with two score
+// GB300: two prompts of 8192 tokens, 32/8 heads of 128: 714 to 780 us (1.54 to 1.41
+// PFLOP/s; a plain bf16 product of the library's 1.95), the longer the more power the values
+// draw; tensor pipe 71 % active on 2048 tokens over 6100; 2 x 4 tokens over up to 131 thousand
+// keys, 1.02 GB: 171 us.  Without the softmax between the products the first runs in 548 us
+// (2.0 PFLOP/s).  Every instance has 168 registers a thread and spills 4 to 8 bytes.  Tried and slower for it: steps of 64 keys with two score
 // buffers a block, which never wait for scores (963 us: a product of 128 x 64 x 16
 // takes 52 cycles instead of 32, the bytes of its operands in shared memory);
 // probabilities in two parts, the first one's product beside the second's
-// exponentials (787); two softmax warps a row (917: 96 registers, and the two
-// have to meet every step); one issuing warp (849 to 1025); a warp each for keys and
+// exponentials (787); two softmax warps a row (917 to 922: 96 registers, and the two
+// have to meet every step); one issuing warp (924 and more); a warp each for keys and
 // values (759).
 // Every wait is bounded as in the batched product.
 #include <cuda.h>
