@@ -110,6 +110,7 @@ typedef enum {
 } bsm_policy;
 
 #define BSM_FLAG_CAUSAL 1u     /* additive -inf mask above each slice's diagonal */
+#define BSM_FLAG_INTERLEAVED 2u /* bsm_paged_write_rotary: a pair's two columns lie side by side */
 
 #define BSM_MAX_DIES 4
 #define BSM_MAX_SM 256
@@ -344,6 +345,48 @@ typedef struct {
     int32_t dtype;
 } bsm_paged_write_desc;
 int bsm_paged_write(const bsm_paged_write_desc *d, bsm_stream_t stream);
+
+/*
+ * bsm_paged_write with the rotation of positions applied on the way: token t, at
+ * position p = positions[t], has the first rotary_dim columns of every key head turned
+ * pair by pair before they go to slots[t], and those of its query heads on the way
+ * from q to q_out.  With h = rotary_dim / 2, pair i < h is columns (i, i + h), with
+ * BSM_FLAG_INTERLEAVED (2 i, 2 i + 1):
+ *     x1' = x1 * cos - x2 * sin,  x2' = x2 * cos + x1 * sin
+ *     cos = table[p][i],  sin = table[p][h + i]
+ * in fp32, rounded once to dtype.  The other columns and the values are copied bit for
+ * bit.  The caller fills the table (any frequencies, any factor on them); angles of far
+ * positions want 64 bits on their way into it.
+ *   positions negative: the token is left out, its row of q_out and its slot stay as they
+ *             were; past the table: the same, and sets BSM_DEV_BOUNDS.
+ *   slots     negative: its key and value are left out; past the cache: the same, and
+ *             sets BSM_DEV_BOUNDS.  (positions and slots as bsm_paged_tables gives them.)
+ *   heads_q   0: no queries (q and q_out may be null).
+ *   q_out     q itself with the same strides (in place), or no place in common with q;
+ *             none with k and v (those and q_out may be parts of one row).
+ *   rotary_dim  even, up to head_dim; 0 copies.  Halves of whole pieces of 16 bytes, and
+ *             interleaved pairs, are fastest.
+ * Types, rows, pointers and strides as bsm_paged_write (table: fp32, any stride of at
+ * least rotary_dim); (heads_q + 2 heads_kv) * head_dim at most 65536 (else
+ * BSM_ERR_UNSUPPORTED).  The caches overlap no other argument, nor does q_out the table,
+ * positions and slots.
+ */
+typedef struct {
+    const void *q, *k, *v;              /* n_tokens x heads_q / heads_kv x head_dim */
+    void *q_out;                        /* n_tokens x heads_q x head_dim */
+    void *k_cache, *v_cache;            /* as bsm_paged_write */
+    const float *table;                 /* n_positions rows of rotary_dim, table_stride apart */
+    const int32_t *positions;           /* n_tokens */
+    const int64_t *slots;               /* n_tokens */
+    int64_t q_stride_token, q_stride_head, k_stride_token, k_stride_head, v_stride_token, v_stride_head;
+    int64_t q_out_stride_token, q_out_stride_head;
+    int64_t kv_stride_page, kv_stride_token, kv_stride_head;    /* of both caches */
+    int64_t table_stride;
+    int32_t n_tokens, heads_q, heads_kv, head_dim, rotary_dim, n_positions, page_size, n_pages;
+    int32_t dtype;
+    uint32_t flags;
+} bsm_paged_write_rotary_desc;
+int bsm_paged_write_rotary(const bsm_paged_write_rotary_desc *d, bsm_stream_t stream);
 
 /*
  * Attention of new tokens over the cache.  Request r's tokens are starts[r] ..

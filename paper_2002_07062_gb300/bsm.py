@@ -25,7 +25,7 @@ POLICY_WHOLE_GPU, POLICY_RR, POLICY_CBMF, POLICY_CBMF_LB, POLICY_DYNAMIC, POLICY
 POLICIES = {"whole_gpu": POLICY_WHOLE_GPU, "rr": POLICY_RR, "cbmf": POLICY_CBMF,
             "cbmf_lb": POLICY_CBMF_LB, "dynamic": POLICY_DYNAMIC, "minimax": POLICY_MINIMAX}
 POLICY_NAMES = {v: k for k, v in POLICIES.items()}
-FLAG_CAUSAL = 1
+FLAG_CAUSAL, FLAG_INTERLEAVED = 1, 2
 OP_FORWARD, OP_BACKWARD = 0, 1
 MAX_DIES = 4
 MAX_SM = 256
@@ -136,6 +136,17 @@ class PagedWriteDesc(ctypes.Structure):
                [(n, ctypes.c_int32) for n in ("n_tokens", "n_heads", "head_dim", "page_size", "n_pages", "dtype")]
 
 
+class PagedWriteRotaryDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k", "v", "q_out", "k_cache", "v_cache", "table", "positions",
+                                               "slots")] + \
+               [(n, ctypes.c_int64) for n in ("q_stride_token", "q_stride_head", "k_stride_token", "k_stride_head",
+                                              "v_stride_token", "v_stride_head", "q_out_stride_token", "q_out_stride_head",
+                                              "kv_stride_page", "kv_stride_token", "kv_stride_head", "table_stride")] + \
+               [(n, ctypes.c_int32) for n in ("n_tokens", "heads_q", "heads_kv", "head_dim", "rotary_dim", "n_positions",
+                                              "page_size", "n_pages", "dtype")] + \
+               [("flags", ctypes.c_uint32)]
+
+
 class PagedDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k_cache", "v_cache", "out", "lse", "starts", "lengths", "tables",
                                                "workspace")] + \
@@ -175,6 +186,7 @@ def lib():
                                         ctypes.c_int),
         "bsm_paged_tables": ([vp, vp], ctypes.c_int),
         "bsm_paged_write": ([vp, vp], ctypes.c_int),
+        "bsm_paged_write_rotary": ([vp, vp], ctypes.c_int),
         "bsm_paged_attention": ([vp, vp], ctypes.c_int),
         "bsm_paged_workspace_bytes": ([ctypes.c_int, i32, i32, i32, i32], i64),
         "bsm_plan_desc_init": ([ctypes.POINTER(PlanDesc)], ctypes.c_int),
@@ -393,6 +405,7 @@ def _packer(desc):
 
 
 _pack_tables, _pack_write, _pack_paged = _packer(PagedTablesDesc), _packer(PagedWriteDesc), _packer(PagedDesc)
+_pack_rotary = _packer(PagedWriteRotaryDesc)
 _PAGED_DTYPES = {}      # torch type -> bsm_dtype, filled on first use
 _INT32 = _INT64 = _FLOAT32 = _cuda = None
 
@@ -510,6 +523,41 @@ def bsm_paged_write(k, v, k_cache, v_cache, slots, stream=None):
     rc = lib().bsm_paged_write(d, _stream(stream))
     if rc:
         _check(rc, "bsm_paged_write")
+
+
+def bsm_paged_write_rotary(q, k, v, q_out, k_cache, v_cache, slots, positions, table, flags: int = 0, stream=None):
+    """bsm_paged_write with the first columns of keys, and of queries q on the way to
+    q_out (both [tokens, heads_q, dim], or None), rotated: table [positions, rotary_dim]
+    fp32 holds rotary_dim / 2 cosines and as many sines of every position."""
+    dtype = _paged_dtype(k, v, k_cache, v_cache) if q is None else _paged_dtype(k, v, k_cache, v_cache, q, q_out)
+    dev = _device(k, "k")
+    ks, vs, cs = _strided(k, "k", 3, dev), _strided(v, "v", 3, dev), _caches(k_cache, v_cache, dev)
+    tokens, heads, dim = shape = k.shape
+    pages, page_size, ch, cd = k_cache.shape
+    if v.shape != shape or heads != ch or dim != cd:
+        raise ValueError("k and v must be [tokens, %d, %d]" % (ch, cd))
+    if q is None:
+        if q_out is not None:
+            raise ValueError("q_out without q")
+        heads_q, qp, op, qs, os_ = 0, 0, 0, (0, 0), (0, 0)
+    else:
+        qs, os_ = _strided(q, "q", 3, dev), _strided(q_out, "q_out", 3, dev)
+        heads_q = q.shape[1]
+        if q.shape[0] != tokens or q.shape[2] != dim or q_out.shape != q.shape:
+            raise ValueError("q and q_out must be [%d, heads, %d]" % (tokens, dim))
+        qp, op = q.data_ptr(), q_out.data_ptr()
+    ts = _strided(table, "table", 2, dev)
+    n_positions, rot = table.shape
+    if table.dtype is not _FLOAT32:
+        raise ValueError("table must be %s (got %s)" % (_FLOAT32, table.dtype))
+    d = _pack_rotary(qp, k.data_ptr(), v.data_ptr(), op, k_cache.data_ptr(), v_cache.data_ptr(), table.data_ptr(),
+                     _vec(positions, "positions", _INT32, tokens, dev), _vec(slots, "slots", _INT64, tokens, dev),
+                     qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], os_[0], os_[1], cs[0], cs[1], cs[2],
+                     ts[0] if n_positions > 1 else rot, tokens, heads_q, heads, dim, rot, n_positions, page_size, pages,
+                     dtype, flags)
+    rc = lib().bsm_paged_write_rotary(d, _stream(stream))
+    if rc:
+        _check(rc, "bsm_paged_write_rotary")
 
 
 def bsm_paged_workspace_bytes(heads_q: int, heads_kv: int, head_dim: int, max_new: int, device: int = -1) -> int:

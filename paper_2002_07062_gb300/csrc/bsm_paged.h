@@ -30,6 +30,27 @@ struct PagedWriteArgs {
     uint32_t *status;
 };
 
+struct PagedRotaryArgs {
+    const unsigned char *src[3];        // queries, new keys, new values
+    unsigned char *dst[3];              // rotated queries, the caches
+    const float *table;                 // cosines and sines of every position
+    const int32_t *positions;
+    const int64_t *slots;
+    int64_t src_token[3], src_head[3];  // strides, bytes
+    int64_t out_token, out_head;        // of dst[0]
+    int64_t dst_page, dst_token, dst_head;
+    int64_t table_stride;               // floats
+    int64_t n_slots_cache;
+    int32_t n_tokens, n_positions, page;
+    int32_t heads_q, heads_kv, half, dim;       // half: pairs of a head
+    int32_t wide_table;                 // its rows can be read 16 bytes at a time
+    // how a token's work is dealt (set by the launch)
+    int32_t groups_q, groups_kv, turned, units, units_v;    // units of a head that turn, all, of a value's head
+    uint32_t per_token, of_qk, by_units, by_units_v;        // threads of a token, those before its values; reciprocals
+    uint64_t by_token;
+    uint32_t *status;
+};
+
 // One kernel's share of bsm_paged_attention: which requests it takes, how their
 // rows are tiled and how the work is split over its units (warps or CTAs).
 struct PagedArgs {
@@ -74,9 +95,11 @@ constexpr int kPagedRowTile = 16;                   // most rows of its tiles
 constexpr int kPagedMaxDim = 128;
 constexpr int kPagedTileRows = 256;                 // of the tile kernel: two blocks of 128
 constexpr int kPagedTileKeys = 128;                 // keys of its steps
+constexpr int64_t kRotaryMost = 1 << 16;            // columns of a rotated token (queries, keys, values): its threads are counted by reciprocals
 
 int launch_paged_tables(const PagedTablesArgs &a, int n_sm, void *stream);
 int launch_paged_write(const PagedWriteArgs &a, int n_sm, void *stream);
+int launch_paged_rotary(PagedRotaryArgs a, int dtype, bool interleaved, int n_sm, void *stream);
 int launch_paged_rows(const PagedArgs &a, bool f16, int grid, void *stream);
 // maps: CUtensorMaps of q, k, v (host); box: rows of one copy of k and v (below 8:
 // those maps are not used); per_page: 0, or whole rows a copy, with the maps' fourth

@@ -12,19 +12,12 @@
 
 #include "bsm_internal.h"
 #include "bsm_paged.h"
+#include "bsm_paged_host.h"
 #include "bsm_trace.h"
 
 namespace bsm {
 
-int device_status_word(int device, uint32_t **out);
-
 namespace {
-
-struct PagedDev {
-    bool ready = false;
-    int n_sm = 0;
-    uint32_t *status = nullptr;
-};
 
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
@@ -33,6 +26,8 @@ using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t,
 std::mutex g_paged_mu;
 PagedDev g_pdev[64];
 EncodeTiled g_paged_encode = nullptr;
+
+}  // namespace
 
 int paged_device(int device, PagedDev **out)
 {
@@ -71,66 +66,7 @@ int paged_device(int device, PagedDev **out)
     return BSM_OK;
 }
 
-bool misaligned(const void *p, int64_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }
-
-// [address, end) of a strided array (non-negative strides).
-struct Span {
-    uintptr_t lo = 0, hi = 0;
-    bool meets(const Span &o) const { return lo < o.hi && o.lo < hi; }
-};
-
-Span span(const void *p, int64_t bytes) { return Span{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes}; }
-
-// A dimension of a strided array, in elements.  The stride of a dimension of one
-// entry is never used and may be anything.
-struct Dim {
-    int64_t n, stride;
-};
-
-// Bytes from the first element to the end of the last row (`row` contiguous
-// elements) of an array with these dimensions, in any order; -1 when its rows
-// overlap or the strides overflow.
-template <size_t N> int64_t extent(Dim (&&d)[N], int64_t row, int es)
-{
-    constexpr int64_t kMost = int64_t(1) << 60;
-    std::sort(d, d + N, [](const Dim &a, const Dim &b) { return a.stride < b.stride; });
-    int64_t cur = row;
-    for (const Dim &x : d) {
-        if (x.n <= 1)
-            continue;
-        if (x.stride < cur || x.stride > kMost / x.n)
-            return -1;
-        cur += (x.n - 1) * x.stride;
-    }
-    return cur < kMost ? cur * es : -1;
-}
-
-// Whether two arrays of these dimensions (the first k, by stride; rows apart as extent() asks)
-// whose first elements lie `delta` elements apart have a place in common: of the largest stride
-// only the two multiples around delta can bring the rest of it within reach.
-bool share_a_place(const Dim *d, int k, int64_t row, int64_t delta)
-{
-    if (k == 0)
-        return delta < row && -delta < row;
-    const Dim &x = d[k - 1];
-    if (x.n <= 1)
-        return share_a_place(d, k - 1, row, delta);
-    const int64_t at = delta / x.stride - (delta % x.stride < 0);
-    for (int64_t i = at; i <= at + 1; ++i)
-        if (i < x.n && -i < x.n && share_a_place(d, k - 1, row, delta - i * x.stride))
-            return true;
-    return false;
-}
-
-template <size_t N> bool unaligned(Dim (&&d)[N], int es)
-{
-    for (const Dim &x : d)
-        if (x.n > 1 && x.stride * es % 16)
-            return true;
-    return false;
-}
-
-int elem_size(int dtype) { return dtype == BSM_F32 ? 4 : 2; }
+namespace {
 
 // Workspace: partial outputs, maxima and sums of cut tiles, and who joins them.
 struct PagedLayout {
@@ -302,6 +238,111 @@ int paged_write(const bsm_paged_write_desc *d, bsm_stream_t stream)
     return BSM_OK;
 }
 
+int paged_write_rotary(const bsm_paged_write_rotary_desc *d, bsm_stream_t stream)
+{
+    if (!d || d->n_tokens < 0 || d->heads_q < 0 || d->heads_kv < 1 || d->head_dim < 1 || d->rotary_dim < 0 ||
+        d->rotary_dim > d->head_dim || d->rotary_dim % 2 || d->n_positions < 0 || d->page_size < 1 || d->n_pages < 0 ||
+        (d->flags & ~BSM_FLAG_INTERLEAVED) ||
+        (d->dtype != BSM_F32 && d->dtype != BSM_BF16 && d->dtype != BSM_F16) ||
+        (d->n_positions > 1 && d->table_stride < d->rotary_dim))
+        return BSM_ERR_INVALID_ARG;
+    if (d->n_tokens == 0)
+        return BSM_OK;
+    if (!d->k || !d->v || !d->k_cache || !d->v_cache || !d->slots || !d->positions || d->n_pages == 0 ||
+        (d->heads_q > 0 && (!d->q || !d->q_out)) || (d->rotary_dim > 0 && d->n_positions > 0 && !d->table))
+        return BSM_ERR_INVALID_ARG;
+    if ((static_cast<int64_t>(d->heads_q) + 2ll * d->heads_kv) * d->head_dim > kRotaryMost)
+        return BSM_ERR_UNSUPPORTED;
+    const int es = elem_size(d->dtype);
+    const int64_t T = d->n_tokens, hq = d->heads_q, hkv = d->heads_kv, row = static_cast<int64_t>(d->head_dim) * es;
+    const int64_t qs = hq ? extent({Dim{T, d->q_stride_token}, Dim{hq, d->q_stride_head}}, d->head_dim, es) : 0;
+    const int64_t os = hq ? extent({Dim{T, d->q_out_stride_token}, Dim{hq, d->q_out_stride_head}}, d->head_dim, es) : 0;
+    const int64_t ks = extent({Dim{T, d->k_stride_token}, Dim{hkv, d->k_stride_head}}, d->head_dim, es);
+    const int64_t vs = extent({Dim{T, d->v_stride_token}, Dim{hkv, d->v_stride_head}}, d->head_dim, es);
+    const int64_t all = extent({Dim{d->n_pages, d->kv_stride_page}, Dim{d->page_size, d->kv_stride_token},
+                                Dim{hkv, d->kv_stride_head}},
+                               d->head_dim, es);
+    const int64_t ts = d->rotary_dim > 0 && d->n_positions > 0
+                           ? extent({Dim{d->n_positions, d->table_stride}}, d->rotary_dim, 4)
+                           : 0;
+    if (qs < 0 || os < 0 || ks < 0 || vs < 0 || all < 0 || ts < 0)
+        return BSM_ERR_INVALID_ARG;
+    if (row % 16 || (hq && (misaligned(d->q, 16) || misaligned(d->q_out, 16))) || misaligned(d->k, 16) ||
+        misaligned(d->v, 16) || misaligned(d->k_cache, 16) || misaligned(d->v_cache, 16) || misaligned(d->slots, 8) ||
+        misaligned(d->positions, 4) || (ts && misaligned(d->table, 4)) ||
+        unaligned({Dim{hq ? T : 1, d->q_stride_token}, Dim{hq, d->q_stride_head}, Dim{hq ? T : 1, d->q_out_stride_token},
+                   Dim{hq, d->q_out_stride_head}, Dim{T, d->k_stride_token}, Dim{hkv, d->k_stride_head},
+                   Dim{T, d->v_stride_token}, Dim{hkv, d->v_stride_head}, Dim{d->n_pages, d->kv_stride_page},
+                   Dim{d->page_size, d->kv_stride_token}, Dim{hkv, d->kv_stride_head}},
+                  es))
+        return BSM_ERR_MISALIGNED;
+    const Span kc = span(d->k_cache, all), vc = span(d->v_cache, all), q = span(d->q, qs), o = span(d->q_out, os),
+               k = span(d->k, ks), v = span(d->v, vs), sl = span(d->slots, 8 * T), po = span(d->positions, 4 * T),
+               ta = span(d->table, ts);
+    for (const Span &c : {kc, vc})
+        for (const Span &s : {q, o, k, v, sl, po, ta})
+            if (c.meets(s))
+                return BSM_ERR_INVALID_ARG;
+    if (o.meets(sl) || o.meets(po) || o.meets(ta))
+        return BSM_ERR_INVALID_ARG;
+    Dim dims[3] = {Dim{d->n_pages, d->kv_stride_page}, Dim{d->page_size, d->kv_stride_token}, Dim{hkv, d->kv_stride_head}};
+    std::sort(dims, dims + 3, [](const Dim &x, const Dim &y) { return x.stride < y.stride; });
+    if (kc.meets(vc) && share_a_place(dims, 3, d->head_dim, (static_cast<int64_t>(vc.lo) - static_cast<int64_t>(kc.lo)) / es))
+        return BSM_ERR_INVALID_ARG;
+    // the rotated queries may lie beside the keys and values that one product made with them:
+    // only equal places clash; in place of q itself, or apart from it
+    auto clash = [&](const Span &s, int64_t token, int64_t head, int64_t n) {
+        return o.meets(s) && heads_share_a_place(T, d->q_out_stride_token, d->q_out_stride_head, hq, token, head, n, d->head_dim,
+                                                 (static_cast<int64_t>(s.lo) - static_cast<int64_t>(o.lo)) / es);
+    };
+    if (hq) {
+        const bool in_place = d->q == d->q_out && (T == 1 || d->q_stride_token == d->q_out_stride_token) &&
+                              (hq == 1 || d->q_stride_head == d->q_out_stride_head);
+        if ((!in_place && clash(q, d->q_stride_token, d->q_stride_head, hq)) ||
+            clash(k, d->k_stride_token, d->k_stride_head, hkv) || clash(v, d->v_stride_token, d->v_stride_head, hkv))
+            return BSM_ERR_INVALID_ARG;
+    }
+    PagedDev *dev = nullptr;
+    if (int rc = paged_device(-1, &dev))
+        return rc;
+    TraceRange tr("bsm_paged_write_rotary");
+    PagedRotaryArgs a{};
+    a.src[0] = static_cast<const unsigned char *>(d->q);
+    a.src[1] = static_cast<const unsigned char *>(d->k);
+    a.src[2] = static_cast<const unsigned char *>(d->v);
+    a.dst[0] = static_cast<unsigned char *>(d->q_out);
+    a.dst[1] = static_cast<unsigned char *>(d->k_cache);
+    a.dst[2] = static_cast<unsigned char *>(d->v_cache);
+    a.table = d->table;
+    a.positions = d->positions;
+    a.slots = d->slots;
+    const int64_t st[3] = {d->q_stride_token, d->k_stride_token, d->v_stride_token};
+    const int64_t sh[3] = {d->q_stride_head, d->k_stride_head, d->v_stride_head};
+    for (int i = 0; i < 3; ++i) {
+        a.src_token[i] = st[i] * es;
+        a.src_head[i] = sh[i] * es;
+    }
+    a.out_token = d->q_out_stride_token * es;
+    a.out_head = d->q_out_stride_head * es;
+    a.dst_page = d->kv_stride_page * es;
+    a.dst_token = d->kv_stride_token * es;
+    a.dst_head = d->kv_stride_head * es;
+    a.table_stride = d->table_stride;
+    a.n_slots_cache = static_cast<int64_t>(d->n_pages) * d->page_size;
+    a.n_tokens = d->n_tokens;
+    // (with nothing to rotate every position will do)
+    a.n_positions = d->rotary_dim > 0 ? d->n_positions : INT_MAX;
+    a.page = d->page_size;
+    a.heads_q = d->heads_q;
+    a.heads_kv = d->heads_kv;
+    a.half = d->rotary_dim / 2;
+    a.dim = d->head_dim;
+    a.status = dev->status;
+    if (int e = launch_paged_rotary(a, d->dtype, (d->flags & BSM_FLAG_INTERLEAVED) != 0, dev->n_sm, stream))
+        return record_cuda_error(e, "paged rotary write launch");
+    return BSM_OK;
+}
+
 int paged_attention(const bsm_paged_desc *d, bsm_stream_t stream)
 {
     if (!d || d->n_requests < 0 || d->n_tokens < 0 || d->page_size < 1 || d->n_pages < 0 || d->table_width < 1 ||
@@ -457,6 +498,11 @@ extern "C" {
 int bsm_paged_tables(const bsm_paged_tables_desc *d, bsm_stream_t stream) { return bsm::paged_tables(d, stream); }
 
 int bsm_paged_write(const bsm_paged_write_desc *d, bsm_stream_t stream) { return bsm::paged_write(d, stream); }
+
+int bsm_paged_write_rotary(const bsm_paged_write_rotary_desc *d, bsm_stream_t stream)
+{
+    return bsm::paged_write_rotary(d, stream);
+}
 
 int bsm_paged_attention(const bsm_paged_desc *d, bsm_stream_t stream) { return bsm::paged_attention(d, stream); }
 
