@@ -454,6 +454,57 @@ int bsm_paged_attention(const bsm_paged_desc *d, bsm_stream_t stream);
  * arguments it would refuse or without a device. */
 int64_t bsm_paged_workspace_bytes(int device, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t max_new);
 
+/* ---- beams: several continuations of a request, kept side by side ----
+ * A request's beams are rows r * beams .. r * beams + beams - 1 of the batch: of its
+ * logits, and of the tables and lengths of the paged cache.  After a step's logits
+ * bsm_beam_select names the best continuations, and bsm_paged_reorder lets the cache
+ * follow the beams that they grow from.  As the paged calls: on the current device, no
+ * synchronisation or allocation but for the library's first call there, nothing shared
+ * but the arguments. */
+
+/*
+ * The `keep` best continuations of every request over its beams and the vocabulary, in
+ * order.  Token t after beam b has the value
+ *     scores[b] + x[b][t] - log sum_t' exp(x[b][t'])
+ * (the logarithm of the row's softmax, added to the beam's score so far); larger values
+ * come first, equal ones by beam, then by token.  The values are held in 48 bits: a beam's
+ * tokens come in the order of their logits, and beams compare within about 1e-7.
+ *   out_scores[r][i]  the value, rounded once; parents[r][i], tokens[r][i]: its beam, 0 ..
+ *                     beams - 1, and its token.  Where a request has fewer candidates the
+ *                     rest is -inf, -1, -1.
+ *   No candidates     tokens at -inf; beams whose score is -inf (not in use yet), +inf or
+ *                     NaN; rows that hold NaN or +inf or nothing above -inf (their
+ *                     softmax is NaN); values that do not fit fp32.
+ *   ended             where ended[r][b] != 0 the beam is finished: its one candidate is
+ *                     end_token with the beam's score as it is, and its logits are not read
+ *                     (nor those of beams without a score).  May be null.
+ *   logits            F32, BF16 or F16, any address a multiple of the element size; vocab
+ *                     contiguous, strides 0 (repeated) or more.
+ *   beams, keep       1 .. 64;  vocab up to 2^20 (else BSM_ERR_UNSUPPORTED; also where
+ *                     n_requests * beams is above 2^24 - 1).
+ *   workspace         bsm_beam_select_workspace_bytes bytes, 256-byte aligned, for this call
+ *                     alone until its work is done; its contents need no preparation.
+ * The outputs and workspace overlap nothing.  The same inputs give the same bits.
+ * Errors: BSM_ERR_INVALID_ARG, BSM_ERR_MISALIGNED, BSM_ERR_UNSUPPORTED, BSM_ERR_CUDA.
+ */
+typedef struct {
+    const void *logits;                 /* n_requests x beams x vocab */
+    const float *scores;                /* n_requests x beams */
+    const uint8_t *ended;               /* n_requests x beams, or null */
+    float *out_scores;                  /* n_requests x keep, all three */
+    int32_t *parents, *tokens;
+    void *workspace;
+    int64_t workspace_bytes;
+    int64_t stride_request, stride_beam;
+    int32_t n_requests, beams, vocab, keep, end_token;
+    int32_t dtype;
+} bsm_beam_select_desc;
+int bsm_beam_select(const bsm_beam_select_desc *d, bsm_stream_t stream);
+
+/* Bytes of workspace that bsm_beam_select wants on `device` (-1: current) for these sizes
+ * and any type; -1 for arguments it would refuse or without a device. */
+int64_t bsm_beam_select_workspace_bytes(int device, int32_t n_requests, int32_t beams, int32_t vocab, int32_t keep);
+
 /* ---- plans: build the schedule once ("upfront", Sec. 5), run it many times ---- */
 
 typedef struct bsm_plan bsm_plan;

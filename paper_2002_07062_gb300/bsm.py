@@ -158,6 +158,13 @@ class PagedDesc(ctypes.Structure):
                [("flags", ctypes.c_uint32), ("scale", ctypes.c_float)]
 
 
+class BeamSelectDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("logits", "scores", "ended", "out_scores", "parents", "tokens",
+                                               "workspace")] + \
+               [(n, ctypes.c_int64) for n in ("workspace_bytes", "stride_request", "stride_beam")] + \
+               [(n, ctypes.c_int32) for n in ("n_requests", "beams", "vocab", "keep", "end_token", "dtype")]
+
+
 _lib = None
 
 
@@ -189,6 +196,8 @@ def lib():
         "bsm_paged_write_rotary": ([vp, vp], ctypes.c_int),
         "bsm_paged_attention": ([vp, vp], ctypes.c_int),
         "bsm_paged_workspace_bytes": ([ctypes.c_int, i32, i32, i32, i32], i64),
+        "bsm_beam_select": ([vp, vp], ctypes.c_int),
+        "bsm_beam_select_workspace_bytes": ([ctypes.c_int, i32, i32, i32, i32], i64),
         "bsm_plan_desc_init": ([ctypes.POINTER(PlanDesc)], ctypes.c_int),
         "bsm_plan_create": ([ctypes.POINTER(vp), ctypes.POINTER(PlanDesc)], ctypes.c_int),
         "bsm_plan_execute": ([vp, vp], ctypes.c_int),
@@ -405,17 +414,19 @@ def _packer(desc):
 
 
 _pack_tables, _pack_write, _pack_paged = _packer(PagedTablesDesc), _packer(PagedWriteDesc), _packer(PagedDesc)
-_pack_rotary = _packer(PagedWriteRotaryDesc)
+_pack_rotary, _pack_select = _packer(PagedWriteRotaryDesc), _packer(BeamSelectDesc)
 _PAGED_DTYPES = {}      # torch type -> bsm_dtype, filled on first use
 _INT32 = _INT64 = _FLOAT32 = _cuda = None
+_BYTES = ()             # types of a byte a value
 
 
 def _paged_types():
-    global _INT32, _INT64, _FLOAT32, _cuda
+    global _INT32, _INT64, _FLOAT32, _BYTES, _cuda
     import torch
     _cuda = torch.cuda
     _PAGED_DTYPES.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
     _INT32, _INT64, _FLOAT32 = torch.int32, torch.int64, torch.float32
+    _BYTES = (torch.bool, torch.uint8, torch.int8)
 
 
 def _device(t, what: str) -> int:
@@ -590,6 +601,38 @@ def bsm_paged_attention(q, k_cache, v_cache, out, starts, lengths, tables, max_n
     rc = lib().bsm_paged_attention(d, _stream(stream))
     if rc:
         _check(rc, "bsm_paged_attention")
+
+
+def bsm_beam_select_workspace_bytes(n_requests: int, beams: int, vocab: int, keep: int, device: int = -1) -> int:
+    n = int(lib().bsm_beam_select_workspace_bytes(device, n_requests, beams, vocab, keep))
+    if n < 0:
+        raise ValueError("no workspace for %d requests of %d beams, %d of %d tokens" % (n_requests, beams, keep, vocab))
+    return n
+
+
+def bsm_beam_select(logits, scores, out_scores, parents, tokens, workspace, ended=None, end_token: int = 0, stream=None):
+    """The best continuations [requests, keep] (the outputs' shape) over beams and
+    vocabulary of logits [requests, beams, vocab] (any strides; the last dimension
+    contiguous) and scores [requests, beams]; ended: bool or bytes [requests, beams]."""
+    dtype = _paged_dtype(logits)
+    dev = _device(logits, "logits")
+    st = _strided(logits, "logits", 3, dev)
+    n, beams, vocab = logits.shape
+    if scores.shape != (n, beams) or (ended is not None and (ended.shape != (n, beams) or ended.dtype not in _BYTES)):
+        raise ValueError("scores must be [%d, %d], and ended bool or bytes of that shape" % (n, beams))
+    if out_scores.dim() != 2 or out_scores.shape[0] != n or parents.shape != out_scores.shape or \
+            tokens.shape != out_scores.shape:
+        raise ValueError("out_scores, parents and tokens must be [%d, keep], all three" % n)
+    keep = out_scores.shape[1]
+    _elsewhere(workspace, "workspace", dev)
+    d = _pack_select(logits.data_ptr(), _vec(scores, "scores", _FLOAT32, 0, dev),
+                     0 if ended is None else _vec(ended, "ended", ended.dtype, 0, dev),
+                     _vec(out_scores, "out_scores", _FLOAT32, 0, dev), _vec(parents, "parents", _INT32, 0, dev),
+                     _vec(tokens, "tokens", _INT32, 0, dev), _dptr(workspace, None, "workspace"), workspace.nbytes,
+                     st[0] if n > 1 else 0, st[1] if beams > 1 else 0, n, beams, vocab, keep, end_token, dtype)
+    rc = lib().bsm_beam_select(d, _stream(stream))
+    if rc:
+        _check(rc, "bsm_beam_select")
 
 
 class Plan:

@@ -480,12 +480,15 @@ int launch_paged_rows(const PagedArgs &a, bool f16, int grid, void *stream)
 
 int paged_tables_set_smem();
 int paged_tiles_set_smem();
+int beam_set_smem_limit();
 
 int paged_set_smem_limit()
 {
     int e = paged_tables_set_smem();
     if (!e)
         e = paged_tiles_set_smem();
+    if (!e)
+        e = beam_set_smem_limit();
     auto set = [&](const void *f) {
         if (!e)
             e = static_cast<int>(cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowSmem));
