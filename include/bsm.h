@@ -313,6 +313,7 @@ int bsm_bmm_ex(const void *a, const void *bt, void *c, int64_t B, int64_t M, int
 #define BSM_PAGED_WIDTH 2u      /* a request needs more than table_width pages: the rest has no slot */
 #define BSM_PAGED_TOKENS 4u     /* more new tokens than n_slots: the rest is not written */
 #define BSM_PAGED_NEGATIVE 8u   /* a negative length, taken as 0 */
+#define BSM_PAGED_DROPPED 16u   /* bsm_paged_reorder: more dropped pages than n_dropped: the rest is not listed */
 typedef struct {
     const int32_t *cached, *fresh;      /* n_requests */
     const int32_t *free_pages;          /* n_free */
@@ -504,6 +505,62 @@ int bsm_beam_select(const bsm_beam_select_desc *d, bsm_stream_t stream);
 /* Bytes of workspace that bsm_beam_select wants on `device` (-1: current) for these sizes
  * and any type; -1 for arguments it would refuse or without a device. */
 int64_t bsm_beam_select_workspace_bytes(int device, int32_t n_requests, int32_t beams, int32_t vocab, int32_t keep);
+
+/*
+ * The paged cache follows the beams that were kept.  New row i of request r goes on where
+ * row p = parents[r][i] (0 .. beams - 1, of the same request) is:
+ *   new_lengths[r * beams + i]  lengths[r * beams + p]
+ *   new_tables[r * beams + i]   its first ceil(length / page_size) entries are row p's;
+ *                               others stay.
+ * Whole pages are shared by the rows that hold them.  A last page that is partly filled (the
+ * next token is written there) stays with the first new row of the request that takes it; every
+ * later one gets the next page of free_pages (in order of requests and rows), with the
+ * tokens in use copied to it, keys and values of all layers, and -1 once they have run out.
+ *   parents   negative: the row is out of use, of length 0 and without entries; beams or
+ *             more: the same, and sets BSM_DEV_BOUNDS.
+ *   dropped   pages that old rows of the request held and no new row holds in that column, each
+ *             once, in order of requests, columns and rows: what the caller may put back to
+ *             its free pages (a page that requests share is dropped by a request when none of
+ *             its rows holds it any more).  Entries past info[2] stay.
+ *   info[0..3]  pages taken; pages missing; pages dropped; BSM_PAGED_* bits
+ * free_pages is not changed: drop its first info[0] entries.  The rows of one request alone
+ * share partly filled pages; a page is in one column.  A row whose last page is missing (-1)
+ * passes that on.  Lengths outside 0 .. table_width * page_size are cut to it and set
+ * BSM_DEV_BOUNDS; so does a last page or a free page whose id lies outside the cache (it is
+ * handed on as it is, and nothing copied).
+ *   new_lengths, new_tables  lengths and tables themselves (in place, the same stride), or
+ *             apart from them.
+ *   caches    dtype, rows, pointers and strides as bsm_paged_write, with a stride from layer
+ *             to layer (n_layers 1: any).
+ *   workspace bsm_paged_reorder_workspace_bytes bytes, 256-byte aligned, for this call alone
+ *             until its work is done; its contents need no preparation.
+ * Out of place a repeated call gives the same answer.  Outputs, caches and workspace
+ * overlap each other and inputs nowhere else (keys and values may interleave).
+ * Errors: BSM_ERR_INVALID_ARG, BSM_ERR_MISALIGNED, BSM_ERR_UNSUPPORTED (more than 64 beams,
+ * tables of 2^20 entries a row and wider, more than 2^31 - 4096 rows, pages of 32 GiB),
+ * BSM_ERR_CUDA.
+ */
+typedef struct {
+    const int32_t *parents;             /* n_requests rows of beams, parent_stride apart */
+    const int32_t *lengths;             /* n_requests * beams */
+    const int32_t *tables;              /* n_requests * beams rows of table_width, table_stride apart */
+    const int32_t *free_pages;          /* n_free */
+    int32_t *new_lengths, *new_tables;  /* as lengths and tables, new_table_stride apart */
+    int32_t *dropped;                   /* n_dropped */
+    int64_t *info;                      /* 4 */
+    void *k_cache, *v_cache;            /* n_layers x n_pages x page_size x n_heads x head_dim, any order of strides */
+    void *workspace;
+    int64_t workspace_bytes;
+    int64_t parent_stride, table_stride, new_table_stride;
+    int64_t kv_stride_layer, kv_stride_page, kv_stride_token, kv_stride_head;   /* of both caches */
+    int32_t n_requests, beams, table_width, n_free, n_dropped, page_size, n_layers, n_pages, n_heads, head_dim;
+    int32_t dtype;
+} bsm_paged_reorder_desc;
+int bsm_paged_reorder(const bsm_paged_reorder_desc *d, bsm_stream_t stream);
+
+/* Bytes of workspace that bsm_paged_reorder wants for these sizes; -1 for arguments it
+ * would refuse. */
+int64_t bsm_paged_reorder_workspace_bytes(int32_t n_requests, int32_t beams, int32_t table_width);
 
 /* ---- plans: build the schedule once ("upfront", Sec. 5), run it many times ---- */
 

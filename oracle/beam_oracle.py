@@ -1,5 +1,5 @@
-"""Rotation by positions and beam selection from their definitions, in 64 bits.
-Shares no code with the library."""
+"""Rotation by positions, beam selection and beam reordering from their
+definitions, by plain loops and in 64 bits.  Shares no code with the library."""
 from __future__ import annotations
 
 import math
@@ -56,3 +56,45 @@ def select(logits, scores, keep, ended=None, end_token=0):
         for i, (v, b, t) in enumerate(cand[:keep]):
             values[r, i], parents[r, i], tokens[r, i] = v, b, t
     return values, parents, tokens
+
+
+def reorder(parents, lengths, tables, free, page):
+    """New (lengths, tables as {(row, column): page}, copies [(source, page, tokens)],
+    missing, dropped) for parents [n][beams], lengths and tables of n * beams rows."""
+    n, B = len(parents), len(parents[0])
+    need = lambda L: -(-L // page)
+    new_len, new_tab, copies, missing, dropped = [], {}, [], 0, []
+    taken = 0
+    for r in range(n):
+        held = set()
+        rows = []
+        for i in range(B):
+            p = parents[r][i]
+            L = lengths[r * B + p] if 0 <= p < B else 0
+            row = [int(tables[r * B + p][c]) for c in range(need(L))] if L else []
+            if L % page and row[-1] >= 0:
+                if row[-1] in held:
+                    if taken < len(free):
+                        copies.append((row[-1], int(free[taken]), L % page))
+                        row[-1] = int(free[taken])
+                        taken += 1
+                    else:
+                        row[-1] = -1
+                        missing += 1
+                else:
+                    held.add(row[-1])
+            rows.append(row)
+            new_len.append(L)
+            for c, v in enumerate(row):
+                new_tab[r * B + i, c] = v
+        most = max(need(lengths[r * B + b]) for b in range(B))
+        for c in range(most):
+            now = {row[c] for row in rows if c < len(row)}
+            seen = set()
+            for b in range(B):
+                if c < need(lengths[r * B + b]):
+                    e = int(tables[r * B + b][c])
+                    if e >= 0 and e not in now and e not in seen:
+                        dropped.append(e)
+                    seen.add(e)
+    return new_len, new_tab, copies, missing, dropped

@@ -30,7 +30,7 @@ OP_FORWARD, OP_BACKWARD = 0, 1
 MAX_DIES = 4
 MAX_SM = 256
 DEV_BOUNDS, DEV_TIMEOUT, DEV_CHECK = 1, 2, 4
-PAGED_PAGES, PAGED_WIDTH, PAGED_TOKENS, PAGED_NEGATIVE = 1, 2, 4, 8
+PAGED_PAGES, PAGED_WIDTH, PAGED_TOKENS, PAGED_NEGATIVE, PAGED_DROPPED = 1, 2, 4, 8, 16
 
 (OK, ERR_INVALID_ARG, ERR_MISALIGNED, ERR_UNSUPPORTED, ERR_CUDA, ERR_DEVICE_BOUNDS,
  ERR_TIMEOUT, ERR_NO_DEVICE, ERR_NOMEM, ERR_TOO_LARGE) = range(10)
@@ -165,6 +165,15 @@ class BeamSelectDesc(ctypes.Structure):
                [(n, ctypes.c_int32) for n in ("n_requests", "beams", "vocab", "keep", "end_token", "dtype")]
 
 
+class PagedReorderDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("parents", "lengths", "tables", "free_pages", "new_lengths", "new_tables",
+                                               "dropped", "info", "k_cache", "v_cache", "workspace")] + \
+               [(n, ctypes.c_int64) for n in ("workspace_bytes", "parent_stride", "table_stride", "new_table_stride",
+                                              "kv_stride_layer", "kv_stride_page", "kv_stride_token", "kv_stride_head")] + \
+               [(n, ctypes.c_int32) for n in ("n_requests", "beams", "table_width", "n_free", "n_dropped", "page_size",
+                                              "n_layers", "n_pages", "n_heads", "head_dim", "dtype")]
+
+
 _lib = None
 
 
@@ -198,6 +207,8 @@ def lib():
         "bsm_paged_workspace_bytes": ([ctypes.c_int, i32, i32, i32, i32], i64),
         "bsm_beam_select": ([vp, vp], ctypes.c_int),
         "bsm_beam_select_workspace_bytes": ([ctypes.c_int, i32, i32, i32, i32], i64),
+        "bsm_paged_reorder": ([vp, vp], ctypes.c_int),
+        "bsm_paged_reorder_workspace_bytes": ([i32, i32, i32], i64),
         "bsm_plan_desc_init": ([ctypes.POINTER(PlanDesc)], ctypes.c_int),
         "bsm_plan_create": ([ctypes.POINTER(vp), ctypes.POINTER(PlanDesc)], ctypes.c_int),
         "bsm_plan_execute": ([vp, vp], ctypes.c_int),
@@ -414,7 +425,7 @@ def _packer(desc):
 
 
 _pack_tables, _pack_write, _pack_paged = _packer(PagedTablesDesc), _packer(PagedWriteDesc), _packer(PagedDesc)
-_pack_rotary, _pack_select = _packer(PagedWriteRotaryDesc), _packer(BeamSelectDesc)
+_pack_rotary, _pack_select, _pack_reorder = _packer(PagedWriteRotaryDesc), _packer(BeamSelectDesc), _packer(PagedReorderDesc)
 _PAGED_DTYPES = {}      # torch type -> bsm_dtype, filled on first use
 _INT32 = _INT64 = _FLOAT32 = _cuda = None
 _BYTES = ()             # types of a byte a value
@@ -481,20 +492,20 @@ def _paged_dtype(first, *others):
     return code
 
 
-def _caches(k_cache, v_cache, dev: int):
-    st, shape = _strided(k_cache, "k_cache", 4, dev), k_cache.shape
-    sv = _strided(v_cache, "v_cache", 4, dev)
+def _caches(k_cache, v_cache, dev: int, ndim: int = 4):
+    st, shape = _strided(k_cache, "k_cache", ndim, dev), k_cache.shape
+    sv = _strided(v_cache, "v_cache", ndim, dev)
     if v_cache.shape != shape or (sv != st and any(x != y and n > 1 for x, y, n in zip(st, sv, shape))):
         raise ValueError("k_cache and v_cache must have the same shape and strides")
     return st
 
 
-def _page_tables(tables, n: int, dev: int):
+def _page_tables(tables, n: int, dev: int, what: str = "tables"):
     """(address, row stride, width) of the page tables of n requests."""
-    st = _strided(tables, "tables", 2, dev)
+    st = _strided(tables, what, 2, dev)
     rows, width = tables.shape
     if tables.dtype is not _INT32 or rows < n:
-        raise ValueError("tables must be %s, a row for each of %d requests" % (_INT32, n))
+        raise ValueError("%s must be %s, a row for each of %d requests" % (what, _INT32, n))
     return tables.data_ptr(), st[0] if rows > 1 else width, width
 
 
@@ -633,6 +644,44 @@ def bsm_beam_select(logits, scores, out_scores, parents, tokens, workspace, ende
     rc = lib().bsm_beam_select(d, _stream(stream))
     if rc:
         _check(rc, "bsm_beam_select")
+
+
+def bsm_paged_reorder_workspace_bytes(n_requests: int, beams: int, table_width: int) -> int:
+    n = int(lib().bsm_paged_reorder_workspace_bytes(n_requests, beams, table_width))
+    if n < 0:
+        raise ValueError("no workspace for %d requests of %d beams, tables of %d" % (n_requests, beams, table_width))
+    return n
+
+
+def bsm_paged_reorder(parents, lengths, tables, free_pages, new_lengths, new_tables, dropped, info, k_cache, v_cache,
+                      workspace, stream=None):
+    """The paged cache [pages, page_size, heads, dim], or that of all layers [layers, pages,
+    page_size, heads, dim], follows parents [requests, beams]; tables and lengths have a row
+    for each beam (new_tables and new_lengths may be the same tensors)."""
+    dtype = _paged_dtype(k_cache, v_cache)
+    dev, ndim = _device(k_cache, "k_cache"), 5 if len(k_cache.shape) == 5 else 4
+    cs, shape = _caches(k_cache, v_cache, dev, ndim), k_cache.shape
+    if ndim == 4:
+        cs, shape = (0, *cs), (1, *shape)
+    ps = _strided(parents, "parents", 2, dev)
+    n, beams = parents.shape
+    if parents.dtype is not _INT32:
+        raise ValueError("parents must be %s (got %s)" % (_INT32, parents.dtype))
+    tab, stride, width = _page_tables(tables, n * beams, dev)
+    new_tab, new_stride, new_width = _page_tables(new_tables, n * beams, dev, "new_tables")
+    if new_width != width:
+        raise ValueError("new_tables must be as wide as tables (%d)" % width)
+    _elsewhere(workspace, "workspace", dev)
+    d = _pack_reorder(parents.data_ptr(), _vec(lengths, "lengths", _INT32, n * beams, dev), tab,
+                      _vec(free_pages, "free_pages", _INT32, 0, dev),
+                      _vec(new_lengths, "new_lengths", _INT32, n * beams, dev), new_tab,
+                      _vec(dropped, "dropped", _INT32, 0, dev), _vec(info, "info", _INT64, 4, dev), k_cache.data_ptr(),
+                      v_cache.data_ptr(), _dptr(workspace, None, "workspace"), workspace.nbytes,
+                      ps[0] if n > 1 else 0, stride, new_stride, *cs[:4], n, beams, width, free_pages.numel(),
+                      dropped.numel(), shape[2], shape[0], shape[1], shape[3], shape[4], dtype)
+    rc = lib().bsm_paged_reorder(d, _stream(stream))
+    if rc:
+        _check(rc, "bsm_paged_reorder")
 
 
 class Plan:

@@ -2,6 +2,7 @@
 // Not part of the public ABI.
 #pragma once
 
+#include <climits>
 #include <cstdint>
 
 #include "../../include/bsm.h"
@@ -37,6 +38,27 @@ struct BeamSelectArgs {
     int32_t n, beams, vocab, keep, end_token;
     int32_t parts, part;                        // parts of a row, logits of each
 };
+
+constexpr int kReorderTile = 128;               // columns of the tables that a CTA takes
+constexpr int64_t kReorderMost = INT32_MAX;     // requests x tiles, and pieces of 16 bytes of a page
+
+struct PagedReorderArgs {
+    const int32_t *parents, *lengths, *tables, *free_pages;
+    int32_t *new_lengths, *new_tables, *dropped;
+    int64_t *info;
+    unsigned char *cache[2];
+    int64_t layer, page_bytes, token, head;     // strides of the caches, bytes
+    int64_t parent_stride, table_stride, new_table_stride;
+    // workspace: per row its new length and the page that it copies from; per request and
+    // tile the rows that copy (a bit each) and the pages that it dropped
+    int32_t *row_length, *row_source;
+    uint64_t *copies;
+    int32_t *counts, *lists;
+    int32_t n, beams, width, tiles, n_free, n_dropped, page, n_pages, heads, chunks, layers;
+    uint32_t *status;
+};
+
+int launch_paged_reorder(const PagedReorderArgs &a, int n_sm, void *stream);
 
 // How rows of `vocab` logits are cut: *parts of *part logits (whole pieces of 16 bytes).
 void beam_parts(int64_t rows, int32_t vocab, int es, int n_sm, int32_t *parts, int32_t *part);
