@@ -13,11 +13,11 @@ constexpr int kBeamMost = 64;                   // beams of a request, and conti
 constexpr int32_t kBeamMostVocab = 1 << 20;
 constexpr int kBeamThreads = 512;               // of a part of a row
 constexpr int kBeamLoads = 4;                   // pieces of 16 bytes that a thread holds
-constexpr int kBeamMostParts = 128;             // of a row: kBeamMostVocab fp32 logits
+constexpr int kBeamMostParts = 128;             // of a row
 
 // The best logits of a part of a row, and what its softmax needs.
 struct BeamPart {
-    double sum;                                 // of exp(x - top)
+    float sum, rest;                            // of exp(x - top): two numbers that add up to it
     float top;
     int32_t count;                              // entries in its list
 };
@@ -37,6 +37,7 @@ struct BeamSelectArgs {
     int64_t stride_request, stride_beam;        // bytes
     int32_t n, beams, vocab, keep, end_token;
     int32_t parts, part;                        // parts of a row, logits of each
+    int32_t list;                               // entries of a part's list (set by the launch)
 };
 
 constexpr int kReorderTile = 128;               // columns of the tables that a CTA takes
@@ -63,7 +64,7 @@ int launch_paged_reorder(const PagedReorderArgs &a, int n_sm, void *stream);
 // How rows of `vocab` logits are cut: *parts of *part logits (whole pieces of 16 bytes).
 void beam_parts(int64_t rows, int32_t vocab, int es, int n_sm, int32_t *parts, int32_t *part);
 
-int launch_beam_select(const BeamSelectArgs &a, int dtype, void *stream);
+int launch_beam_select(BeamSelectArgs a, int dtype, void *stream);
 int beam_set_smem_limit();
 
 }  // namespace bsm

@@ -16,9 +16,12 @@ NEG = -float("inf")
 
 def _tol(V, v):
     """The sum's terms: 2^-22 of the exponential and, for its argument (a difference and a product, half a
-    step each, and log2(e) in fp32), 3 x 2^-24 of its size, whose mean under the softmax is at most log V; 37 + 7
-    additions of half a step; the join's weights 2 x 2^-24.  And the value's own rounding."""
-    return 2.0 ** -24 * (4 + 3 * math.log(V + 1) + 44 + 2 + np.abs(v))
+    step each, and log2(e) in fp32), 3 x 2^-24 of its size, whose mean under the softmax is at most log V;
+    additions of half a step: 16 of a block, one for each of up to 64 blocks, 5 over a warp, one of a block's two
+    halves; what was summed before a larger maximum came is multiplied by another such exponential, at
+    most once a block and at the end, and the parts by one of 2 x 2^-24.  And the value's own rounding."""
+    blocks = -(-V // 8192)
+    return 2.0 ** -24 * ((blocks + 2) * (4 + 3 * math.log(V + 1)) + 22 + blocks + 2 + np.abs(v))
 
 
 def _run(logits, scores, keep, ended=None, end_token=0, stream=None, ws=None):
