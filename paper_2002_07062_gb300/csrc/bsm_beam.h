@@ -11,9 +11,11 @@ namespace bsm {
 
 constexpr int kBeamMost = 64;                   // beams of a request, and continuations kept
 constexpr int32_t kBeamMostVocab = 1 << 20;
+constexpr int64_t kBeamMostRows = (1 << 24) - 1;
 constexpr int kBeamThreads = 512;               // of a part of a row
 constexpr int kBeamLoads = 4;                   // pieces of 16 bytes that a thread holds
-constexpr int kBeamMostParts = 128;             // of a row
+constexpr int kBeamMostLists = 128;             // parts of all rows of a request
+constexpr int64_t kTogetherBytes = 128 << 10;   // of logits that a CTA of a cluster reads at most
 
 // The best logits of a part of a row, and what its softmax needs.
 struct BeamPart {
@@ -61,10 +63,14 @@ struct PagedReorderArgs {
 
 int launch_paged_reorder(const PagedReorderArgs &a, int n_sm, void *stream);
 
-// How rows of `vocab` logits are cut: *parts of *part logits (whole pieces of 16 bytes).
-void beam_parts(int64_t rows, int32_t vocab, int es, int n_sm, int32_t *parts, int32_t *part);
+// How rows of `vocab` logits are cut: parts of `part` logits (whole pieces of 16 bytes).
+struct BeamCut {
+    int32_t parts, part;
+    bool together;                              // a cluster takes a request, in one launch
+};
+BeamCut beam_cut(int32_t n, int32_t beams, int32_t vocab, int es, int n_sm);
 
-int launch_beam_select(BeamSelectArgs a, int dtype, void *stream);
+int launch_beam_select(BeamSelectArgs a, int dtype, bool together, void *stream);
 int beam_set_smem_limit();
 
 }  // namespace bsm

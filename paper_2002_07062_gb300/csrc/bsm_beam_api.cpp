@@ -18,15 +18,15 @@ namespace {
 int64_t up256(int64_t x) { return (x + 255) & ~int64_t(255); }
 
 struct SelectLayout {
-    int32_t parts, part;
+    BeamCut cut;
     int64_t meta, bytes;
 };
 
-SelectLayout select_layout(int64_t rows, int32_t vocab, int32_t keep, int es, int n_sm)
+SelectLayout select_layout(int32_t n, int32_t beams, int32_t vocab, int32_t keep, int es, int n_sm)
 {
     SelectLayout l{};
-    beam_parts(rows, vocab, es, n_sm, &l.parts, &l.part);
-    const int64_t lists = rows * l.parts;
+    l.cut = beam_cut(n, beams, vocab, es, n_sm);
+    const int64_t lists = static_cast<int64_t>(n) * beams * l.cut.parts;
     l.meta = up256(lists * keep * static_cast<int64_t>(sizeof(BeamEntry)));
     l.bytes = l.meta + up256(lists * static_cast<int64_t>(sizeof(BeamPart)));
     return l;
@@ -40,7 +40,7 @@ bool select_sizes(int32_t n, int32_t beams, int32_t vocab, int32_t keep)
 bool select_limits(int32_t n, int32_t beams, int32_t vocab, int32_t keep)
 {
     return beams <= kBeamMost && keep <= kBeamMost && vocab <= kBeamMostVocab &&
-           static_cast<int64_t>(n) * beams * kBeamMostParts <= INT32_MAX;
+           static_cast<int64_t>(n) * beams <= kBeamMostRows;
 }
 
 int beam_select(const bsm_beam_select_desc *d, bsm_stream_t stream)
@@ -78,7 +78,7 @@ int beam_select(const bsm_beam_select_desc *d, bsm_stream_t stream)
     PagedDev *dev = nullptr;
     if (int rc = paged_device(-1, &dev))
         return rc;
-    const SelectLayout l = select_layout(rows, d->vocab, d->keep, es, dev->n_sm);
+    const SelectLayout l = select_layout(d->n_requests, d->beams, d->vocab, d->keep, es, dev->n_sm);
     if (d->workspace_bytes < l.bytes)
         return BSM_ERR_INVALID_ARG;
     TraceRange tr("bsm_beam_select");
@@ -99,9 +99,9 @@ int beam_select(const bsm_beam_select_desc *d, bsm_stream_t stream)
     a.vocab = d->vocab;
     a.keep = d->keep;
     a.end_token = d->end_token;
-    a.parts = l.parts;
-    a.part = l.part;
-    if (int e = launch_beam_select(a, d->dtype, stream))
+    a.parts = l.cut.parts;
+    a.part = l.cut.part;
+    if (int e = launch_beam_select(a, d->dtype, l.cut.together, stream))
         return record_cuda_error(e, "beam select launch");
     return BSM_OK;
 }
@@ -254,9 +254,8 @@ int64_t bsm_beam_select_workspace_bytes(int device, int32_t n_requests, int32_t 
     bsm::PagedDev *dev = nullptr;
     if (bsm::paged_device(device, &dev))
         return -1;
-    const int64_t rows = static_cast<int64_t>(n_requests) * beams;
-    return std::max(bsm::select_layout(rows, vocab, keep, 2, dev->n_sm).bytes,
-                    bsm::select_layout(rows, vocab, keep, 4, dev->n_sm).bytes);
+    return std::max(bsm::select_layout(n_requests, beams, vocab, keep, 2, dev->n_sm).bytes,
+                    bsm::select_layout(n_requests, beams, vocab, keep, 4, dev->n_sm).bytes);
 }
 
 }  // extern "C"

@@ -21,6 +21,7 @@ constexpr int kGroups = 128;                    // groups of neighbouring thread
 constexpr int kGroupLanes = kBeamThreads / kGroups;
 constexpr int kWarps = kBeamThreads / 32;
 constexpr int kRowCtas = 3;                      // of select_rows on an SM
+constexpr int kCluster = 16;                     // CTAs of select_together that share a request
 
 __device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
 
@@ -77,11 +78,39 @@ __device__ __forceinline__ uint4 shifted(const uint4 &a, const uint4 &b, uint32_
                       __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits));
 }
 
-// A thread's pieces of the block that starts at `first`, -inf from hi on (the end of the part, or
-// of the row of n).  A row may start `off` bytes past a 16-byte boundary: its pieces are put
-// together from two neighbouring aligned ones (the second is the next lane's first and comes
-// from the first-level cache), at the row's ends from single values.  Which values a
-// thread gets depends on their index alone, so equal rows give equal sums wherever they lie.
+// Values [i, i + W) of a row of n, -inf from hi on (the end of a part, or of the row).  A row may
+// start `off` bytes past a 16-byte boundary: its pieces are put together from two neighbouring aligned
+// ones (the second is the next lane's first and comes from the first-level cache), at the row's ends from
+// single values.  Which values a thread gets depends on their index alone, so equal rows give equal
+// sums wherever they lie.
+template <int kType>
+__device__ __forceinline__ uint4 load_piece(const unsigned char *row, uint32_t off, int32_t i, int32_t hi, int32_t n)
+{
+    using T = Word<kType>;
+    constexpr int W = T::kW;
+    uint32_t w[4] = {T::kNone, T::kNone, T::kNone, T::kNone};
+    if (i >= hi)
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    const unsigned char *p = row + static_cast<int64_t>(i) * T::kEs;
+    if (off == 0 ? i + W <= n : i > 0 && i + 2 * W <= n) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(p - off);
+        return off == 0 ? v : shifted(v, *reinterpret_cast<const uint4 *>(p - off + 16), off);
+    }
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+        if (i + k >= n)
+            continue;
+        if (T::kN == 1) {
+            w[k % 4] = reinterpret_cast<const uint32_t *>(p)[k];
+        } else {
+            const uint32_t h = reinterpret_cast<const uint16_t *>(p)[k];
+            w[k / 2 % 4] = k % 2 ? (w[k / 2 % 4] & 0xffffu) | h << 16 : (w[k / 2 % 4] & 0xffff0000u) | h;
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// A thread's pieces of the block that starts at `first`.
 template <int kType>
 __device__ __forceinline__ void load_block(uint4 (&v)[kBeamLoads], const unsigned char *row, uint32_t off, int32_t first,
                                            int32_t hi, int32_t n)
@@ -89,8 +118,8 @@ __device__ __forceinline__ void load_block(uint4 (&v)[kBeamLoads], const unsigne
     using T = Word<kType>;
     constexpr int W = T::kW, kStep = kBeamThreads * W;          // values between a thread's pieces
     const int32_t mine = first + static_cast<int32_t>(threadIdx.x) * W;
-    const unsigned char *p = row + static_cast<int64_t>(mine) * T::kEs - off;
     if (first + kBeamLoads * kStep <= hi && (off == 0 || (first > 0 && first + kBeamLoads * kStep + W <= n))) {
+        const unsigned char *p = row + static_cast<int64_t>(mine) * T::kEs - off;
 #pragma unroll
         for (int j = 0; j < kBeamLoads; ++j)
             v[j] = *reinterpret_cast<const uint4 *>(p + j * kStep * T::kEs);
@@ -102,32 +131,8 @@ __device__ __forceinline__ void load_block(uint4 (&v)[kBeamLoads], const unsigne
         return;
     }
 #pragma unroll
-    for (int j = 0; j < kBeamLoads; ++j) {
-        const int32_t i = mine + j * kStep;
-        const unsigned char *q = p + j * kStep * T::kEs;
-        v[j] = make_uint4(T::kNone, T::kNone, T::kNone, T::kNone);
-        if (i >= hi)
-            continue;
-        if (off == 0 ? i + W <= n : i > 0 && i + 2 * W <= n) {
-            v[j] = *reinterpret_cast<const uint4 *>(q);
-            if (off != 0)
-                v[j] = shifted(v[j], *reinterpret_cast<const uint4 *>(q + 16), off);
-            continue;
-        }
-        uint32_t w[4] = {T::kNone, T::kNone, T::kNone, T::kNone};
-#pragma unroll
-        for (int k = 0; k < W; ++k) {
-            if (i + k >= n)
-                continue;
-            if (T::kN == 1) {
-                w[k % 4] = reinterpret_cast<const uint32_t *>(q + off)[k];
-            } else {
-                const uint32_t h = reinterpret_cast<const uint16_t *>(q + off)[k];
-                w[k / 2 % 4] = k % 2 ? (w[k / 2 % 4] & 0xffffu) | h << 16 : (w[k / 2 % 4] & 0xffff0000u) | h;
-            }
-        }
-        v[j] = make_uint4(w[0], w[1], w[2], w[3]);
-    }
+    for (int j = 0; j < kBeamLoads; ++j)
+        v[j] = load_piece<kType>(row, off, mine + j * kStep, hi, n);
 }
 
 // Two fp32 numbers whose sum stands for a value of 48 bits.
@@ -149,8 +154,7 @@ __device__ __forceinline__ Pair add(const Pair &x, const Pair &y)
 struct PartSmem {
     float group[kGroups];               // the largest value of each group
     int32_t first[kGroups];             // where a group's value ties with the bound: its lowest token
-    float warp_top[kWarps], warp_sum[kWarps], warp_bound[kWarps];
-    uint4 hit[kWarps][kBeamLoads];      // the pieces of a lane that has something for the list
+    float warp_top[kWarps], warp_sum[kWarps], warp_bound[kWarps];   // (tops and sums: one pair a warp)
     int32_t count, last;
 };
 
@@ -201,9 +205,10 @@ __device__ __forceinline__ void rank_list(const BeamEntry *list, int count, int 
         const int i = i0 + lane / 4;
         const BeamEntry e = list[i < count ? i : 0];
         int better = 0;
+#pragma unroll 4
         for (int k = quarter; k < count; k += 4) {
             const BeamEntry o = list[k];
-            better += o.x > e.x || (o.x == e.x && o.token < e.token);
+            better += (o.x > e.x) | ((o.x == e.x) & (o.token < e.token));
         }
         better += __shfl_xor_sync(0xffffffffu, better, 1);
         better += __shfl_xor_sync(0xffffffffu, better, 2);
@@ -212,20 +217,16 @@ __device__ __forceinline__ void rank_list(const BeamEntry *list, int count, int 
     }
 }
 
-// A block's bound: the smallest of its group maxima that fewer than `keep` exceed, so that `keep`
-// of its values reach it (-inf where fewer than `keep` groups have any).  Where more groups than that
-// reach it some tie there: of values equal to the bound only those up to token *last are
-// needed then, and those that count lie in `keep` groups at most.
-template <int kType>
-__device__ __forceinline__ float block_bound(PartSmem &s, const uint4 (&v)[kBeamLoads], float mine, int32_t first, int keep, int32_t *last)
+// The smallest of the group maxima that fewer than `keep` groups exceed, so that `keep` values reach it
+// (-inf where fewer than `keep` groups have any).  best: this thread's largest value; becomes
+// its group's.  Everything written before by the block can be read after it.
+__device__ __forceinline__ float group_bound(PartSmem &s, float &best, int keep)
 {
     const int tid = threadIdx.x, lane = tid & 31;
-    float best = mine;
 #pragma unroll
     for (int o = 1; o < kGroupLanes; o <<= 1)
         best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, o));
-    const bool speaks = tid % kGroupLanes == 0;
-    if (speaks)
+    if (tid % kGroupLanes == 0)
         s.group[tid / kGroupLanes] = best;
     __syncthreads();
     int over = 0;                       // (a group's threads share the count)
@@ -248,6 +249,18 @@ __device__ __forceinline__ float block_bound(PartSmem &s, const uint4 (&v)[kBeam
 #pragma unroll
     for (int o = 1; o < kWarps; o <<= 1)
         bound = fminf(bound, __shfl_xor_sync(0xffffffffu, bound, o));
+    return bound;
+}
+
+// A block's bound.  Where more than `keep` groups reach it some tie there: of values equal to the bound
+// only those up to token *last are needed then, and those that count lie in `keep` groups at most.
+template <int kType>
+__device__ __forceinline__ float block_bound(PartSmem &s, const uint4 (&v)[kBeamLoads], float mine, int32_t first, int keep, int32_t *last)
+{
+    const int tid = threadIdx.x;
+    const bool speaks = tid % kGroupLanes == 0;
+    float best = mine;
+    const float bound = group_bound(s, best, keep);
     *last = bound == neg_inf() ? -1 : INT_MAX;
     if (bound == neg_inf() || __syncthreads_count(speaks && best >= bound) <= keep)
         return bound;
@@ -278,39 +291,34 @@ __device__ __forceinline__ float block_bound(PartSmem &s, const uint4 (&v)[kBeam
     return bound;
 }
 
-// Values above the bound, and equal ones up to token `last`, to the list, in any order.  Few
-// lanes have one: each such lane's values are looked at by the whole warp.  Entries past the
-// list's end are counted only.
+// Values above the bound, and equal ones up to token `last`, to the list, in any order; pieces
+// without one are skipped.  Entries past the list's end are counted only.
 template <int kType>
 __device__ __forceinline__ void to_list(PartSmem &s, BeamEntry *list, int room, const uint4 (&v)[kBeamLoads], float mine, int32_t first,
                                         float bound, int32_t last)
 {
     using T = Word<kType>;
-    constexpr int kMine = kBeamLoads * T::kW;
-    static_assert(kMine <= 32, "a lane each");
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    uint32_t has = __ballot_sync(0xffffffffu, (last < 0 ? mine > bound : mine >= bound) && mine > neg_inf());
-    while (has) {
-        const int l = __ffs(static_cast<int>(has)) - 1;
-        has &= has - 1;
-        if (lane == l) {
+    if ((last < 0 ? mine <= bound : mine < bound) || mine == neg_inf())
+        return;
 #pragma unroll
-            for (int j = 0; j < kBeamLoads; ++j)
-                s.hit[warp][j] = v[j];
-        }
-        __syncwarp();
-        if (lane < kMine) {
+    for (int j = 0; j < kBeamLoads; ++j) {
+        const uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
+        float ends[T::kN];
+        T::get(T::larger(T::larger(w[0], w[1]), T::larger(w[2], w[3])), ends);
+        if (!(fmaxf(ends[0], ends[T::kN - 1]) >= bound))
+            continue;
+        const int32_t token = first + (j * kBeamThreads + static_cast<int>(threadIdx.x)) * T::kW;
+#pragma unroll
+        for (int k = 0; k < T::kW; ++k) {
             float x[T::kN];
-            T::get(reinterpret_cast<const uint32_t *>(s.hit[warp])[lane / T::kN], x);
-            const float one = T::kN == 2 && lane % 2 ? x[T::kN - 1] : x[0];
-            const int32_t token = first + (lane / T::kW * kBeamThreads + warp * 32 + l) * T::kW + lane % T::kW;
-            if (one > bound || (one == bound && token <= last)) {
+            T::get(w[k / T::kN], x);
+            const float one = x[k % T::kN];
+            if ((one > bound) | ((one == bound) & (token + k <= last))) {
                 const int i = atomicAdd(&s.count, 1);
                 if (i < room)
-                    list[i] = BeamEntry{one, token};
+                    list[i] = BeamEntry{one, token + k};
             }
         }
-        __syncwarp();
     }
 }
 
@@ -363,48 +371,45 @@ __device__ __noinline__ int list_again(PartSmem &s, BeamEntry *list, int room, i
 }
 
 // One part of a row, a block of values (64 bytes a thread) after the other.  Each thread keeps a
-// maximum and a sum of exponentials of its own.  What can be among the part's best goes to
-// a list: the first block's values that reach its bound, and later ones that exceed it, about `keep`
-// a block where the row is in no order; the warps go their own ways from the second block on.
-template <int kType> __global__ void __launch_bounds__(kBeamThreads, kRowCtas) select_rows(const BeamSelectArgs a)
+// maximum and a sum of exponentials of its own and waits for nobody.  At the end the keep-th largest
+// of 128 group maxima is a bound that the part's best `keep` values reach and few others (about
+// as many again): the threads whose maximum reaches it are few, and what they have seen is
+// read once more, from the L2 cache, by their warps.
+// kEager: the first block is asked for before it is known whether the beam needs it.
+template <int kType, bool kEager>
+__device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, BeamEntry *list, uint32_t at, BeamPart *meta, BeamEntry *to)
 {
     using T = Word<kType>;
     constexpr int kBlock = kBeamThreads * kBeamLoads * T::kW;           // values of a block
-    __shared__ PartSmem s;
-    extern __shared__ __align__(16) unsigned char raw_list[];
-    BeamEntry *list = reinterpret_cast<BeamEntry *>(raw_list);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    grid_dependency_wait();
-    grid_launch_dependents();
-    const uint32_t row = blockIdx.x / static_cast<uint32_t>(a.parts);
-    const int32_t part = static_cast<int32_t>(blockIdx.x - row * a.parts);
+    const uint32_t row = at / static_cast<uint32_t>(a.parts);
+    const int32_t part = static_cast<int32_t>(at - row * a.parts);
     const float score = a.scores[row];
-    if (!(fabsf(score) < __int_as_float(0x7f800000)) || (a.ended && a.ended[row]))
-        return;                         // no candidate, or one that needs no logits
+    const bool ended = a.ended && a.ended[row];
     const uint32_t request = row / static_cast<uint32_t>(a.beams), beam = row - request * a.beams;
     const unsigned char *base = a.logits + request * a.stride_request + beam * a.stride_beam;
     const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(base)) & 15u;
     const int32_t lo = part * a.part, hi = min(lo + a.part, a.vocab);
+    uint4 v[kBeamLoads];
+    if (kEager)
+        load_block<kType>(v, base, off, lo, hi, a.vocab);
+    if (!(fabsf(score) < __int_as_float(0x7f800000)) || ended)
+        return;                         // no candidate, or one that needs no logits
     if (tid == 0)
         s.count = 0;
-    float top = neg_inf(), sum = 0.0f, bound = neg_inf();               // of this thread; of the part
+    float top = neg_inf(), sum = 0.0f;
     for (int32_t first = lo; first < hi; first += kBlock) {
-        uint4 v[kBeamLoads];
-        load_block<kType>(v, base, off, first, hi, a.vocab);
+        if (!kEager || first > lo)
+            load_block<kType>(v, base, off, first, hi, a.vocab);
         const float mine = largest<kType>(v);
-        int32_t last = -1;
-        if (first == lo)
-            bound = block_bound<kType>(s, v, mine, first, a.keep, &last);
-        to_list<kType>(s, list, a.list, v, mine, first, bound, last);
         // exp(x - top) = 2^((x - top) log2(e)); nothing but -inf sums up to 0
         const float was = top;
         top = fmaxf(top, mine);
         const float from = top == neg_inf() ? 0.0f : top;
         const uint64_t from2 = pack2(-from, -from), log2e = pack2(1.4426950408889634f, 1.4426950408889634f);
         uint64_t sum2 = 0;
-#pragma unroll
-        for (int j = 0; j < kBeamLoads; ++j) {
-            const uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
+        auto add_piece = [&](const uint4 &piece) {
+            const uint32_t w[4] = {piece.x, piece.y, piece.z, piece.w};
 #pragma unroll
             for (int k = 0; k < 4; k += 2 / T::kN) {
                 float x[T::kN], y[T::kN];
@@ -413,40 +418,82 @@ template <int kType> __global__ void __launch_bounds__(kBeamThreads, kRowCtas) s
                 const uint64_t t = mul2(add2(pack2(x[0], T::kN == 2 ? x[T::kN - 1] : y[0]), from2), log2e);
                 sum2 = add2(sum2, pack2(pg_exp2(low2(t)), pg_exp2(high2(t))));
             }
+        };
+        if (first + kBlock - kBeamThreads * T::kW < hi) {
+#pragma unroll
+            for (int j = 0; j < kBeamLoads; ++j)
+                add_piece(v[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kBeamLoads - 1; ++j)
+                if (first + j * kBeamThreads * T::kW < hi)
+                    add_piece(v[j]);
         }
         sum = __fmaf_rn(sum, pg_exp2((was - from) * 1.4426950408889634f), low2(sum2) + high2(sum2));
     }
-    // the part's maximum and sum
+    // the part's maximum and sum: each warp's here, of them all by one warp below
     float all = top;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1)
-        all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, o));
-    if (lane == 0)
-        s.warp_top[warp] = all;
-    __syncthreads();
-    int count = s.count;
-    all = s.warp_top[lane % kWarps];
-#pragma unroll
-    for (int o = 1; o < kWarps; o <<= 1)
         all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, o));
     sum *= all == neg_inf() ? 1.0f : pg_exp2((top - all) * 1.4426950408889634f);
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1)
         sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (lane == 0)
+    if (lane == 0) {
+        s.warp_top[warp] = all;
         s.warp_sum[warp] = sum;
+    }
+    float best = top;
+    const float bound = group_bound(s, best, a.keep);
+    uint32_t has = __ballot_sync(0xffffffffu, top >= bound && top > neg_inf());
+    while (has) {
+        const int thread = warp * 32 + __ffs(static_cast<int>(has)) - 1;
+        has &= has - 1;
+        // its pieces, one a lane
+        for (int32_t first = lo + (lane / kBeamLoads) * kBlock; first < hi; first += 32 / kBeamLoads * kBlock) {
+            const int32_t i = first + (lane % kBeamLoads * kBeamThreads + thread) * T::kW;
+            const uint4 x = load_piece<kType>(base, off, i, hi, a.vocab);
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+            uint32_t hits = 0;
+#pragma unroll
+            for (int k = 0; k < T::kW; ++k) {
+                float y[T::kN];
+                T::get(w[k / T::kN], y);
+                hits |= (y[k % T::kN] >= bound && y[k % T::kN] > neg_inf()) ? 1u << k : 0u;
+            }
+            while (hits) {
+                const int k = __ffs(static_cast<int>(hits)) - 1, word = k / T::kN;
+                hits &= hits - 1;
+                float y[T::kN];
+                T::get(word == 0 ? w[0] : word == 1 ? w[1] : word == 2 ? w[2] : w[3], y);
+                const int at_list = atomicAdd(&s.count, 1);
+                if (at_list < a.list)
+                    list[at_list] = BeamEntry{T::kN == 2 && k % 2 ? y[T::kN - 1] : y[0], i + k};
+            }
+        }
+    }
     __syncthreads();
-    if (count > a.list)
+    int count = s.count;
+    if (count > a.list) {
+        __syncthreads();                // (every thread has read the count)
         count = list_again<kType>(s, list, a.list, a.keep, base, off, lo, hi, a.vocab);
-    rank_list(list, count, a.keep, a.entries + static_cast<int64_t>(blockIdx.x) * a.keep);
-    if (warp == 0) {
-        Pair z{lane < kWarps ? s.warp_sum[lane] : 0.0f, 0.0f};
+    }
+    if (warp == kWarps - 1) {           // (the last one to have entries to rank)
+        const float warp_top = lane < kWarps ? s.warp_top[lane] : neg_inf();
+        all = warp_top;
+#pragma unroll
+        for (int o = 1; o < kWarps; o <<= 1)
+            all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, o));
+        all = __shfl_sync(0xffffffffu, all, 0);
+        Pair z{lane < kWarps ? s.warp_sum[lane] * (all == neg_inf() ? 1.0f : pg_exp2((warp_top - all) * 1.4426950408889634f)) : 0.0f, 0.0f};
 #pragma unroll
         for (int o = 1; o < kWarps; o <<= 1)
             z = add(z, Pair{__shfl_xor_sync(0xffffffffu, z.hi, o), __shfl_xor_sync(0xffffffffu, z.lo, o)});
         if (lane == 0)
-            a.meta[blockIdx.x] = BeamPart{z.hi, z.lo, all, min(count, a.keep)};
+            *meta = BeamPart{z.hi, z.lo, all, min(count, a.keep)};
     }
+    rank_list(list, count, a.keep, to);
 }
 
 // A candidate: its value as a whole number of the same order, and its place among the
@@ -464,56 +511,16 @@ __device__ __forceinline__ float disordered(uint32_t u)
 {
     return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
 }
-__device__ __forceinline__ bool better(const Cand &a, const Cand &b) { return a.key > b.key || (a.key == b.key && a.at < b.at); }
-__device__ __forceinline__ Cand other(const Cand &c, int mask)
+__device__ __forceinline__ Cand no_cand() { return Cand{0, INT_MAX}; }
+__device__ __forceinline__ Cand cand(const Pair &x, int32_t at)
 {
-    Cand o;
-    o.key = __shfl_xor_sync(0xffffffffu, c.key, mask);
-    o.at = __shfl_xor_sync(0xffffffffu, c.at, mask);
-    return o;
+    return Cand{static_cast<uint64_t>(ordered(x.hi)) << 32 | ordered(x.lo), at};
 }
-
-// A warp's sorted list of 32 R candidates (lane l holds ranks l, l + 32), best first.
-template <int R> struct Best {
-    Cand c[R];
-
-    __device__ __forceinline__ void clear()
-    {
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-            c[r] = Cand{0, INT_MAX};
-    }
-    // The best of this list and another sorted one: rank i against the other's rank from the
-    // end leaves the best half as a sequence that rises once and falls once, which log2
-    // exchanges sort.
-    __device__ __forceinline__ void merge(const Best &o, int lane)
-    {
-        Cand m[R];
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const Cand x = other(o.c[R - 1 - r], 31);
-            m[r] = better(c[r], x) ? c[r] : x;
-        }
-        if (R == 2 && better(m[R - 1], m[0])) {
-            const Cand x = m[0];
-            m[0] = m[R - 1];
-            m[R - 1] = x;
-        }
-#pragma unroll
-        for (int k = 16; k > 0; k >>= 1) {
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const Cand x = other(m[r], k);
-                const bool want = (lane & k) == 0;
-                m[r] = better(m[r], x) == want ? m[r] : x;
-            }
-        }
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-            c[r] = m[r];
-    }
-};
-
+// (without branches: it runs in loops over shared memory)
+__device__ __forceinline__ bool better(const Cand &a, const Cand &b)
+{
+    return (a.key > b.key) | ((a.key == b.key) & (a.at < b.at));
+}
 // log(x) of x > 0 given as a pair, within about 2^-30: x = 2^e f, f in [3/4, 3/2), and with z = (f - 1) / (f + 1)
 // log(f) = 2 (z + z^3 / 3 + z^5 / 5 + ..); only the first term needs more than fp32.
 __device__ __forceinline__ Pair log_of(const Pair &x)
@@ -535,204 +542,312 @@ __device__ __forceinline__ Pair log_of(const Pair &x)
     return two_sum(whole.hi, whole.lo + (tail + low + e * 3.194618498e-5f));
 }
 
-struct JoinSmem {
-    float top[kBeamMost];
-    Pair sum[kBeamMost];
+struct JoinSmem {   // (score and kind are set before the join)
+    float score[kBeamMost], top[kBeamMost];
     Pair shift[kBeamMost];              // score - log(sum): what a row adds to x - top
     int32_t kind[kBeamMost];            // 0: no candidate, 1: one (an ended beam), 2: its parts' lists
-    Cand best[kWarps][kBeamMost];
+    Cand bound;
+    int32_t count;
 };
 
-// The lists of all parts of all beams of a request, in order by value: score + (x - top) -
-// log(sum), held in two fp32 numbers.  Every warp merges its share of the lists,
-// skipping those whose first entry does not get in, then pairs of warps join.
-template <int R> __global__ void __launch_bounds__(kBeamThreads) select_join(const BeamSelectArgs a)
+// A request's lists in shared memory.
+struct Lists {
+    BeamPart *meta;
+    BeamEntry *entries;                 // `keep` each
+    Cand *heads, *kept;
+};
+
+// Entry i of list l, by value: score + (x - top) - log(sum) in two fp32 numbers.
+__device__ __forceinline__ Cand entry(const BeamSelectArgs &a, const JoinSmem &s, const Lists &z, int l, int i)
 {
-    __shared__ JoinSmem s;
+    const int b = static_cast<int>(static_cast<uint32_t>(l) / static_cast<uint32_t>(a.parts));
+    if (s.kind[b] != 2)
+        return s.kind[b] == 1 && l == b * a.parts && i == 0 ? cand(s.shift[b], b * a.vocab + a.end_token) : no_cand();
+    if (i >= z.meta[l].count)
+        return no_cand();
+    const BeamEntry e = z.entries[l * a.keep + i];
+    const Pair x = add(two_sum(e.x, -s.top[b]), s.shift[b]);
+    return x.hi > neg_inf() ? cand(x, b * a.vocab + e.token) : no_cand();      // (not beyond fp32's range)
+}
+
+// How many of n candidates are better than c, which four neighbouring threads share.
+__device__ __forceinline__ int count_better(const Cand *all, int n, const Cand &c)
+{
+    int before = 0;
+#pragma unroll 4
+    for (int k = threadIdx.x & 3; k < n; k += 4)
+        before += better(all[k], c);
+    before += __shfl_xor_sync(0xffffffffu, before, 1);
+    before += __shfl_xor_sync(0xffffffffu, before, 2);
+    return before;
+}
+
+// The lists of all parts of all beams of a request, in order.  Of the q-th entries of all lists (the
+// first ones, or as deep as it takes) the need-th best is a bound that need x q >= keep
+// entries reach; the few that do are ordered by counting for each how many are better.
+__device__ __forceinline__ void join(const BeamSelectArgs &a, JoinSmem &s, const Lists &z, int32_t request)
+{
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int32_t request = blockIdx.x;
-    grid_dependency_wait();
-    grid_launch_dependents();
+    if (tid == 0) {
+        s.bound = no_cand();
+        s.count = 0;
+    }
     for (int b = warp; b < a.beams; b += kWarps) {
-        const int64_t row = static_cast<int64_t>(request) * a.beams + b;
-        const float score = a.scores[row];
-        int32_t kind = 2;
-        if (!(fabsf(score) < __int_as_float(0x7f800000)))
-            kind = 0;
-        else if (a.ended && a.ended[row])
-            kind = 1;
+        const float score = s.score[b];
+        int32_t kind = s.kind[b];
         float top = neg_inf();
-        Pair sum{0.0f, 0.0f};
+        Pair shift{score, 0.0f};
         if (kind == 2) {
-            float m[kBeamMostParts / 32];
-            Pair z[kBeamMostParts / 32];
+            const BeamPart *meta = z.meta + b * a.parts;
+            for (int p = lane; p < a.parts; p += 32)
+                top = fmaxf(top, meta[p].top);
 #pragma unroll
-            for (int i = 0; i < kBeamMostParts / 32; ++i) {
-                const int p = lane + 32 * i;
-                m[i] = neg_inf();
-                z[i] = Pair{0.0f, 0.0f};
-                if (p < a.parts) {
-                    const BeamPart &part = a.meta[row * a.parts + p];
-                    m[i] = part.top;
-                    z[i] = Pair{part.sum, part.rest};
-                }
-                top = fmaxf(top, m[i]);
-            }
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1)
+            for (int o = 16; o > 0; o >>= 1)
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-#pragma unroll
-            for (int i = 0; i < kBeamMostParts / 32; ++i)
-                if (z[i].hi != 0.0f) {  // (an empty part: -inf - -inf)
-                    const float w = expf(m[i] - top);
-                    sum = add(sum, Pair{z[i].hi * w, __fmaf_rn(z[i].lo, w, __fmaf_rn(z[i].hi, w, -(z[i].hi * w)))});
+            Pair sum{0.0f, 0.0f};
+            for (int p = lane; p < a.parts; p += 32) {
+                const BeamPart x = meta[p];
+                if (x.sum != 0.0f) {    // (an empty part: -inf - -inf)
+                    const float w = expf(x.top - top), m = x.sum * w;
+                    sum = add(sum, Pair{m, __fmaf_rn(x.rest, w, __fmaf_rn(x.sum, w, -m))});
                 }
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1)
-                sum = add(sum, Pair{__shfl_xor_sync(0xffffffffu, sum.hi, o), __shfl_xor_sync(0xffffffffu, sum.lo, o)});
+            }
+            for (int o = 16; o > 0; o >>= 1)
+                if (o < a.parts)
+                    sum = add(sum, Pair{__shfl_xor_sync(0xffffffffu, sum.hi, o), __shfl_xor_sync(0xffffffffu, sum.lo, o)});
+            // NaN or +inf among the logits, or none above -inf: the row's softmax is NaN
+            if (!(sum.hi > 0.0f))
+                kind = 0;
+            const Pair l = log_of(sum);
+            shift = add(shift, Pair{-l.hi, -l.lo});
         }
         if (lane == 0) {
             s.top[b] = top;
-            s.sum[b] = sum;
+            s.shift[b] = shift;
             s.kind[b] = kind;
         }
     }
     __syncthreads();
-    if (tid < a.beams) {
-        const float score = a.scores[static_cast<int64_t>(request) * a.beams + tid];
-        Pair shift{score, 0.0f};
-        if (s.kind[tid] == 2) {
-            // NaN or +inf among the logits, or none above -inf: the row's softmax is NaN
-            if (!(s.sum[tid].hi > 0.0f))
-                s.kind[tid] = 0;
-            const Pair l = log_of(s.sum[tid]);
-            shift = add(shift, Pair{-l.hi, -l.lo});
-        }
-        s.shift[tid] = shift;
+    const int lists = a.beams * a.parts;
+    const int q = (a.keep + lists - 1) / lists, need = (a.keep + q - 1) / q;
+    for (int l = tid; l < lists; l += kBeamThreads)
+        z.heads[l] = entry(a, s, z, l, q - 1);
+    __syncthreads();
+    static_assert(kBeamMostLists * 4 <= kBeamThreads, "four threads a list");
+    if (warp * 8 < lists) {
+        const Cand h = tid / 4 < lists ? z.heads[tid / 4] : no_cand();
+        const int before = count_better(z.heads, lists, h);
+        if (h.key != 0 && before == need - 1)
+            s.bound = h;
     }
     __syncthreads();
-    Best<R> best;
-    best.clear();
-    const int lists = a.beams * a.parts;
+    const Cand bound = s.bound;
     for (int l = warp; l < lists; l += kWarps) {
-        const int b = l / a.parts, p = l - b * a.parts;
-        const int kind = s.kind[b];
-        if (kind == 0 || (kind == 1 && p > 0))
+        if (q == 1 && better(bound, z.heads[l]))
             continue;
-        Best<R> next;
-        next.clear();
-        if (kind == 1) {
-            if (lane == 0)
-                next.c[0] = Cand{static_cast<uint64_t>(ordered(s.shift[b].hi)) << 32 | ordered(s.shift[b].lo),
-                                 b * a.vocab + a.end_token};
-        } else {
-            const int64_t at = (static_cast<int64_t>(request) * a.beams + b) * a.parts + p;
-            const int count = a.meta[at].count;
-            const Pair shift = s.shift[b];
-            const float top = s.top[b];
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const int i = lane + 32 * r;
-                if (i < count) {
-                    const BeamEntry e = a.entries[at * a.keep + i];
-                    const Pair x = add(two_sum(e.x, -top), shift);
-                    if (x.hi > neg_inf())           // (not beyond fp32's range)
-                        next.c[r] = Cand{static_cast<uint64_t>(ordered(x.hi)) << 32 | ordered(x.lo), b * a.vocab + e.token};
-                }
-            }
+        for (int i = lane; i < a.keep; i += 32) {
+            const Cand c = entry(a, s, z, l, i);
+            if (c.key != 0 && !better(bound, c))
+                z.kept[atomicAdd(&s.count, 1)] = c;
         }
-        // a list whose first does not beat the last kept one has nothing to add
-        const int worst = a.keep - 1;
-        Cand first, least = best.c[R - 1];         // (keep is above 32 where R is 2)
-        first.key = __shfl_sync(0xffffffffu, next.c[0].key, 0);
-        first.at = __shfl_sync(0xffffffffu, next.c[0].at, 0);
-        least.key = __shfl_sync(0xffffffffu, least.key, worst % 32);
-        least.at = __shfl_sync(0xffffffffu, least.at, worst % 32);
-        if (better(first, least))
-            best.merge(next, lane);
     }
-    for (int half = kWarps / 2; half > 0; half >>= 1) {
-        if (warp >= half && warp < 2 * half) {
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-                s.best[warp][lane + 32 * r] = best.c[r];
+    __syncthreads();
+    const int count = s.count;
+    const int64_t to = static_cast<int64_t>(request) * a.keep;
+    for (int i0 = warp * 8; i0 < count; i0 += kWarps * 8) {
+        const int i = i0 + lane / 4;
+        const Cand c = z.kept[i < count ? i : 0];
+        const int before = count_better(z.kept, count, c);
+        if (lane % 4 == 0 && i < count && before < a.keep) {
+            // (the larger of the two numbers is the value rounded to fp32)
+            const int32_t parent = static_cast<int32_t>(static_cast<uint32_t>(c.at) / static_cast<uint32_t>(a.vocab));
+            a.out_scores[to + before] = disordered(static_cast<uint32_t>(c.key >> 32));
+            a.parents[to + before] = parent;
+            a.tokens[to + before] = c.at - parent * a.vocab;
         }
+    }
+    for (int i = count + tid; i < a.keep; i += kBeamThreads) {
+        a.out_scores[to + i] = neg_inf();
+        a.parents[to + i] = -1;
+        a.tokens[to + i] = -1;
+    }
+}
+
+// A request's beams: scores, and which have candidates.
+__device__ __forceinline__ void get_beams(const BeamSelectArgs &a, JoinSmem &s, int32_t request)
+{
+    const int b = threadIdx.x;
+    if (b < a.beams) {
+        const int64_t row = static_cast<int64_t>(request) * a.beams + b;
+        const float score = a.scores[row];
+        const bool ended = a.ended && a.ended[row];
+        s.score[b] = score;
+        s.kind[b] = !(fabsf(score) < __int_as_float(0x7f800000)) ? 0 : ended ? 1 : 2;
+    }
+}
+
+// Dynamic shared memory of a join: the lists, then candidates (past what a part needs, where one was
+// taken before).
+__device__ __forceinline__ Lists lists_at(const BeamSelectArgs &a, unsigned char *raw)
+{
+    const int lists = a.beams * a.parts;
+    Lists z;
+    z.meta = reinterpret_cast<BeamPart *>(raw);
+    z.heads = reinterpret_cast<Cand *>(z.meta + lists);
+    z.kept = z.heads + lists;
+    z.entries = reinterpret_cast<BeamEntry *>(z.kept + a.keep * (a.keep + 1));
+    return z;
+}
+
+template <int kType> __global__ void __launch_bounds__(kBeamThreads, kRowCtas) select_rows(const BeamSelectArgs a)
+{
+    __shared__ PartSmem s;
+    extern __shared__ __align__(16) unsigned char raw[];
+    grid_dependency_wait();
+    grid_launch_dependents();
+    take_part<kType, false>(a, s, reinterpret_cast<BeamEntry *>(raw), blockIdx.x, a.meta + blockIdx.x,
+                            a.entries + static_cast<int64_t>(blockIdx.x) * a.keep);
+}
+
+__global__ void __launch_bounds__(kBeamThreads) select_join(const BeamSelectArgs a)
+{
+    __shared__ JoinSmem s;
+    extern __shared__ __align__(16) unsigned char raw[];
+    const int32_t request = blockIdx.x, lists = a.beams * a.parts;
+    const Lists z = lists_at(a, raw);
+    grid_dependency_wait();
+    grid_launch_dependents();
+    // (of beams without a list it copies what happens to be there, and nobody reads it)
+    const int64_t first = static_cast<int64_t>(request) * lists;
+    for (int i = threadIdx.x; i < lists; i += kBeamThreads)
+        reinterpret_cast<uint4 *>(z.meta)[i] = reinterpret_cast<const uint4 *>(a.meta + first)[i];
+    for (int i = threadIdx.x; i < lists * a.keep; i += kBeamThreads)
+        z.entries[i] = a.entries[first * a.keep + i];
+    get_beams(a, s, request);
+    __syncthreads();
+    join(a, s, z, request);
+}
+
+// Both in one launch: a cluster takes a request's parts, their lists go to the first CTA's shared memory,
+// and it joins them.
+template <int kType> __global__ void __launch_bounds__(kBeamThreads, kRowCtas) select_together(const BeamSelectArgs a)
+{
+    __shared__ PartSmem s;
+    __shared__ JoinSmem j;
+    extern __shared__ __align__(16) unsigned char raw[];
+    const uint32_t request = blockIdx.x / kCluster, rank = blockIdx.x % kCluster, lists = static_cast<uint32_t>(a.beams) * a.parts;
+    // the first CTA's shared memory may be written once it runs
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    const Lists z = lists_at(a, raw + static_cast<size_t>(a.list + a.keep) * sizeof(BeamEntry));
+    BeamPart *meta;
+    BeamEntry *entries;
+    asm("mapa.u64 %0, %1, 0;" : "=l"(meta) : "l"(z.meta));
+    asm("mapa.u64 %0, %1, 0;" : "=l"(entries) : "l"(z.entries));
+    grid_dependency_wait();
+    grid_launch_dependents();
+    if (rank == 0)
+        get_beams(a, j, static_cast<int32_t>(request));
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+    for (uint32_t l = rank; l < lists; l += kCluster) {
+        take_part<kType, true>(a, s, reinterpret_cast<BeamEntry *>(raw), request * lists + l, meta + l, entries + l * a.keep);
         __syncthreads();
-        if (warp < half) {
-            Best<R> next;
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-                next.c[r] = s.best[warp + half][lane + 32 * r];
-            best.merge(next, lane);
-        }
     }
-    if (warp == 0) {
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int i = lane + 32 * r;
-            if (i < a.keep) {
-                const int64_t to = static_cast<int64_t>(request) * a.keep + i;
-                const Cand c = best.c[r];
-                const bool there = c.key != 0;
-                const int32_t parent = there ? c.at / a.vocab : -1;
-                // (the larger of the two numbers is the value rounded to fp32)
-                a.out_scores[to] = there ? disordered(static_cast<uint32_t>(c.key >> 32)) : neg_inf();
-                a.parents[to] = parent;
-                a.tokens[to] = there ? c.at - parent * a.vocab : -1;
-            }
-        }
-    }
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+    if (rank == 0)
+        join(a, j, z, static_cast<int32_t>(request));
+}
+
+int launch_cluster(void (*kernel)(BeamSelectArgs), dim3 grid, size_t smem, cudaStream_t st, const BeamSelectArgs &a)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(kBeamThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = kCluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return static_cast<int>(cudaLaunchKernelEx(&cfg, kernel, a));
+}
+
+// Entries of a part's list: what a block with a bound of its own may add to what is kept.
+int32_t list_entries(int32_t keep, int dtype)
+{
+    return std::max(keep, 16) * kGroupLanes * kBeamLoads * (dtype == BSM_F32 ? 4 : 8) + keep;
+}
+size_t part_smem(int32_t keep, int dtype) { return static_cast<size_t>(list_entries(keep, dtype) + keep) * sizeof(BeamEntry); }
+size_t join_smem(int32_t lists, int32_t keep)
+{
+    return lists * sizeof(BeamPart) + (lists + keep * (keep + 1)) * sizeof(Cand) + static_cast<size_t>(lists) * keep * sizeof(BeamEntry);
 }
 
 }  // namespace
 
-void beam_parts(int64_t rows, int32_t vocab, int es, int n_sm, int32_t *parts, int32_t *part)
+// Requests whose beams are few and short go to a cluster each, in one launch; the others' parts to all
+// SMs, and their joins to a second launch.
+BeamCut beam_cut(int32_t n, int32_t beams, int32_t vocab, int es, int n_sm)
 {
     const int64_t piece = 16 / es, least = kBeamThreads * piece, block = kBeamLoads * least;
     auto up = [](int64_t x, int64_t d) { return (x + d - 1) / d; };
+    const int64_t rows = static_cast<int64_t>(n) * beams;
+    BeamCut c{};
+    c.together = static_cast<int64_t>(n) * kCluster <= kRowCtas * static_cast<int64_t>(n_sm) &&
+                 static_cast<int64_t>(beams) * vocab * es <= kCluster * kTogetherBytes;
     // about eight parts an SM, of one piece a thread at least, and of whole blocks past one
-    int64_t n = up(8 * n_sm, rows < 1 ? 1 : rows);
-    n = std::min(std::min(n, up(vocab, least)), int64_t(kBeamMostParts));
-    int64_t each = up(up(vocab, n), piece) * piece;
-    if (each > block)
+    int64_t parts = c.together ? kCluster / beams : up(8 * n_sm, rows < 1 ? 1 : rows);
+    parts = std::min(std::min(parts, up(vocab, least)), static_cast<int64_t>(kBeamMostLists / beams));
+    parts = std::max<int64_t>(parts, 1);
+    int64_t each = up(up(vocab, parts), piece) * piece;
+    if (each > block && !c.together)
         each = up(each, block) * block;
-    *part = static_cast<int32_t>(each);
-    *parts = static_cast<int32_t>(up(vocab, each));
+    c.part = static_cast<int32_t>(each);
+    c.parts = static_cast<int32_t>(up(vocab, each));
+    return c;
 }
 
-// Entries of a part's list: what a block with a bound of its own may add to what is kept.
-static int32_t list_entries(int32_t keep, int dtype)
-{
-    return std::max(keep, 16) * kGroupLanes * kBeamLoads * (dtype == BSM_F32 ? 4 : 8) + keep;
-}
-
-int launch_beam_select(BeamSelectArgs a, int dtype, void *stream)
+int launch_beam_select(BeamSelectArgs a, int dtype, bool together, void *stream)
 {
     a.list = list_entries(a.keep, dtype);
-    const size_t smem = static_cast<size_t>(a.list + a.keep) * sizeof(BeamEntry);
+    const size_t part = part_smem(a.keep, dtype), joint = join_smem(a.beams * a.parts, a.keep);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (together) {
+        const dim3 grid(static_cast<unsigned>(a.n) * kCluster);
+        const size_t smem = part + joint;
+        return dtype == BSM_F32    ? launch_cluster(select_together<BSM_F32>, grid, smem, st, a)
+               : dtype == BSM_BF16 ? launch_cluster(select_together<BSM_BF16>, grid, smem, st, a)
+                                   : launch_cluster(select_together<BSM_F16>, grid, smem, st, a);
+    }
     const dim3 grid(static_cast<unsigned>(a.n) * a.beams * a.parts);
-    int e = dtype == BSM_F32    ? launch_early(select_rows<BSM_F32>, grid, kBeamThreads, smem, st, a)
-            : dtype == BSM_BF16 ? launch_early(select_rows<BSM_BF16>, grid, kBeamThreads, smem, st, a)
-                                : launch_early(select_rows<BSM_F16>, grid, kBeamThreads, smem, st, a);
-    if (e)
-        return e;
-    return a.keep <= 32 ? launch_early(select_join<1>, dim3(a.n), kBeamThreads, 0, st, a)
-                        : launch_early(select_join<2>, dim3(a.n), kBeamThreads, 0, st, a);
+    const int e = dtype == BSM_F32    ? launch_early(select_rows<BSM_F32>, grid, kBeamThreads, part, st, a)
+                  : dtype == BSM_BF16 ? launch_early(select_rows<BSM_BF16>, grid, kBeamThreads, part, st, a)
+                                      : launch_early(select_rows<BSM_F16>, grid, kBeamThreads, part, st, a);
+    return e ? e : launch_early(select_join, dim3(a.n), kBeamThreads, joint, st, a);
 }
 
 int beam_set_smem_limit()
 {
     int e = 0;
-    auto set = [&](const void *f, int dtype) {
+    auto set = [&](const void *f, size_t smem, bool cluster) {
         if (!e)
-            e = static_cast<int>(cudaFuncSetAttribute(
-                f, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                static_cast<int>((list_entries(kBeamMost, dtype) + kBeamMost) * sizeof(BeamEntry))));
+            e = static_cast<int>(cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+        if (!e && cluster)
+            e = static_cast<int>(cudaFuncSetAttribute(f, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
     };
-    set(reinterpret_cast<const void *>(&select_rows<BSM_F32>), BSM_F32);
-    set(reinterpret_cast<const void *>(&select_rows<BSM_BF16>), BSM_BF16);
-    set(reinterpret_cast<const void *>(&select_rows<BSM_F16>), BSM_F16);
+    const size_t joint = join_smem(kBeamMostLists, kBeamMost);
+    auto rows = [&](const void *f, const void *both, int dtype) {
+        set(f, part_smem(kBeamMost, dtype), false);
+        set(both, part_smem(kBeamMost, dtype) + joint, true);
+    };
+    rows(reinterpret_cast<const void *>(&select_rows<BSM_F32>), reinterpret_cast<const void *>(&select_together<BSM_F32>), BSM_F32);
+    rows(reinterpret_cast<const void *>(&select_rows<BSM_BF16>), reinterpret_cast<const void *>(&select_together<BSM_BF16>), BSM_BF16);
+    rows(reinterpret_cast<const void *>(&select_rows<BSM_F16>), reinterpret_cast<const void *>(&select_together<BSM_F16>), BSM_F16);
+    set(reinterpret_cast<const void *>(&select_join), joint, false);
     return e;
 }
 
