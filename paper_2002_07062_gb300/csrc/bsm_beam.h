@@ -12,7 +12,6 @@ namespace bsm {
 constexpr int kBeamMost = 64;                   // beams of a request, and continuations kept
 constexpr int32_t kBeamMostVocab = 1 << 20;
 constexpr int64_t kBeamMostRows = (1 << 24) - 1;
-constexpr int kBeamThreads = 512;               // of a part of a row
 constexpr int kBeamLoads = 4;                   // pieces of 16 bytes that a thread holds
 constexpr int kBeamMostLists = 128;             // parts of all rows of a request
 constexpr int64_t kTogetherBytes = 128 << 10;   // of logits that a CTA of a cluster reads at most
@@ -20,7 +19,7 @@ constexpr int64_t kTogetherBytes = 128 << 10;   // of logits that a CTA of a clu
 // The best logits of a part of a row, and what its softmax needs.
 struct BeamPart {
     float sum, rest;                            // of exp(x - top): two numbers that add up to it
-    float top;
+    float top;                                  // one of the part's largest values
     int32_t count;                              // entries in its list
 };
 struct BeamEntry {

@@ -18,9 +18,9 @@ namespace bsm {
 namespace {
 
 constexpr int kGroups = 128;                    // groups of neighbouring threads, more than are ever kept
-constexpr int kGroupLanes = kBeamThreads / kGroups;
-constexpr int kWarps = kBeamThreads / 32;
-constexpr int kRowCtas = 3;                      // of select_rows on an SM
+constexpr int kMostWarps = 16;
+constexpr int kRowThreads = 512, kRowCtas = 3;  // of select_rows; its CTAs on an SM
+constexpr int kJoinThreads = 512;                // of select_join and select_together
 constexpr int kCluster = 16;                     // CTAs of select_together that share a request
 
 __device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
@@ -110,31 +110,6 @@ __device__ __forceinline__ uint4 load_piece(const unsigned char *row, uint32_t o
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// A thread's pieces of the block that starts at `first`.
-template <int kType>
-__device__ __forceinline__ void load_block(uint4 (&v)[kBeamLoads], const unsigned char *row, uint32_t off, int32_t first,
-                                           int32_t hi, int32_t n)
-{
-    using T = Word<kType>;
-    constexpr int W = T::kW, kStep = kBeamThreads * W;          // values between a thread's pieces
-    const int32_t mine = first + static_cast<int32_t>(threadIdx.x) * W;
-    if (first + kBeamLoads * kStep <= hi && (off == 0 || (first > 0 && first + kBeamLoads * kStep + W <= n))) {
-        const unsigned char *p = row + static_cast<int64_t>(mine) * T::kEs - off;
-#pragma unroll
-        for (int j = 0; j < kBeamLoads; ++j)
-            v[j] = *reinterpret_cast<const uint4 *>(p + j * kStep * T::kEs);
-        if (off != 0) {
-#pragma unroll
-            for (int j = 0; j < kBeamLoads; ++j)
-                v[j] = shifted(v[j], *reinterpret_cast<const uint4 *>(p + j * kStep * T::kEs + 16), off);
-        }
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < kBeamLoads; ++j)
-        v[j] = load_piece<kType>(row, off, mine + j * kStep, hi, n);
-}
-
 // Two fp32 numbers whose sum stands for a value of 48 bits.
 struct Pair {
     float hi, lo;
@@ -154,8 +129,9 @@ __device__ __forceinline__ Pair add(const Pair &x, const Pair &y)
 struct PartSmem {
     float group[kGroups];               // the largest value of each group
     int32_t first[kGroups];             // where a group's value ties with the bound: its lowest token
-    float warp_top[kWarps], warp_sum[kWarps], warp_bound[kWarps];   // (tops and sums: one pair a warp)
-    int32_t count, last;
+    float warp_top[kMostWarps], warp_sum[kMostWarps], warp_bound[kMostWarps];
+    int32_t count, last, hits;
+    int16_t hit[kMostWarps * 32];       // threads whose largest value reaches the bound
 };
 
 // Two fp32 numbers at once.
@@ -179,13 +155,13 @@ __device__ __forceinline__ float low2(uint64_t a) { return __uint_as_float(stati
 __device__ __forceinline__ float high2(uint64_t a) { return __uint_as_float(static_cast<uint32_t>(a >> 32)); }
 
 // Calls f(value, token) for every value of a thread's pieces of a block that starts at `first`.
-template <int kType, typename F> __device__ __forceinline__ void each_value(const uint4 (&v)[kBeamLoads], int32_t first, F &&f)
+template <int kType, int kThreads, typename F> __device__ __forceinline__ void each_value(const uint4 (&v)[kBeamLoads], int32_t first, F &&f)
 {
     using T = Word<kType>;
 #pragma unroll
     for (int j = 0; j < kBeamLoads; ++j) {
         const uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
-        const int32_t token = first + (j * kBeamThreads + static_cast<int>(threadIdx.x)) * T::kW;
+        const int32_t token = first + (j * kThreads + static_cast<int>(threadIdx.x)) * T::kW;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             float x[T::kN];
@@ -198,10 +174,10 @@ template <int kType, typename F> __device__ __forceinline__ void each_value(cons
 }
 
 // The list's best `keep` in order to `to`: four threads count for each entry how many are better.
-__device__ __forceinline__ void rank_list(const BeamEntry *list, int count, int keep, BeamEntry *to)
+template <int kThreads> __device__ __forceinline__ void rank_list(const BeamEntry *list, int count, int keep, BeamEntry *to)
 {
     const int lane = threadIdx.x & 31, quarter = lane & 3;
-    for (int i0 = (threadIdx.x >> 5) * 8; i0 < count; i0 += kWarps * 8) {
+    for (int i0 = (threadIdx.x >> 5) * 8; i0 < count; i0 += kThreads / 4) {
         const int i = i0 + lane / 4;
         const BeamEntry e = list[i < count ? i : 0];
         int better = 0;
@@ -220,27 +196,28 @@ __device__ __forceinline__ void rank_list(const BeamEntry *list, int count, int 
 // The smallest of the group maxima that fewer than `keep` groups exceed, so that `keep` values reach it
 // (-inf where fewer than `keep` groups have any).  best: this thread's largest value; becomes
 // its group's.  Everything written before by the block can be read after it.
-__device__ __forceinline__ float group_bound(PartSmem &s, float &best, int keep)
+template <int kThreads> __device__ __forceinline__ float group_bound(PartSmem &s, float &best, int keep)
 {
+    constexpr int kLanes = kThreads / kGroups, kWarps = kThreads / 32;
     const int tid = threadIdx.x, lane = tid & 31;
 #pragma unroll
-    for (int o = 1; o < kGroupLanes; o <<= 1)
+    for (int o = 1; o < kLanes; o <<= 1)
         best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, o));
-    if (tid % kGroupLanes == 0)
-        s.group[tid / kGroupLanes] = best;
+    if (tid % kLanes == 0)
+        s.group[tid / kLanes] = best;
     __syncthreads();
     int over = 0;                       // (a group's threads share the count)
 #pragma unroll
-    for (int k = 0; k < kGroups / 4 / kGroupLanes; ++k) {
-        const float4 o = reinterpret_cast<const float4 *>(s.group)[k * kGroupLanes + tid % kGroupLanes];
+    for (int k = 0; k < kGroups / 4 / kLanes; ++k) {
+        const float4 o = reinterpret_cast<const float4 *>(s.group)[k * kLanes + tid % kLanes];
         over += (o.x > best) + (o.y > best) + (o.z > best) + (o.w > best);
     }
 #pragma unroll
-    for (int o = 1; o < kGroupLanes; o <<= 1)
+    for (int o = 1; o < kLanes; o <<= 1)
         over += __shfl_xor_sync(0xffffffffu, over, o);
     float bound = over < keep ? best : __int_as_float(0x7f800000);
 #pragma unroll
-    for (int o = kGroupLanes; o < 32; o <<= 1)
+    for (int o = kLanes; o < 32; o <<= 1)
         bound = fminf(bound, __shfl_xor_sync(0xffffffffu, bound, o));
     if (lane == 0)
         s.warp_bound[tid >> 5] = bound;
@@ -254,28 +231,29 @@ __device__ __forceinline__ float group_bound(PartSmem &s, float &best, int keep)
 
 // A block's bound.  Where more than `keep` groups reach it some tie there: of values equal to the bound
 // only those up to token *last are needed then, and those that count lie in `keep` groups at most.
-template <int kType>
+template <int kType, int kThreads>
 __device__ __forceinline__ float block_bound(PartSmem &s, const uint4 (&v)[kBeamLoads], float mine, int32_t first, int keep, int32_t *last)
 {
+    constexpr int kLanes = kThreads / kGroups;
     const int tid = threadIdx.x;
-    const bool speaks = tid % kGroupLanes == 0;
+    const bool speaks = tid % kLanes == 0;
     float best = mine;
-    const float bound = group_bound(s, best, keep);
+    const float bound = group_bound<kThreads>(s, best, keep);
     *last = bound == neg_inf() ? -1 : INT_MAX;
     if (bound == neg_inf() || __syncthreads_count(speaks && best >= bound) <= keep)
         return bound;
     const int above = __syncthreads_count(speaks && best > bound);
     int32_t at = INT_MAX;
     if (mine == bound)
-        each_value<kType>(v, first, [&](float x, int32_t token) {
+        each_value<kType, kThreads>(v, first, [&](float x, int32_t token) {
             if (x == bound)
                 at = min(at, token);
         });
 #pragma unroll
-    for (int o = 1; o < kGroupLanes; o <<= 1)
+    for (int o = 1; o < kLanes; o <<= 1)
         at = min(at, __shfl_xor_sync(0xffffffffu, at, o));
     if (speaks)
-        s.first[tid / kGroupLanes] = best == bound ? at : INT_MAX;
+        s.first[tid / kLanes] = best == bound ? at : INT_MAX;
     __syncthreads();
     if (tid < kGroups) {
         const int32_t f = s.first[tid];
@@ -293,7 +271,7 @@ __device__ __forceinline__ float block_bound(PartSmem &s, const uint4 (&v)[kBeam
 
 // Values above the bound, and equal ones up to token `last`, to the list, in any order; pieces
 // without one are skipped.  Entries past the list's end are counted only.
-template <int kType>
+template <int kType, int kThreads>
 __device__ __forceinline__ void to_list(PartSmem &s, BeamEntry *list, int room, const uint4 (&v)[kBeamLoads], float mine, int32_t first,
                                         float bound, int32_t last)
 {
@@ -307,7 +285,7 @@ __device__ __forceinline__ void to_list(PartSmem &s, BeamEntry *list, int room, 
         T::get(T::larger(T::larger(w[0], w[1]), T::larger(w[2], w[3])), ends);
         if (!(fmaxf(ends[0], ends[T::kN - 1]) >= bound))
             continue;
-        const int32_t token = first + (j * kBeamThreads + static_cast<int>(threadIdx.x)) * T::kW;
+        const int32_t token = first + (j * kThreads + static_cast<int>(threadIdx.x)) * T::kW;
 #pragma unroll
         for (int k = 0; k < T::kW; ++k) {
             float x[T::kN];
@@ -336,29 +314,31 @@ template <int kType> __device__ __forceinline__ float largest(const uint4 (&v)[k
 
 // The list once more, where it overflowed: every block with a bound of its own, what is listed cut
 // to the best `keep` before it.  Rows that rise along the part and the like come here.
-template <int kType>
+template <int kType, int kThreads>
 __device__ __noinline__ int list_again(PartSmem &s, BeamEntry *list, int room, int keep, const unsigned char *row, uint32_t off,
                                        int32_t lo, int32_t hi, int32_t n)
 {
     const int tid = threadIdx.x;
     int count = 0;
     float bound = neg_inf();
-    for (int32_t first = lo; first < hi; first += kBeamThreads * kBeamLoads * Word<kType>::kW) {
+    for (int32_t first = lo; first < hi; first += kThreads * kBeamLoads * Word<kType>::kW) {
         uint4 v[kBeamLoads];
-        load_block<kType>(v, row, off, first, hi, n);
+#pragma unroll
+        for (int j = 0; j < kBeamLoads; ++j)
+            v[j] = load_piece<kType>(row, off, first + (j * kThreads + tid) * Word<kType>::kW, hi, n);
         const float mine = largest<kType>(v);
         if (tid == 0)
             s.count = count;
         int32_t last;
-        const float b = block_bound<kType>(s, v, mine, first, keep, &last);     // (its barriers order the count)
+        const float b = block_bound<kType, kThreads>(s, v, mine, first, keep, &last);     // (its barriers order the count)
         if (b > bound)
             bound = b;
         else
             last = -1;
-        to_list<kType>(s, list, room, v, mine, first, bound, last);
+        to_list<kType, kThreads>(s, list, room, v, mine, first, bound, last);
         __syncthreads();
         count = s.count;
-        rank_list(list, count, keep, list + room);
+        rank_list<kThreads>(list, count, keep, list + room);
         __syncthreads();
         count = min(count, keep);
         if (tid < count)
@@ -370,17 +350,18 @@ __device__ __noinline__ int list_again(PartSmem &s, BeamEntry *list, int room, i
     return count;
 }
 
-// One part of a row, a block of values (64 bytes a thread) after the other.  Each thread keeps a
-// maximum and a sum of exponentials of its own and waits for nobody.  At the end the keep-th largest
-// of 128 group maxima is a bound that the part's best `keep` values reach and few others (about
-// as many again): the threads whose maximum reaches it are few, and what they have seen is
-// read once more, from the L2 cache, by their warps.
-// kEager: the first block is asked for before it is known whether the beam needs it.
-template <int kType, bool kEager>
+// One part of a row.  A thread takes a piece of 16 bytes from each 8 KiB (whole rows of the block's
+// threads): four are on their way or at hand, and each makes room for the one four further.  A
+// thread keeps a maximum and a sum of exponentials of its own and waits for nobody.  At the end the
+// keep-th largest of 128 group maxima is a bound that the part's best `keep` values reach and few
+// others (about as many again): the threads whose maximum reaches it are few, and what they have
+// seen is read once more, from the L2 cache, by their warps.
+// kEager: the first pieces are asked for before it is known whether the beam needs them.
+template <int kType, int kThreads, bool kEager>
 __device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, BeamEntry *list, uint32_t at, BeamPart *meta, BeamEntry *to)
 {
     using T = Word<kType>;
-    constexpr int kBlock = kBeamThreads * kBeamLoads * T::kW;           // values of a block
+    constexpr int kWarps = kThreads / 32, kRow = kThreads * T::kW;                          // values of a row of pieces
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t row = at / static_cast<uint32_t>(a.parts);
     const int32_t part = static_cast<int32_t>(at - row * a.parts);
@@ -391,52 +372,92 @@ __device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, 
     const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(base)) & 15u;
     const int32_t lo = part * a.part, hi = min(lo + a.part, a.vocab);
     uint4 v[kBeamLoads];
-    if (kEager)
-        load_block<kType>(v, base, off, lo, hi, a.vocab);
+    auto load = [&](int32_t first) { return load_piece<kType>(base, off, first + tid * T::kW, hi, a.vocab); };
+    if (kEager) {
+#pragma unroll
+        for (int j = 0; j < kBeamLoads; ++j)
+            v[j] = load(lo + j * kRow);
+    }
     if (!(fabsf(score) < __int_as_float(0x7f800000)) || ended)
         return;                         // no candidate, or one that needs no logits
     if (tid == 0)
-        s.count = 0;
-    float top = neg_inf(), sum = 0.0f;
-    for (int32_t first = lo; first < hi; first += kBlock) {
-        if (!kEager || first > lo)
-            load_block<kType>(v, base, off, first, hi, a.vocab);
-        const float mine = largest<kType>(v);
-        // exp(x - top) = 2^((x - top) log2(e)); nothing but -inf sums up to 0
-        const float was = top;
-        top = fmaxf(top, mine);
-        const float from = top == neg_inf() ? 0.0f : top;
-        const uint64_t from2 = pack2(-from, -from), log2e = pack2(1.4426950408889634f, 1.4426950408889634f);
-        uint64_t sum2 = 0;
-        auto add_piece = [&](const uint4 &piece) {
-            const uint32_t w[4] = {piece.x, piece.y, piece.z, piece.w};
-#pragma unroll
-            for (int k = 0; k < 4; k += 2 / T::kN) {
-                float x[T::kN], y[T::kN];
-                T::get(w[k], x);
-                T::get(w[(k + 1) % 4], y);
-                const uint64_t t = mul2(add2(pack2(x[0], T::kN == 2 ? x[T::kN - 1] : y[0]), from2), log2e);
-                sum2 = add2(sum2, pack2(pg_exp2(low2(t)), pg_exp2(high2(t))));
-            }
-        };
-        if (first + kBlock - kBeamThreads * T::kW < hi) {
+        s.count = s.hits = 0;
+    if (!kEager) {
+        if (off == 0 && lo + kBeamLoads * kRow <= hi) {
 #pragma unroll
             for (int j = 0; j < kBeamLoads; ++j)
-                add_piece(v[j]);
+                v[j] = *reinterpret_cast<const uint4 *>(base + static_cast<int64_t>(lo + j * kRow + tid * T::kW) * T::kEs);
         } else {
 #pragma unroll
-            for (int j = 0; j < kBeamLoads - 1; ++j)
-                if (first + j * kBeamThreads * T::kW < hi)
-                    add_piece(v[j]);
+            for (int j = 0; j < kBeamLoads; ++j)
+                v[j] = load(lo + j * kRow);
         }
-        sum = __fmaf_rn(sum, pg_exp2((was - from) * 1.4426950408889634f), low2(sum2) + high2(sum2));
     }
+    // exp(x - from) = 2^((x - from) log2(e)), where `from` is a value seen that lies 4 below the largest at
+    // most: it seldom moves, and the arguments of the terms that matter stay small, so exact
+    float top = neg_inf(), from = neg_inf(), limit = neg_inf(), sum = 0.0f;
+    uint64_t minus = 0, sum2 = 0;       // -from twice (0 while nothing but -inf was seen: it sums up to 0); sums of four pieces
+    auto take = [&](const uint4 &x) {
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        float ends[T::kN];
+        T::get(T::larger(T::larger(w[0], w[1]), T::larger(w[2], w[3])), ends);
+        const float most = fmaxf(ends[0], ends[T::kN - 1]);
+        top = fmaxf(top, most);
+        if (most > limit) {
+            const float scale = pg_exp2((from - most) * 1.4426950408889634f);
+            sum *= scale;
+            sum2 = mul2(sum2, pack2(scale, scale));
+            from = most;
+            limit = from + 4.0f;
+            minus = pack2(-from, -from);
+        }
+        const uint64_t log2e = pack2(1.4426950408889634f, 1.4426950408889634f);
+#pragma unroll
+        for (int k = 0; k < 4; k += 2 / T::kN) {
+            float y[T::kN], z[T::kN];
+            T::get(w[k], y);
+            T::get(w[(k + 1) % 4], z);
+            const uint64_t t = mul2(add2(pack2(y[0], T::kN == 2 ? y[T::kN - 1] : z[0]), minus), log2e);
+            sum2 = add2(sum2, pack2(pg_exp2(low2(t)), pg_exp2(high2(t))));
+        }
+    };
+    int32_t first = lo;
+    bool raw = false;                   // the pieces at hand wait to be shifted into place
+    const unsigned char *p = base + static_cast<int64_t>(lo + tid * T::kW) * T::kEs - off;
+    while (first < hi) {
+        // four rows of pieces; those four further are on their way while the next ones are worked on
+        const int32_t next = first + kBeamLoads * kRow;
+        const bool whole = next + kBeamLoads * kRow <= hi && (off == 0 || next + kBeamLoads * kRow + T::kW <= a.vocab);
+        p += kBeamLoads * kRow * T::kEs;
+        if (whole && off == 0) {
+#pragma unroll
+            for (int j = 0; j < kBeamLoads; ++j) {
+                take(v[j]);
+                v[j] = *reinterpret_cast<const uint4 *>(p + j * kRow * T::kEs);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < kBeamLoads; ++j) {
+                if (first + j * kRow < hi)
+                    take(raw ? shifted(v[j], *reinterpret_cast<const uint4 *>(p + (j - kBeamLoads) * kRow * T::kEs + 16), off) : v[j]);
+                if (whole)
+                    v[j] = *reinterpret_cast<const uint4 *>(p + j * kRow * T::kEs);
+                else if (next + j * kRow < hi)
+                    v[j] = load(next + j * kRow);
+            }
+            raw = whole;
+        }
+        sum += low2(sum2) + high2(sum2);
+        sum2 = 0;
+        first = next;
+    }
+    top = fmaxf(top, neg_inf());        // (not NaN)
     // the part's maximum and sum: each warp's here, of them all by one warp below
-    float all = top;
+    float all = from;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1)
         all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, o));
-    sum *= all == neg_inf() ? 1.0f : pg_exp2((top - all) * 1.4426950408889634f);
+    sum *= from == all ? 1.0f : pg_exp2((from - all) * 1.4426950408889634f);
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1)
         sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -445,31 +466,35 @@ __device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, 
         s.warp_sum[warp] = sum;
     }
     float best = top;
-    const float bound = group_bound(s, best, a.keep);
-    uint32_t has = __ballot_sync(0xffffffffu, top >= bound && top > neg_inf());
-    while (has) {
-        const int thread = warp * 32 + __ffs(static_cast<int>(has)) - 1;
-        has &= has - 1;
-        // its pieces, one a lane
-        for (int32_t first = lo + (lane / kBeamLoads) * kBlock; first < hi; first += 32 / kBeamLoads * kBlock) {
-            const int32_t i = first + (lane % kBeamLoads * kBeamThreads + thread) * T::kW;
-            const uint4 x = load_piece<kType>(base, off, i, hi, a.vocab);
-            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-            uint32_t hits = 0;
+    const float bound = group_bound<kThreads>(s, best, a.keep);
+    if (top >= bound && top > neg_inf())
+        s.hit[atomicAdd(&s.hits, 1)] = static_cast<int16_t>(tid);
+    __syncthreads();
+    // a piece a thread
+    const uint32_t rows = static_cast<uint32_t>(hi - lo + kRow - 1) / kRow, pieces = static_cast<uint32_t>(s.hits) * rows;
+#pragma unroll 2
+    for (uint32_t y = tid; y < pieces; y += kThreads) {
+        const uint32_t h = y / rows;
+        const int32_t i = lo + static_cast<int32_t>(y - h * rows) * kRow + s.hit[h] * T::kW;
+        const uint4 x = load_piece<kType>(base, off, i, hi, a.vocab);
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        uint32_t hits = 0;
 #pragma unroll
-            for (int k = 0; k < T::kW; ++k) {
-                float y[T::kN];
-                T::get(w[k / T::kN], y);
-                hits |= (y[k % T::kN] >= bound && y[k % T::kN] > neg_inf()) ? 1u << k : 0u;
-            }
-            while (hits) {
-                const int k = __ffs(static_cast<int>(hits)) - 1, word = k / T::kN;
-                hits &= hits - 1;
-                float y[T::kN];
-                T::get(word == 0 ? w[0] : word == 1 ? w[1] : word == 2 ? w[2] : w[3], y);
-                const int at_list = atomicAdd(&s.count, 1);
-                if (at_list < a.list)
-                    list[at_list] = BeamEntry{T::kN == 2 && k % 2 ? y[T::kN - 1] : y[0], i + k};
+        for (int k = 0; k < T::kW; ++k) {
+            float z[T::kN];
+            T::get(w[k / T::kN], z);
+            hits |= z[k % T::kN] >= bound ? 1u << k : 0u;
+        }
+        while (hits) {
+            const int k = __ffs(static_cast<int>(hits)) - 1, word = k / T::kN;
+            hits &= hits - 1;
+            float z[T::kN];
+            T::get(word == 0 ? w[0] : word == 1 ? w[1] : word == 2 ? w[2] : w[3], z);
+            const float one = T::kN == 2 && k % 2 ? z[T::kN - 1] : z[0];
+            if (one > neg_inf()) {
+                const int to_at = atomicAdd(&s.count, 1);
+                if (to_at < a.list)
+                    list[to_at] = BeamEntry{one, i + k};
             }
         }
     }
@@ -477,7 +502,7 @@ __device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, 
     int count = s.count;
     if (count > a.list) {
         __syncthreads();                // (every thread has read the count)
-        count = list_again<kType>(s, list, a.list, a.keep, base, off, lo, hi, a.vocab);
+        count = list_again<kType, kThreads>(s, list, a.list, a.keep, base, off, lo, hi, a.vocab);
     }
     if (warp == kWarps - 1) {           // (the last one to have entries to rank)
         const float warp_top = lane < kWarps ? s.warp_top[lane] : neg_inf();
@@ -493,7 +518,7 @@ __device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, 
         if (lane == 0)
             *meta = BeamPart{z.hi, z.lo, all, min(count, a.keep)};
     }
-    rank_list(list, count, a.keep, to);
+    rank_list<kThreads>(list, count, a.keep, to);
 }
 
 // A candidate: its value as a whole number of the same order, and its place among the
@@ -592,7 +617,7 @@ __device__ __forceinline__ void join(const BeamSelectArgs &a, JoinSmem &s, const
         s.bound = no_cand();
         s.count = 0;
     }
-    for (int b = warp; b < a.beams; b += kWarps) {
+    for (int b = warp; b < a.beams; b += (kJoinThreads / 32)) {
         const float score = s.score[b];
         int32_t kind = s.kind[b];
         float top = neg_inf();
@@ -630,10 +655,10 @@ __device__ __forceinline__ void join(const BeamSelectArgs &a, JoinSmem &s, const
     __syncthreads();
     const int lists = a.beams * a.parts;
     const int q = (a.keep + lists - 1) / lists, need = (a.keep + q - 1) / q;
-    for (int l = tid; l < lists; l += kBeamThreads)
+    for (int l = tid; l < lists; l += kJoinThreads)
         z.heads[l] = entry(a, s, z, l, q - 1);
     __syncthreads();
-    static_assert(kBeamMostLists * 4 <= kBeamThreads, "four threads a list");
+    static_assert(kBeamMostLists * 4 <= kJoinThreads, "four threads a list");
     if (warp * 8 < lists) {
         const Cand h = tid / 4 < lists ? z.heads[tid / 4] : no_cand();
         const int before = count_better(z.heads, lists, h);
@@ -642,7 +667,7 @@ __device__ __forceinline__ void join(const BeamSelectArgs &a, JoinSmem &s, const
     }
     __syncthreads();
     const Cand bound = s.bound;
-    for (int l = warp; l < lists; l += kWarps) {
+    for (int l = warp; l < lists; l += (kJoinThreads / 32)) {
         if (q == 1 && better(bound, z.heads[l]))
             continue;
         for (int i = lane; i < a.keep; i += 32) {
@@ -654,7 +679,7 @@ __device__ __forceinline__ void join(const BeamSelectArgs &a, JoinSmem &s, const
     __syncthreads();
     const int count = s.count;
     const int64_t to = static_cast<int64_t>(request) * a.keep;
-    for (int i0 = warp * 8; i0 < count; i0 += kWarps * 8) {
+    for (int i0 = warp * 8; i0 < count; i0 += kJoinThreads / 4) {
         const int i = i0 + lane / 4;
         const Cand c = z.kept[i < count ? i : 0];
         const int before = count_better(z.kept, count, c);
@@ -666,7 +691,7 @@ __device__ __forceinline__ void join(const BeamSelectArgs &a, JoinSmem &s, const
             a.tokens[to + before] = c.at - parent * a.vocab;
         }
     }
-    for (int i = count + tid; i < a.keep; i += kBeamThreads) {
+    for (int i = count + tid; i < a.keep; i += kJoinThreads) {
         a.out_scores[to + i] = neg_inf();
         a.parents[to + i] = -1;
         a.tokens[to + i] = -1;
@@ -699,17 +724,17 @@ __device__ __forceinline__ Lists lists_at(const BeamSelectArgs &a, unsigned char
     return z;
 }
 
-template <int kType> __global__ void __launch_bounds__(kBeamThreads, kRowCtas) select_rows(const BeamSelectArgs a)
+template <int kType> __global__ void __launch_bounds__(kRowThreads, kRowCtas) select_rows(const BeamSelectArgs a)
 {
     __shared__ PartSmem s;
     extern __shared__ __align__(16) unsigned char raw[];
     grid_dependency_wait();
     grid_launch_dependents();
-    take_part<kType, false>(a, s, reinterpret_cast<BeamEntry *>(raw), blockIdx.x, a.meta + blockIdx.x,
+    take_part<kType, kRowThreads, false>(a, s, reinterpret_cast<BeamEntry *>(raw), blockIdx.x, a.meta + blockIdx.x,
                             a.entries + static_cast<int64_t>(blockIdx.x) * a.keep);
 }
 
-__global__ void __launch_bounds__(kBeamThreads) select_join(const BeamSelectArgs a)
+__global__ void __launch_bounds__(kJoinThreads) select_join(const BeamSelectArgs a)
 {
     __shared__ JoinSmem s;
     extern __shared__ __align__(16) unsigned char raw[];
@@ -719,9 +744,9 @@ __global__ void __launch_bounds__(kBeamThreads) select_join(const BeamSelectArgs
     grid_launch_dependents();
     // (of beams without a list it copies what happens to be there, and nobody reads it)
     const int64_t first = static_cast<int64_t>(request) * lists;
-    for (int i = threadIdx.x; i < lists; i += kBeamThreads)
+    for (int i = threadIdx.x; i < lists; i += kJoinThreads)
         reinterpret_cast<uint4 *>(z.meta)[i] = reinterpret_cast<const uint4 *>(a.meta + first)[i];
-    for (int i = threadIdx.x; i < lists * a.keep; i += kBeamThreads)
+    for (int i = threadIdx.x; i < lists * a.keep; i += kJoinThreads)
         z.entries[i] = a.entries[first * a.keep + i];
     get_beams(a, s, request);
     __syncthreads();
@@ -730,7 +755,7 @@ __global__ void __launch_bounds__(kBeamThreads) select_join(const BeamSelectArgs
 
 // Both in one launch: a cluster takes a request's parts, their lists go to the first CTA's shared memory,
 // and it joins them.
-template <int kType> __global__ void __launch_bounds__(kBeamThreads, kRowCtas) select_together(const BeamSelectArgs a)
+template <int kType> __global__ void __launch_bounds__(kJoinThreads, 3) select_together(const BeamSelectArgs a)
 {
     __shared__ PartSmem s;
     __shared__ JoinSmem j;
@@ -749,7 +774,7 @@ template <int kType> __global__ void __launch_bounds__(kBeamThreads, kRowCtas) s
         get_beams(a, j, static_cast<int32_t>(request));
     asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
     for (uint32_t l = rank; l < lists; l += kCluster) {
-        take_part<kType, true>(a, s, reinterpret_cast<BeamEntry *>(raw), request * lists + l, meta + l, entries + l * a.keep);
+        take_part<kType, kJoinThreads, true>(a, s, reinterpret_cast<BeamEntry *>(raw), request * lists + l, meta + l, entries + l * a.keep);
         __syncthreads();
     }
     asm volatile("barrier.cluster.arrive.release;" ::: "memory");
@@ -762,7 +787,7 @@ int launch_cluster(void (*kernel)(BeamSelectArgs), dim3 grid, size_t smem, cudaS
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
-    cfg.blockDim = dim3(kBeamThreads);
+    cfg.blockDim = dim3(kJoinThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
@@ -777,11 +802,11 @@ int launch_cluster(void (*kernel)(BeamSelectArgs), dim3 grid, size_t smem, cudaS
 }
 
 // Entries of a part's list: what a block with a bound of its own may add to what is kept.
-int32_t list_entries(int32_t keep, int dtype)
+int32_t list_entries(int32_t keep, int dtype, int threads)
 {
-    return std::max(keep, 16) * kGroupLanes * kBeamLoads * (dtype == BSM_F32 ? 4 : 8) + keep;
+    return std::max(keep, 16) * (threads / kGroups) * kBeamLoads * (dtype == BSM_F32 ? 4 : 8) + keep;
 }
-size_t part_smem(int32_t keep, int dtype) { return static_cast<size_t>(list_entries(keep, dtype) + keep) * sizeof(BeamEntry); }
+size_t part_smem(int32_t keep, int dtype, int threads) { return static_cast<size_t>(list_entries(keep, dtype, threads) + keep) * sizeof(BeamEntry); }
 size_t join_smem(int32_t lists, int32_t keep)
 {
     return lists * sizeof(BeamPart) + (lists + keep * (keep + 1)) * sizeof(Cand) + static_cast<size_t>(lists) * keep * sizeof(BeamEntry);
@@ -793,19 +818,18 @@ size_t join_smem(int32_t lists, int32_t keep)
 // SMs, and their joins to a second launch.
 BeamCut beam_cut(int32_t n, int32_t beams, int32_t vocab, int es, int n_sm)
 {
-    const int64_t piece = 16 / es, least = kBeamThreads * piece, block = kBeamLoads * least;
+    const int64_t piece = 16 / es;
     auto up = [](int64_t x, int64_t d) { return (x + d - 1) / d; };
     const int64_t rows = static_cast<int64_t>(n) * beams;
     BeamCut c{};
-    c.together = static_cast<int64_t>(n) * kCluster <= kRowCtas * static_cast<int64_t>(n_sm) &&
+    c.together = static_cast<int64_t>(n) * kCluster <= 3 * static_cast<int64_t>(n_sm) &&
                  static_cast<int64_t>(beams) * vocab * es <= kCluster * kTogetherBytes;
-    // about eight parts an SM, of one piece a thread at least, and of whole blocks past one
-    int64_t parts = c.together ? kCluster / beams : up(8 * n_sm, rows < 1 ? 1 : rows);
+    // one part for each place on an SM, of four pieces a thread at least
+    const int64_t least = c.together ? kJoinThreads * piece : kBeamLoads * kRowThreads * piece;
+    int64_t parts = c.together ? kCluster / beams : up(4 * static_cast<int64_t>(n_sm), rows < 1 ? 1 : rows);
     parts = std::min(std::min(parts, up(vocab, least)), static_cast<int64_t>(kBeamMostLists / beams));
     parts = std::max<int64_t>(parts, 1);
-    int64_t each = up(up(vocab, parts), piece) * piece;
-    if (each > block && !c.together)
-        each = up(each, block) * block;
+    const int64_t each = up(up(vocab, parts), piece) * piece;
     c.part = static_cast<int32_t>(each);
     c.parts = static_cast<int32_t>(up(vocab, each));
     return c;
@@ -813,8 +837,9 @@ BeamCut beam_cut(int32_t n, int32_t beams, int32_t vocab, int es, int n_sm)
 
 int launch_beam_select(BeamSelectArgs a, int dtype, bool together, void *stream)
 {
-    a.list = list_entries(a.keep, dtype);
-    const size_t part = part_smem(a.keep, dtype), joint = join_smem(a.beams * a.parts, a.keep);
+    const int threads = together ? kJoinThreads : kRowThreads;
+    a.list = list_entries(a.keep, dtype, threads);
+    const size_t part = part_smem(a.keep, dtype, threads), joint = join_smem(a.beams * a.parts, a.keep);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (together) {
         const dim3 grid(static_cast<unsigned>(a.n) * kCluster);
@@ -824,10 +849,10 @@ int launch_beam_select(BeamSelectArgs a, int dtype, bool together, void *stream)
                                    : launch_cluster(select_together<BSM_F16>, grid, smem, st, a);
     }
     const dim3 grid(static_cast<unsigned>(a.n) * a.beams * a.parts);
-    const int e = dtype == BSM_F32    ? launch_early(select_rows<BSM_F32>, grid, kBeamThreads, part, st, a)
-                  : dtype == BSM_BF16 ? launch_early(select_rows<BSM_BF16>, grid, kBeamThreads, part, st, a)
-                                      : launch_early(select_rows<BSM_F16>, grid, kBeamThreads, part, st, a);
-    return e ? e : launch_early(select_join, dim3(a.n), kBeamThreads, joint, st, a);
+    const int e = dtype == BSM_F32    ? launch_early(select_rows<BSM_F32>, grid, kRowThreads, part, st, a)
+                  : dtype == BSM_BF16 ? launch_early(select_rows<BSM_BF16>, grid, kRowThreads, part, st, a)
+                                      : launch_early(select_rows<BSM_F16>, grid, kRowThreads, part, st, a);
+    return e ? e : launch_early(select_join, dim3(a.n), kJoinThreads, joint, st, a);
 }
 
 int beam_set_smem_limit()
@@ -841,8 +866,8 @@ int beam_set_smem_limit()
     };
     const size_t joint = join_smem(kBeamMostLists, kBeamMost);
     auto rows = [&](const void *f, const void *both, int dtype) {
-        set(f, part_smem(kBeamMost, dtype), false);
-        set(both, part_smem(kBeamMost, dtype) + joint, true);
+        set(f, part_smem(kBeamMost, dtype, kRowThreads), false);
+        set(both, part_smem(kBeamMost, dtype, kJoinThreads) + joint, true);
     };
     rows(reinterpret_cast<const void *>(&select_rows<BSM_F32>), reinterpret_cast<const void *>(&select_together<BSM_F32>), BSM_F32);
     rows(reinterpret_cast<const void *>(&select_rows<BSM_BF16>), reinterpret_cast<const void *>(&select_together<BSM_BF16>), BSM_BF16);

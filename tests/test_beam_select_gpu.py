@@ -16,12 +16,12 @@ NEG = -float("inf")
 
 def _tol(V, v):
     """The sum's terms: 2^-22 of the exponential and, for its argument (a difference and a product, half a
-    step each, and log2(e) in fp32), 3 x 2^-24 of its size, whose mean under the softmax is at most log V;
-    additions of half a step: 16 of a block, one for each of up to 64 blocks, 5 over a warp, one of a block's two
-    halves; what was summed before a larger maximum came is multiplied by another such exponential, at
-    most once a block and at the end, and the parts by one of 2 x 2^-24.  And the value's own rounding."""
-    blocks = -(-V // 8192)
-    return 2.0 ** -24 * ((blocks + 2) * (4 + 3 * math.log(V + 1)) + 22 + blocks + 2 + np.abs(v))
+    step each, and log2(e) in fp32), 3 x 2^-24 of its size, whose mean under the softmax is at most log V, and
+    4 more where the reference lags; what was summed before the reference moved is multiplied by such
+    an exponential (by less than e^-4 each time: all of them together count as 1.02), once more at the end of a
+    warp and of a part, and the parts by one of 2 x 2^-24.  Additions of half a step: 4 of a piece, one
+    for each of V / 2048 pieces at most, 5 over a warp.  And the value's own rounding."""
+    return 2.0 ** -24 * (4.1 * (4 + 3 * (math.log(V + 1) + 4)) + 2 + 9 + V / 2048 + np.abs(v))
 
 
 def _run(logits, scores, keep, ended=None, end_token=0, stream=None, ws=None):
