@@ -91,9 +91,10 @@ __global__ void __launch_bounds__(kReorderTile) reorder_tables(const PagedReorde
         const int32_t e = col < s_had[b] ? old[b * kReorderTile] : -1;
         if (e < 0 || (held >> b & 1))
             continue;
-        bool other = false;
-        for (int k = 0; k < B && !other; ++k)
-            other = old[k * kReorderTile] == e && (k < b ? col < s_had[k] : (held >> k & 1) != 0);
+        bool other = false;             // (without branches: the loads follow one another closely)
+#pragma unroll 4
+        for (int k = 0; k < B; ++k)
+            other |= (old[k * kReorderTile] == e) & (k < b ? col < s_had[k] : (held >> k & 1) != 0);
         if (!other)
             gone |= uint64_t(1) << b;
     }
@@ -130,6 +131,7 @@ __global__ void __launch_bounds__(kReorderTile) reorder_tables(const PagedReorde
 
 constexpr int kFinishThreads = 256;
 constexpr int kFinishAhead = 4;                         // pieces of a thread in flight
+constexpr uint32_t kUnitPieces = 512;                   // 16-byte pieces that a warp copies at a time, about
 
 // Sum over the block's threads before this one; *all gets the block's.
 __device__ __forceinline__ int32_t before_me(int32_t x, int32_t *warps, int32_t *all)
@@ -156,16 +158,21 @@ __device__ __forceinline__ int32_t before_me(int32_t x, int32_t *warps, int32_t 
     return base + sum - x;
 }
 
-// Pages for the rows that copy, in order of requests and rows, and the copies: a CTA takes
-// one row's tokens of one layer's keys or values at a time.  Every CTA counts all requests'
-// copies itself (256 at once) instead of waiting for another's sums.
+// Pages for the rows that copy, in order of requests and rows, and the copies, a warp at a time about
+// 8 KiB (some tokens of one row in one layer's keys or values).  Every CTA counts all requests' copies
+// itself (256 at once) instead of waiting for another's sums.
 __global__ void __launch_bounds__(kFinishThreads) reorder_pages(const PagedReorderArgs a)
 {
     __shared__ uint64_t s_rows[kFinishThreads];         // rows of a request that copy
-    __shared__ int32_t s_copies[kFinishThreads + 1], s_dropped[kFinishThreads];
-    __shared__ int32_t s_warp[2][kFinishThreads / 32];
-    const int tid = threadIdx.x;
+    __shared__ int32_t s_copies[kFinishThreads], s_dropped[kFinishThreads];
+    __shared__ int32_t s_from[kFinishThreads], s_to[kFinishThreads], s_part[kFinishThreads], s_units[kFinishThreads];
+    __shared__ int32_t s_warp[3][kFinishThreads / 32];
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int warps = gridDim.x * (kFinishThreads / 32), me = blockIdx.x * (kFinishThreads / 32) + (tid >> 5);
     const int32_t B = a.beams;
+    const uint32_t per = static_cast<uint32_t>(a.heads) * a.chunks, both = static_cast<uint32_t>(a.layers) * 2;
+    const bool whole = a.head == a.chunks * 16ll && a.token == per * 16ll;      // a page's tokens are one run of bytes
+    const int32_t tokens = per >= kUnitPieces ? 1 : static_cast<int32_t>(kUnitPieces / per);       // of a unit
     grid_dependency_wait();
     grid_launch_dependents();
     const int64_t rows = static_cast<int64_t>(a.n) * B;
@@ -185,77 +192,103 @@ __global__ void __launch_bounds__(kFinishThreads) reorder_pages(const PagedReord
         }
         int32_t all_copies, all_dropped;
         const int32_t pc = before_me(__popcll(mask), s_warp[0], &all_copies);
-        const int32_t pd = before_me(count, s_warp[1], &all_dropped);
+        s_dropped[tid] = before_me(count, s_warp[1], &all_dropped);
         s_rows[tid] = mask;
         s_copies[tid] = pc;
-        s_dropped[tid] = pd;
-        if (tid == 0)
-            s_copies[kFinishThreads] = all_copies;
         __syncthreads();
-        const int64_t items = static_cast<int64_t>(all_copies) * a.layers * 2;
-        for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
-            const int32_t e = static_cast<int32_t>(pg_div(it, a.layers * 2));
-            const int32_t which = static_cast<int32_t>(it - static_cast<int64_t>(e) * a.layers * 2);
-            int lo = 0, hi = kFinishThreads;            // the request of copy e
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (s_copies[mid] <= e)
-                    lo = mid;
-                else
-                    hi = mid;
-            }
-            uint64_t m = s_rows[lo];
-            for (int k = e - s_copies[lo]; k > 0; --k)
-                m &= m - 1;
-            const int64_t row = static_cast<int64_t>(r0 + lo) * B + (__ffsll(static_cast<long long>(m)) - 1);
-            const int32_t length = a.row_length[row], source = a.row_source[row];
-            const int32_t full = length / a.page, part = length - full * a.page;
-            const int64_t k = taken + e;
-            const int32_t page = k < a.n_free ? a.free_pages[k] : -1;
-            if (which == 0 && tid == 0)
-                a.new_tables[row * a.new_table_stride + full] = page;
-            if (page < 0)
-                continue;
-            if (page >= a.n_pages) {
-                if (tid == 0)
-                    atomicOr(a.status, BSM_DEV_BOUNDS);
-                continue;
-            }
-            unsigned char *base = a.cache[which & 1] + static_cast<int64_t>(which >> 1) * a.layer;
-            const unsigned char *from = base + source * a.page_bytes;
-            unsigned char *to = base + page * a.page_bytes;
-            const uint32_t per = static_cast<uint32_t>(a.heads) * a.chunks, pieces = static_cast<uint32_t>(part) * per;
-            for (uint32_t x = tid; x < pieces; x += kFinishThreads * kFinishAhead) {
-                uint4 v[kFinishAhead];
-                int64_t off[kFinishAhead];
-#pragma unroll
-                for (int u = 0; u < kFinishAhead; ++u) {
-                    const uint32_t y = x + u * kFinishThreads;
-                    if (y >= pieces)
-                        continue;
-                    const uint32_t t = y / per, rest = y - t * per, h = rest / static_cast<uint32_t>(a.chunks);
-                    off[u] = t * a.token + h * a.head + (rest - h * a.chunks) * 16;
-                    v[u] = *reinterpret_cast<const uint4 *>(from + off[u]);
+        for (int32_t e0 = 0; e0 < all_copies; e0 += kFinishThreads) {
+            // copy e0 + tid: its row, where from and where to
+            int32_t units = 0;
+            if (e0 + tid < all_copies) {
+                const int32_t e = e0 + tid;
+                int lo = 0, hi = kFinishThreads;        // its request
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) >> 1;
+                    if (s_copies[mid] <= e)
+                        lo = mid;
+                    else
+                        hi = mid;
                 }
+                uint64_t m = s_rows[lo];
+                for (int k = e - s_copies[lo]; k > 0; --k)
+                    m &= m - 1;
+                const int64_t row = static_cast<int64_t>(r0 + lo) * B + (__ffsll(static_cast<long long>(m)) - 1);
+                const int64_t k = taken + e;
+                const int32_t length = a.row_length[row], full = length / a.page, part = length - full * a.page;
+                const int32_t page = k < a.n_free ? a.free_pages[k] : -1;
+                if (blockIdx.x == 0) {
+                    a.new_tables[row * a.new_table_stride + full] = page;
+                    if (page >= a.n_pages)
+                        atomicOr(a.status, BSM_DEV_BOUNDS);
+                }
+                if (page >= 0 && page < a.n_pages)
+                    units = (part + tokens - 1) / tokens;
+                s_from[tid] = a.row_source[row];
+                s_to[tid] = page;
+                s_part[tid] = part;
+            }
+            int32_t all_units;
+            s_units[tid] = before_me(units, s_warp[2], &all_units);
+            __syncthreads();
+            const int64_t items = static_cast<int64_t>(all_units) * both;
+            for (int64_t it = me; it < items; it += warps) {
+                const int32_t unit = static_cast<int32_t>(pg_div(it, both));
+                const uint32_t which = static_cast<uint32_t>(it - static_cast<int64_t>(unit) * both);
+                int lo = 0, hi = kFinishThreads;        // the copy it belongs to
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) >> 1;
+                    if (s_units[mid] <= unit)
+                        lo = mid;
+                    else
+                        hi = mid;
+                }
+                const int32_t t0 = (unit - s_units[lo]) * tokens, t1 = min(t0 + tokens, s_part[lo]);
+                unsigned char *base = a.cache[which & 1] + static_cast<int64_t>(which >> 1) * a.layer + t0 * a.token;
+                const unsigned char *from = base + s_from[lo] * a.page_bytes;
+                unsigned char *to = base + s_to[lo] * a.page_bytes;
+                const uint32_t pieces = static_cast<uint32_t>(t1 - t0) * per;
+                for (uint32_t x = lane; x < pieces; x += 32 * kFinishAhead) {
+                    uint4 v[kFinishAhead];
+                    int64_t off[kFinishAhead];
 #pragma unroll
-                for (int u = 0; u < kFinishAhead; ++u)
-                    if (x + u * kFinishThreads < pieces)
-                        *reinterpret_cast<uint4 *>(to + off[u]) = v[u];
+                    for (int u = 0; u < kFinishAhead; ++u) {
+                        const uint32_t y = x + u * 32;
+                        if (y >= pieces)
+                            continue;
+                        if (whole) {
+                            off[u] = y * 16ll;
+                        } else {
+                            const uint32_t t = y / per, rest = y - t * per, h = rest / static_cast<uint32_t>(a.chunks);
+                            off[u] = t * a.token + h * a.head + (rest - h * a.chunks) * 16;
+                        }
+                        v[u] = *reinterpret_cast<const uint4 *>(from + off[u]);
+                    }
+#pragma unroll
+                    for (int u = 0; u < kFinishAhead; ++u)
+                        if (x + u * 32 < pieces)
+                            *reinterpret_cast<uint4 *>(to + off[u]) = v[u];
+                }
             }
+            __syncthreads();
         }
-        // the dropped pages, a warp a request
-        const int warps = gridDim.x * (kFinishThreads / 32), lane = tid & 31;
-        for (int q = blockIdx.x * (kFinishThreads / 32) + (tid >> 5); q < kFinishThreads && r0 + q < a.n; q += warps) {
-            int64_t at = dropped + s_dropped[q];
-            for (int z = 0; z < a.tiles; ++z) {
-                const int64_t l = static_cast<int64_t>(r0 + q) * a.tiles + z;
-                const int32_t c = a.counts[l];
-                const int32_t *list = a.lists + l * kReorderTile * B;
-                for (int i = lane; i < c; i += 32)
-                    if (at + i < a.n_dropped)
-                        a.dropped[at + i] = list[i];
-                at += c;
-            }
+        // the dropped pages, a warp a tile of a request
+        const int32_t here = min(kFinishThreads, a.n - r0);
+        for (int64_t l = me; l < static_cast<int64_t>(here) * a.tiles; l += warps) {
+            const int32_t q = static_cast<int32_t>(pg_div(l, a.tiles)), z = static_cast<int32_t>(l - static_cast<int64_t>(q) * a.tiles);
+            const int64_t first = static_cast<int64_t>(r0 + q) * a.tiles;
+            int32_t before = 0;                         // of the request's tiles before
+            for (int k = lane; k < z; k += 32)
+                before += a.counts[first + k];
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1)
+                before += __shfl_xor_sync(0xffffffffu, before, o);
+            const int64_t at = dropped + s_dropped[q] + before;
+            const int32_t c = a.counts[first + z];
+            const int32_t *list = a.lists + (first + z) * kReorderTile * B;
+            const int32_t room = static_cast<int32_t>(at >= a.n_dropped ? 0 : min(static_cast<int64_t>(c), a.n_dropped - at));
+#pragma unroll 4
+            for (int i = lane; i < room; i += 32)
+                a.dropped[at + i] = list[i];
         }
         taken += all_copies;
         dropped += all_dropped;
