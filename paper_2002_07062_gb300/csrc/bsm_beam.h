@@ -57,10 +57,11 @@ struct PagedReorderArgs {
     uint64_t *copies;
     int32_t *counts, *lists;
     int32_t n, beams, width, tiles, n_free, n_dropped, page, n_pages, heads, chunks, layers;
+    int32_t listers;                            // CTAs of the second launch for the dropped pages (set by it)
     uint32_t *status;
 };
 
-int launch_paged_reorder(const PagedReorderArgs &a, int n_sm, void *stream);
+int launch_paged_reorder(PagedReorderArgs a, int n_sm, void *stream);
 
 // How rows of `vocab` logits are cut: parts of `part` logits (whole pieces of 16 bytes).
 struct BeamCut {
