@@ -427,8 +427,17 @@ def _packer(desc):
 _pack_tables, _pack_write, _pack_paged = _packer(PagedTablesDesc), _packer(PagedWriteDesc), _packer(PagedDesc)
 _pack_rotary, _pack_select, _pack_reorder = _packer(PagedWriteRotaryDesc), _packer(BeamSelectDesc), _packer(PagedReorderDesc)
 _PAGED_DTYPES = {}      # torch type -> bsm_dtype, filled on first use
-_INT32 = _INT64 = _FLOAT32 = _cuda = None
+_INT32 = _INT64 = _FLOAT32 = None
 _BYTES = ()             # types of a byte a value
+
+
+class _NoDevice:        # stands for torch.cuda until the types are known
+    @staticmethod
+    def current_device():
+        return -2
+
+
+_cuda = _NoDevice
 
 
 def _paged_types():
@@ -500,12 +509,12 @@ def _caches(k_cache, v_cache, dev: int, ndim: int = 4):
     return st
 
 
-def _page_tables(tables, n: int, dev: int, what: str = "tables"):
+def _page_tables(tables, n: int, dev: int):
     """(address, row stride, width) of the page tables of n requests."""
-    st = _strided(tables, what, 2, dev)
+    st = _strided(tables, "tables", 2, dev)
     rows, width = tables.shape
     if tables.dtype is not _INT32 or rows < n:
-        raise ValueError("%s must be %s, a row for each of %d requests" % (what, _INT32, n))
+        raise ValueError("tables must be %s, a row for each of %d requests" % (_INT32, n))
     return tables.data_ptr(), st[0] if rows > 1 else width, width
 
 
@@ -551,32 +560,50 @@ def bsm_paged_write_rotary(q, k, v, q_out, k_cache, v_cache, slots, positions, t
     """bsm_paged_write with the first columns of keys, and of queries q on the way to
     q_out (both [tokens, heads_q, dim], or None), rotated: table [positions, rotary_dim]
     fp32 holds rotary_dim / 2 cosines and as many sines of every position."""
-    dtype = _paged_dtype(k, v, k_cache, v_cache) if q is None else _paged_dtype(k, v, k_cache, v_cache, q, q_out)
-    dev = _device(k, "k")
-    ks, vs, cs = _strided(k, "k", 3, dev), _strided(v, "v", 3, dev), _caches(k_cache, v_cache, dev)
+    kind, dev = k.dtype, k.get_device()
+    code = _PAGED_DTYPES.get(kind)
+    ks, vs, cs, ts = k.stride(), v.stride(), k_cache.stride(), table.stride()
+    # the usual case at once; whatever fails here is looked at one by one
+    if not (code is not None and dev >= 0 and dev == _cuda.current_device() and len(cs) == 4 and len(ks) == 3 and len(vs) == 3
+            and len(ts) == 2 and ks[2] == 1 and vs[2] == 1 and cs[3] == 1 and ts[1] == 1 and v_cache.stride() == cs and v.dtype is kind
+            and k_cache.dtype is kind and v_cache.dtype is kind and table.dtype is _FLOAT32 and positions.dtype is _INT32
+            and slots.dtype is _INT64 and v.get_device() == dev and k_cache.get_device() == dev
+            and v_cache.get_device() == dev and table.get_device() == dev and positions.get_device() == dev
+            and slots.get_device() == dev and positions.is_contiguous() and slots.is_contiguous()):
+        code = _paged_dtype(k, v, k_cache, v_cache)
+        dev = _device(k, "k")
+        ks, vs, cs = _strided(k, "k", 3, dev), _strided(v, "v", 3, dev), _caches(k_cache, v_cache, dev)
+        ts = _strided(table, "table", 2, dev)
+        if table.dtype is not _FLOAT32:
+            raise ValueError("table must be %s (got %s)" % (_FLOAT32, table.dtype))
+        _vec(positions, "positions", _INT32, 0, dev)
+        _vec(slots, "slots", _INT64, 0, dev)
     tokens, heads, dim = shape = k.shape
-    pages, page_size, ch, cd = k_cache.shape
-    if v.shape != shape or heads != ch or dim != cd:
-        raise ValueError("k and v must be [tokens, %d, %d]" % (ch, cd))
+    pages, page_size, ch, cd = cache = k_cache.shape
+    if v.shape != shape or heads != ch or dim != cd or v_cache.shape != cache:
+        raise ValueError("k and v must be [tokens, %d, %d], and the caches of one shape" % (ch, cd))
+    if positions.numel() < tokens or slots.numel() < tokens:
+        raise ValueError("positions and slots must have %d entries" % tokens)
     if q is None:
         if q_out is not None:
             raise ValueError("q_out without q")
         heads_q, qp, op, qs, os_ = 0, 0, 0, (0, 0), (0, 0)
     else:
-        qs, os_ = _strided(q, "q", 3, dev), _strided(q_out, "q_out", 3, dev)
-        heads_q = q.shape[1]
-        if q.shape[0] != tokens or q.shape[2] != dim or q_out.shape != q.shape:
+        qs, os_, qshape = q.stride(), q_out.stride(), q.shape
+        if not (q.dtype is kind and q_out.dtype is kind and q.get_device() == dev and q_out.get_device() == dev
+                and len(qs) == 3 and len(os_) == 3 and qs[2] == 1 and os_[2] == 1):
+            _paged_dtype(k, q, q_out)
+            qs, os_ = _strided(q, "q", 3, dev), _strided(q_out, "q_out", 3, dev)
+        heads_q = qshape[1]
+        if qshape[0] != tokens or qshape[2] != dim or q_out.shape != qshape:
             raise ValueError("q and q_out must be [%d, heads, %d]" % (tokens, dim))
         qp, op = q.data_ptr(), q_out.data_ptr()
-    ts = _strided(table, "table", 2, dev)
     n_positions, rot = table.shape
-    if table.dtype is not _FLOAT32:
-        raise ValueError("table must be %s (got %s)" % (_FLOAT32, table.dtype))
     d = _pack_rotary(qp, k.data_ptr(), v.data_ptr(), op, k_cache.data_ptr(), v_cache.data_ptr(), table.data_ptr(),
-                     _vec(positions, "positions", _INT32, tokens, dev), _vec(slots, "slots", _INT64, tokens, dev),
+                     positions.data_ptr(), slots.data_ptr(),
                      qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], os_[0], os_[1], cs[0], cs[1], cs[2],
                      ts[0] if n_positions > 1 else rot, tokens, heads_q, heads, dim, rot, n_positions, page_size, pages,
-                     dtype, flags)
+                     code, flags)
     rc = lib().bsm_paged_write_rotary(d, _stream(stream))
     if rc:
         _check(rc, "bsm_paged_write_rotary")
@@ -625,22 +652,31 @@ def bsm_beam_select(logits, scores, out_scores, parents, tokens, workspace, ende
     """The best continuations [requests, keep] (the outputs' shape) over beams and
     vocabulary of logits [requests, beams, vocab] (any strides; the last dimension
     contiguous) and scores [requests, beams]; ended: bool or bytes [requests, beams]."""
-    dtype = _paged_dtype(logits)
-    dev = _device(logits, "logits")
-    st = _strided(logits, "logits", 3, dev)
+    code, dev, st = _PAGED_DTYPES.get(logits.dtype), logits.get_device(), logits.stride()
+    # the usual case at once; whatever fails here is looked at one by one
+    if not (code is not None and dev >= 0 and dev == _cuda.current_device() and len(st) == 3 and st[2] == 1 and scores.dtype is _FLOAT32
+            and out_scores.dtype is _FLOAT32 and parents.dtype is _INT32 and tokens.dtype is _INT32
+            and scores.get_device() == dev and out_scores.get_device() == dev and parents.get_device() == dev
+            and tokens.get_device() == dev and workspace.get_device() == dev and scores.is_contiguous()
+            and out_scores.is_contiguous() and parents.is_contiguous() and tokens.is_contiguous()
+            and workspace.is_contiguous()):
+        code = _paged_dtype(logits)
+        dev = _device(logits, "logits")
+        st = _strided(logits, "logits", 3, dev)
+        for t, what, kind in ((scores, "scores", _FLOAT32), (out_scores, "out_scores", _FLOAT32),
+                              (parents, "parents", _INT32), (tokens, "tokens", _INT32)):
+            _vec(t, what, kind, 0, dev)
+        _elsewhere(workspace, "workspace", dev)
+        _dptr(workspace, None, "workspace")
     n, beams, vocab = logits.shape
+    shape = out_scores.shape
     if scores.shape != (n, beams) or (ended is not None and (ended.shape != (n, beams) or ended.dtype not in _BYTES)):
         raise ValueError("scores must be [%d, %d], and ended bool or bytes of that shape" % (n, beams))
-    if out_scores.dim() != 2 or out_scores.shape[0] != n or parents.shape != out_scores.shape or \
-            tokens.shape != out_scores.shape:
+    if len(shape) != 2 or shape[0] != n or parents.shape != shape or tokens.shape != shape:
         raise ValueError("out_scores, parents and tokens must be [%d, keep], all three" % n)
-    keep = out_scores.shape[1]
-    _elsewhere(workspace, "workspace", dev)
-    d = _pack_select(logits.data_ptr(), _vec(scores, "scores", _FLOAT32, 0, dev),
-                     0 if ended is None else _vec(ended, "ended", ended.dtype, 0, dev),
-                     _vec(out_scores, "out_scores", _FLOAT32, 0, dev), _vec(parents, "parents", _INT32, 0, dev),
-                     _vec(tokens, "tokens", _INT32, 0, dev), _dptr(workspace, None, "workspace"), workspace.nbytes,
-                     st[0] if n > 1 else 0, st[1] if beams > 1 else 0, n, beams, vocab, keep, end_token, dtype)
+    d = _pack_select(logits.data_ptr(), scores.data_ptr(), 0 if ended is None else _vec(ended, "ended", ended.dtype, 0, dev),
+                     out_scores.data_ptr(), parents.data_ptr(), tokens.data_ptr(), workspace.data_ptr(), workspace.nbytes,
+                     st[0] if n > 1 else 0, st[1] if beams > 1 else 0, n, beams, vocab, shape[1], end_token, code)
     rc = lib().bsm_beam_select(d, _stream(stream))
     if rc:
         _check(rc, "bsm_beam_select")
@@ -658,27 +694,45 @@ def bsm_paged_reorder(parents, lengths, tables, free_pages, new_lengths, new_tab
     """The paged cache [pages, page_size, heads, dim], or that of all layers [layers, pages,
     page_size, heads, dim], follows parents [requests, beams]; tables and lengths have a row
     for each beam (new_tables and new_lengths may be the same tensors)."""
-    dtype = _paged_dtype(k_cache, v_cache)
-    dev, ndim = _device(k_cache, "k_cache"), 5 if len(k_cache.shape) == 5 else 4
-    cs, shape = _caches(k_cache, v_cache, dev, ndim), k_cache.shape
+    kind, dev, cs, shape = k_cache.dtype, k_cache.get_device(), k_cache.stride(), k_cache.shape
+    code, ps, ts, ns, ndim = _PAGED_DTYPES.get(kind), parents.stride(), tables.stride(), new_tables.stride(), len(cs)
+    # the usual case at once; whatever fails here is looked at one by one
+    if not (code is not None and dev >= 0 and dev == _cuda.current_device() and (ndim == 4 or ndim == 5) and cs[-1] == 1 and v_cache.stride() == cs
+            and v_cache.shape == shape and v_cache.dtype is kind and len(ps) == 2 and ps[1] == 1 and len(ts) == 2 and ts[1] == 1
+            and len(ns) == 2 and ns[1] == 1 and parents.dtype is _INT32 and lengths.dtype is _INT32 and tables.dtype is _INT32
+            and free_pages.dtype is _INT32 and new_lengths.dtype is _INT32 and new_tables.dtype is _INT32
+            and dropped.dtype is _INT32 and info.dtype is _INT64 and v_cache.get_device() == dev
+            and parents.get_device() == dev and lengths.get_device() == dev and tables.get_device() == dev
+            and free_pages.get_device() == dev and new_lengths.get_device() == dev and new_tables.get_device() == dev
+            and dropped.get_device() == dev and info.get_device() == dev and workspace.get_device() == dev
+            and lengths.is_contiguous() and free_pages.is_contiguous() and new_lengths.is_contiguous()
+            and dropped.is_contiguous() and info.is_contiguous() and workspace.is_contiguous()):
+        code = _paged_dtype(k_cache, v_cache)
+        dev, ndim = _device(k_cache, "k_cache"), 5 if ndim == 5 else 4
+        cs = _caches(k_cache, v_cache, dev, ndim)
+        ps = _strided(parents, "parents", 2, dev)
+        ts, ns = _strided(tables, "tables", 2, dev), _strided(new_tables, "new_tables", 2, dev)
+        for t, what, kind in ((lengths, "lengths", _INT32), (free_pages, "free_pages", _INT32),
+                              (new_lengths, "new_lengths", _INT32), (dropped, "dropped", _INT32), (info, "info", _INT64)):
+            _vec(t, what, kind, 0, dev)
+        for t, what in ((parents, "parents"), (tables, "tables"), (new_tables, "new_tables")):
+            if t.dtype is not _INT32:
+                raise ValueError("%s must be %s (got %s)" % (what, _INT32, t.dtype))
+        _elsewhere(workspace, "workspace", dev)
+        _dptr(workspace, None, "workspace")
     if ndim == 4:
         cs, shape = (0, *cs), (1, *shape)
-    ps = _strided(parents, "parents", 2, dev)
     n, beams = parents.shape
-    if parents.dtype is not _INT32:
-        raise ValueError("parents must be %s (got %s)" % (_INT32, parents.dtype))
-    tab, stride, width = _page_tables(tables, n * beams, dev)
-    new_tab, new_stride, new_width = _page_tables(new_tables, n * beams, dev, "new_tables")
-    if new_width != width:
-        raise ValueError("new_tables must be as wide as tables (%d)" % width)
-    _elsewhere(workspace, "workspace", dev)
-    d = _pack_reorder(parents.data_ptr(), _vec(lengths, "lengths", _INT32, n * beams, dev), tab,
-                      _vec(free_pages, "free_pages", _INT32, 0, dev),
-                      _vec(new_lengths, "new_lengths", _INT32, n * beams, dev), new_tab,
-                      _vec(dropped, "dropped", _INT32, 0, dev), _vec(info, "info", _INT64, 4, dev), k_cache.data_ptr(),
-                      v_cache.data_ptr(), _dptr(workspace, None, "workspace"), workspace.nbytes,
-                      ps[0] if n > 1 else 0, stride, new_stride, *cs[:4], n, beams, width, free_pages.numel(),
-                      dropped.numel(), shape[2], shape[0], shape[1], shape[3], shape[4], dtype)
+    rows, width = tables.shape
+    if rows < n * beams or new_tables.shape[0] < n * beams or new_tables.shape[1] != width:
+        raise ValueError("tables and new_tables must have a row of %d for each of %d x %d beams" % (width, n, beams))
+    if lengths.numel() < n * beams or new_lengths.numel() < n * beams or info.numel() < 4:
+        raise ValueError("lengths and new_lengths must have %d entries, info 4" % (n * beams))
+    d = _pack_reorder(parents.data_ptr(), lengths.data_ptr(), tables.data_ptr(), free_pages.data_ptr(),
+                      new_lengths.data_ptr(), new_tables.data_ptr(), dropped.data_ptr(), info.data_ptr(),
+                      k_cache.data_ptr(), v_cache.data_ptr(), workspace.data_ptr(), workspace.nbytes,
+                      ps[0] if n > 1 else 0, ts[0] if rows > 1 else width, ns[0] if rows > 1 else width, *cs[:4], n, beams,
+                      width, free_pages.numel(), dropped.numel(), shape[2], shape[0], shape[1], shape[3], shape[4], code)
     rc = lib().bsm_paged_reorder(d, _stream(stream))
     if rc:
         _check(rc, "bsm_paged_reorder")
