@@ -25,6 +25,17 @@ constexpr int kCluster = 16;                     // CTAs of select_together that
 
 __device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
 
+// A number as a whole one of the same order.
+__device__ __forceinline__ uint32_t ordered(float x)
+{
+    const uint32_t b = __float_as_uint(x + 0.0f);               // (-0 becomes 0)
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float disordered(uint32_t u)
+{
+    return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
+}
+
 // The values of a 32-bit word of logits.
 template <int kType> struct Word {
     static constexpr int kN = kType == BSM_F32 ? 1 : 2;         // values of a word
@@ -56,6 +67,32 @@ template <int kType> struct Word {
         }
         const __half2 m = __hmax2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
         return *reinterpret_cast<const uint32_t *>(&m);
+    }
+    // whether a value of a is above its counterpart in b (or NaN)
+    static __device__ __forceinline__ bool above(uint32_t a, uint32_t b)
+    {
+        if (kType == BSM_F32)
+            return !(__uint_as_float(a) <= __uint_as_float(b));
+        if (kType == BSM_BF16)
+            return !__hble2(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&b));
+        return !__hble2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
+    }
+    static __device__ __forceinline__ uint32_t twice(float x)
+    {
+        if (kType == BSM_F32)
+            return __float_as_uint(x);
+        if (kType == BSM_BF16) {
+            const __nv_bfloat162 v = __float2bfloat162_rn(x);
+            return *reinterpret_cast<const uint32_t *>(&v);
+        }
+        const __half2 v = __float2half2_rn(x);
+        return *reinterpret_cast<const uint32_t *>(&v);
+    }
+    static __device__ __forceinline__ float most(uint32_t w)            // (not NaN)
+    {
+        float x[kN];
+        get(w, x);
+        return fmaxf(fmaxf(x[0], x[kN - 1]), neg_inf());
     }
 };
 
@@ -129,7 +166,8 @@ __device__ __forceinline__ Pair add(const Pair &x, const Pair &y)
 struct PartSmem {
     float group[kGroups];               // the largest value of each group
     int32_t first[kGroups];             // where a group's value ties with the bound: its lowest token
-    float warp_top[kMostWarps], warp_sum[kMostWarps], warp_bound[kMostWarps];
+    float warp_top[kMostWarps], warp_sum[kMostWarps];
+    uint32_t bound;
     int32_t count, last, hits;
     int16_t hit[kMostWarps * 32];       // threads whose largest value reaches the bound
 };
@@ -198,13 +236,15 @@ template <int kThreads> __device__ __forceinline__ void rank_list(const BeamEntr
 // its group's.  Everything written before by the block can be read after it.
 template <int kThreads> __device__ __forceinline__ float group_bound(PartSmem &s, float &best, int keep)
 {
-    constexpr int kLanes = kThreads / kGroups, kWarps = kThreads / 32;
-    const int tid = threadIdx.x, lane = tid & 31;
+    constexpr int kLanes = kThreads / kGroups;
+    const int tid = threadIdx.x;
 #pragma unroll
     for (int o = 1; o < kLanes; o <<= 1)
         best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, o));
     if (tid % kLanes == 0)
         s.group[tid / kLanes] = best;
+    if (tid == 0)
+        s.bound = 0xffffffffu;
     __syncthreads();
     int over = 0;                       // (a group's threads share the count)
 #pragma unroll
@@ -215,18 +255,10 @@ template <int kThreads> __device__ __forceinline__ float group_bound(PartSmem &s
 #pragma unroll
     for (int o = 1; o < kLanes; o <<= 1)
         over += __shfl_xor_sync(0xffffffffu, over, o);
-    float bound = over < keep ? best : __int_as_float(0x7f800000);
-#pragma unroll
-    for (int o = kLanes; o < 32; o <<= 1)
-        bound = fminf(bound, __shfl_xor_sync(0xffffffffu, bound, o));
-    if (lane == 0)
-        s.warp_bound[tid >> 5] = bound;
+    if (over < keep && tid % kLanes == 0)
+        atomicMin(&s.bound, ordered(best));
     __syncthreads();
-    bound = s.warp_bound[lane % kWarps];
-#pragma unroll
-    for (int o = 1; o < kWarps; o <<= 1)
-        bound = fminf(bound, __shfl_xor_sync(0xffffffffu, bound, o));
-    return bound;
+    return disordered(s.bound);
 }
 
 // A block's bound.  Where more than `keep` groups reach it some tie there: of values equal to the bound
@@ -363,12 +395,13 @@ __device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, 
     using T = Word<kType>;
     constexpr int kWarps = kThreads / 32, kRow = kThreads * T::kW;                          // values of a row of pieces
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const uint32_t row = at / static_cast<uint32_t>(a.parts);
+    const uint32_t row = a.parts == 1 ? at : at / static_cast<uint32_t>(a.parts);
     const int32_t part = static_cast<int32_t>(at - row * a.parts);
     const float score = a.scores[row];
     const bool ended = a.ended && a.ended[row];
-    const uint32_t request = row / static_cast<uint32_t>(a.beams), beam = row - request * a.beams;
-    const unsigned char *base = a.logits + request * a.stride_request + beam * a.stride_beam;
+    const unsigned char *base = a.logits + row * a.stride_beam;
+    if (a.stride_request != a.beams * a.stride_beam)
+        base += row / static_cast<uint32_t>(a.beams) * (a.stride_request - a.beams * a.stride_beam);
     const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(base)) & 15u;
     const int32_t lo = part * a.part, hi = min(lo + a.part, a.vocab);
     uint4 v[kBeamLoads];
@@ -395,21 +428,23 @@ __device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, 
     }
     // exp(x - from) = 2^((x - from) log2(e)), where `from` is a value seen that lies 4 below the largest at
     // most: it seldom moves, and the arguments of the terms that matter stay small, so exact
-    float top = neg_inf(), from = neg_inf(), limit = neg_inf(), sum = 0.0f;
+    float from = neg_inf(), sum = 0.0f;
+    uint32_t most = T::kNone, limit = T::kNone;         // the largest so far; from + 4
     uint64_t minus = 0, sum2 = 0;       // -from twice (0 while nothing but -inf was seen: it sums up to 0); sums of four pieces
     auto take = [&](const uint4 &x) {
         const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-        float ends[T::kN];
-        T::get(T::larger(T::larger(w[0], w[1]), T::larger(w[2], w[3])), ends);
-        const float most = fmaxf(ends[0], ends[T::kN - 1]);
-        top = fmaxf(top, most);
-        if (most > limit) {
-            const float scale = pg_exp2((from - most) * 1.4426950408889634f);
-            sum *= scale;
-            sum2 = mul2(sum2, pack2(scale, scale));
-            from = most;
-            limit = from + 4.0f;
-            minus = pack2(-from, -from);
+        const uint32_t here = T::larger(T::larger(w[0], w[1]), T::larger(w[2], w[3]));
+        most = T::larger(most, here);
+        if (T::above(here, limit)) {
+            const float high = T::most(here);
+            if (high > from) {
+                const float scale = pg_exp2((from - high) * 1.4426950408889634f);
+                sum *= scale;
+                sum2 = mul2(sum2, pack2(scale, scale));
+                from = high;
+                limit = T::twice(from + 4.0f);
+                minus = pack2(-from, -from);
+            }
         }
         const uint64_t log2e = pack2(1.4426950408889634f, 1.4426950408889634f);
 #pragma unroll
@@ -421,43 +456,59 @@ __device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, 
             sum2 = add2(sum2, pack2(pg_exp2(low2(t)), pg_exp2(high2(t))));
         }
     };
+    auto fold = [&]() {
+        sum += low2(sum2) + high2(sum2);
+        sum2 = 0;
+    };
+    // four rows of pieces are at hand; those four further are on their way while these are worked on
+    constexpr int kSpan = kBeamLoads * kRow;
+    int further = (hi - lo) / kSpan - 1;                // spans past the first that need no look at the ends
+    if (off != 0 && lo + (further + 1) * kSpan + T::kW > a.vocab)
+        --further;
     int32_t first = lo;
-    bool raw = false;                   // the pieces at hand wait to be shifted into place
     const unsigned char *p = base + static_cast<int64_t>(lo + tid * T::kW) * T::kEs - off;
-    while (first < hi) {
-        // four rows of pieces; those four further are on their way while the next ones are worked on
-        const int32_t next = first + kBeamLoads * kRow;
-        const bool whole = next + kBeamLoads * kRow <= hi && (off == 0 || next + kBeamLoads * kRow + T::kW <= a.vocab);
-        p += kBeamLoads * kRow * T::kEs;
-        if (whole && off == 0) {
+    bool raw = false;                   // the pieces at hand wait to be shifted into place
+    if (off == 0) {
+        for (int g = 0; g < further; ++g) {
+            p += kSpan * T::kEs;
 #pragma unroll
             for (int j = 0; j < kBeamLoads; ++j) {
                 take(v[j]);
                 v[j] = *reinterpret_cast<const uint4 *>(p + j * kRow * T::kEs);
             }
-        } else {
+            fold();
+        }
+    } else {
+        for (int g = 0; g < further; ++g) {
+            p += kSpan * T::kEs;
 #pragma unroll
             for (int j = 0; j < kBeamLoads; ++j) {
-                if (first + j * kRow < hi)
-                    take(raw ? shifted(v[j], *reinterpret_cast<const uint4 *>(p + (j - kBeamLoads) * kRow * T::kEs + 16), off) : v[j]);
-                if (whole)
-                    v[j] = *reinterpret_cast<const uint4 *>(p + j * kRow * T::kEs);
-                else if (next + j * kRow < hi)
-                    v[j] = load(next + j * kRow);
+                take(raw ? shifted(v[j], *reinterpret_cast<const uint4 *>(p + (j - kBeamLoads) * kRow * T::kEs + 16), off) : v[j]);
+                v[j] = *reinterpret_cast<const uint4 *>(p + j * kRow * T::kEs);
             }
-            raw = whole;
+            raw = true;
+            fold();
         }
-        sum += low2(sum2) + high2(sum2);
-        sum2 = 0;
-        first = next;
     }
-    top = fmaxf(top, neg_inf());        // (not NaN)
+    first += (further > 0 ? further : 0) * kSpan;
+    for (; first < hi; first += kSpan) {
+#pragma unroll
+        for (int j = 0; j < kBeamLoads; ++j) {
+            if (first + j * kRow < hi)
+                take(raw ? shifted(v[j], *reinterpret_cast<const uint4 *>(p + j * kRow * T::kEs + 16), off) : v[j]);
+            if (first + kSpan + j * kRow < hi)
+                v[j] = load(first + kSpan + j * kRow);
+        }
+        raw = false;
+        fold();
+    }
+    const float top = T::most(most);
     // the part's maximum and sum: each warp's here, of them all by one warp below
-    float all = from;
+    float all = top;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1)
         all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, o));
-    sum *= from == all ? 1.0f : pg_exp2((from - all) * 1.4426950408889634f);
+    sum *= all == neg_inf() ? 1.0f : pg_exp2((from - all) * 1.4426950408889634f);
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1)
         sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -527,15 +578,6 @@ struct Cand {
     uint64_t key;                       // 0: none
     int32_t at;
 };
-__device__ __forceinline__ uint32_t ordered(float x)
-{
-    const uint32_t b = __float_as_uint(x + 0.0f);               // (-0 becomes 0)
-    return b & 0x80000000u ? ~b : b | 0x80000000u;
-}
-__device__ __forceinline__ float disordered(uint32_t u)
-{
-    return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
-}
 __device__ __forceinline__ Cand no_cand() { return Cand{0, INT_MAX}; }
 __device__ __forceinline__ Cand cand(const Pair &x, int32_t at)
 {
@@ -641,7 +683,7 @@ __device__ __forceinline__ void join(const BeamSelectArgs &a, JoinSmem &s, const
                 if (o < a.parts)
                     sum = add(sum, Pair{__shfl_xor_sync(0xffffffffu, sum.hi, o), __shfl_xor_sync(0xffffffffu, sum.lo, o)});
             // NaN or +inf among the logits, or none above -inf: the row's softmax is NaN
-            if (!(sum.hi > 0.0f))
+            if (!(sum.hi > 0.0f && sum.hi < __int_as_float(0x7f800000)))
                 kind = 0;
             const Pair l = log_of(sum);
             shift = add(shift, Pair{-l.hi, -l.lo});

@@ -180,6 +180,14 @@ def test_rows_with_nan_or_infinity_have_no_candidates():
     assert (out[1][0] == 0).all() and (out[1][1] == -1).all() and (out[1][2] > 0).all()
 
 
+def test_infinity_beside_the_largest_f16_value():
+    x, s = _data(2, 2, 700, "f16", seed=12)
+    x[0, 0, 3], x[0, 0, 650] = 65504.0, float("inf")
+    x[1, 0, 3] = 65504.0
+    out = _check(x, s, 5)
+    assert (out[1][0] == 1).all() and out[2][1, 0] == 3
+
+
 def test_large_and_far_values():
     x, s = _data(2, 3, 6000, "f32", seed=7)
     x[0] *= 1e4                                     # one token has all the mass
