@@ -26,9 +26,8 @@ SelectLayout select_layout(int32_t n, int32_t beams, int32_t vocab, int32_t keep
 {
     SelectLayout l{};
     l.cut = beam_cut(n, beams, vocab, es, n_sm);
-    const int64_t lists = static_cast<int64_t>(n) * beams * l.cut.parts;
-    l.meta = up256(lists * keep * static_cast<int64_t>(sizeof(BeamEntry)));
-    l.bytes = l.meta + up256(lists * static_cast<int64_t>(sizeof(BeamPart)));
+    l.meta = up256(l.cut.lists * keep * static_cast<int64_t>(sizeof(BeamEntry)));
+    l.bytes = l.meta + up256(l.cut.lists * static_cast<int64_t>(sizeof(BeamPart)));
     return l;
 }
 
@@ -99,9 +98,7 @@ int beam_select(const bsm_beam_select_desc *d, bsm_stream_t stream)
     a.vocab = d->vocab;
     a.keep = d->keep;
     a.end_token = d->end_token;
-    a.parts = l.cut.parts;
-    a.part = l.cut.part;
-    if (int e = launch_beam_select(a, d->dtype, l.cut.together, stream))
+    if (int e = launch_beam_select(a, d->dtype, l.cut, stream))
         return record_cuda_error(e, "beam select launch");
     return BSM_OK;
 }

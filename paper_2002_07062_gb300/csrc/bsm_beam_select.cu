@@ -390,20 +390,18 @@ __device__ __noinline__ int list_again(PartSmem &s, BeamEntry *list, int room, i
 // seen is read once more, from the L2 cache, by their warps.
 // kEager: the first pieces are asked for before it is known whether the beam needs them.
 template <int kType, int kThreads, bool kEager>
-__device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, BeamEntry *list, uint32_t at, BeamPart *meta, BeamEntry *to)
+__device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, BeamEntry *list, uint32_t row, int32_t lo, int32_t hi,
+                                          BeamPart *meta, BeamEntry *to)
 {
     using T = Word<kType>;
     constexpr int kWarps = kThreads / 32, kRow = kThreads * T::kW;                          // values of a row of pieces
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const uint32_t row = a.parts == 1 ? at : at / static_cast<uint32_t>(a.parts);
-    const int32_t part = static_cast<int32_t>(at - row * a.parts);
     const float score = a.scores[row];
     const bool ended = a.ended && a.ended[row];
     const unsigned char *base = a.logits + row * a.stride_beam;
     if (a.stride_request != a.beams * a.stride_beam)
         base += row / static_cast<uint32_t>(a.beams) * (a.stride_request - a.beams * a.stride_beam);
     const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(base)) & 15u;
-    const int32_t lo = part * a.part, hi = min(lo + a.part, a.vocab);
     uint4 v[kBeamLoads];
     auto load = [&](int32_t first) { return load_piece<kType>(base, off, first + tid * T::kW, hi, a.vocab); };
     if (kEager) {
@@ -613,6 +611,8 @@ struct JoinSmem {   // (score and kind are set before the join)
     float score[kBeamMost], top[kBeamMost];
     Pair shift[kBeamMost];              // score - log(sum): what a row adds to x - top
     int32_t kind[kBeamMost];            // 0: no candidate, 1: one (an ended beam), 2: its parts' lists
+    int32_t first[kBeamMost + 1], end[kBeamMost];       // its lists
+    int8_t beam[kBeamMostLists];        // of a list, -1: none
     Cand bound;
     int32_t count;
 };
@@ -627,9 +627,11 @@ struct Lists {
 // Entry i of list l, by value: score + (x - top) - log(sum) in two fp32 numbers.
 __device__ __forceinline__ Cand entry(const BeamSelectArgs &a, const JoinSmem &s, const Lists &z, int l, int i)
 {
-    const int b = static_cast<int>(static_cast<uint32_t>(l) / static_cast<uint32_t>(a.parts));
+    const int b = s.beam[l];
+    if (b < 0)
+        return no_cand();
     if (s.kind[b] != 2)
-        return s.kind[b] == 1 && l == b * a.parts && i == 0 ? cand(s.shift[b], b * a.vocab + a.end_token) : no_cand();
+        return s.kind[b] == 1 && l == s.first[b] && i == 0 ? cand(s.shift[b], b * a.vocab + a.end_token) : no_cand();
     if (i >= z.meta[l].count)
         return no_cand();
     const BeamEntry e = z.entries[l * a.keep + i];
@@ -652,7 +654,7 @@ __device__ __forceinline__ int count_better(const Cand *all, int n, const Cand &
 // The lists of all parts of all beams of a request, in order.  Of the q-th entries of all lists (the
 // first ones, or as deep as it takes) the need-th best is a bound that need x q >= keep
 // entries reach; the few that do are ordered by counting for each how many are better.
-__device__ __forceinline__ void join(const BeamSelectArgs &a, JoinSmem &s, const Lists &z, int32_t request)
+__device__ __forceinline__ void join(const BeamSelectArgs &a, JoinSmem &s, const Lists &z, int32_t request, int lists)
 {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid == 0) {
@@ -665,14 +667,15 @@ __device__ __forceinline__ void join(const BeamSelectArgs &a, JoinSmem &s, const
         float top = neg_inf();
         Pair shift{score, 0.0f};
         if (kind == 2) {
-            const BeamPart *meta = z.meta + b * a.parts;
-            for (int p = lane; p < a.parts; p += 32)
+            const BeamPart *meta = z.meta + s.first[b];
+            const int parts = s.end[b] - s.first[b];
+            for (int p = lane; p < parts; p += 32)
                 top = fmaxf(top, meta[p].top);
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1)
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
             Pair sum{0.0f, 0.0f};
-            for (int p = lane; p < a.parts; p += 32) {
+            for (int p = lane; p < parts; p += 32) {
                 const BeamPart x = meta[p];
                 if (x.sum != 0.0f) {    // (an empty part: -inf - -inf)
                     const float w = expf(x.top - top), m = x.sum * w;
@@ -680,7 +683,7 @@ __device__ __forceinline__ void join(const BeamSelectArgs &a, JoinSmem &s, const
                 }
             }
             for (int o = 16; o > 0; o >>= 1)
-                if (o < a.parts)
+                if (o < parts)
                     sum = add(sum, Pair{__shfl_xor_sync(0xffffffffu, sum.hi, o), __shfl_xor_sync(0xffffffffu, sum.lo, o)});
             // NaN or +inf among the logits, or none above -inf: the row's softmax is NaN
             if (!(sum.hi > 0.0f && sum.hi < __int_as_float(0x7f800000)))
@@ -695,7 +698,6 @@ __device__ __forceinline__ void join(const BeamSelectArgs &a, JoinSmem &s, const
         }
     }
     __syncthreads();
-    const int lists = a.beams * a.parts;
     const int q = (a.keep + lists - 1) / lists, need = (a.keep + q - 1) / q;
     for (int l = tid; l < lists; l += kJoinThreads)
         z.heads[l] = entry(a, s, z, l, q - 1);
@@ -740,8 +742,8 @@ __device__ __forceinline__ void join(const BeamSelectArgs &a, JoinSmem &s, const
     }
 }
 
-// A request's beams: scores, and which have candidates.
-__device__ __forceinline__ void get_beams(const BeamSelectArgs &a, JoinSmem &s, int32_t request)
+// A request's beams: scores, which have candidates, and their lists ([first, end) of beam b).
+template <typename F> __device__ __forceinline__ void get_beams(const BeamSelectArgs &a, JoinSmem &s, int32_t request, F &&lists_of)
 {
     const int b = threadIdx.x;
     if (b < a.beams) {
@@ -750,14 +752,18 @@ __device__ __forceinline__ void get_beams(const BeamSelectArgs &a, JoinSmem &s, 
         const bool ended = a.ended && a.ended[row];
         s.score[b] = score;
         s.kind[b] = !(fabsf(score) < __int_as_float(0x7f800000)) ? 0 : ended ? 1 : 2;
+        int first, end;
+        lists_of(b, first, end);
+        s.first[b] = first;
+        s.end[b] = end;
+        for (int l = first; l < end; ++l)
+            s.beam[l] = static_cast<int8_t>(b);
     }
 }
 
-// Dynamic shared memory of a join: the lists, then candidates (past what a part needs, where one was
-// taken before).
-__device__ __forceinline__ Lists lists_at(const BeamSelectArgs &a, unsigned char *raw)
+// Dynamic shared memory of a join.
+__device__ __forceinline__ Lists lists_at(const BeamSelectArgs &a, unsigned char *raw, int lists)
 {
-    const int lists = a.beams * a.parts;
     Lists z;
     z.meta = reinterpret_cast<BeamPart *>(raw);
     z.heads = reinterpret_cast<Cand *>(z.meta + lists);
@@ -766,33 +772,60 @@ __device__ __forceinline__ Lists lists_at(const BeamSelectArgs &a, unsigned char
     return z;
 }
 
+// All rows' logits form a line of rows of pieces (kRowThreads x 16 bytes), `line` of them; unit u (a CTA) takes
+// those from line u / units to line (u + 1) / units: the same amount each, whatever rows are cut.  The part
+// of row r that unit u takes has list r + u.
+__device__ __forceinline__ int64_t line_at(const BeamSelectArgs &a, uint32_t u) { return a.line * u / a.units; }
+__device__ __forceinline__ int64_t unit_of(const BeamSelectArgs &a, int64_t x) { return ((x + 1) * a.units - 1) / a.line; }
+
 template <int kType> __global__ void __launch_bounds__(kRowThreads, kRowCtas) select_rows(const BeamSelectArgs a)
 {
+    constexpr int kRow = kRowThreads * Word<kType>::kW;
     __shared__ PartSmem s;
     extern __shared__ __align__(16) unsigned char raw[];
     grid_dependency_wait();
     grid_launch_dependents();
-    take_part<kType, kRowThreads, false>(a, s, reinterpret_cast<BeamEntry *>(raw), blockIdx.x, a.meta + blockIdx.x,
-                            a.entries + static_cast<int64_t>(blockIdx.x) * a.keep);
+    int64_t x = line_at(a, blockIdx.x);
+    const int64_t end = line_at(a, blockIdx.x + 1);
+    uint32_t row = static_cast<uint32_t>(x / a.row_pieces);
+    int32_t at = static_cast<int32_t>(x - static_cast<int64_t>(row) * a.row_pieces);
+    while (x < end) {
+        const int32_t n = static_cast<int32_t>(min(end - x, static_cast<int64_t>(a.row_pieces - at)));
+        const int64_t list = static_cast<int64_t>(row) + blockIdx.x;
+        take_part<kType, kRowThreads, false>(a, s, reinterpret_cast<BeamEntry *>(raw), row, at * kRow, min((at + n) * kRow, a.vocab),
+                                             a.meta + list, a.entries + list * a.keep);
+        x += n;
+        ++row;
+        at = 0;
+        __syncthreads();
+    }
 }
 
 __global__ void __launch_bounds__(kJoinThreads) select_join(const BeamSelectArgs a)
 {
     __shared__ JoinSmem s;
     extern __shared__ __align__(16) unsigned char raw[];
-    const int32_t request = blockIdx.x, lists = a.beams * a.parts;
-    const Lists z = lists_at(a, raw);
+    const int32_t request = blockIdx.x;
+    const int64_t row0 = static_cast<int64_t>(request) * a.beams;
+    const int64_t first = row0 + unit_of(a, row0 * a.row_pieces);
+    const int lists = static_cast<int>(row0 + a.beams - 1 + unit_of(a, (row0 + a.beams) * a.row_pieces - 1) - first + 1);
+    const Lists z = lists_at(a, raw, lists);
+    for (int l = threadIdx.x; l < lists; l += kJoinThreads)
+        s.beam[l] = -1;
     grid_dependency_wait();
     grid_launch_dependents();
     // (of beams without a list it copies what happens to be there, and nobody reads it)
-    const int64_t first = static_cast<int64_t>(request) * lists;
     for (int i = threadIdx.x; i < lists; i += kJoinThreads)
         reinterpret_cast<uint4 *>(z.meta)[i] = reinterpret_cast<const uint4 *>(a.meta + first)[i];
     for (int i = threadIdx.x; i < lists * a.keep; i += kJoinThreads)
         z.entries[i] = a.entries[first * a.keep + i];
-    get_beams(a, s, request);
     __syncthreads();
-    join(a, s, z, request);
+    get_beams(a, s, request, [&](int b, int &from, int &to) {
+        from = static_cast<int>(row0 + b + unit_of(a, (row0 + b) * a.row_pieces) - first);
+        to = static_cast<int>(row0 + b + unit_of(a, (row0 + b + 1) * a.row_pieces - 1) - first + 1);
+    });
+    __syncthreads();
+    join(a, s, z, request, lists);
 }
 
 // Both in one launch: a cluster takes a request's parts, their lists go to the first CTA's shared memory,
@@ -805,7 +838,7 @@ template <int kType> __global__ void __launch_bounds__(kJoinThreads, 3) select_t
     const uint32_t request = blockIdx.x / kCluster, rank = blockIdx.x % kCluster, lists = static_cast<uint32_t>(a.beams) * a.parts;
     // the first CTA's shared memory may be written once it runs
     asm volatile("barrier.cluster.arrive.release;" ::: "memory");
-    const Lists z = lists_at(a, raw + static_cast<size_t>(a.list + a.keep) * sizeof(BeamEntry));
+    const Lists z = lists_at(a, raw + static_cast<size_t>(a.list + a.keep) * sizeof(BeamEntry), lists);
     BeamPart *meta;
     BeamEntry *entries;
     asm("mapa.u64 %0, %1, 0;" : "=l"(meta) : "l"(z.meta));
@@ -813,16 +846,22 @@ template <int kType> __global__ void __launch_bounds__(kJoinThreads, 3) select_t
     grid_dependency_wait();
     grid_launch_dependents();
     if (rank == 0)
-        get_beams(a, j, static_cast<int32_t>(request));
+        get_beams(a, j, static_cast<int32_t>(request), [&](int b, int &from, int &to) {
+            from = b * a.parts;
+            to = from + a.parts;
+        });
     asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
     for (uint32_t l = rank; l < lists; l += kCluster) {
-        take_part<kType, kJoinThreads, true>(a, s, reinterpret_cast<BeamEntry *>(raw), request * lists + l, meta + l, entries + l * a.keep);
+        const uint32_t b = l / static_cast<uint32_t>(a.parts);
+        const int32_t lo = static_cast<int32_t>(l - b * a.parts) * a.part;
+        take_part<kType, kJoinThreads, true>(a, s, reinterpret_cast<BeamEntry *>(raw), request * a.beams + b, lo,
+                                             min(lo + a.part, a.vocab), meta + l, entries + l * a.keep);
         __syncthreads();
     }
     asm volatile("barrier.cluster.arrive.release;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
     if (rank == 0)
-        join(a, j, z, static_cast<int32_t>(request));
+        join(a, j, z, static_cast<int32_t>(request), static_cast<int>(lists));
 }
 
 int launch_cluster(void (*kernel)(BeamSelectArgs), dim3 grid, size_t smem, cudaStream_t st, const BeamSelectArgs &a)
@@ -860,37 +899,52 @@ size_t join_smem(int32_t lists, int32_t keep)
 // SMs, and their joins to a second launch.
 BeamCut beam_cut(int32_t n, int32_t beams, int32_t vocab, int es, int n_sm)
 {
-    const int64_t piece = 16 / es;
+    const int64_t piece = 16 / es, rows = static_cast<int64_t>(n) * beams;
     auto up = [](int64_t x, int64_t d) { return (x + d - 1) / d; };
-    const int64_t rows = static_cast<int64_t>(n) * beams;
     BeamCut c{};
     c.together = static_cast<int64_t>(n) * kCluster <= 3 * static_cast<int64_t>(n_sm) &&
                  static_cast<int64_t>(beams) * vocab * es <= kCluster * kTogetherBytes;
-    // one part for each place on an SM, of four pieces a thread at least
-    const int64_t least = c.together ? kJoinThreads * piece : kBeamLoads * kRowThreads * piece;
-    int64_t parts = c.together ? kCluster / beams : up(4 * static_cast<int64_t>(n_sm), rows < 1 ? 1 : rows);
-    parts = std::min(std::min(parts, up(vocab, least)), static_cast<int64_t>(kBeamMostLists / beams));
-    parts = std::max<int64_t>(parts, 1);
-    const int64_t each = up(up(vocab, parts), piece) * piece;
-    c.part = static_cast<int32_t>(each);
-    c.parts = static_cast<int32_t>(up(vocab, each));
+    if (c.together) {
+        // parts of a piece a thread at least
+        int64_t parts = std::min<int64_t>(kCluster / beams, up(vocab, kJoinThreads * piece));
+        parts = std::max<int64_t>(parts, 1);
+        c.part = static_cast<int32_t>(up(up(vocab, parts), piece) * piece);
+        c.parts = static_cast<int32_t>(up(vocab, c.part));
+        c.request_lists = beams * c.parts;
+        c.lists = rows * c.parts;
+        return c;
+    }
+    // a unit for each place on an SM, of four pieces a thread at least; a request's lists, at most one more than
+    // its beams and the units that it touches, fit the join
+    c.row_pieces = static_cast<int32_t>(up(vocab, kRowThreads * piece));
+    c.line = rows * c.row_pieces;
+    int64_t units = std::min<int64_t>(static_cast<int64_t>(n_sm) * kRowCtas, up(c.line, kBeamLoads));
+    units = std::min(units, static_cast<int64_t>(n) * (kBeamMostLists - 2 - beams));
+    c.units = static_cast<int32_t>(std::max<int64_t>(units, 1));
+    c.request_lists = static_cast<int32_t>(beams + up(c.units, n) + 2);
+    c.lists = rows + c.units;
     return c;
 }
 
-int launch_beam_select(BeamSelectArgs a, int dtype, bool together, void *stream)
+int launch_beam_select(BeamSelectArgs a, int dtype, const BeamCut &cut, void *stream)
 {
-    const int threads = together ? kJoinThreads : kRowThreads;
+    const int threads = cut.together ? kJoinThreads : kRowThreads;
     a.list = list_entries(a.keep, dtype, threads);
-    const size_t part = part_smem(a.keep, dtype, threads), joint = join_smem(a.beams * a.parts, a.keep);
+    a.parts = cut.parts;
+    a.part = cut.part;
+    a.row_pieces = cut.row_pieces;
+    a.units = cut.units;
+    a.line = cut.line;
+    const size_t part = part_smem(a.keep, dtype, threads), joint = join_smem(cut.request_lists, a.keep);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (together) {
+    if (cut.together) {
         const dim3 grid(static_cast<unsigned>(a.n) * kCluster);
         const size_t smem = part + joint;
         return dtype == BSM_F32    ? launch_cluster(select_together<BSM_F32>, grid, smem, st, a)
                : dtype == BSM_BF16 ? launch_cluster(select_together<BSM_BF16>, grid, smem, st, a)
                                    : launch_cluster(select_together<BSM_F16>, grid, smem, st, a);
     }
-    const dim3 grid(static_cast<unsigned>(a.n) * a.beams * a.parts);
+    const dim3 grid(static_cast<unsigned>(a.units));
     const int e = dtype == BSM_F32    ? launch_early(select_rows<BSM_F32>, grid, kRowThreads, part, st, a)
                   : dtype == BSM_BF16 ? launch_early(select_rows<BSM_BF16>, grid, kRowThreads, part, st, a)
                                       : launch_early(select_rows<BSM_F16>, grid, kRowThreads, part, st, a);
