@@ -37,8 +37,8 @@ struct BeamSelectArgs {
     BeamPart *meta;
     int64_t stride_request, stride_beam;        // bytes
     int32_t n, beams, vocab, keep, end_token;
-    // how the rows are cut (set by the launch): by the beam, or by the line
-    int32_t parts, part;                        // parts of a row, logits of each
+    // how the rows are cut (set by the launch)
+    int32_t parts, part;                        // parts of a row, logits of each (whole pieces of 16 bytes)
     int32_t row_pieces, units;                  // rows of pieces of a row of logits; CTAs that share the line
     int64_t line;                               // rows of pieces of all rows
     int32_t list;                               // entries of a part's list (set by the launch)
@@ -69,8 +69,8 @@ int launch_paged_reorder(PagedReorderArgs a, int n_sm, void *stream);
 // How the rows are cut.
 struct BeamCut {
     bool together;                              // a cluster takes a request, in one launch
-    int32_t parts, part;                        // then: parts of a row, logits of each (whole pieces of 16 bytes)
-    int32_t row_pieces, units;                  // else: see BeamSelectArgs
+    int32_t parts, part;                        // then: see BeamSelectArgs
+    int32_t row_pieces, units;                  // else: see there
     int64_t line;
     int32_t request_lists;                      // of a request at most
     int64_t lists;                              // of all

@@ -21,6 +21,7 @@ constexpr int kGroups = 128;                    // groups of neighbouring thread
 constexpr int kMostWarps = 16;
 constexpr int kRowThreads = 512, kRowCtas = 3;  // of select_rows; its CTAs on an SM
 constexpr int kJoinThreads = 512;                // of select_join and select_together
+constexpr int kMostTogether = 8;                 // requests (a cluster takes about 0.3 us to start)
 constexpr int kCluster = 16;                     // CTAs of select_together that share a request
 
 __device__ __forceinline__ float neg_inf() { return __int_as_float(0xff800000); }
@@ -76,6 +77,15 @@ template <int kType> struct Word {
         if (kType == BSM_BF16)
             return !__hble2(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&b));
         return !__hble2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
+    }
+    // whether a value of a is not below its counterpart in b
+    static __device__ __forceinline__ bool reaches(uint32_t a, uint32_t b)
+    {
+        if (kType == BSM_F32)
+            return __uint_as_float(a) >= __uint_as_float(b);
+        if (kType == BSM_BF16)
+            return !__hblt2(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&b));
+        return !__hblt2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
     }
     static __device__ __forceinline__ uint32_t twice(float x)
     {
@@ -164,12 +174,13 @@ __device__ __forceinline__ Pair add(const Pair &x, const Pair &y)
 }
 
 struct PartSmem {
-    float group[kGroups];               // the largest value of each group
+    alignas(16) float group[kGroups];               // the largest value of each group
     int32_t first[kGroups];             // where a group's value ties with the bound: its lowest token
     float warp_top[kMostWarps], warp_sum[kMostWarps];
     uint32_t bound;
     int32_t count, last, hits;
-    int16_t hit[kMostWarps * 32];       // threads whose largest value reaches the bound
+    int16_t hit[kMostWarps * 32];       // threads whose largest value reaches the bound; entries of a long list
+    uint64_t key[kGroups], key_bound;
 };
 
 // Two fp32 numbers at once.
@@ -211,22 +222,66 @@ template <int kType, int kThreads, typename F> __device__ __forceinline__ void e
     }
 }
 
-// The list's best `keep` in order to `to`: four threads count for each entry how many are better.
-template <int kThreads> __device__ __forceinline__ void rank_list(const BeamEntry *list, int count, int keep, BeamEntry *to)
+// An entry as a whole number of its order: larger values first, then lower tokens.
+__device__ __forceinline__ uint64_t key_of(const BeamEntry &e)
 {
-    const int lane = threadIdx.x & 31, quarter = lane & 3;
-    for (int i0 = (threadIdx.x >> 5) * 8; i0 < count; i0 += kThreads / 4) {
+    return static_cast<uint64_t>(ordered(e.x)) << 32 | ~static_cast<uint32_t>(e.token);
+}
+
+// The list's best `keep` in order to `to`: four threads count for each entry how many are better.  In
+// a long list (equal values, or a part with few of any) the keep-th largest of 128 group maxima first
+// says which ones that can be.
+template <int kThreads> __device__ __forceinline__ void rank_list(PartSmem &s, const BeamEntry *list, int count, int keep, BeamEntry *to)
+{
+    constexpr int kLanes = kThreads / kGroups;
+    const int tid = threadIdx.x, lane = tid & 31;
+    int few = -1;
+    if (count > kGroups) {
+        uint64_t best = 0;
+        for (int i = tid; i < count; i += kThreads)
+            best = max(best, key_of(list[i]));
+#pragma unroll
+        for (int o = 1; o < kLanes; o <<= 1)
+            best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
+        if (tid % kLanes == 0)
+            s.key[tid / kLanes] = best;
+        if (tid == 0) {
+            s.key_bound = 0;
+            s.hits = 0;
+        }
+        __syncthreads();
+        int over = 0;
+        for (int k = tid % kLanes; k < kGroups; k += kLanes)
+            over += s.key[k] > best;
+#pragma unroll
+        for (int o = 1; o < kLanes; o <<= 1)
+            over += __shfl_xor_sync(0xffffffffu, over, o);
+        if (over == keep - 1 && best != 0)
+            s.key_bound = best;
+        __syncthreads();
+        const uint64_t bound = s.key_bound;
+        for (int i = tid; i < count; i += kThreads)
+            if (key_of(list[i]) >= bound) {
+                const int at = atomicAdd(&s.hits, 1);
+                if (at < kMostWarps * 32)
+                    s.hit[at] = static_cast<int16_t>(i);
+            }
+        __syncthreads();
+        few = s.hits <= kMostWarps * 32 ? s.hits : -1;
+    }
+    const int of = few >= 0 ? few : count;
+    for (int i0 = (tid >> 5) * 8; i0 < of; i0 += kThreads / 4) {
         const int i = i0 + lane / 4;
-        const BeamEntry e = list[i < count ? i : 0];
+        const BeamEntry e = list[i >= of ? 0 : few >= 0 ? s.hit[i] : i];
         int better = 0;
 #pragma unroll 4
-        for (int k = quarter; k < count; k += 4) {
-            const BeamEntry o = list[k];
+        for (int k = lane & 3; k < of; k += 4) {
+            const BeamEntry o = list[few >= 0 ? s.hit[k] : k];
             better += (o.x > e.x) | ((o.x == e.x) & (o.token < e.token));
         }
         better += __shfl_xor_sync(0xffffffffu, better, 1);
         better += __shfl_xor_sync(0xffffffffu, better, 2);
-        if (quarter == 0 && i < count && better < keep)
+        if (lane % 4 == 0 && i < of && better < keep)
             to[better] = e;
     }
 }
@@ -370,7 +425,7 @@ __device__ __noinline__ int list_again(PartSmem &s, BeamEntry *list, int room, i
         to_list<kType, kThreads>(s, list, room, v, mine, first, bound, last);
         __syncthreads();
         count = s.count;
-        rank_list<kThreads>(list, count, keep, list + room);
+        rank_list<kThreads>(s, list, count, keep, list + room);
         __syncthreads();
         count = min(count, keep);
         if (tid < count)
@@ -388,42 +443,53 @@ __device__ __noinline__ int list_again(PartSmem &s, BeamEntry *list, int room, i
 // keep-th largest of 128 group maxima is a bound that the part's best `keep` values reach and few
 // others (about as many again): the threads whose maximum reaches it are few, and what they have
 // seen is read once more, from the L2 cache, by their warps.
-// kEager: the first pieces are asked for before it is known whether the beam needs them.
-template <int kType, int kThreads, bool kEager>
-__device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, BeamEntry *list, uint32_t row, int32_t lo, int32_t hi,
-                                          BeamPart *meta, BeamEntry *to)
+// Where a row of logits starts.
+__device__ __forceinline__ const unsigned char *row_at(const BeamSelectArgs &a, uint32_t row)
 {
-    using T = Word<kType>;
-    constexpr int kWarps = kThreads / 32, kRow = kThreads * T::kW;                          // values of a row of pieces
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const float score = a.scores[row];
-    const bool ended = a.ended && a.ended[row];
     const unsigned char *base = a.logits + row * a.stride_beam;
     if (a.stride_request != a.beams * a.stride_beam)
         base += row / static_cast<uint32_t>(a.beams) * (a.stride_request - a.beams * a.stride_beam);
+    return base;
+}
+
+// Whether a beam's logits matter: it has a score, and is not finished.
+__device__ __forceinline__ bool reads_logits(const BeamSelectArgs &a, uint32_t row)
+{
+    return fabsf(a.scores[row]) < __int_as_float(0x7f800000) && !(a.ended && a.ended[row]);
+}
+
+// A thread's first pieces of logits [lo, hi) of a row.
+template <int kType, int kThreads>
+__device__ __forceinline__ void load_first(uint4 (&v)[kBeamLoads], const unsigned char *base, int32_t lo, int32_t hi, int32_t n)
+{
+    using T = Word<kType>;
+    constexpr int kRow = kThreads * T::kW;
+    const int tid = threadIdx.x;
     const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(base)) & 15u;
-    uint4 v[kBeamLoads];
-    auto load = [&](int32_t first) { return load_piece<kType>(base, off, first + tid * T::kW, hi, a.vocab); };
-    if (kEager) {
+    if (off == 0 && lo + kBeamLoads * kRow <= hi) {
 #pragma unroll
         for (int j = 0; j < kBeamLoads; ++j)
-            v[j] = load(lo + j * kRow);
+            v[j] = *reinterpret_cast<const uint4 *>(base + static_cast<int64_t>(lo + j * kRow + tid * T::kW) * T::kEs);
+    } else {
+#pragma unroll
+        for (int j = 0; j < kBeamLoads; ++j)
+            v[j] = load_piece<kType>(base, off, lo + (j * kThreads + tid) * T::kW, hi, n);
     }
-    if (!(fabsf(score) < __int_as_float(0x7f800000)) || ended)
-        return;                         // no candidate, or one that needs no logits
+}
+
+// v: the thread's first pieces; next(v) is called when they and all others have been taken, before the part's
+// list is made.
+template <int kType, int kThreads, typename F>
+__device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, BeamEntry *list, const unsigned char *base, int32_t lo,
+                                          int32_t hi, uint4 (&v)[kBeamLoads], F &&next, BeamPart *meta, BeamEntry *to)
+{
+    using T = Word<kType>;
+    constexpr int kWarps = kThreads / 32, kRow = kThreads * T::kW;      // values of a row of pieces
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(base)) & 15u;
+    auto load = [&](int32_t first) { return load_piece<kType>(base, off, first + tid * T::kW, hi, a.vocab); };
     if (tid == 0)
         s.count = s.hits = 0;
-    if (!kEager) {
-        if (off == 0 && lo + kBeamLoads * kRow <= hi) {
-#pragma unroll
-            for (int j = 0; j < kBeamLoads; ++j)
-                v[j] = *reinterpret_cast<const uint4 *>(base + static_cast<int64_t>(lo + j * kRow + tid * T::kW) * T::kEs);
-        } else {
-#pragma unroll
-            for (int j = 0; j < kBeamLoads; ++j)
-                v[j] = load(lo + j * kRow);
-        }
-    }
     // exp(x - from) = 2^((x - from) log2(e)), where `from` is a value seen that lies 4 below the largest at
     // most: it seldom moves, and the arguments of the terms that matter stay small, so exact
     float from = neg_inf(), sum = 0.0f;
@@ -494,13 +560,18 @@ __device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, 
         for (int j = 0; j < kBeamLoads; ++j) {
             if (first + j * kRow < hi)
                 take(raw ? shifted(v[j], *reinterpret_cast<const uint4 *>(p + j * kRow * T::kEs + 16), off) : v[j]);
-            if (first + kSpan + j * kRow < hi)
-                v[j] = load(first + kSpan + j * kRow);
+            const int32_t then = first + kSpan + j * kRow;
+            if (off == 0 && then + kRow <= hi)
+                v[j] = *reinterpret_cast<const uint4 *>(p + (kBeamLoads + j) * kRow * T::kEs);
+            else if (then < hi)
+                v[j] = load(then);
         }
+        p += kSpan * T::kEs;
         raw = false;
         fold();
     }
     const float top = T::most(most);
+    next(v);
     // the part's maximum and sum: each warp's here, of them all by one warp below
     float all = top;
 #pragma unroll
@@ -519,34 +590,30 @@ __device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, 
     if (top >= bound && top > neg_inf())
         s.hit[atomicAdd(&s.hits, 1)] = static_cast<int16_t>(tid);
     __syncthreads();
-    // a piece a thread
-    const uint32_t rows = static_cast<uint32_t>(hi - lo + kRow - 1) / kRow, pieces = static_cast<uint32_t>(s.hits) * rows;
-#pragma unroll 2
-    for (uint32_t y = tid; y < pieces; y += kThreads) {
-        const uint32_t h = y / rows;
-        const int32_t i = lo + static_cast<int32_t>(y - h * rows) * kRow + s.hit[h] * T::kW;
-        const uint4 x = load_piece<kType>(base, off, i, hi, a.vocab);
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-        uint32_t hits = 0;
+    // a piece a lane, for each as many lanes as it has pieces, in powers of two
+    const int rows = (hi - lo + kRow - 1) / kRow, found = s.hits, lanes = rows <= 4 ? 4 : rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
+    const uint32_t bound2 = T::twice(bound);            // (a value of this type)
+    for (int h = tid / lanes; h < found; h += kThreads / lanes)
+        for (int r = tid % lanes; r < rows; r += lanes) {
+            const int32_t i = lo + r * kRow + s.hit[h] * T::kW;
+            const uint4 x = load_piece<kType>(base, off, i, hi, a.vocab);
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-        for (int k = 0; k < T::kW; ++k) {
-            float z[T::kN];
-            T::get(w[k / T::kN], z);
-            hits |= z[k % T::kN] >= bound ? 1u << k : 0u;
-        }
-        while (hits) {
-            const int k = __ffs(static_cast<int>(hits)) - 1, word = k / T::kN;
-            hits &= hits - 1;
-            float z[T::kN];
-            T::get(word == 0 ? w[0] : word == 1 ? w[1] : word == 2 ? w[2] : w[3], z);
-            const float one = T::kN == 2 && k % 2 ? z[T::kN - 1] : z[0];
-            if (one > neg_inf()) {
-                const int to_at = atomicAdd(&s.count, 1);
-                if (to_at < a.list)
-                    list[to_at] = BeamEntry{one, i + k};
+            for (int k = 0; k < 4; ++k) {
+                if (!T::reaches(w[k], bound2))
+                    continue;
+                float z[T::kN];
+                T::get(w[k], z);
+#pragma unroll
+                for (int e = 0; e < T::kN; ++e) {
+                    if (!(z[e] >= bound) || z[e] == neg_inf())
+                        continue;
+                    const int to_at = atomicAdd(&s.count, 1);
+                    if (to_at < a.list)
+                        list[to_at] = BeamEntry{z[e], i + k * T::kN + e};
+                }
             }
         }
-    }
     __syncthreads();
     int count = s.count;
     if (count > a.list) {
@@ -567,7 +634,7 @@ __device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, 
         if (lane == 0)
             *meta = BeamPart{z.hi, z.lo, all, min(count, a.keep)};
     }
-    rank_list<kThreads>(list, count, a.keep, to);
+    rank_list<kThreads>(s, list, count, a.keep, to);
 }
 
 // A candidate: its value as a whole number of the same order, and its place among the
@@ -605,6 +672,15 @@ __device__ __forceinline__ Pair log_of(const Pair &x)
     // e log(2): the first part of log(2) has 12 bits, so its product is exact
     const Pair whole = two_sum(e * 0.693115234375f, 2.0f * z);
     return two_sum(whole.hi, whole.lo + (tail + low + e * 3.194618498e-5f));
+}
+
+constexpr int kJoinAll = 128;                    // entries that are ordered without a bound
+
+// Entries that a join orders at most: those of fewer groups than are kept (each has the entries of 4 threads), or all.
+__host__ __device__ __forceinline__ int most_kept(int keep)
+{
+    const int n = keep * 4 * ((kBeamMostLists * keep + kJoinThreads - 1) / kJoinThreads);
+    return n > kJoinAll ? n : kJoinAll;
 }
 
 struct JoinSmem {   // (score and kind are set before the join)
@@ -651,9 +727,8 @@ __device__ __forceinline__ int count_better(const Cand *all, int n, const Cand &
     return before;
 }
 
-// The lists of all parts of all beams of a request, in order.  Of the q-th entries of all lists (the
-// first ones, or as deep as it takes) the need-th best is a bound that need x q >= keep
-// entries reach; the few that do are ordered by counting for each how many are better.
+// The lists of all parts of all beams of a request, in order: the few entries that reach a bound are
+// ordered by counting for each how many are better.
 __device__ __forceinline__ void join(const BeamSelectArgs &a, JoinSmem &s, const Lists &z, int32_t request, int lists)
 {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -698,27 +773,36 @@ __device__ __forceinline__ void join(const BeamSelectArgs &a, JoinSmem &s, const
         }
     }
     __syncthreads();
-    const int q = (a.keep + lists - 1) / lists, need = (a.keep + q - 1) / q;
-    for (int l = tid; l < lists; l += kJoinThreads)
-        z.heads[l] = entry(a, s, z, l, q - 1);
-    __syncthreads();
-    static_assert(kBeamMostLists * 4 <= kJoinThreads, "four threads a list");
-    if (warp * 8 < lists) {
-        const Cand h = tid / 4 < lists ? z.heads[tid / 4] : no_cand();
-        const int before = count_better(z.heads, lists, h);
-        if (h.key != 0 && before == need - 1)
-            s.bound = h;
-    }
-    __syncthreads();
-    const Cand bound = s.bound;
-    for (int l = warp; l < lists; l += (kJoinThreads / 32)) {
-        if (q == 1 && better(bound, z.heads[l]))
-            continue;
-        for (int i = lane; i < a.keep; i += 32) {
-            const Cand c = entry(a, s, z, l, i);
-            if (c.key != 0 && !better(bound, c))
-                z.kept[atomicAdd(&s.count, 1)] = c;
+    // the keep-th largest of the maxima of 128 groups of entries (of the lists' first ones, of their second ones,
+    // ..) is a bound that `keep` of them reach
+    const int entries = lists * a.keep;
+    const bool all = entries <= kJoinAll;
+    if (!all) {
+        Cand best = no_cand();
+        for (int e = tid; e < entries; e += kJoinThreads) {
+            const int i = e / lists;
+            const Cand c = entry(a, s, z, e - i * lists, i);
+            best = better(c, best) ? c : best;
         }
+#pragma unroll
+        for (int o = 1; o < 4; o <<= 1) {
+            const Cand c{__shfl_xor_sync(0xffffffffu, best.key, o), __shfl_xor_sync(0xffffffffu, best.at, o)};
+            best = better(c, best) ? c : best;
+        }
+        if (tid % 4 == 0)
+            z.heads[tid / 4] = best;
+        __syncthreads();
+        const int before = count_better(z.heads, kJoinThreads / 4, best);
+        if (best.key != 0 && before == a.keep - 1)
+            s.bound = best;             // (four threads, the same one)
+        __syncthreads();
+    }
+    const Cand bound = s.bound;         // none where fewer groups have an entry
+    for (int e = tid; e < entries; e += kJoinThreads) {
+        const int i = e / lists;
+        const Cand c = entry(a, s, z, e - i * lists, i);
+        if (c.key != 0 && !better(bound, c))
+            z.kept[atomicAdd(&s.count, 1)] = c;
     }
     __syncthreads();
     const int count = s.count;
@@ -742,16 +826,11 @@ __device__ __forceinline__ void join(const BeamSelectArgs &a, JoinSmem &s, const
     }
 }
 
-// A request's beams: scores, which have candidates, and their lists ([first, end) of beam b).
-template <typename F> __device__ __forceinline__ void get_beams(const BeamSelectArgs &a, JoinSmem &s, int32_t request, F &&lists_of)
+// The lists of a request's beams: [first, end) of beam b.
+template <typename F> __device__ __forceinline__ void place_lists(const BeamSelectArgs &a, JoinSmem &s, F &&lists_of)
 {
     const int b = threadIdx.x;
     if (b < a.beams) {
-        const int64_t row = static_cast<int64_t>(request) * a.beams + b;
-        const float score = a.scores[row];
-        const bool ended = a.ended && a.ended[row];
-        s.score[b] = score;
-        s.kind[b] = !(fabsf(score) < __int_as_float(0x7f800000)) ? 0 : ended ? 1 : 2;
         int first, end;
         lists_of(b, first, end);
         s.first[b] = first;
@@ -761,14 +840,27 @@ template <typename F> __device__ __forceinline__ void get_beams(const BeamSelect
     }
 }
 
+// Its scores, and which beams have candidates.
+__device__ __forceinline__ void get_beams(const BeamSelectArgs &a, JoinSmem &s, int32_t request)
+{
+    const int b = threadIdx.x;
+    if (b < a.beams) {
+        const int64_t row = static_cast<int64_t>(request) * a.beams + b;
+        const float score = a.scores[row];
+        const bool ended = a.ended && a.ended[row];
+        s.score[b] = score;
+        s.kind[b] = !(fabsf(score) < __int_as_float(0x7f800000)) ? 0 : ended ? 1 : 2;
+    }
+}
+
 // Dynamic shared memory of a join.
 __device__ __forceinline__ Lists lists_at(const BeamSelectArgs &a, unsigned char *raw, int lists)
 {
     Lists z;
-    z.meta = reinterpret_cast<BeamPart *>(raw);
-    z.heads = reinterpret_cast<Cand *>(z.meta + lists);
-    z.kept = z.heads + lists;
-    z.entries = reinterpret_cast<BeamEntry *>(z.kept + a.keep * (a.keep + 1));
+    z.heads = reinterpret_cast<Cand *>(raw);
+    z.kept = z.heads + kJoinThreads / 4;
+    z.meta = reinterpret_cast<BeamPart *>(z.kept + most_kept(a.keep));
+    z.entries = reinterpret_cast<BeamEntry *>(z.meta + lists);
     return z;
 }
 
@@ -789,14 +881,38 @@ template <int kType> __global__ void __launch_bounds__(kRowThreads, kRowCtas) se
     const int64_t end = line_at(a, blockIdx.x + 1);
     uint32_t row = static_cast<uint32_t>(x / a.row_pieces);
     int32_t at = static_cast<int32_t>(x - static_cast<int64_t>(row) * a.row_pieces);
-    while (x < end) {
-        const int32_t n = static_cast<int32_t>(min(end - x, static_cast<int64_t>(a.row_pieces - at)));
-        const int64_t list = static_cast<int64_t>(row) + blockIdx.x;
-        take_part<kType, kRowThreads, false>(a, s, reinterpret_cast<BeamEntry *>(raw), row, at * kRow, min((at + n) * kRow, a.vocab),
-                                             a.meta + list, a.entries + list * a.keep);
+    // rows of pieces of the part that starts here
+    auto of_part = [&]() { return static_cast<int32_t>(min(end - x, static_cast<int64_t>(a.row_pieces - at))); };
+    auto ends_at = [&](int32_t n) { return min((at + n) * kRow, a.vocab); };
+    uint4 v[kBeamLoads];
+    bool here = reads_logits(a, row);
+    int32_t n = of_part();
+    if (here)
+        load_first<kType, kRowThreads>(v, row_at(a, row), at * kRow, ends_at(n), a.vocab);
+    while (true) {
+        const int32_t lo = at * kRow, hi = ends_at(n);
+        const uint32_t this_row = row;
+        // the next part's first pieces are on their way while this one's list is made
         x += n;
         ++row;
         at = 0;
+        const bool more = x < end, there = more && reads_logits(a, row);
+        if (more)
+            n = of_part();
+        auto next = [&](uint4 (&w)[kBeamLoads]) {
+            if (there)
+                load_first<kType, kRowThreads>(w, row_at(a, row), 0, ends_at(n), a.vocab);
+        };
+        if (here) {
+            const int64_t to = static_cast<int64_t>(this_row) + blockIdx.x;
+            take_part<kType, kRowThreads>(a, s, reinterpret_cast<BeamEntry *>(raw), row_at(a, this_row), lo, hi, v, next,
+                                          a.meta + to, a.entries + to * a.keep);
+        } else {
+            next(v);
+        }
+        if (!more)
+            break;
+        here = there;
         __syncthreads();
     }
 }
@@ -812,6 +928,11 @@ __global__ void __launch_bounds__(kJoinThreads) select_join(const BeamSelectArgs
     const Lists z = lists_at(a, raw, lists);
     for (int l = threadIdx.x; l < lists; l += kJoinThreads)
         s.beam[l] = -1;
+    __syncthreads();
+    place_lists(a, s, [&](int b, int &from, int &to) {
+        from = static_cast<int>(row0 + b + unit_of(a, (row0 + b) * a.row_pieces) - first);
+        to = static_cast<int>(row0 + b + unit_of(a, (row0 + b + 1) * a.row_pieces - 1) - first + 1);
+    });
     grid_dependency_wait();
     grid_launch_dependents();
     // (of beams without a list it copies what happens to be there, and nobody reads it)
@@ -819,11 +940,7 @@ __global__ void __launch_bounds__(kJoinThreads) select_join(const BeamSelectArgs
         reinterpret_cast<uint4 *>(z.meta)[i] = reinterpret_cast<const uint4 *>(a.meta + first)[i];
     for (int i = threadIdx.x; i < lists * a.keep; i += kJoinThreads)
         z.entries[i] = a.entries[first * a.keep + i];
-    __syncthreads();
-    get_beams(a, s, request, [&](int b, int &from, int &to) {
-        from = static_cast<int>(row0 + b + unit_of(a, (row0 + b) * a.row_pieces) - first);
-        to = static_cast<int>(row0 + b + unit_of(a, (row0 + b + 1) * a.row_pieces - 1) - first + 1);
-    });
+    get_beams(a, s, request);
     __syncthreads();
     join(a, s, z, request, lists);
 }
@@ -843,19 +960,26 @@ template <int kType> __global__ void __launch_bounds__(kJoinThreads, 3) select_t
     BeamEntry *entries;
     asm("mapa.u64 %0, %1, 0;" : "=l"(meta) : "l"(z.meta));
     asm("mapa.u64 %0, %1, 0;" : "=l"(entries) : "l"(z.entries));
-    grid_dependency_wait();
-    grid_launch_dependents();
     if (rank == 0)
-        get_beams(a, j, static_cast<int32_t>(request), [&](int b, int &from, int &to) {
+        place_lists(a, j, [&](int b, int &from, int &to) {
             from = b * a.parts;
             to = from + a.parts;
         });
+    grid_dependency_wait();
+    grid_launch_dependents();
+    if (rank == 0)
+        get_beams(a, j, static_cast<int32_t>(request));
     asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
     for (uint32_t l = rank; l < lists; l += kCluster) {
-        const uint32_t b = l / static_cast<uint32_t>(a.parts);
-        const int32_t lo = static_cast<int32_t>(l - b * a.parts) * a.part;
-        take_part<kType, kJoinThreads, true>(a, s, reinterpret_cast<BeamEntry *>(raw), request * a.beams + b, lo,
-                                             min(lo + a.part, a.vocab), meta + l, entries + l * a.keep);
+        const uint32_t b = l / static_cast<uint32_t>(a.parts), row = request * a.beams + b;
+        const int32_t lo = static_cast<int32_t>(l - b * a.parts) * a.part, hi = min(lo + a.part, a.vocab);
+        const unsigned char *base = row_at(a, row);
+        // (asked for before it is known whether the beam needs them)
+        uint4 v[kBeamLoads];
+        load_first<kType, kJoinThreads>(v, base, lo, hi, a.vocab);
+        if (reads_logits(a, row))
+            take_part<kType, kJoinThreads>(a, s, reinterpret_cast<BeamEntry *>(raw), base, lo, hi, v, [](uint4 (&)[kBeamLoads]) {},
+                                           meta + l, entries + l * a.keep);
         __syncthreads();
     }
     asm volatile("barrier.cluster.arrive.release;" ::: "memory");
@@ -890,7 +1014,7 @@ int32_t list_entries(int32_t keep, int dtype, int threads)
 size_t part_smem(int32_t keep, int dtype, int threads) { return static_cast<size_t>(list_entries(keep, dtype, threads) + keep) * sizeof(BeamEntry); }
 size_t join_smem(int32_t lists, int32_t keep)
 {
-    return lists * sizeof(BeamPart) + (lists + keep * (keep + 1)) * sizeof(Cand) + static_cast<size_t>(lists) * keep * sizeof(BeamEntry);
+    return (kJoinThreads / 4 + most_kept(keep)) * sizeof(Cand) + lists * (sizeof(BeamPart) + keep * sizeof(BeamEntry));
 }
 
 }  // namespace
@@ -902,8 +1026,7 @@ BeamCut beam_cut(int32_t n, int32_t beams, int32_t vocab, int es, int n_sm)
     const int64_t piece = 16 / es, rows = static_cast<int64_t>(n) * beams;
     auto up = [](int64_t x, int64_t d) { return (x + d - 1) / d; };
     BeamCut c{};
-    c.together = static_cast<int64_t>(n) * kCluster <= 3 * static_cast<int64_t>(n_sm) &&
-                 static_cast<int64_t>(beams) * vocab * es <= kCluster * kTogetherBytes;
+    c.together = n <= kMostTogether && static_cast<int64_t>(beams) * vocab * es <= kCluster * kTogetherBytes;
     if (c.together) {
         // parts of a piece a thread at least
         int64_t parts = std::min<int64_t>(kCluster / beams, up(vocab, kJoinThreads * piece));
@@ -911,14 +1034,13 @@ BeamCut beam_cut(int32_t n, int32_t beams, int32_t vocab, int es, int n_sm)
         c.part = static_cast<int32_t>(up(up(vocab, parts), piece) * piece);
         c.parts = static_cast<int32_t>(up(vocab, c.part));
         c.request_lists = beams * c.parts;
-        c.lists = rows * c.parts;
         return c;
     }
-    // a unit for each place on an SM, of four pieces a thread at least; a request's lists, at most one more than
+    // a unit for each place on an SM, of four pieces a thread or a row at least; a request's lists, at most one more than
     // its beams and the units that it touches, fit the join
     c.row_pieces = static_cast<int32_t>(up(vocab, kRowThreads * piece));
     c.line = rows * c.row_pieces;
-    int64_t units = std::min<int64_t>(static_cast<int64_t>(n_sm) * kRowCtas, up(c.line, kBeamLoads));
+    int64_t units = std::min<int64_t>(static_cast<int64_t>(n_sm) * kRowCtas, std::max(rows, up(c.line, kBeamLoads)));
     units = std::min(units, static_cast<int64_t>(n) * (kBeamMostLists - 2 - beams));
     c.units = static_cast<int32_t>(std::max<int64_t>(units, 1));
     c.request_lists = static_cast<int32_t>(beams + up(c.units, n) + 2);
