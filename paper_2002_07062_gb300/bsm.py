@@ -564,12 +564,14 @@ def bsm_paged_write_rotary(q, k, v, q_out, k_cache, v_cache, slots, positions, t
     code = _PAGED_DTYPES.get(kind)
     ks, vs, cs, ts = k.stride(), v.stride(), k_cache.stride(), table.stride()
     # the usual case at once; whatever fails here is looked at one by one
-    if not (code is not None and dev >= 0 and dev == _cuda.current_device() and len(cs) == 4 and len(ks) == 3 and len(vs) == 3
-            and len(ts) == 2 and ks[2] == 1 and vs[2] == 1 and cs[3] == 1 and ts[1] == 1 and v_cache.stride() == cs and v.dtype is kind
-            and k_cache.dtype is kind and v_cache.dtype is kind and table.dtype is _FLOAT32 and positions.dtype is _INT32
-            and slots.dtype is _INT64 and v.get_device() == dev and k_cache.get_device() == dev
-            and v_cache.get_device() == dev and table.get_device() == dev and positions.get_device() == dev
-            and slots.get_device() == dev and positions.is_contiguous() and slots.is_contiguous()):
+    if not (code is not None and dev >= 0 and dev == _cuda.current_device()
+            and len(cs) == 4 and len(ks) == 3 and len(vs) == 3 and len(ts) == 2
+            and ks[2] == 1 and vs[2] == 1 and cs[3] == 1 and ts[1] == 1 and v_cache.stride() == cs
+            and v.dtype is kind and k_cache.dtype is kind and v_cache.dtype is kind and table.dtype is _FLOAT32
+            and positions.dtype is _INT32 and slots.dtype is _INT64 and v.get_device() == dev
+            and k_cache.get_device() == dev and v_cache.get_device() == dev and table.get_device() == dev
+            and positions.get_device() == dev and slots.get_device() == dev
+            and positions.is_contiguous() and slots.is_contiguous()):
         code = _paged_dtype(k, v, k_cache, v_cache)
         dev = _device(k, "k")
         ks, vs, cs = _strided(k, "k", 3, dev), _strided(v, "v", 3, dev), _caches(k_cache, v_cache, dev)
@@ -654,12 +656,12 @@ def bsm_beam_select(logits, scores, out_scores, parents, tokens, workspace, ende
     contiguous) and scores [requests, beams]; ended: bool or bytes [requests, beams]."""
     code, dev, st = _PAGED_DTYPES.get(logits.dtype), logits.get_device(), logits.stride()
     # the usual case at once; whatever fails here is looked at one by one
-    if not (code is not None and dev >= 0 and dev == _cuda.current_device() and len(st) == 3 and st[2] == 1 and scores.dtype is _FLOAT32
-            and out_scores.dtype is _FLOAT32 and parents.dtype is _INT32 and tokens.dtype is _INT32
-            and scores.get_device() == dev and out_scores.get_device() == dev and parents.get_device() == dev
-            and tokens.get_device() == dev and workspace.get_device() == dev and scores.is_contiguous()
-            and out_scores.is_contiguous() and parents.is_contiguous() and tokens.is_contiguous()
-            and workspace.is_contiguous()):
+    if not (code is not None and dev >= 0 and dev == _cuda.current_device() and len(st) == 3 and st[2] == 1
+            and scores.dtype is _FLOAT32 and out_scores.dtype is _FLOAT32 and parents.dtype is _INT32
+            and tokens.dtype is _INT32 and scores.get_device() == dev and out_scores.get_device() == dev
+            and parents.get_device() == dev and tokens.get_device() == dev and workspace.get_device() == dev
+            and scores.is_contiguous() and out_scores.is_contiguous() and parents.is_contiguous()
+            and tokens.is_contiguous() and workspace.is_contiguous()):
         code = _paged_dtype(logits)
         dev = _device(logits, "logits")
         st = _strided(logits, "logits", 3, dev)
@@ -697,9 +699,10 @@ def bsm_paged_reorder(parents, lengths, tables, free_pages, new_lengths, new_tab
     kind, dev, cs, shape = k_cache.dtype, k_cache.get_device(), k_cache.stride(), k_cache.shape
     code, ps, ts, ns, ndim = _PAGED_DTYPES.get(kind), parents.stride(), tables.stride(), new_tables.stride(), len(cs)
     # the usual case at once; whatever fails here is looked at one by one
-    if not (code is not None and dev >= 0 and dev == _cuda.current_device() and (ndim == 4 or ndim == 5) and cs[-1] == 1 and v_cache.stride() == cs
-            and v_cache.shape == shape and v_cache.dtype is kind and len(ps) == 2 and ps[1] == 1 and len(ts) == 2 and ts[1] == 1
-            and len(ns) == 2 and ns[1] == 1 and parents.dtype is _INT32 and lengths.dtype is _INT32 and tables.dtype is _INT32
+    if not (code is not None and dev >= 0 and dev == _cuda.current_device() and (ndim == 4 or ndim == 5)
+            and cs[-1] == 1 and v_cache.stride() == cs and v_cache.shape == shape and v_cache.dtype is kind
+            and len(ps) == 2 and ps[1] == 1 and len(ts) == 2 and ts[1] == 1 and len(ns) == 2 and ns[1] == 1
+            and parents.dtype is _INT32 and lengths.dtype is _INT32 and tables.dtype is _INT32
             and free_pages.dtype is _INT32 and new_lengths.dtype is _INT32 and new_tables.dtype is _INT32
             and dropped.dtype is _INT32 and info.dtype is _INT64 and v_cache.get_device() == dev
             and parents.get_device() == dev and lengths.get_device() == dev and tables.get_device() == dev
