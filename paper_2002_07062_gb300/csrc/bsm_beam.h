@@ -37,10 +37,7 @@ struct BeamSelectArgs {
     BeamPart *meta;
     int64_t stride_request, stride_beam;        // bytes
     int32_t n, beams, vocab, keep, end_token;
-    // how the rows are cut (set by the launch)
     int32_t parts, part;                        // parts of a row, logits of each (whole pieces of 16 bytes)
-    int32_t row_pieces, units;                  // rows of pieces of a row of logits; CTAs that share the line
-    int64_t line;                               // rows of pieces of all rows
     int32_t list;                               // entries of a part's list (set by the launch)
 };
 
@@ -66,14 +63,10 @@ struct PagedReorderArgs {
 
 int launch_paged_reorder(PagedReorderArgs a, int n_sm, void *stream);
 
-// How the rows are cut.
+// How the rows are cut: parts of `part` logits.
 struct BeamCut {
+    int32_t parts, part;
     bool together;                              // a cluster takes a request, in one launch
-    int32_t parts, part;                        // then: see BeamSelectArgs
-    int32_t row_pieces, units;                  // else: see there
-    int64_t line;
-    int32_t request_lists;                      // of a request at most
-    int64_t lists;                              // of all
 };
 BeamCut beam_cut(int32_t n, int32_t beams, int32_t vocab, int es, int n_sm);
 

@@ -26,8 +26,9 @@ SelectLayout select_layout(int32_t n, int32_t beams, int32_t vocab, int32_t keep
 {
     SelectLayout l{};
     l.cut = beam_cut(n, beams, vocab, es, n_sm);
-    l.meta = up256(l.cut.lists * keep * static_cast<int64_t>(sizeof(BeamEntry)));
-    l.bytes = l.meta + up256(1 + l.cut.lists * static_cast<int64_t>(sizeof(BeamPart)));
+    const int64_t lists = static_cast<int64_t>(n) * beams * l.cut.parts;        // (a cluster's are in shared memory)
+    l.meta = up256(lists * keep * static_cast<int64_t>(sizeof(BeamEntry)));
+    l.bytes = l.meta + up256(lists * static_cast<int64_t>(sizeof(BeamPart)));
     return l;
 }
 

@@ -21,6 +21,7 @@ constexpr int kGroups = 128;                    // groups of neighbouring thread
 constexpr int kMostWarps = 16;
 constexpr int kRowThreads = 512, kRowCtas = 3;  // of select_rows; its CTAs on an SM
 constexpr int kJoinThreads = 512;                // of select_join and select_together
+constexpr int kListRows = 20;                    // see beam_cut
 constexpr int kMostTogether = 8;                 // requests (a cluster takes about 0.3 us to start)
 constexpr int kCluster = 16;                     // CTAs of select_together that share a request
 
@@ -477,11 +478,10 @@ __device__ __forceinline__ void load_first(uint4 (&v)[kBeamLoads], const unsigne
     }
 }
 
-// v: the thread's first pieces; next(v) is called when they and all others have been taken, before the part's
-// list is made.
-template <int kType, int kThreads, typename F>
+// v: the thread's first pieces.
+template <int kType, int kThreads>
 __device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, BeamEntry *list, const unsigned char *base, int32_t lo,
-                                          int32_t hi, uint4 (&v)[kBeamLoads], F &&next, BeamPart *meta, BeamEntry *to)
+                                          int32_t hi, uint4 (&v)[kBeamLoads], BeamPart *meta, BeamEntry *to)
 {
     using T = Word<kType>;
     constexpr int kWarps = kThreads / 32, kRow = kThreads * T::kW;      // values of a row of pieces
@@ -571,7 +571,6 @@ __device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, 
         fold();
     }
     const float top = T::most(most);
-    next(v);
     // the part's maximum and sum: each warp's here, of them all by one warp below
     float all = top;
 #pragma unroll
@@ -687,8 +686,7 @@ struct JoinSmem {   // (score and kind are set before the join)
     float score[kBeamMost], top[kBeamMost];
     Pair shift[kBeamMost];              // score - log(sum): what a row adds to x - top
     int32_t kind[kBeamMost];            // 0: no candidate, 1: one (an ended beam), 2: its parts' lists
-    int32_t first[kBeamMost + 1], end[kBeamMost];       // its lists
-    int8_t beam[kBeamMostLists];        // of a list, -1: none
+    int8_t beam[kBeamMostLists];        // of a list
     Cand bound;
     int32_t count;
 };
@@ -704,10 +702,8 @@ struct Lists {
 __device__ __forceinline__ Cand entry(const BeamSelectArgs &a, const JoinSmem &s, const Lists &z, int l, int i)
 {
     const int b = s.beam[l];
-    if (b < 0)
-        return no_cand();
     if (s.kind[b] != 2)
-        return s.kind[b] == 1 && l == s.first[b] && i == 0 ? cand(s.shift[b], b * a.vocab + a.end_token) : no_cand();
+        return s.kind[b] == 1 && l == b * a.parts && i == 0 ? cand(s.shift[b], b * a.vocab + a.end_token) : no_cand();
     if (i >= z.meta[l].count)
         return no_cand();
     const BeamEntry e = z.entries[l * a.keep + i];
@@ -742,15 +738,14 @@ __device__ __forceinline__ void join(const BeamSelectArgs &a, JoinSmem &s, const
         float top = neg_inf();
         Pair shift{score, 0.0f};
         if (kind == 2) {
-            const BeamPart *meta = z.meta + s.first[b];
-            const int parts = s.end[b] - s.first[b];
-            for (int p = lane; p < parts; p += 32)
+            const BeamPart *meta = z.meta + b * a.parts;
+            for (int p = lane; p < a.parts; p += 32)
                 top = fmaxf(top, meta[p].top);
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1)
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
             Pair sum{0.0f, 0.0f};
-            for (int p = lane; p < parts; p += 32) {
+            for (int p = lane; p < a.parts; p += 32) {
                 const BeamPart x = meta[p];
                 if (x.sum != 0.0f) {    // (an empty part: -inf - -inf)
                     const float w = expf(x.top - top), m = x.sum * w;
@@ -758,7 +753,7 @@ __device__ __forceinline__ void join(const BeamSelectArgs &a, JoinSmem &s, const
                 }
             }
             for (int o = 16; o > 0; o >>= 1)
-                if (o < parts)
+                if (o < a.parts)
                     sum = add(sum, Pair{__shfl_xor_sync(0xffffffffu, sum.hi, o), __shfl_xor_sync(0xffffffffu, sum.lo, o)});
             // NaN or +inf among the logits, or none above -inf: the row's softmax is NaN
             if (!(sum.hi > 0.0f && sum.hi < __int_as_float(0x7f800000)))
@@ -826,21 +821,7 @@ __device__ __forceinline__ void join(const BeamSelectArgs &a, JoinSmem &s, const
     }
 }
 
-// The lists of a request's beams: [first, end) of beam b.
-template <typename F> __device__ __forceinline__ void place_lists(const BeamSelectArgs &a, JoinSmem &s, F &&lists_of)
-{
-    const int b = threadIdx.x;
-    if (b < a.beams) {
-        int first, end;
-        lists_of(b, first, end);
-        s.first[b] = first;
-        s.end[b] = end;
-        for (int l = first; l < end; ++l)
-            s.beam[l] = static_cast<int8_t>(b);
-    }
-}
-
-// Its scores, and which beams have candidates.
+// A request's scores, which beams have candidates, and whose each list is.
 __device__ __forceinline__ void get_beams(const BeamSelectArgs &a, JoinSmem &s, int32_t request)
 {
     const int b = threadIdx.x;
@@ -851,6 +832,8 @@ __device__ __forceinline__ void get_beams(const BeamSelectArgs &a, JoinSmem &s, 
         s.score[b] = score;
         s.kind[b] = !(fabsf(score) < __int_as_float(0x7f800000)) ? 0 : ended ? 1 : 2;
     }
+    for (int l = threadIdx.x; l < a.beams * a.parts; l += kJoinThreads)
+        s.beam[l] = static_cast<int8_t>(l / a.parts);
 }
 
 // Dynamic shared memory of a join.
@@ -864,75 +847,30 @@ __device__ __forceinline__ Lists lists_at(const BeamSelectArgs &a, unsigned char
     return z;
 }
 
-// All rows' logits form a line of rows of pieces (kRowThreads x 16 bytes), `line` of them; unit u (a CTA) takes
-// those from line u / units to line (u + 1) / units: the same amount each, whatever rows are cut.  The part
-// of row r that unit u takes has list r + u.
-__device__ __forceinline__ int64_t line_at(const BeamSelectArgs &a, uint32_t u) { return a.line * u / a.units; }
-__device__ __forceinline__ int64_t unit_of(const BeamSelectArgs &a, int64_t x) { return ((x + 1) * a.units - 1) / a.line; }
-
 template <int kType> __global__ void __launch_bounds__(kRowThreads, kRowCtas) select_rows(const BeamSelectArgs a)
 {
-    constexpr int kRow = kRowThreads * Word<kType>::kW;
     __shared__ PartSmem s;
     extern __shared__ __align__(16) unsigned char raw[];
     grid_dependency_wait();
     grid_launch_dependents();
-    int64_t x = line_at(a, blockIdx.x);
-    const int64_t end = line_at(a, blockIdx.x + 1);
-    uint32_t row = static_cast<uint32_t>(x / a.row_pieces);
-    int32_t at = static_cast<int32_t>(x - static_cast<int64_t>(row) * a.row_pieces);
-    // rows of pieces of the part that starts here
-    auto of_part = [&]() { return static_cast<int32_t>(min(end - x, static_cast<int64_t>(a.row_pieces - at))); };
-    auto ends_at = [&](int32_t n) { return min((at + n) * kRow, a.vocab); };
+    const uint32_t row = a.parts == 1 ? blockIdx.x : blockIdx.x / static_cast<uint32_t>(a.parts);
+    const int32_t lo = static_cast<int32_t>(blockIdx.x - row * a.parts) * a.part, hi = min(lo + a.part, a.vocab);
+    if (!reads_logits(a, row))
+        return;
+    const unsigned char *base = row_at(a, row);
     uint4 v[kBeamLoads];
-    bool here = reads_logits(a, row);
-    int32_t n = of_part();
-    if (here)
-        load_first<kType, kRowThreads>(v, row_at(a, row), at * kRow, ends_at(n), a.vocab);
-    while (true) {
-        const int32_t lo = at * kRow, hi = ends_at(n);
-        const uint32_t this_row = row;
-        // the next part's first pieces are on their way while this one's list is made
-        x += n;
-        ++row;
-        at = 0;
-        const bool more = x < end, there = more && reads_logits(a, row);
-        if (more)
-            n = of_part();
-        auto next = [&](uint4 (&w)[kBeamLoads]) {
-            if (there)
-                load_first<kType, kRowThreads>(w, row_at(a, row), 0, ends_at(n), a.vocab);
-        };
-        if (here) {
-            const int64_t to = static_cast<int64_t>(this_row) + blockIdx.x;
-            take_part<kType, kRowThreads>(a, s, reinterpret_cast<BeamEntry *>(raw), row_at(a, this_row), lo, hi, v, next,
-                                          a.meta + to, a.entries + to * a.keep);
-        } else {
-            next(v);
-        }
-        if (!more)
-            break;
-        here = there;
-        __syncthreads();
-    }
+    load_first<kType, kRowThreads>(v, base, lo, hi, a.vocab);
+    take_part<kType, kRowThreads>(a, s, reinterpret_cast<BeamEntry *>(raw), base, lo, hi, v, a.meta + blockIdx.x,
+                                  a.entries + static_cast<int64_t>(blockIdx.x) * a.keep);
 }
 
 __global__ void __launch_bounds__(kJoinThreads) select_join(const BeamSelectArgs a)
 {
     __shared__ JoinSmem s;
     extern __shared__ __align__(16) unsigned char raw[];
-    const int32_t request = blockIdx.x;
-    const int64_t row0 = static_cast<int64_t>(request) * a.beams;
-    const int64_t first = row0 + unit_of(a, row0 * a.row_pieces);
-    const int lists = static_cast<int>(row0 + a.beams - 1 + unit_of(a, (row0 + a.beams) * a.row_pieces - 1) - first + 1);
+    const int32_t request = blockIdx.x, lists = a.beams * a.parts;
+    const int64_t first = static_cast<int64_t>(request) * lists;
     const Lists z = lists_at(a, raw, lists);
-    for (int l = threadIdx.x; l < lists; l += kJoinThreads)
-        s.beam[l] = -1;
-    __syncthreads();
-    place_lists(a, s, [&](int b, int &from, int &to) {
-        from = static_cast<int>(row0 + b + unit_of(a, (row0 + b) * a.row_pieces) - first);
-        to = static_cast<int>(row0 + b + unit_of(a, (row0 + b + 1) * a.row_pieces - 1) - first + 1);
-    });
     grid_dependency_wait();
     grid_launch_dependents();
     // (of beams without a list it copies what happens to be there, and nobody reads it)
@@ -960,11 +898,6 @@ template <int kType> __global__ void __launch_bounds__(kJoinThreads, 3) select_t
     BeamEntry *entries;
     asm("mapa.u64 %0, %1, 0;" : "=l"(meta) : "l"(z.meta));
     asm("mapa.u64 %0, %1, 0;" : "=l"(entries) : "l"(z.entries));
-    if (rank == 0)
-        place_lists(a, j, [&](int b, int &from, int &to) {
-            from = b * a.parts;
-            to = from + a.parts;
-        });
     grid_dependency_wait();
     grid_launch_dependents();
     if (rank == 0)
@@ -978,8 +911,8 @@ template <int kType> __global__ void __launch_bounds__(kJoinThreads, 3) select_t
         uint4 v[kBeamLoads];
         load_first<kType, kJoinThreads>(v, base, lo, hi, a.vocab);
         if (reads_logits(a, row))
-            take_part<kType, kJoinThreads>(a, s, reinterpret_cast<BeamEntry *>(raw), base, lo, hi, v, [](uint4 (&)[kBeamLoads]) {},
-                                           meta + l, entries + l * a.keep);
+            take_part<kType, kJoinThreads>(a, s, reinterpret_cast<BeamEntry *>(raw), base, lo, hi, v, meta + l,
+                                           entries + l * a.keep);
         __syncthreads();
     }
     asm volatile("barrier.cluster.arrive.release;" ::: "memory");
@@ -1019,8 +952,8 @@ size_t join_smem(int32_t lists, int32_t keep)
 
 }  // namespace
 
-// Requests whose beams are few and short go to a cluster each, in one launch; the others' parts to all
-// SMs, and their joins to a second launch.
+// Requests that are few and short go to a cluster each, in one launch; the others' parts to all SMs, and
+// their joins to a second launch.  Every row is cut alike, so equal rows give equal bits.
 BeamCut beam_cut(int32_t n, int32_t beams, int32_t vocab, int es, int n_sm)
 {
     const int64_t piece = 16 / es, rows = static_cast<int64_t>(n) * beams;
@@ -1033,18 +966,20 @@ BeamCut beam_cut(int32_t n, int32_t beams, int32_t vocab, int es, int n_sm)
         parts = std::max<int64_t>(parts, 1);
         c.part = static_cast<int32_t>(up(up(vocab, parts), piece) * piece);
         c.parts = static_cast<int32_t>(up(vocab, c.part));
-        c.request_lists = beams * c.parts;
         return c;
     }
-    // a unit for each place on an SM, of four pieces a thread or a row at least; a request's lists, at most one more than
-    // its beams and the units that it touches, fit the join
-    c.row_pieces = static_cast<int32_t>(up(vocab, kRowThreads * piece));
-    c.line = rows * c.row_pieces;
-    int64_t units = std::min<int64_t>(static_cast<int64_t>(n_sm) * kRowCtas, std::max(rows, up(c.line, kBeamLoads)));
-    units = std::min(units, static_cast<int64_t>(n) * (kBeamMostLists - 2 - beams));
-    c.units = static_cast<int32_t>(std::max<int64_t>(units, 1));
-    c.request_lists = static_cast<int32_t>(beams + up(c.units, n) + 2);
-    c.lists = rows + c.units;
+    // The parts whose waves take least: a part's list costs as much as kListRows of its rows of pieces.
+    const int64_t row = kRowThreads * piece, pieces = up(vocab, row), at_once = static_cast<int64_t>(n_sm) * kRowCtas;
+    const int64_t most = std::min<int64_t>(kBeamMostLists / beams, up(pieces, kBeamLoads));
+    int64_t best = 0;
+    for (int64_t parts = 1; parts <= most; ++parts) {
+        const int64_t each = up(pieces, parts), cost = up(rows * up(pieces, each), at_once) * (each + kListRows);
+        if (parts == 1 || cost < best) {
+            best = cost;
+            c.part = static_cast<int32_t>(std::min(each * row, up(vocab, piece) * piece));
+            c.parts = static_cast<int32_t>(up(pieces, each));
+        }
+    }
     return c;
 }
 
@@ -1054,10 +989,7 @@ int launch_beam_select(BeamSelectArgs a, int dtype, const BeamCut &cut, void *st
     a.list = list_entries(a.keep, dtype, threads);
     a.parts = cut.parts;
     a.part = cut.part;
-    a.row_pieces = cut.row_pieces;
-    a.units = cut.units;
-    a.line = cut.line;
-    const size_t part = part_smem(a.keep, dtype, threads), joint = join_smem(cut.request_lists, a.keep);
+    const size_t part = part_smem(a.keep, dtype, threads), joint = join_smem(a.beams * a.parts, a.keep);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (cut.together) {
         const dim3 grid(static_cast<unsigned>(a.n) * kCluster);
@@ -1066,7 +998,7 @@ int launch_beam_select(BeamSelectArgs a, int dtype, const BeamCut &cut, void *st
                : dtype == BSM_BF16 ? launch_cluster(select_together<BSM_BF16>, grid, smem, st, a)
                                    : launch_cluster(select_together<BSM_F16>, grid, smem, st, a);
     }
-    const dim3 grid(static_cast<unsigned>(a.units));
+    const dim3 grid(static_cast<unsigned>(a.n) * a.beams * a.parts);
     const int e = dtype == BSM_F32    ? launch_early(select_rows<BSM_F32>, grid, kRowThreads, part, st, a)
                   : dtype == BSM_BF16 ? launch_early(select_rows<BSM_BF16>, grid, kRowThreads, part, st, a)
                                       : launch_early(select_rows<BSM_F16>, grid, kRowThreads, part, st, a);

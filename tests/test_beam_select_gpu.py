@@ -114,6 +114,18 @@ def test_equal_beams_tie_exactly():
     assert torch.equal(v[0, :4], v[0, :1].expand(4))
     v, p, t = _run(x.contiguous(), s, 8)            # the same values at four different alignments
     assert p[0].tolist() == [0, 1, 2, 3] * 2
+    # and of a batch that all SMs share
+    v, p, t = _run(row.expand(60, 4, 50001).contiguous(), torch.full((60, 4), -2.25, device="cuda"), 8)
+    assert p.tolist() == [[0, 1, 2, 3] * 2] * 60 and (t == t[0]).all() and (v == v[0]).all()
+
+
+def test_few_values_in_a_part_and_long_lists():
+    # the last part of a row with fewer values than groups, values that all reach the bound, allowed tokens side by side
+    _check(*_data(40, 4, 16384 * 2 + 9, "bf16", seed=21), 16)
+    x, s = _data(12, 3, 30000, "bf16", seed=22)
+    x[:, :, :20000], x[:, :, 21500:] = NEG, NEG
+    _check(x, s, 30)
+    _check(torch.zeros((9, 64, 700), device="cuda"), s[:9, :1].expand(9, 64).contiguous() - torch.arange(64, device="cuda") / 16, 64)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
