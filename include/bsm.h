@@ -502,8 +502,9 @@ typedef struct {
 } bsm_beam_select_desc;
 int bsm_beam_select(const bsm_beam_select_desc *d, bsm_stream_t stream);
 
-/* Bytes of workspace that bsm_beam_select wants on `device` (-1: current) for these sizes
- * and any type; -1 for arguments it would refuse or without a device. */
+/* Bytes of workspace that bsm_beam_select wants on `device` (-1: current) for at most so many
+ * requests, beams and kept continuations, any vocabulary and type; -1 for arguments it would
+ * refuse or without a device. */
 int64_t bsm_beam_select_workspace_bytes(int device, int32_t n_requests, int32_t beams, int32_t vocab, int32_t keep);
 
 /*

@@ -68,6 +68,8 @@ struct BeamCut {
     int32_t parts, part;
     bool together;                              // a cluster takes a request, in one launch
 };
+// Lists that any cut of at most `rows` rows makes, whatever the vocabulary.
+int64_t beam_most_lists(int64_t rows, int n_sm);
 BeamCut beam_cut(int32_t n, int32_t beams, int32_t vocab, int es, int n_sm);
 
 int launch_beam_select(BeamSelectArgs a, int dtype, const BeamCut &cut, void *stream);

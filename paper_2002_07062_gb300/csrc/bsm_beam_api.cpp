@@ -22,13 +22,16 @@ struct SelectLayout {
     int64_t meta, bytes;
 };
 
+int64_t entries_bytes(int64_t lists, int32_t keep) { return up256(lists * keep * static_cast<int64_t>(sizeof(BeamEntry))); }
+int64_t meta_bytes(int64_t lists) { return up256(lists * static_cast<int64_t>(sizeof(BeamPart))); }
+
 SelectLayout select_layout(int32_t n, int32_t beams, int32_t vocab, int32_t keep, int es, int n_sm)
 {
     SelectLayout l{};
     l.cut = beam_cut(n, beams, vocab, es, n_sm);
     const int64_t lists = static_cast<int64_t>(n) * beams * l.cut.parts;        // (a cluster's are in shared memory)
-    l.meta = up256(lists * keep * static_cast<int64_t>(sizeof(BeamEntry)));
-    l.bytes = l.meta + up256(lists * static_cast<int64_t>(sizeof(BeamPart)));
+    l.meta = entries_bytes(lists, keep);
+    l.bytes = l.meta + meta_bytes(lists);
     return l;
 }
 
@@ -252,8 +255,9 @@ int64_t bsm_beam_select_workspace_bytes(int device, int32_t n_requests, int32_t 
     bsm::PagedDev *dev = nullptr;
     if (bsm::paged_device(device, &dev))
         return -1;
-    return std::max(bsm::select_layout(n_requests, beams, vocab, keep, 2, dev->n_sm).bytes,
-                    bsm::select_layout(n_requests, beams, vocab, keep, 4, dev->n_sm).bytes);
+    // (enough for fewer requests too, which may be cut into more parts)
+    const int64_t lists = bsm::beam_most_lists(static_cast<int64_t>(n_requests) * beams, dev->n_sm);
+    return bsm::entries_bytes(lists, keep) + bsm::meta_bytes(lists);
 }
 
 }  // extern "C"

@@ -952,6 +952,8 @@ size_t join_smem(int32_t lists, int32_t keep)
 
 }  // namespace
 
+int64_t beam_most_lists(int64_t rows, int n_sm) { return std::max<int64_t>(rows, 8ll * n_sm * kRowCtas); }
+
 // Requests that are few and short go to a cluster each, in one launch; the others' parts to all SMs, and
 // their joins to a second launch.  Every row is cut alike, so equal rows give equal bits.
 BeamCut beam_cut(int32_t n, int32_t beams, int32_t vocab, int es, int n_sm)
@@ -970,7 +972,8 @@ BeamCut beam_cut(int32_t n, int32_t beams, int32_t vocab, int es, int n_sm)
     }
     // The parts whose waves take least: a part's list costs as much as kListRows of its rows of pieces.
     const int64_t row = kRowThreads * piece, pieces = up(vocab, row), at_once = static_cast<int64_t>(n_sm) * kRowCtas;
-    const int64_t most = std::min<int64_t>(kBeamMostLists / beams, up(pieces, kBeamLoads));
+    const int64_t most = std::min(std::min<int64_t>(kBeamMostLists / beams, up(pieces, kBeamLoads)),
+                                  std::max<int64_t>(beam_most_lists(rows, n_sm) / rows, 1));
     int64_t best = 0;
     for (int64_t parts = 1; parts <= most; ++parts) {
         const int64_t each = up(pieces, parts), cost = up(rows * up(pieces, each), at_once) * (each + kListRows);

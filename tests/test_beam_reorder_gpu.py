@@ -241,3 +241,27 @@ def test_captured_and_on_another_stream():
     ref.run()
     torch.cuda.synchronize()
     assert torch.equal(c.new_tables, ref.new_tables) and torch.equal(c.dropped, ref.dropped)
+
+
+def test_pages_far_into_the_cache():
+    # pages past 2^31 elements and 2^32 bytes
+    pages, page, hkv, d = 70000, 16, 16, 128
+    k, v = (torch.zeros((pages, page, hkv, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    i32 = dict(dtype=torch.int32, device="cuda")
+    tables = torch.tensor([[69999, 69990], [3, 5], [4, 6]], **i32)
+    lengths, free = torch.tensor([20, 20, 20], **i32), torch.tensor([69950, 69951], **i32)
+    k[69990, :4], v[69990, :4] = 2.0, 3.0
+    dropped, info = torch.zeros(6, **i32), torch.zeros(4, dtype=torch.int64, device="cuda")
+    ws = torch.empty(bsm.bsm_paged_reorder_workspace_bytes(1, 3, 2), dtype=torch.uint8, device="cuda")
+    bsm.bsm_paged_reorder(torch.zeros((1, 3), **i32), lengths, tables, free, lengths, tables, dropped, info, k, v, ws)
+    assert tables.tolist() == [[69999, 69990], [69999, 69950], [69999, 69951]] and info.tolist() == [2, 0, 4, 0]
+    for p in (69950, 69951):
+        assert (k[p, :4] == 2).all() and (v[p, :4] == 3).all() and (k[p, 4:] == 0).all()
+    # and keys rotated to slots there
+    slots = torch.tensor([69999 * page + 7, 1], dtype=torch.int64, device="cuda")
+    new = torch.randn((2, hkv, d), device="cuda").bfloat16()
+    table = torch.cat([torch.zeros((9, 32)), torch.ones((9, 32))], 1).cuda()        # a quarter turn
+    bsm.bsm_paged_write_rotary(None, new, new, None, k, v, slots, torch.tensor([8, 0], **i32), table)
+    assert torch.equal(k[69999, 7, :, :32], -new[0, :, 32:64]) and torch.equal(k[69999, 7, :, 32:64], new[0, :, :32])
+    assert torch.equal(k[69999, 7, :, 64:], new[0, :, 64:]) and torch.equal(v[69999, 7], new[0]) and torch.equal(v[0, 1], new[1])
+    assert bsm.bsm_device_status() == 0

@@ -240,3 +240,19 @@ def test_captured_on_another_stream_and_side_by_side():
     graph.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(first, got))
+
+
+def test_workspace_of_the_most_requests_serves_fewer():
+    ws = torch.empty(bsm.bsm_beam_select_workspace_bytes(40, 4, 50001, 8), dtype=torch.uint8, device="cuda")
+    for n, V in ((40, 50001), (9, 200000), (12, 50001), (8, 100), (1, 400000)):
+        x, s = _data(n, 4, V, "bf16", seed=n)
+        _check(x, s, 8, got=_run(x, s, 8, ws=ws))
+
+
+def test_rows_far_apart():
+    # more than 2^31 elements and 2^32 bytes from row to row
+    far = 1_500_000_007
+    flat = torch.zeros(3 * far + 3000, dtype=torch.bfloat16, device="cuda")
+    x = flat.as_strided((2, 2, 2500), (2 * far - 5, far, 1))
+    x.copy_(_data(2, 2, 2500, "bf16", seed=30)[0])
+    _check(x, torch.tensor([[-1.0, -1.3], [-0.2, -2.0]], device="cuda"), 7)
