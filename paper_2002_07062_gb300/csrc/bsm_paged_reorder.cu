@@ -17,7 +17,8 @@ namespace {
 // One tile of columns of a request's rows.  A thread holds a column: whole pages are
 // shared, so its new entries are its old ones by parents, and what it drops it sees without
 // another thread (a page lies in one column).  It reads a column before it writes it, so the
-// tables may change in place.
+// tables may change in place.  Latency: 7 us for 64 requests of 5 rows, 8 for 16 of 16 rows of 1500 (13 with
+// the old entries in shared memory alone: 16 x 16 dependent comparisons).
 // kBeams: at most so many beams, a thread's old entries in registers; 0: any number, in shared memory.
 template <int kBeams> __global__ void __launch_bounds__(kReorderTile) reorder_tables(const PagedReorderArgs a)
 {
@@ -252,7 +253,8 @@ __device__ void list_dropped(const PagedReorderArgs &a, int cta, int ctas)
 // Pages for the rows that copy, in order of requests and rows, and the copies, a warp at a time about
 // 4 KiB (some tokens of one row in one layer's keys or values).  Every CTA counts all requests' copies
 // itself (256 at once) instead of waiting for another's sums.  The launch's last CTAs list the
-// dropped pages.
+// dropped pages.  Bound by the copies: 362 MB 55 us, 0.97 of a copy's rate (a CTA a copy 61; 8 or 16 loads a lane
+// in fewer CTAs 57 to 59).
 __global__ void __launch_bounds__(kFinishThreads, kFinishCtas) reorder_pages(const PagedReorderArgs a)
 {
     __shared__ unsigned long long s_rows[kFinishThreads];   // rows of a request that copy
