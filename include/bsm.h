@@ -98,7 +98,7 @@ typedef enum {
     BSM_ERR_TOO_LARGE = 9      /* more patches than bsm_softmax_noalloc's fixed scratch holds */
 } bsm_status;
 
-typedef enum { BSM_F32 = 0, BSM_BF16 = 1, BSM_F16 = 2 } bsm_dtype;   /* input type == output type; F16: paged calls only */
+typedef enum { BSM_F32 = 0, BSM_BF16 = 1, BSM_F16 = 2 } bsm_dtype;   /* input type == output type; F16: paged and beam calls only */
 
 typedef enum {
     BSM_POLICY_WHOLE_GPU = 0,
@@ -361,7 +361,8 @@ int bsm_paged_write(const bsm_paged_write_desc *d, bsm_stream_t stream);
  *   positions negative: the token is left out, its row of q_out and its slot stay as they
  *             were; past the table: the same, and sets BSM_DEV_BOUNDS.
  *   slots     negative: its key and value are left out; past the cache: the same, and
- *             sets BSM_DEV_BOUNDS.  (positions and slots as bsm_paged_tables gives them.)
+ *             sets BSM_DEV_BOUNDS; two tokens with the same slot leave either, piece by
+ *             piece.  (positions and slots as bsm_paged_tables gives them.)
  *   heads_q   0: no queries (q and q_out may be null).
  *   q_out     q itself with the same strides (in place), or no place in common with q;
  *             none with k and v (those and q_out may be parts of one row).

@@ -20,7 +20,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "_lib", "libbsm.so")
 HEADER = os.path.join(os.path.dirname(PKG), "include", "bsm.h")
 
-F32, BF16, F16 = 0, 1, 2       # (F16: the paged-cache calls only)
+F32, BF16, F16 = 0, 1, 2       # (F16: the paged-cache and beam calls only)
 POLICY_WHOLE_GPU, POLICY_RR, POLICY_CBMF, POLICY_CBMF_LB, POLICY_DYNAMIC, POLICY_MINIMAX = range(6)
 POLICIES = {"whole_gpu": POLICY_WHOLE_GPU, "rr": POLICY_RR, "cbmf": POLICY_CBMF,
             "cbmf_lb": POLICY_CBMF_LB, "dynamic": POLICY_DYNAMIC, "minimax": POLICY_MINIMAX}

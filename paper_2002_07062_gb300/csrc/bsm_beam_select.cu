@@ -438,18 +438,6 @@ __device__ __noinline__ int list_again(PartSmem &s, BeamEntry *list, int room, i
     return count;
 }
 
-// One part of a row.  A thread takes a piece of 16 bytes from each 8 KiB (whole rows of the block's
-// threads): four are on their way or at hand, and each makes room for the one four further.  A
-// thread keeps a maximum and a sum of exponentials of its own and waits for nobody.  At the end the
-// keep-th largest of 128 group maxima is a bound that the part's best `keep` values reach and few
-// others (about as many again): the threads whose maximum reaches it are few, and what they have
-// seen is read once more, from the L2 cache.
-//
-// Bound by the bytes while it streams (2048 rows of 131072 bf16, 98 us, 5.5 TB/s with all the rest), by about 500
-// instructions a warp for the list at each part's end: 1024 rows of 128000, 249 MB, 57 us.  Three CTAs of 512
-// threads (40 registers) 64 us with the join, of 256 or 128 threads 64 to 82; eight pieces at hand and two
-// CTAs 71; the values listed on the way, under a bound carried from block to block, 82 to 109; the next
-// CTA's part asked into the L2 cache 80.
 // Where a row of logits starts.
 __device__ __forceinline__ const unsigned char *row_at(const BeamSelectArgs &a, uint32_t row)
 {
@@ -484,7 +472,19 @@ __device__ __forceinline__ void load_first(uint4 (&v)[kBeamLoads], const unsigne
     }
 }
 
-// v: the thread's first pieces.
+// One part of a row.  A thread takes a piece of 16 bytes from each 8 KiB (whole rows of the block's
+// threads): four are on their way or at hand, and each makes room for the one four further.  A
+// thread keeps a maximum and a sum of exponentials of its own and waits for nobody.  At the end the
+// keep-th largest of 128 group maxima is a bound that the part's best `keep` values reach and few
+// others (about as many again): the threads whose maximum reaches it are few, and what they have
+// seen is read once more, from the L2 cache.
+//
+// Bound by the bytes while it streams (2048 rows of 131072 bf16, 98 us, 5.5 TB/s with all the rest), by about 500
+// instructions a warp for the list at each part's end: 1024 rows of 128000, 249 MB, 57 us.  Three CTAs of 512
+// threads (40 registers) 64 us with the join, of 256 or 128 threads 64 to 82; eight pieces at hand and two
+// CTAs 71; the values listed on the way, under a bound carried from block to block, 82 to 109; the next
+// CTA's part asked into the L2 cache 80.
+// (v: the thread's first pieces.)
 template <int kType, int kThreads>
 __device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, BeamEntry *list, const unsigned char *base, int32_t lo,
                                           int32_t hi, uint4 (&v)[kBeamLoads], BeamPart *meta, BeamEntry *to)
