@@ -126,6 +126,16 @@ __device__ __forceinline__ uint4 shifted(const uint4 &a, const uint4 &b, uint32_
                       __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits));
 }
 
+// Logits that are not kept in the first-level cache, which has room for what is on its way and little else.  With the
+// join: 82 MB of fp32 on changing inputs 27 -> 25 us, 252 MB of bf16 there no change (65), the same ones again, half
+// of them in the L2 cache, 64 -> 56; 82 MB that all lie there 18.7 -> 22.
+__device__ __forceinline__ uint4 stream_load(const unsigned char *p)
+{
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+
 // Values [i, i + W) of a row of n, -inf from hi on (the end of a part, or of the row).  A row may
 // start `off` bytes past a 16-byte boundary: its pieces are put together from two neighbouring aligned
 // ones (the second is the next lane's first and comes from the first-level cache), at the row's ends from
@@ -464,7 +474,7 @@ __device__ __forceinline__ void load_first(uint4 (&v)[kBeamLoads], const unsigne
     if (off == 0 && lo + kBeamLoads * kRow <= hi) {
 #pragma unroll
         for (int j = 0; j < kBeamLoads; ++j)
-            v[j] = *reinterpret_cast<const uint4 *>(base + static_cast<int64_t>(lo + j * kRow + tid * T::kW) * T::kEs);
+            v[j] = stream_load(base + static_cast<int64_t>(lo + j * kRow + tid * T::kW) * T::kEs);
     } else {
 #pragma unroll
         for (int j = 0; j < kBeamLoads; ++j)
@@ -479,11 +489,10 @@ __device__ __forceinline__ void load_first(uint4 (&v)[kBeamLoads], const unsigne
 // others (about as many again): the threads whose maximum reaches it are few, and what they have
 // seen is read once more, from the L2 cache.
 //
-// Bound by the bytes while it streams (2048 rows of 131072 bf16, 98 us, 5.5 TB/s with all the rest), by about 500
-// instructions a warp for the list at each part's end: 1024 rows of 128000, 249 MB, 57 us.  Three CTAs of 512
-// threads (40 registers) 64 us with the join, of 256 or 128 threads 64 to 82; eight pieces at hand and two
-// CTAs 71; the values listed on the way, under a bound carried from block to block, 82 to 109; the next
-// CTA's part asked into the L2 cache 80.
+// Bound by the bytes while it streams, by about 500 instructions a warp for the list at each part's end: 1024 rows
+// of 128000, 249 MB, 57 us, 64 with the join.  That is with three CTAs of 512 threads (40 registers); of 256 or 128
+// threads 64 to 82; eight pieces at hand and two CTAs 71; the values listed on the way under a bound
+// carried from block to block 82 to 109; the next CTA's part asked into the L2 cache 80.
 // (v: the thread's first pieces.)
 template <int kType, int kThreads>
 __device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, BeamEntry *list, const unsigned char *base, int32_t lo,
@@ -544,7 +553,7 @@ __device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, 
 #pragma unroll
             for (int j = 0; j < kBeamLoads; ++j) {
                 take(v[j]);
-                v[j] = *reinterpret_cast<const uint4 *>(p + j * kRow * T::kEs);
+                v[j] = stream_load(p + j * kRow * T::kEs);
             }
             fold();
         }
