@@ -191,6 +191,7 @@ struct PartSmem {
     uint32_t bound;
     int32_t count, last, hits;
     int16_t hit[kMostWarps * 32];       // threads whose largest value reaches the bound; entries of a long list
+    int16_t four[kMostWarps * 32];      // which four pieces of theirs it is in, -1: several
     uint64_t key[kGroups], key_bound;
 };
 
@@ -486,11 +487,12 @@ __device__ __forceinline__ void load_first(uint4 (&v)[kBeamLoads], const unsigne
 // threads): four are on their way or at hand, and each makes room for the one four further.  A
 // thread keeps a maximum and a sum of exponentials of its own and waits for nobody.  At the end the
 // keep-th largest of 128 group maxima is a bound that the part's best `keep` values reach and few
-// others (about as many again): the threads whose maximum reaches it are few, and what they have
-// seen is read once more, from the L2 cache.
+// others (about as many again): the threads whose maximum reaches it are few, and the four pieces that it was in
+// are read once more (all of theirs, where others of them reach the bound too).
 //
 // Bound by the bytes while it streams, by about 500 instructions a warp for the list at each part's end: 1024 rows
-// of 128000, 249 MB, 57 us, 64 with the join.  That is with three CTAs of 512 threads (40 registers); of 256 or 128
+// of 128000, 249 MB, 55 us, 63 with the join (65 with all pieces of those threads read again: they lie 8 KiB apart
+// and may have left the L2 cache).  That is with three CTAs of 512 threads (40 registers); of 256 or 128
 // threads 64 to 82; eight pieces at hand and two CTAs 71; the values listed on the way under a bound
 // carried from block to block 82 to 109; the next CTA's part asked into the L2 cache 80.
 // (v: the thread's first pieces.)
@@ -508,7 +510,9 @@ __device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, 
     // exp(x - from) = 2^((x - from) log2(e)), where `from` is a value seen that lies 4 below the largest at
     // most: it seldom moves, and the arguments of the terms that matter stay small, so exact
     float from = neg_inf(), sum = 0.0f;
-    uint32_t most = T::kNone, limit = T::kNone;         // the largest so far; from + 4
+    uint32_t most = T::kNone, limit = T::kNone;         // the largest of four pieces; from + 4
+    float top = neg_inf(), second = neg_inf();          // the largest of all; that of the other fours
+    int32_t top_at = 0, four = 0;                       // which four pieces it is in
     uint64_t minus = 0, sum2 = 0;       // -from twice (0 while nothing but -inf was seen: it sums up to 0); sums of four pieces
     auto take = [&](const uint4 &x) {
         const uint32_t w[4] = {x.x, x.y, x.z, x.w};
@@ -538,6 +542,12 @@ __device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, 
     auto fold = [&]() {
         sum += low2(sum2) + high2(sum2);
         sum2 = 0;
+        const float high = T::most(most);
+        second = fmaxf(second, fminf(top, high));
+        top_at = high > top ? four : top_at;
+        top = fmaxf(top, high);
+        most = T::kNone;
+        ++four;
     };
     // four rows of pieces are at hand; those four further are on their way while these are worked on
     constexpr int kSpan = kBeamLoads * kRow;
@@ -585,7 +595,6 @@ __device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, 
         raw = false;
         fold();
     }
-    const float top = T::most(most);
     // the part's maximum and sum: each warp's here, of them all by one warp below
     float all = top;
 #pragma unroll
@@ -601,33 +610,42 @@ __device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, 
     }
     float best = top;
     const float bound = group_bound<kThreads>(s, best, a.keep);
-    if (top >= bound && top > neg_inf())
-        s.hit[atomicAdd(&s.hits, 1)] = static_cast<int16_t>(tid);
+    if (top >= bound && top > neg_inf()) {
+        const int h = atomicAdd(&s.hits, 1);
+        s.hit[h] = static_cast<int16_t>(tid);
+        s.four[h] = static_cast<int16_t>(second >= bound ? -1 : top_at);
+    }
     __syncthreads();
-    // a piece a lane, for each as many lanes as it has pieces, in powers of two
-    const int rows = (hi - lo + kRow - 1) / kRow, found = s.hits, lanes = rows <= 4 ? 4 : rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
+    const int rows = (hi - lo + kRow - 1) / kRow, found = s.hits;
     const uint32_t bound2 = T::twice(bound);            // (a value of this type)
-    for (int h = tid / lanes; h < found; h += kThreads / lanes)
-        for (int r = tid % lanes; r < rows; r += lanes) {
-            const int32_t i = lo + r * kRow + s.hit[h] * T::kW;
-            const uint4 x = load_piece<kType>(base, off, i, hi, a.vocab);
-            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    auto look = [&](int h, int r) {
+        const int32_t i = lo + r * kRow + s.hit[h] * T::kW;
+        const uint4 x = load_piece<kType>(base, off, i, hi, a.vocab);
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (!T::reaches(w[k], bound2))
+        for (int k = 0; k < 4; ++k) {
+            if (!T::reaches(w[k], bound2))
+                continue;
+            float z[T::kN];
+            T::get(w[k], z);
+#pragma unroll
+            for (int e = 0; e < T::kN; ++e) {
+                if (!(z[e] >= bound) || z[e] == neg_inf())
                     continue;
-                float z[T::kN];
-                T::get(w[k], z);
-#pragma unroll
-                for (int e = 0; e < T::kN; ++e) {
-                    if (!(z[e] >= bound) || z[e] == neg_inf())
-                        continue;
-                    const int to_at = atomicAdd(&s.count, 1);
-                    if (to_at < a.list)
-                        list[to_at] = BeamEntry{z[e], i + k * T::kN + e};
-                }
+                const int to_at = atomicAdd(&s.count, 1);
+                if (to_at < a.list)
+                    list[to_at] = BeamEntry{z[e], i + k * T::kN + e};
             }
         }
+    };
+    // nearly always in four pieces alone: a piece a lane; else all of them, by a warp
+    for (int h = tid / kBeamLoads; h < found; h += kThreads / kBeamLoads)
+        if (s.four[h] >= 0)
+            look(h, s.four[h] * kBeamLoads + tid % kBeamLoads);
+    for (int h = warp; h < found; h += kWarps)
+        if (s.four[h] < 0)
+            for (int r = lane; r < rows; r += 32)
+                look(h, r);
     __syncthreads();
     int count = s.count;
     if (count > a.list) {
