@@ -59,6 +59,15 @@ template <int kType, int kBytes> struct Values {
     }
 };
 
+// A unit of `pairs` pairs side by side of which the first `turned` are taken from x and the others
+// from `as_it_was`, bit for bit (a NaN would not come back from fp32 with its own bits).
+__device__ __forceinline__ uint4 first_pairs(const uint4 &x, const uint4 &as_it_was, int turned, int pairs)
+{
+    const int words = turned * 4 / pairs;               // (a pair is one word or two)
+    return make_uint4(words > 0 ? x.x : as_it_was.x, words > 1 ? x.y : as_it_was.y, words > 2 ? x.z : as_it_was.z,
+                      words > 3 ? x.w : as_it_was.w);
+}
+
 template <int N> __device__ __forceinline__ void load_floats(const float *p, bool wide, float (&x)[N])
 {
     if (N % 4 == 0 && wide) {
@@ -148,7 +157,7 @@ __global__ void __launch_bounds__(kRotThreads, fit<kBytes, kSide>()) paged_rotar
             continue;
         }
         const float *row = a.table + pos * a.table_stride;
-        if (kSide) {
+        if constexpr (kSide) {
             const int32_t col = u * W;
             constexpr int N = W > 1 ? W / 2 : 1;
             float c[N], s[N];
@@ -161,7 +170,7 @@ __global__ void __launch_bounds__(kRotThreads, fit<kBytes, kSide>()) paged_rotar
                 load_floats<N>(row + first, a.wide_table, c);
                 load_floats<N>(row + a.half + first, a.wide_table, s);
             } else {
-                // the last unit: its columns past the rotated ones stay
+                // the last unit: its columns past the rotated ones stay (see first_pairs)
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     c[i] = first + i < a.half ? row[first + i] : 1.0f;
@@ -177,11 +186,10 @@ __global__ void __launch_bounds__(kRotThreads, fit<kBytes, kSide>()) paged_rotar
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
                     const float p = v[2 * j], q = v[(2 * j + 1) % W];
-                    const bool in = first + j < a.half;
-                    r[2 * j] = in ? __fmaf_rn(p, c[j], -(q * s[j])) : p;
-                    r[(2 * j + 1) % W] = in ? __fmaf_rn(q, c[j], p * s[j]) : q;
+                    r[2 * j] = __fmaf_rn(p, c[j], -(q * s[j]));
+                    r[(2 * j + 1) % W] = __fmaf_rn(q, c[j], p * s[j]);
                 }
-                *reinterpret_cast<Raw *>(dst + i * dh + col * kEs) = V::put(r);
+                *reinterpret_cast<Raw *>(dst + i * dh + col * kEs) = first_pairs(V::put(r), lo[i], a.half - first, N);
             }
         } else {
             Raw hi[kHeads];

@@ -161,6 +161,29 @@ def test_infinities_and_nans_stay_in_their_pair():
     assert torch.equal(vc[slots // 16, slots % 16].view(torch.int16), v.view(torch.int16))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("rot", [2, 18, 20, 30])
+def test_columns_that_are_not_rotated_keep_their_bits(dtype, inter, rot):
+    # NaNs of every kind beside the last pair, in queries and keys
+    q, k, v, kc, vc, slots, pos, table = _case(40, 4, 2, 64, rot, inter, dtype, seed=rot)
+    bits = torch.int32 if dtype == "f32" else torch.int16
+    nans = {"bf16": [0x7fb1, 0x7f81, 0xff81 - 65536, 0xffc5 - 65536], "f16": [0x7d01, 0x7e55, 0xfc01 - 65536, 0xff33 - 65536],
+            "f32": [0x7f800123, 0x7fc00345, 0xff800001 - (1 << 32), 0xffc0ffee - (1 << 32)]}[dtype]
+    for x in (q, k):
+        some = torch.tensor(nans, dtype=bits, device="cuda")[torch.arange(64 - rot, device="cuda") % 4]
+        x.view(bits)[::2, :, rot:] = some
+        assert torch.isnan(x[::2, :, rot:]).all()
+    out = torch.empty_like(q)
+    bsm.bsm_paged_write_rotary(q, k, v, out, kc, vc, slots, pos, table, flags=bsm.FLAG_INTERLEAVED if inter else 0)
+    got = kc[slots // 16, slots % 16]
+    assert torch.equal(out.view(bits)[..., rot:], q.view(bits)[..., rot:])
+    assert torch.equal(got.view(bits)[..., rot:], k.view(bits)[..., rot:])
+    for x, src in ((out, q), (got, k)):
+        ref, size = O.rotary(src, pos.tolist(), table, inter)
+        _close(x[..., :rot], ref[..., :rot], size[..., :rot], "rotated columns")
+
+
 def test_captured_and_on_two_streams():
     a = _case(600, 8, 2, 128, 128, False, "bf16", seed=6)
     b = _case(3, 8, 2, 128, 128, True, "bf16", seed=7)
