@@ -528,8 +528,9 @@ int64_t bsm_beam_select_workspace_bytes(int device, int32_t n_requests, int32_t 
  * free_pages is not changed: drop its first info[0] entries.  The rows of one request alone
  * share partly filled pages; a page is in one column.  A row whose last page is missing (-1)
  * passes that on.  Lengths outside 0 .. table_width * page_size are cut to it and set
- * BSM_DEV_BOUNDS; so does a last page or a free page whose id lies outside the cache (it is
- * handed on as it is, and nothing copied).
+ * BSM_DEV_BOUNDS; so does a partly filled last page whose id lies outside the cache (other than
+ * -1), or a free page that is taken and does (negative ones too): the id is handed on as it
+ * is, and nothing copied.
  *   new_lengths, new_tables  lengths and tables themselves (in place, the same stride), or
  *             apart from them.
  *   caches    dtype, rows, pointers and strides as bsm_paged_write, with a stride from layer

@@ -71,8 +71,9 @@ template <int kBeams> __global__ void __launch_bounds__(kReorderTile) reorder_ta
             a.row_length[row0 + tid] = length;
         if (length % a.page && full >= first && full < first + kReorderTile) {
             tail = old_rows[mine * kReorderTile + full - first];
-            if (tail >= a.n_pages) {
-                atomicOr(a.status, BSM_DEV_BOUNDS);     // passed on as it is
+            // (-1: a page that was missing before; what lies outside the cache is passed on as it is)
+            if (tail < -1 || tail >= a.n_pages) {
+                atomicOr(a.status, BSM_DEV_BOUNDS);
                 tail = -1;
             }
         }
@@ -311,12 +312,13 @@ __global__ void __launch_bounds__(kFinishThreads, kFinishCtas) reorder_pages(con
                 const int64_t k = taken + e;
                 const int32_t length = a.row_length[row], full = length / a.page, part = length - full * a.page;
                 const int32_t page = k < a.n_free ? a.free_pages[k] : -1;
+                const bool there = page >= 0 && page < a.n_pages;
                 if (blockIdx.x == 0) {
                     a.new_tables[row * a.new_table_stride + full] = page;
-                    if (page >= a.n_pages)
+                    if (k < a.n_free && !there)
                         atomicOr(a.status, BSM_DEV_BOUNDS);
                 }
-                if (page >= 0 && page < a.n_pages)
+                if (there)
                     units = (part + tokens - 1) / tokens;
                 s_from[tid] = a.row_source[row];
                 s_to[tid] = page;

@@ -196,6 +196,45 @@ def test_lengths_and_pages_outside_the_buffers():
     assert c.info[0] == 2 and torch.equal(c.k[:, int(c.new_tables[2, 2]), :8], before[:, int(c.tables[0, 2]), :8])
 
 
+@pytest.mark.parametrize("bad", [-1, -2, -(1 << 31)])
+def test_free_pages_with_negative_ids_are_reported(bad):
+    c = Case(1, 3, 16, 40, 40, seed=8)
+    c.parents[:] = 0
+    c.free[0] = bad                             # (a list that was padded)
+    k, v, second = c.k.clone(), c.v.clone(), int(c.free[1])
+    c.run()
+    assert bsm.bsm_device_status() == bsm.DEV_BOUNDS
+    assert c.new_tables[:, 2].tolist() == [int(c.tables[0, 2]), bad, second] and c.info.tolist()[:2] == [2, 0]
+    for x, before in ((c.k, k), (c.v, v)):      # the other copy is made, and no other byte changes
+        before[:, second, :8] = before[:, int(c.tables[0, 2]), :8].clone()
+        assert torch.equal(x, before)
+    # one that is not taken does not matter
+    bsm.bsm_device_status_clear()
+    c = Case(1, 3, 16, 40, 40, seed=8, n_free=5)
+    c.free[2:] = bad
+    c.parents[:] = 0
+    c.check()
+    assert bsm.bsm_device_status() == 0
+
+
+@pytest.mark.parametrize("bad", [-2, -(1 << 31)])
+def test_last_pages_with_negative_ids_are_reported(bad):
+    c = Case(1, 3, 16, 40, 40, seed=8)
+    c.parents[:] = _i32([[0, 0, 1]])
+    c.tables[0, 2] = bad
+    before = c.k.clone()
+    c.run()
+    assert bsm.bsm_device_status() == bsm.DEV_BOUNDS and c.new_tables[:2, 2].tolist() == [bad, bad]
+    assert c.info.tolist()[:2] == [0, 0] and torch.equal(c.k, before)
+    # a page that was missing already is passed on without a report
+    bsm.bsm_device_status_clear()
+    c = Case(1, 3, 16, 40, 40, seed=8)
+    c.parents[:] = 0
+    c.tables[0, 2] = -1
+    c.check()
+    assert bsm.bsm_device_status() == 0 and (c.new_tables[:, 2] == -1).all()
+
+
 def test_no_requests():
     c = Case(1, 2, 16, 5, 5)
     bsm.bsm_paged_reorder(c.parents[:0], c.lengths[:0], c.tables[:0], c.free, c.lengths[:0], c.tables[:0], c.dropped, c.info,
