@@ -233,7 +233,8 @@ __device__ void list_dropped(const PagedReorderArgs &a, int cta, int ctas)
         for (int x = cta * (kFinishThreads / 32) + (tid >> 5); x < here * kSlices; x += ctas * (kFinishThreads / 32)) {
             const int l = x / kSlices, slice = x % kSlices, count = s_first[l + 1] - s_first[l];
             const int64_t to = dropped + s_first[l], room = a.n_dropped - to;
-            const int32_t end = count * (slice + 1) / kSlices, n = room < end ? static_cast<int32_t>(room) : end;
+            // (more than 2^31 may be past the caller's room, so its sign is asked for in 64 bits)
+            const int32_t end = count * (slice + 1) / kSlices, n = room < end ? static_cast<int32_t>(room > 0 ? room : 0) : end;
             const int32_t *list = a.lists + (l0 + l) * kReorderTile * a.beams;
 #pragma unroll 4
             for (int i = count * slice / kSlices + lane; i < n; i += 32)

@@ -172,6 +172,25 @@ def test_more_dropped_pages_than_listed():
     assert c.info.tolist()[2:] == [want.info[2], bsm.PAGED_DROPPED]
 
 
+def test_more_than_2_31_dropped_pages_and_few_listed():
+    # 33 requests whose 64 rows of 2^20 - 1 pages are all given up: 2.2e9 dropped pages, room for 10 (27 GB)
+    n, B, width = 33, 64, (1 << 20) - 1
+    assert n * B * width > (1 << 31) + 10
+    tables = torch.arange(B, dtype=torch.int32, device="cuda")[:, None].repeat(n, width)
+    new = torch.full((n * B, width), -9, dtype=torch.int32, device="cuda")
+    lengths = torch.full((n * B,), width, dtype=torch.int32, device="cuda")
+    new_lengths = torch.full_like(lengths, -9)
+    k, v = (torch.ones((70, 1, 1, 8), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    dropped = torch.full((12,), -7, dtype=torch.int32, device="cuda")
+    info = torch.full((4,), -7, dtype=torch.int64, device="cuda")
+    ws = torch.empty(bsm.bsm_paged_reorder_workspace_bytes(n, B, width), dtype=torch.uint8, device="cuda")
+    bsm.bsm_paged_reorder(torch.full((n, B), -1, dtype=torch.int32, device="cuda"), lengths, tables, _i32([1]), new_lengths, new,
+                          dropped[:10], info, k, v, ws)
+    assert info.tolist() == [0, 0, n * B * width, bsm.PAGED_DROPPED]
+    assert dropped.tolist() == list(range(10)) + [-7, -7] and (new_lengths == 0).all()
+    assert bool((new == -9).all()) and bsm.bsm_device_status() == 0
+
+
 def test_lengths_and_pages_outside_the_buffers():
     c = Case(2, 3, 16, 40, 40, seed=8, width=4)
     c.parents[:] = _i32([[0, 0, 1], [2, 2, 2]])
