@@ -99,6 +99,19 @@ template <int kType> struct Word {
         const __half2 v = __float2half2_rn(x);
         return *reinterpret_cast<const uint32_t *>(&v);
     }
+    // The largest value of the type, twice, that is at most x + 4.
+    static __device__ __forceinline__ uint32_t four_above(float x)
+    {
+        const float y = __fadd_rd(x, 4.0f);
+        if (kType == BSM_F32)
+            return __float_as_uint(y);
+        if (kType == BSM_BF16) {
+            const __nv_bfloat162 v = __bfloat162bfloat162(__float2bfloat16_rd(y));
+            return *reinterpret_cast<const uint32_t *>(&v);
+        }
+        const __half2 v = __half2half2(__float2half_rd(y));
+        return *reinterpret_cast<const uint32_t *>(&v);
+    }
     static __device__ __forceinline__ float most(uint32_t w)            // (not NaN)
     {
         float x[kN];
@@ -512,7 +525,7 @@ __device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, 
     // exp(x - from) = 2^((x - from) log2(e)), where `from` is a value seen that lies 4 below the largest at
     // most: it seldom moves, and the arguments of the terms that matter stay small, so exact
     float from = neg_inf(), sum = 0.0f;
-    uint32_t most = T::kNone, limit = T::kNone;         // the largest of four pieces; from + 4
+    uint32_t most = T::kNone, limit = T::kNone;         // the largest of four pieces; from + 4, rounded down
     float top = neg_inf(), second = neg_inf();          // the largest of all; that of the other fours
     int32_t top_at = 0, four = 0;                       // which four pieces it is in
     uint64_t minus = 0, sum2 = 0;       // -from twice (0 while nothing but -inf was seen: it sums up to 0); sums of four pieces
@@ -527,7 +540,7 @@ __device__ __forceinline__ void take_part(const BeamSelectArgs &a, PartSmem &s, 
                 sum *= scale;
                 sum2 = mul2(sum2, pack2(scale, scale));
                 from = high;
-                limit = T::twice(from + 4.0f);
+                limit = T::four_above(from);
                 minus = pack2(-from, -from);
             }
         }

@@ -208,6 +208,21 @@ def test_large_and_far_values():
     _check(x, s, 12)
 
 
+@pytest.mark.parametrize("dtype,at,step", [
+    ("bf16", 1032, 8), ("bf16", -1032, 8), ("bf16", 508, 2), ("f16", 8200, 8), ("f16", -8200, 8), ("f16", 4100, 4), ("f32", 2 ** 26, 8)])
+def test_values_about_as_far_apart_as_their_type_resolves(dtype, at, step):
+    # the reference of the exponentials lags 4 at most where at + 4 is no number of the type, too
+    g = torch.Generator(device="cuda").manual_seed(abs(at))
+    x = at + step * (torch.rand((2, 3, 40001), generator=g, device="cuda") < 0.5).double()
+    x[:, :, :17000] = at                                # (the larger value comes late)
+    assert torch.equal(x.to(DT[dtype]).double(), x)
+    s = torch.tensor([[-1.0, -1.3, -2.0], [-3.0, -1.0, -9.0]], device="cuda")
+    out = _check(x.to(DT[dtype]), s, 7)
+    count = (x[0, 0] == at + step).sum()
+    want = -1 - math.log(int(count) + (40001 - int(count)) * math.exp(-step))
+    assert abs(float(out[0][0, 0]) - want) <= _tol(40001, abs(want))
+
+
 def test_sums_of_long_rows_by_their_own_formula():
     x, s = _data(1, 2, 1 << 20, "f32", seed=8)
     v, p, t = _check(x, s, 4)
