@@ -469,8 +469,12 @@ int64_t bsm_paged_workspace_bytes(int device, int32_t heads_q, int32_t heads_kv,
  * order.  Token t after beam b has the value
  *     scores[b] + x[b][t] - log sum_t' exp(x[b][t'])
  * (the logarithm of the row's softmax, added to the beam's score so far); larger values
- * come first, equal ones by beam, then by token.  The values are held in 48 bits: a beam's
- * tokens come in the order of their logits, and beams compare within about 1e-7.
+ * come first, equal ones by beam, then by token.  The values are held in two fp32 numbers: a
+ * beam's tokens come in the order of their logits as far as these are 2^-44 of the largest of
+ * |x - max x|, |score| and the logarithm apart, or equal; closer ones may be taken as equal or
+ * change places.  Different beams compare within the error of their sums, which are fp32: of
+ * the logarithm at most 2e-5 at 128000 tokens and 5e-5 at 2^20 (measured: 7e-8 on random rows,
+ * 3e-7 on rows of two values or of a slope); equal rows of a call have equal sums.
  *   out_scores[r][i]  the value, rounded once; parents[r][i], tokens[r][i]: its beam, 0 ..
  *                     beams - 1, and its token.  Where a request has fewer candidates the
  *                     rest is -inf, -1, -1.

@@ -136,6 +136,20 @@ def test_order_within_ascending_and_descending_rows(dtype, V):
     _check(x, torch.tensor([[-0.5, -0.7]], device="cuda"), 20)
 
 
+@pytest.mark.parametrize("V", [60, 9000, 120000])
+@pytest.mark.parametrize("n", [1, 12])
+def test_tokens_of_a_beam_follow_logits_that_lie_close(n, V):
+    # 1e-12 apart beside a maximum of 5 and a logarithm below 13: more than 2^-44 of the largest
+    assert 1e-12 > 2.0 ** -44 * 13
+    g = torch.Generator(device="cuda").manual_seed(V)
+    x = torch.full((n, 1, V), -20.0, device="cuda")
+    for r in range(n):
+        at = torch.randperm(V, generator=g, device="cuda")[:41]
+        x[r, 0, at[0]] = 5.0
+        x[r, 0, at[1:]] = (torch.arange(40, device="cuda") - 20) * 1e-12
+    _check(x, torch.full((n, 1), -0.75, device="cuda"), 30)
+
+
 def test_beams_without_a_score():
     x, s = _data(4, 4, 3000, "bf16", seed=3)
     s[0, 1:] = NEG                                  # the first step: one beam
