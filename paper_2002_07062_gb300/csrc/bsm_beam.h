@@ -70,9 +70,11 @@ struct BeamCut {
 };
 // Lists that any cut of at most `rows` rows makes, whatever the vocabulary.
 int64_t beam_most_lists(int64_t rows, int n_sm);
-BeamCut beam_cut(int32_t n, int32_t beams, int32_t vocab, int es, int n_sm);
+BeamCut beam_cut(int32_t n, int32_t beams, int32_t vocab, int es, int n_sm, bool clusters);
 
 int launch_beam_select(BeamSelectArgs a, int dtype, const BeamCut &cut, void *stream);
 int beam_set_smem_limit();
+// Whether the current device places a cluster of the one-launch form at its largest (after beam_set_smem_limit).
+bool beam_clusters_fit();
 
 }  // namespace bsm

@@ -25,10 +25,10 @@ struct SelectLayout {
 int64_t entries_bytes(int64_t lists, int32_t keep) { return up256(lists * keep * static_cast<int64_t>(sizeof(BeamEntry))); }
 int64_t meta_bytes(int64_t lists) { return up256(lists * static_cast<int64_t>(sizeof(BeamPart))); }
 
-SelectLayout select_layout(int32_t n, int32_t beams, int32_t vocab, int32_t keep, int es, int n_sm)
+SelectLayout select_layout(int32_t n, int32_t beams, int32_t vocab, int32_t keep, int es, const PagedDev &dev)
 {
     SelectLayout l{};
-    l.cut = beam_cut(n, beams, vocab, es, n_sm);
+    l.cut = beam_cut(n, beams, vocab, es, dev.n_sm, dev.clusters);
     const int64_t lists = static_cast<int64_t>(n) * beams * l.cut.parts;        // (a cluster's are in shared memory)
     l.meta = entries_bytes(lists, keep);
     l.bytes = l.meta + meta_bytes(lists);
@@ -81,7 +81,7 @@ int beam_select(const bsm_beam_select_desc *d, bsm_stream_t stream)
     PagedDev *dev = nullptr;
     if (int rc = paged_device(-1, &dev))
         return rc;
-    const SelectLayout l = select_layout(d->n_requests, d->beams, d->vocab, d->keep, es, dev->n_sm);
+    const SelectLayout l = select_layout(d->n_requests, d->beams, d->vocab, d->keep, es, *dev);
     if (d->workspace_bytes < l.bytes)
         return BSM_ERR_INVALID_ARG;
     TraceRange tr("bsm_beam_select");

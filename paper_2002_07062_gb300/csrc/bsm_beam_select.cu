@@ -975,23 +975,26 @@ template <int kType> __global__ void __launch_bounds__(kJoinThreads, 2) select_t
         join(a, j, z, static_cast<int32_t>(request), static_cast<int>(lists));
 }
 
-int launch_cluster(void (*kernel)(BeamSelectArgs), dim3 grid, size_t smem, cudaStream_t st, const BeamSelectArgs &a)
-{
+// The launch of a cluster a request.
+struct ClusterLaunch {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(kJoinThreads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
     cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = kCluster;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 2;
-    return static_cast<int>(cudaLaunchKernelEx(&cfg, kernel, a));
-}
+    ClusterLaunch(unsigned requests, size_t smem, cudaStream_t st)
+    {
+        cfg.gridDim = dim3(requests * kCluster);
+        cfg.blockDim = dim3(kJoinThreads);
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = st;
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = kCluster;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[1].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 2;
+    }
+    ClusterLaunch(const ClusterLaunch &) = delete;
+};
 
 // Entries of a part's list: what a block with a bound of its own may add to what is kept.
 int32_t list_entries(int32_t keep, int dtype, int threads)
@@ -1009,13 +1012,14 @@ size_t join_smem(int32_t lists, int32_t keep)
 int64_t beam_most_lists(int64_t rows, int n_sm) { return std::max<int64_t>(rows, 8ll * n_sm * kRowCtas); }
 
 // Requests that are few and short go to a cluster each, in one launch; the others' parts to all SMs, and
-// their joins to a second launch.  Every row is cut alike, so equal rows give equal bits.
-BeamCut beam_cut(int32_t n, int32_t beams, int32_t vocab, int es, int n_sm)
+// their joins to a second launch; so do all where a device (a share of a GPU) places no cluster.  Every row is cut
+// alike, so equal rows give equal bits.
+BeamCut beam_cut(int32_t n, int32_t beams, int32_t vocab, int es, int n_sm, bool clusters)
 {
     const int64_t piece = 16 / es, rows = static_cast<int64_t>(n) * beams;
     auto up = [](int64_t x, int64_t d) { return (x + d - 1) / d; };
     BeamCut c{};
-    c.together = n <= kMostTogether && static_cast<int64_t>(beams) * vocab * es <= kCluster * kTogetherBytes;
+    c.together = clusters && n <= kMostTogether && static_cast<int64_t>(beams) * vocab * es <= kCluster * kTogetherBytes;
     if (c.together) {
         // parts of a piece a thread at least
         int64_t parts = std::min<int64_t>(kCluster / beams, up(vocab, kJoinThreads * piece));
@@ -1049,11 +1053,10 @@ int launch_beam_select(BeamSelectArgs a, int dtype, const BeamCut &cut, void *st
     const size_t part = part_smem(a.keep, dtype, threads), joint = join_smem(a.beams * a.parts, a.keep);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (cut.together) {
-        const dim3 grid(static_cast<unsigned>(a.n) * kCluster);
-        const size_t smem = part + joint;
-        return dtype == BSM_F32    ? launch_cluster(select_together<BSM_F32>, grid, smem, st, a)
-               : dtype == BSM_BF16 ? launch_cluster(select_together<BSM_BF16>, grid, smem, st, a)
-                                   : launch_cluster(select_together<BSM_F16>, grid, smem, st, a);
+        const ClusterLaunch l(static_cast<unsigned>(a.n), part + joint, st);
+        return static_cast<int>(dtype == BSM_F32    ? cudaLaunchKernelEx(&l.cfg, select_together<BSM_F32>, a)
+                                : dtype == BSM_BF16 ? cudaLaunchKernelEx(&l.cfg, select_together<BSM_BF16>, a)
+                                                    : cudaLaunchKernelEx(&l.cfg, select_together<BSM_F16>, a));
     }
     const dim3 grid(static_cast<unsigned>(a.n) * a.beams * a.parts);
     const int e = dtype == BSM_F32    ? launch_early(select_rows<BSM_F32>, grid, kRowThreads, part, st, a)
@@ -1081,6 +1084,22 @@ int beam_set_smem_limit()
     rows(reinterpret_cast<const void *>(&select_rows<BSM_F16>), reinterpret_cast<const void *>(&select_together<BSM_F16>), BSM_F16);
     set(reinterpret_cast<const void *>(&select_join), joint, false);
     return e;
+}
+
+bool beam_clusters_fit()
+{
+    auto fits = [](void (*f)(BeamSelectArgs), int dtype) {
+        ClusterLaunch l(1, part_smem(kBeamMost, dtype, kJoinThreads) + join_smem(kBeamMostLists, kBeamMost), nullptr);
+        l.cfg.numAttrs = 1;             // (the cluster alone)
+        int n = 0;
+        if (cudaOccupancyMaxActiveClusters(&n, f, &l.cfg) != cudaSuccess) {
+            cudaGetLastError();
+            return false;
+        }
+        return n > 0;
+    };
+    return fits(select_together<BSM_F32>, BSM_F32) && fits(select_together<BSM_BF16>, BSM_BF16) &&
+           fits(select_together<BSM_F16>, BSM_F16);
 }
 
 }  // namespace bsm

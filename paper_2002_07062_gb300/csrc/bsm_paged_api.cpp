@@ -10,6 +10,7 @@
 #include <cstring>
 #include <mutex>
 
+#include "bsm_beam.h"
 #include "bsm_internal.h"
 #include "bsm_paged.h"
 #include "bsm_paged_host.h"
@@ -56,6 +57,7 @@ int paged_device(int device, PagedDev **out)
         if (cudaGetDevice(&prev) != cudaSuccess || (prev != device && cudaSetDevice(device) != cudaSuccess))
             return BSM_ERR_NO_DEVICE;
         const int e = paged_set_smem_limit();
+        d.clusters = !e && beam_clusters_fit();
         if (prev != device)
             cudaSetDevice(prev);
         if (e)

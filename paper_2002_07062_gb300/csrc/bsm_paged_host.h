@@ -14,6 +14,7 @@ struct PagedDev {
     bool ready = false;
     int n_sm = 0;
     uint32_t *status = nullptr;
+    bool clusters = false;              // the beam selection's clusters can be placed (see beam_cut)
 };
 
 int device_status_word(int device, uint32_t **out);
