@@ -96,7 +96,7 @@ def main(argv=None):
         bsm.bsm_beam_select(logits, scores, best, parents, tokens, work_select, stream=stream)
         bsm.bsm_paged_reorder(parents, lengths, tables, free, lengths, tables, dropped, info, k_cache, v_cache, work_reorder,
                               stream=stream)
-        taken, missing, gone, flags = info.tolist()     # (the one place that waits for the device)
+        taken, missing, gone, flags = info.tolist()     # (waits for the device, as reading info above does)
         if flags:
             raise RuntimeError("step does not fit: %d pages missing, flags %d" % (missing, flags))
         free = torch.cat([free[taken:], dropped[:gone]])
@@ -122,6 +122,8 @@ def check(embed, weights, rotary, history, lengths, got, hq, hkv, d):
     layers, against the step's."""
     worst = 0.0
     for r, length in enumerate(lengths.tolist()):
+        if length == 0:                 # (a beam that is not in use yet)
+            continue
         x = embed[history[r, :length]]
         turn = rotary[:length].double()
         c, s = turn[:, None, :d // 2], turn[:, None, d // 2:]

@@ -139,3 +139,15 @@ def test_example_runs():
     spec.loader.exec_module(m)
     # bf16 keys and probabilities against float64: a few roundings of 2^-8
     assert m.main(["--requests", "3", "--beams", "4", "--steps", "10", "--layers", "2", "--vocab", "1000", "--check"]) < 0.05
+
+
+@pytest.mark.parametrize("steps", [1, 2])
+def test_example_checks_its_first_steps(steps):
+    # in the first one only one beam of a request has a history
+    at = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "beam_search.py")
+    spec = importlib.util.spec_from_file_location("beam_search_first", at)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    worst = m.main(["--requests", "2", "--beams", "3", "--steps", str(steps), "--layers", "2", "--vocab", "500", "--prompt", "40",
+                    "--check"])
+    assert 0.0 < worst < 0.05
