@@ -591,6 +591,8 @@ def bsm_paged_write_rotary(q, k, v, q_out, k_cache, v_cache, slots, positions, t
             raise ValueError("q_out without q")
         heads_q, qp, op, qs, os_ = 0, 0, 0, (0, 0), (0, 0)
     else:
+        if q_out is None:
+            raise ValueError("q without q_out")
         qs, os_, qshape = q.stride(), q_out.stride(), q.shape
         if not (q.dtype is kind and q_out.dtype is kind and q.get_device() == dev and q_out.get_device() == dev
                 and len(qs) == 3 and len(os_) == 3 and qs[2] == 1 and os_[2] == 1):

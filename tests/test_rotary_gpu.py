@@ -134,6 +134,14 @@ def test_without_queries_or_positions():
     assert torch.equal(kc, before) and bsm.bsm_device_status() == bsm.DEV_BOUNDS
 
 
+def test_queries_come_with_a_place_to_go():
+    q, k, v, kc, vc, slots, pos, table = _case(4, 4, 2, 64, 64, False, "bf16", seed=9)
+    with pytest.raises(ValueError):
+        bsm.bsm_paged_write_rotary(q, k, v, None, kc, vc, slots, pos, table)
+    with pytest.raises(ValueError):
+        bsm.bsm_paged_write_rotary(None, k, v, torch.empty_like(q), kc, vc, slots, pos, table)
+
+
 def test_rotation_of_nothing_is_the_plain_write():
     q, k, v, kc, vc, slots, pos, table = _case(500, 4, 2, 64, 0, False, "bf16", seed=2)
     k2, v2 = kc.clone(), vc.clone()
