@@ -43,7 +43,7 @@ def main(argv=None):
     rows, wide = n * B, (a.heads + 2 * a.heads_kv) * a.dim
     prompts = torch.randint(1, a.prompt + 1, (n,)).tolist()
     width = -(-(a.prompt + a.steps) // a.page)
-    pages = rows * width
+    pages = rows * (width + 1)          # (a row's copied page is taken before any dropped one is free again)
     i32 = dict(dtype=torch.int32, device="cuda")
     k_cache = torch.zeros((a.layers, pages, a.page, hkv, d), dtype=torch.bfloat16, device="cuda")
     v_cache = torch.zeros_like(k_cache)

@@ -529,7 +529,8 @@ int64_t bsm_beam_select_workspace_bytes(int device, int32_t n_requests, int32_t 
  *             its free pages (a page that requests share is dropped by a request when none of
  *             its rows holds it any more).  Entries past info[2] stay.
  *   info[0..3]  pages taken; pages missing; pages dropped; BSM_PAGED_* bits
- * free_pages is not changed: drop its first info[0] entries.  The rows of one request alone
+ * free_pages is not changed: drop its first info[0] entries.  Up to beams - 1 pages a request are
+ * taken before the call gives any back: keep as many free.  The rows of one request alone
  * share partly filled pages; a page is in one column.  A row whose last page is missing (-1)
  * passes that on.  Lengths outside 0 .. table_width * page_size are cut to it and set
  * BSM_DEV_BOUNDS; so does a partly filled last page whose id lies outside the cache (other than

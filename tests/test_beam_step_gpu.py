@@ -151,3 +151,13 @@ def test_example_checks_its_first_steps(steps):
     worst = m.main(["--requests", "2", "--beams", "3", "--steps", str(steps), "--layers", "2", "--vocab", "500", "--prompt", "40",
                     "--check"])
     assert 0.0 < worst < 0.05
+
+
+def test_example_has_pages_for_copies_that_come_before_dropped_ones():
+    # a page a row holds everything; a step whose rows share a beam takes one more
+    at = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "beam_search.py")
+    spec = importlib.util.spec_from_file_location("beam_search_small", at)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    assert m.main(["--requests", "1", "--beams", "4", "--steps", "15", "--layers", "1", "--vocab", "300", "--prompt", "1",
+                   "--check"]) < 0.05
