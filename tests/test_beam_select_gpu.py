@@ -278,6 +278,23 @@ def test_workspace_of_the_most_requests_serves_fewer():
         _check(x, s, 8, got=_run(x, s, 8, ws=ws))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,B,V", [(1, 1, 1 << 20), (1, 2, 1 << 20), (2, 3, 700001), (9, 1, 300000)])
+def test_most_lists_of_the_most_kept_in_two_launches(dtype, n, B, V):
+    # up to 128 lists of 64 entries join: random rows, rows that rise or fall (every part has the largest of the
+    # parts before it below it), few levels (ties over all parts)
+    x, s = _data(n, B, V, dtype, seed=B)
+    _check(x, s, 64)
+    up = torch.linspace(-6, 6, V, device="cuda").to(DT[dtype])
+    _check(torch.stack([up, up.flip(0), up])[:B].expand(n, B, V).contiguous(), s, 64)
+    _check((torch.randint(0, 2, (n, B, V), device="cuda") * 0.5).to(DT[dtype]), s, 64)
+    # the 64 best one by one in different parts
+    x[:] = -9.0
+    at = (torch.arange(64, device="cuda") * (V // 64) + 11) % V
+    x[:, :, at] = torch.arange(64, device="cuda").flip(0).to(DT[dtype]) * 0.125
+    _check(x, s, 64)
+
+
 def test_rows_far_apart():
     # more than 2^31 elements and 2^32 bytes from row to row
     far = 1_500_000_007
