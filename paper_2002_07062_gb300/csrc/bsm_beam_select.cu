@@ -141,7 +141,8 @@ __device__ __forceinline__ uint4 shifted(const uint4 &a, const uint4 &b, uint32_
 
 // Logits that are not kept in the first-level cache, which has room for what is on its way and little else.  With the
 // join: 82 MB of fp32 on changing inputs 27 -> 25 us, 252 MB of bf16 there no change (65), the same ones again, half
-// of them in the L2 cache, 64 -> 56; 82 MB that all lie there 18.7 -> 22.
+// of them in the L2 cache, 64 -> 56; but 82 MB that all lie there 18.7 -> 22, what a product that has just written
+// fewer than 100 MB of logits leaves: there plain loads would be better.
 __device__ __forceinline__ uint4 stream_load(const unsigned char *p)
 {
     uint4 v;
@@ -506,8 +507,8 @@ __device__ __forceinline__ void load_first(uint4 (&v)[kBeamLoads], const unsigne
 // are read once more (all of theirs, where others of them reach the bound too).
 //
 // Bound by the bytes while it streams, by about 500 instructions a warp for the list at each part's end: 1024 rows
-// of 128000, 249 MB, 55 us, 63 with the join (65 with all pieces of those threads read again: they lie 8 KiB apart
-// and may have left the L2 cache).  That is with three CTAs of 512 threads (40 registers); of 256 or 128
+// of 128000, 249 MB, the join with it: 63 us on changing inputs, 55 on the same ones again, half of them in the L2
+// cache (65 and 56 with all pieces of those threads read again: they lie 8 KiB apart and may have left it).  That is with three CTAs of 512 threads (40 registers); of 256 or 128
 // threads 64 to 82; eight pieces at hand and two CTAs 71; the values listed on the way under a bound
 // carried from block to block 82 to 109; the next CTA's part asked into the L2 cache 80.
 // (v: the thread's first pieces.)
