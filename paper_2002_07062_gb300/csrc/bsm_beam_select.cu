@@ -937,8 +937,8 @@ __global__ void __launch_bounds__(kJoinThreads) select_join(const BeamSelectArgs
 // Both in one launch: a cluster takes a request's parts, their lists go to the first CTA's shared memory,
 // and it joins them.  One request of 4 beams over 32000: 7 to 8 us, 9.6 in two launches; a call costs the host 2 us
 // less.  A cluster of 16 takes its time to start: 28 requests of one beam over 4000 took 13 us, 7 in two launches.
-// Which beams have logits to read is known before the first load, while the cluster starts: 7.7 us, 7.65 where every row is
-// read; with a third CTA on an SM, 40 registers and spills, 8.1.
+// Whether a list's beam has logits to read is known before its first load, and asked for while the cluster starts: 7.6 us, 7.65
+// where every row was read (8 requests of 8 beams 11.25 and 10.95); with a third CTA on an SM, 40 registers and spills, 8.1.
 template <int kType> __global__ void __launch_bounds__(kJoinThreads, 2) select_together(const BeamSelectArgs a)
 {
     __shared__ PartSmem s;
@@ -954,13 +954,16 @@ template <int kType> __global__ void __launch_bounds__(kJoinThreads, 2) select_t
     asm("mapa.u64 %0, %1, 0;" : "=l"(entries) : "l"(z.entries));
     grid_dependency_wait();
     grid_launch_dependents();
-    // (every CTA: logits of finished and of unused beams are not read, as in select_rows)
-    get_beams(a, j, static_cast<int32_t>(request));
-    __syncthreads();
+    // (logits of finished and of unused beams are not read, as in select_rows; which a list's are is asked for ahead)
+    auto wanted = [&](uint32_t l) { return l < lists && reads_logits(a, request * a.beams + l / static_cast<uint32_t>(a.parts)); };
+    bool reads = wanted(rank);
+    if (rank == 0)
+        get_beams(a, j, static_cast<int32_t>(request));
     asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
     for (uint32_t l = rank; l < lists; l += kCluster) {
-        const uint32_t b = l / static_cast<uint32_t>(a.parts);
-        if (j.kind[b] == 2) {
+        const bool then = wanted(l + kCluster);
+        if (reads) {
+            const uint32_t b = l / static_cast<uint32_t>(a.parts);
             const int32_t lo = static_cast<int32_t>(l - b * a.parts) * a.part, hi = min(lo + a.part, a.vocab);
             const unsigned char *base = row_at(a, request * a.beams + b);
             uint4 v[kBeamLoads];
@@ -968,6 +971,7 @@ template <int kType> __global__ void __launch_bounds__(kJoinThreads, 2) select_t
             take_part<kType, kJoinThreads>(a, s, reinterpret_cast<BeamEntry *>(raw), base, lo, hi, v, meta + l,
                                            entries + l * a.keep);
         }
+        reads = then;
         __syncthreads();
     }
     asm volatile("barrier.cluster.arrive.release;" ::: "memory");
