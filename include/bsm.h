@@ -365,7 +365,8 @@ int bsm_paged_write(const bsm_paged_write_desc *d, bsm_stream_t stream);
  *             piece.  (positions and slots as bsm_paged_tables gives them.)
  *   heads_q   0: no queries (q and q_out may be null).
  *   q_out     q itself with the same strides (in place), or no place in common with q;
- *             none with k and v (those and q_out may be parts of one row).
+ *             none with k and v (those and q_out may be parts of one row).  Where their
+ *             spans meet their strides must be equal, else they are refused.
  *   rotary_dim  even, up to head_dim; 0 copies.  Halves of whole pieces of 16 bytes, and
  *             interleaved pairs, are fastest.
  * Types, rows, pointers and strides as bsm_paged_write (table: fp32, any stride of at
@@ -531,7 +532,8 @@ int64_t bsm_beam_select_workspace_bytes(int device, int32_t n_requests, int32_t 
  *   info[0..3]  pages taken; pages missing; pages dropped; BSM_PAGED_* bits
  * free_pages is not changed: drop its first info[0] entries.  Up to beams - 1 pages a request are
  * taken before the call gives any back: keep as many free.  The rows of one request alone
- * share partly filled pages; a page is in one column.  A row whose last page is missing (-1)
+ * share partly filled pages; a page is in one column, and what one row fills only in part is
+ * the last page of every row that holds it.  A row whose last page is missing (-1)
  * passes that on.  Lengths outside 0 .. table_width * page_size are cut to it and set
  * BSM_DEV_BOUNDS; so does a partly filled last page whose id lies outside the cache (other than
  * -1), or a free page that is taken and does (negative ones too): the id is handed on as it
