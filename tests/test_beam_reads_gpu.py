@@ -69,6 +69,6 @@ def test_logits_of_finished_and_unused_beams_are_not_touched(n, beams, vocab):
     val, par, tok = O.select(x.values, scores, keep, ended, 3)
     assert np.array_equal(parents.cpu().numpy(), par) and np.array_equal(tokens.cpu().numpy(), tok)
     assert np.abs(out.cpu().numpy() - val).max() < 1e-4
-    # the same rows with nobody finished are read, and then they are there (and what the driver brings beside them)
+    # the same rows with nobody finished are read, and then they are there (and what the system brings beside them)
     run(None)
     assert x.touched()[np.isfinite(scores)].all()
